@@ -382,6 +382,107 @@ DLM_API int lsq_gram_build(int n, int p, int q, const float* A, const float* b, 
                            void* cuda_stream);
 DLM_API int lsq_grad_gram(int n, int q, const float* H, const float* c, const float* x, float* g, void* cuda_stream);
 
+/* ------------------------------------------------------------------------------------
+ * Training operators: what a language model's training step needs between the model and the update rules
+ * above.  They take the same stacking (node i's part of every array is its i-th slice) and read weights from, and
+ * write their gradients to, column ranges of the stacked x and g.  Types are DLM_G_F32 and DLM_G_BF16; statistics,
+ * sums and losses are fp32 or wider.  All are enqueue-only and capturable, and give bitwise the same result every time.
+ * ------------------------------------------------------------------------------------ */
+
+/*
+ * Gradient list: n nodes with the same `tensors` parameter tensors each, wherever their gradients sit.
+ *   sizes   : host [tensors], elements of each tensor (0 allowed)
+ *   dtypes  : host [tensors], DLM_G_F32 or DLM_G_BF16
+ *   data    : host [n * tensors] device pointers, data[i * tensors + t] = node i's gradient of tensor t, contiguous,
+ *             aligned to its element size (any further alignment is faster but not needed)
+ *   offsets : host [tensors], first column of each tensor in a node's stacked row; NULL packs them without gaps.
+ *             Columns that no tensor covers are never written.
+ * The handle keeps the addresses: the buffers stay where they are while it is used (their contents change from step to
+ * step); build another one when they move.  It owns device scratch, so calls with one handle are ordered (one stream,
+ * or events).  Without a CUDA device the handle is host-only and the calls below fail with DLM_ERR_CUDA.
+ * Errors: DLM_ERR_NULL, DLM_ERR_SHAPE, DLM_ERR_KIND, DLM_ERR_ALIGN, DLM_ERR_ALIAS (two tensors sharing bytes, or
+ * columns), DLM_ERR_UNSUPPORTED (n above DLM_MAX_NODES), DLM_ERR_CUDA.
+ */
+typedef struct dlm_gradients dlm_gradients;
+DLM_API int gradients_build(int n, int tensors, const int64_t* sizes, const int* dtypes, const void* const* data,
+                            const int64_t* offsets, dlm_gradients** out);
+/* First column of each tensor (borrowed, valid until gradients_destroy) and the stacked row's width.  Either may be NULL. */
+DLM_API int gradients_layout(const dlm_gradients* list, const int64_t** offsets, int64_t* columns);
+DLM_API int gradients_destroy(dlm_gradients* list);
+
+/*
+ * Norm of every node's whole gradient, and clipping by it:
+ *   norm_i = sqrt(sum_t ||G_it||_2^2)  (DLM_NORM_L2)   or   max |G_it|  (DLM_NORM_MAX)
+ *   s_i = min(1, max_norm / (norm_i + 1e-6)) ,   out_i = s_i G_i
+ * Each node is clipped by its own norm: no node needs another's, so a decentralised run exchanges nothing for it.
+ *   norms : device fp32 [n], written (the norm before clipping)
+ *   g     : NULL: clip in place.  Else device [n, ldg] of g_dtype, ldg >= the list's width: the scaled gradients are
+ *           gathered into the stacked rows, as the update rules read them, and the tensors are left as they are.
+ * The L2 norm is exact to fp32 rounding over the whole fp32 range (squares that overflow or vanish in fp32 are summed
+ * again in double).  A NaN or infinity in a node's gradient shows in its norm; the scale is then NaN or 0 by the
+ * formula.  Reads the list once for the norm, and once more for the copy.
+ * Errors: DLM_ERR_NULL, DLM_ERR_KIND, DLM_ERR_SHAPE, DLM_ERR_ALIGN, DLM_ERR_ALIAS (g's rows or norms overlapping a
+ * tensor of the list), DLM_ERR_HYPER (max_norm not finite or <= 0), DLM_ERR_CUDA.
+ */
+enum { DLM_NORM_L2 = 0, DLM_NORM_MAX = 1 };
+DLM_API int gradient_norm(dlm_gradients* list, int kind, float* norms, void* cuda_stream);
+DLM_API int gradient_clip(dlm_gradients* list, int kind, float max_norm, float* norms, void* g, int g_dtype, int64_t ldg,
+                          void* cuda_stream);
+
+/*
+ * Layer norm of n nodes' activations, each node with its own weight w_i and bias b_i:
+ *   mean = sum_c x / c ;  rstd = 1 / sqrt(sum_c (x - mean)^2 / c + eps) ;  y = (x - mean) rstd w_i + b_i
+ *   x, y       : device [n * rows, c] of dtype, row strides ldx, ldy; y == x (same stride) is allowed
+ *   weight     : device fp32 [n, c], row stride ldw (a column range of the stacked x, for instance)
+ *   bias       : as weight with stride ldb, or NULL
+ *   mean, rstd : device fp32 [n * rows], written; the backward pass reads them
+ *   eps        : finite, >= 0
+ * layer_norm_grad, with xh = (x - mean) rstd and v = w_i dy:
+ *   dx = rstd (v - sum_c v / c - xh sum_c (v xh) / c) ;  dweight_i = sum_rows dy xh ;  dbias_i = sum_rows dy
+ *   dy, dx     : device [n * rows, c] of dtype; dx == dy or dx == x (same stride) is allowed
+ *   dweight    : device [n, c] of g_dtype, row stride ldgw; dbias likewise, or NULL.  Overwritten, in column ranges of the
+ *                stacked g, for instance.
+ *   workspace  : device, layer_norm_grad_workspace_bytes(n, rows, c) bytes, 256-byte aligned, owned by the caller
+ * rows may be 0 (the weight gradients are then 0).  Fast path: c a multiple of 16 bytes' worth and every activation row
+ * 16-byte aligned; rows of up to 32768 (backward 16384) elements are held in registers, wider ones are read again.
+ * Errors: DLM_ERR_NULL, DLM_ERR_SHAPE, DLM_ERR_KIND, DLM_ERR_ALIGN, DLM_ERR_ALIAS, DLM_ERR_HYPER, DLM_ERR_WORKSPACE,
+ * DLM_ERR_UNSUPPORTED, DLM_ERR_CUDA.
+ */
+DLM_API int layer_norm(int n, int64_t rows, int64_t c, const void* x, int dtype, int64_t ldx, const float* weight,
+                       int64_t ldw, const float* bias, int64_t ldb, float eps, void* y, int64_t ldy, float* mean,
+                       float* rstd, void* cuda_stream);
+DLM_API int64_t layer_norm_grad_workspace_bytes(int n, int64_t rows, int64_t c); /* negative dlm_status on bad sizes */
+DLM_API int layer_norm_grad(int n, int64_t rows, int64_t c, const void* x, int dtype, int64_t ldx, const void* dy,
+                            int64_t lddy, const float* weight, int64_t ldw, const float* mean, const float* rstd, void* dx,
+                            int64_t lddx, void* dweight, int64_t ldgw, void* dbias, int64_t ldgb, int g_dtype,
+                            void* workspace, int64_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Clipped policy loss with a KL term, and its gradient, from the logits.  For row r of node i, with z its logits, t its
+ * token, A its advantage and w its weight:
+ *   logp = z_t - log sum_v exp z_v ;  ratio = exp(logp - old_logp) ;  held = min(max(ratio, 1 - clip_low), 1 + clip_high)
+ *   l = w ( -min(ratio A, held A) + kl_coef (exp(ref_logp - logp) - (ref_logp - logp) - 1) ) ;   loss_i = sum_r l
+ *   dlogits_v = s ([v = t] - exp(z_v) / sum exp z) ,   s = w ( -[ratio A <= held A] ratio A + kl_coef (1 - exp(ref_logp - logp)) )
+ *   logits     : device [n * rows, vocab] of dtype, row stride ldl
+ *   tokens     : device int64 [n * rows]
+ *   weight     : device fp32 [n * rows]: the mask and the normalisation in one (1 / tokens of the batch, for instance).  A row
+ *                with weight 0, or whose token is outside [0, vocab), is masked: whatever its logits hold, it adds nothing
+ *                to the loss, its logp is 0 and its gradient row is 0.
+ *   advantage, old_logp, ref_logp : device fp32 [n * rows]; ref_logp may be NULL where kl_coef is 0
+ *   loss       : device fp32 [n], written;  logp: device fp32 [n * rows], written
+ *   dlogits    : device [n * rows, vocab] of dtype, row stride ldd, written; NULL: loss and logp only;
+ *                dlogits == logits (same stride) is allowed
+ *   workspace  : device, policy_loss_workspace_bytes(n, rows, vocab) bytes, 256-byte aligned, owned by the caller
+ * clip_low, clip_high, kl_coef: finite, >= 0.  rows may be 0.  The sums run in a fixed order.
+ * Errors: DLM_ERR_NULL, DLM_ERR_SHAPE, DLM_ERR_KIND, DLM_ERR_ALIGN, DLM_ERR_ALIAS, DLM_ERR_HYPER, DLM_ERR_WORKSPACE,
+ * DLM_ERR_UNSUPPORTED (n * rows or vocab above 2^31 - 1), DLM_ERR_CUDA.
+ */
+DLM_API int64_t policy_loss_workspace_bytes(int n, int64_t rows, int64_t vocab); /* negative dlm_status on bad sizes */
+DLM_API int policy_loss_grad(int n, int64_t rows, int64_t vocab, const void* logits, int dtype, int64_t ldl,
+                             const int64_t* tokens, const float* weight, const float* advantage, const float* old_logp,
+                             const float* ref_logp, float clip_low, float clip_high, float kl_coef, float* loss, float* logp,
+                             void* dlogits, int64_t ldd, void* workspace, int64_t workspace_bytes, void* cuda_stream);
+
 /* Kernel launches issued by this library in the calling process so far (all entry points). */
 DLM_API int64_t dlm_launch_count(void);
 

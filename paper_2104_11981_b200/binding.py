@@ -14,6 +14,7 @@ LIB_PATH = os.path.join(_HERE, "libdecentlam.so")
 RING, STATIC_EXP, ONE_PEER_EXP, COMPLETE, CSR_MH, CSR_WEIGHTS, SYM_EXP, MESH = range(8)
 G_F32, G_BF16 = 0, 1
 DSGD_ATC, DSGD_AWC = 0, 1
+NORM_L2, NORM_MAX = 0, 1
 MAX_NODES = 2048
 
 STATUS = {0: "DLM_OK", -1: "DLM_ERR_NULL", -2: "DLM_ERR_SHAPE", -3: "DLM_ERR_ALIGN", -4: "DLM_ERR_ALIAS",
@@ -71,6 +72,21 @@ _lib.lsq_grad.argtypes = [_int, _int, _int, _vp, _vp, _vp, _vp, _flt, _vp, _i64,
 _lib.lsq_grad_static.argtypes = [_int, _int, _int, _vp, _vp, _vp, _vp, _flt, _vp]
 _lib.lsq_gram_build.argtypes = [_int, _int, _int, _vp, _vp, _flt, _vp, _vp, _vp]
 _lib.lsq_grad_gram.argtypes = [_int, _int, _vp, _vp, _vp, _vp, _vp]
+_lib.gradients_build.argtypes = [_int, _int, ctypes.POINTER(_i64), ctypes.POINTER(_int), ctypes.POINTER(_vp),
+                                 ctypes.POINTER(_i64), ctypes.POINTER(_vp)]
+_lib.gradients_layout.argtypes = [_vp, ctypes.POINTER(ctypes.POINTER(_i64)), ctypes.POINTER(_i64)]
+_lib.gradients_destroy.argtypes = [_vp]
+_lib.gradient_norm.argtypes = [_vp, _int, _vp, _vp]
+_lib.gradient_clip.argtypes = [_vp, _int, _flt, _vp, _vp, _int, _i64, _vp]
+_lib.layer_norm.argtypes = [_int, _i64, _i64, _vp, _int, _i64, _vp, _i64, _vp, _i64, _flt, _vp, _i64, _vp, _vp, _vp]
+_lib.layer_norm_grad_workspace_bytes.argtypes = [_int, _i64, _i64]
+_lib.layer_norm_grad_workspace_bytes.restype = _i64
+_lib.layer_norm_grad.argtypes = [_int, _i64, _i64, _vp, _int, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _vp,
+                                 _i64, _int, _vp, _i64, _vp]
+_lib.policy_loss_workspace_bytes.argtypes = [_int, _i64, _i64]
+_lib.policy_loss_workspace_bytes.restype = _i64
+_lib.policy_loss_grad.argtypes = [_int, _i64, _i64, _vp, _int, _i64, _vp, _vp, _vp, _vp, _vp, _flt, _flt, _flt, _vp, _vp, _vp,
+                                  _i64, _vp, _i64, _vp]
 _lib.dlm_launch_count.argtypes = []
 _lib.dlm_launch_count.restype = _i64
 _lib.dlm_kernel_error.argtypes = [ctypes.POINTER(_int)]
@@ -80,7 +96,9 @@ EXPORTS = ["dlm_status_string", "topology_build", "topology_build_periodic", "to
            "topology_tables_device", "topology_destroy", "decentlam_step", "decentlam_step_host_gradients", "dmsgd_step", "dsgd_step", "pmsgd_step",
            "topology_shard", "topology_shard_destroy", "topology_shard_rows", "topology_halo", "topology_halo_sends",
            "decentlam_step_sharded", "dmsgd_local_sharded", "partial_average_sharded",
-           "lsq_grad_workspace_bytes", "lsq_grad", "lsq_grad_static", "lsq_gram_build", "lsq_grad_gram", "dlm_launch_count", "dlm_kernel_error", "dlm_set_tuning"]
+           "lsq_grad_workspace_bytes", "lsq_grad", "lsq_grad_static", "lsq_gram_build", "lsq_grad_gram",
+           "gradients_build", "gradients_layout", "gradients_destroy", "gradient_norm", "gradient_clip", "layer_norm",
+           "layer_norm_grad_workspace_bytes", "layer_norm_grad", "policy_loss_workspace_bytes", "policy_loss_grad", "dlm_launch_count", "dlm_kernel_error", "dlm_set_tuning"]
 
 
 def _check(rc, where):
@@ -376,6 +394,180 @@ def lsq_grad_gram(H, c, x, g, stream=None):
     assert H.shape == (n, q, q) and c.shape == (n, q) and x.shape == (n, q) and g.shape == (n, q)
     _check(_lib.lsq_grad_gram(n, q, _vp(H.data_ptr()), _vp(c.data_ptr()), _vp(x.data_ptr()), _vp(g.data_ptr()),
                               _stream_ptr(stream)), "lsq_grad_gram")
+
+
+def _dtype(t):
+    import torch
+    if t.dtype == torch.float32:
+        return G_F32
+    if t.dtype == torch.bfloat16:
+        return G_BF16
+    raise TypeError("float32 or bfloat16 expected")
+
+
+def _ptr(t):
+    return _vp(t.data_ptr()) if t is not None else None
+
+
+class Gradients:
+    """Owner of a dlm_gradients handle: n nodes' lists of parameter gradients.  Keeps the tensors alive."""
+
+    def __init__(self, handle, n, tensors, keep):
+        self.handle, self.n, self.tensors, self.keep = handle, n, tensors, keep
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+    def destroy(self):
+        if getattr(self, "handle", None):
+            _lib.gradients_destroy(self.handle)
+            self.handle = None
+
+    def _layout(self):
+        po, c = ctypes.POINTER(_i64)(), _i64()
+        _check(_lib.gradients_layout(self.handle, ctypes.byref(po), ctypes.byref(c)), "gradients_layout")
+        return po, c.value
+
+    @property
+    def offsets(self):
+        """First column of each tensor in a stacked row."""
+        po, _ = self._layout()
+        return [po[t] for t in range(self.tensors)]
+
+    @property
+    def columns(self):
+        """Width of a stacked row."""
+        return self._layout()[1]
+
+
+def gradients_build(nodes, offsets=None):
+    """nodes: one list of gradient tensors per node, the same sizes and types in every node, each contiguous.
+    offsets: first column of each tensor in a node's stacked row (None: packed without gaps)."""
+    n, tensors = len(nodes), len(nodes[0]) if nodes else 0
+    sizes, dtypes = [t.numel() for t in nodes[0]] if n else [], [_dtype(t) for t in nodes[0]] if n else []
+    data = (_vp * max(1, n * tensors))()
+    for i, node in enumerate(nodes):
+        assert len(node) == tensors, "every node has the same tensors"
+        for t, g in enumerate(node):
+            assert g.is_contiguous() and g.numel() == sizes[t] and _dtype(g) == dtypes[t]
+            data[i * tensors + t] = g.data_ptr()
+    assert offsets is None or len(offsets) == tensors
+    po = (_i64 * tensors)(*offsets) if offsets is not None else None
+    out = _vp()
+    _check(_lib.gradients_build(n, tensors, (_i64 * max(1, tensors))(*sizes), (_int * max(1, tensors))(*dtypes), data, po,
+                                ctypes.byref(out)), "gradients_build")
+    return Gradients(out, n, tensors, [list(node) for node in nodes])
+
+
+def _check_norms(grads, norms):
+    import torch
+    assert norms.is_cuda and norms.dtype == torch.float32 and norms.is_contiguous() and norms.numel() == grads.n
+
+
+def gradient_norm(grads, norms, kind=NORM_L2, stream=None):
+    """norms[i] <- norm of node i's whole gradient (fp32 device tensor of n elements)."""
+    _check_norms(grads, norms)
+    _check(_lib.gradient_norm(grads.handle, kind, _ptr(norms), _stream_ptr(stream)), "gradient_norm")
+
+
+def gradient_clip(grads, max_norm, norms, g=None, kind=NORM_L2, stream=None):
+    """Clip every node's gradient to max_norm by its own norm (written to norms): in place, or (g [n, >= columns],
+    fp32 or bf16) gathered into the stacked rows that the update rules read, the tensors left as they are."""
+    _check_norms(grads, norms)
+    gd, ldg = G_F32, 0
+    if g is not None:
+        assert g.is_cuda and g.dim() == 2 and g.shape[0] == grads.n and g.shape[1] >= grads.columns and g.stride(1) == 1
+        gd, ldg = _dtype(g), g.stride(0) if grads.n > 1 else max(g.stride(0), g.shape[1])
+    _check(_lib.gradient_clip(grads.handle, kind, max_norm, _ptr(norms), _ptr(g), gd, ldg, _stream_ptr(stream)), "gradient_clip")
+
+
+def _node_rows(t, like=None):
+    """Row stride of activations [n, rows, c] whose nodes follow one another."""
+    assert t.is_cuda and t.dim() == 3 and (like is None or (t.shape == like.shape and t.dtype == like.dtype))
+    n, rows, c = t.shape
+    assert t.stride(2) == 1 or c == 1, "unit column stride expected"
+    if rows == 1:
+        return max(c, t.stride(0)) if n > 1 else c
+    assert n <= 1 or rows == 0 or t.stride(0) == rows * t.stride(1), "the nodes' rows must be evenly spaced"
+    return t.stride(1)
+
+
+def _node_vectors(t, n, c, what):
+    """(pointer, row stride) of per-node vectors [n, c] with unit column stride, or of None."""
+    if t is None:
+        return None, 0
+    assert t.is_cuda and t.shape == (n, c) and (t.stride(1) == 1 or c == 1), what
+    return _ptr(t), t.stride(0) if n > 1 else c
+
+
+def _per_row(t, n, rows, dtype):
+    assert t.is_cuda and t.dtype == dtype and t.is_contiguous() and t.numel() == n * rows
+    return _ptr(t)
+
+
+def layer_norm(x, weight, bias, eps, y, mean, rstd, stream=None):
+    """y <- (x - mean) rstd weight + bias over the last axis of x [n, rows, c] (fp32 or bf16); weight, bias fp32 [n, c]
+    (views of the stacked parameters, for instance; bias may be None); mean, rstd fp32 [n, rows] are written."""
+    import torch
+    n, rows, c = x.shape
+    ldx, ldy = _node_rows(x), _node_rows(y, x)
+    assert weight.dtype == torch.float32 and (bias is None or bias.dtype == torch.float32)
+    (pw, ldw), (pb, ldb) = _node_vectors(weight, n, c, "weight [n, c]"), _node_vectors(bias, n, c, "bias [n, c]")
+    _check(_lib.layer_norm(n, rows, c, _ptr(x), _dtype(x), ldx, pw, ldw, pb, ldb, eps, _ptr(y), ldy,
+                           _per_row(mean, n, rows, torch.float32), _per_row(rstd, n, rows, torch.float32),
+                           _stream_ptr(stream)), "layer_norm")
+
+
+def layer_norm_grad_workspace_bytes(n, rows, c):
+    v = _lib.layer_norm_grad_workspace_bytes(n, rows, c)
+    if v < 0:
+        raise DecentlamError(v, "layer_norm_grad_workspace_bytes")
+    return int(v)
+
+
+def layer_norm_grad(x, dy, weight, mean, rstd, dx, dweight, dbias, workspace, stream=None):
+    """Backward pass of layer_norm: dx of x's shape and type; dweight, dbias [n, c] fp32 or bf16 (views of the stacked
+    gradient, for instance; dbias may be None) are overwritten; workspace: uint8 device tensor of at least
+    layer_norm_grad_workspace_bytes(n, rows, c) bytes."""
+    import torch
+    n, rows, c = x.shape
+    ldx, lddy, lddx = _node_rows(x), _node_rows(dy, x), _node_rows(dx, x)
+    assert weight.dtype == torch.float32 and (dbias is None or dbias.dtype == dweight.dtype)
+    pw, ldw = _node_vectors(weight, n, c, "weight [n, c]")
+    (pgw, ldgw), (pgb, ldgb) = _node_vectors(dweight, n, c, "dweight [n, c]"), _node_vectors(dbias, n, c, "dbias [n, c]")
+    _check(_lib.layer_norm_grad(n, rows, c, _ptr(x), _dtype(x), ldx, _ptr(dy), lddy, pw, ldw,
+                                _per_row(mean, n, rows, torch.float32), _per_row(rstd, n, rows, torch.float32), _ptr(dx),
+                                lddx, pgw, ldgw, pgb, ldgb, _dtype(dweight), _ptr(workspace),
+                                workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "layer_norm_grad")
+
+
+def policy_loss_workspace_bytes(n, rows, vocab):
+    v = _lib.policy_loss_workspace_bytes(n, rows, vocab)
+    if v < 0:
+        raise DecentlamError(v, "policy_loss_workspace_bytes")
+    return int(v)
+
+
+def policy_loss_grad(logits, tokens, weight, advantage, old_logp, ref_logp, clip_low, clip_high, kl_coef, loss, logp,
+                     dlogits, workspace, stream=None):
+    """Clipped policy loss with a KL term, and its gradient: logits [n, rows, vocab] fp32 or bf16; tokens int64, weight,
+    advantage, old_logp, ref_logp (or None) fp32 [n, rows]; loss fp32 [n] and logp fp32 [n, rows] are written, and dlogits
+    (of the logits' shape and type; None: no gradient; the logits themselves: in place).  workspace: uint8 device tensor
+    of at least policy_loss_workspace_bytes(n, rows, vocab) bytes."""
+    import torch
+    n, rows, vocab = logits.shape
+    f32 = torch.float32
+    ldl, ldd = _node_rows(logits), _node_rows(dlogits, logits) if dlogits is not None else 0
+    assert loss.is_cuda and loss.dtype == f32 and loss.is_contiguous() and loss.numel() == n
+    _check(_lib.policy_loss_grad(n, rows, vocab, _ptr(logits), _dtype(logits), ldl, _per_row(tokens, n, rows, torch.int64),
+                                 _per_row(weight, n, rows, f32), _per_row(advantage, n, rows, f32),
+                                 _per_row(old_logp, n, rows, f32), _per_row(ref_logp, n, rows, f32) if ref_logp is not None else None,
+                                 clip_low, clip_high, kl_coef, _ptr(loss), _per_row(logp, n, rows, f32), _ptr(dlogits), ldd,
+                                 _ptr(workspace), workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
+           "policy_loss_grad")
 
 
 def launch_count():

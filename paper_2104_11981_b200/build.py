@@ -16,7 +16,8 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 OBJ = os.path.join(HERE, "_build")
 OUT = os.path.join(HERE, "libdecentlam.so")
 SOURCES = ["api.cpp", "topology.cpp", "sharded.cpp", "step_kernels.cu", "step_merged.cu", "step_sharded.cu",
-           "pmsgd_kernel.cu", "lsq_kernels.cu"]
+           "pmsgd_kernel.cu", "lsq_kernels.cu", "gradients.cpp", "gradient_kernels.cu", "train.cpp", "layer_norm.cu",
+           "policy_loss.cu"]
 ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]
 
 

@@ -54,6 +54,12 @@ def to64(t):
     return t.detach().to(torch.float32).cpu().numpy().astype(np.float64)
 
 
+def half_unit(typ, v):
+    """Half a unit in the last place of each value in "f32" (24 significant bits) or "bf16" (8): what rounding once to
+    nearest may change it by (0 at 0).  np.frexp gives v = f 2^e with f in [1/2, 1), so the unit is 2^(e - bits)."""
+    return np.where(v == 0.0, 0.0, np.ldexp(0.5, np.frexp(v)[1] - (8 if typ == "bf16" else 24)))
+
+
 def bf16_tensor(g32, device):
     """The harness's rounding of fp32 gradients to bfloat16: round to nearest, ties to even, done by
     inputs.f32_to_bf16_bits on the host (pinned bit by bit in test_bf16_rounding.py); returns a torch
