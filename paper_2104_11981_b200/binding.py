@@ -193,9 +193,11 @@ def topology_build_periodic(kind, n, period, rowptr, col, val=None):
 
 
 def _stream_ptr(stream):
+    if stream is not None:
+        return _vp(stream.cuda_stream)
     import torch
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return _vp(s.cuda_stream)
+    # the raw handle of the current stream: building a torch.cuda.Stream object for it costs 3.5 us a call
+    return _vp(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
 
 
 def _state_args(x, m, g):
@@ -396,24 +398,29 @@ def lsq_grad_gram(H, c, x, g, stream=None):
                               _stream_ptr(stream)), "lsq_grad_gram")
 
 
+_G_DTYPES = {}  # torch dtype -> DLM_G_*, filled on first use so that importing this module does not import torch
+
+
 def _dtype(t):
-    import torch
-    if t.dtype == torch.float32:
-        return G_F32
-    if t.dtype == torch.bfloat16:
-        return G_BF16
-    raise TypeError("float32 or bfloat16 expected")
-
-
-def _ptr(t):
-    return _vp(t.data_ptr()) if t is not None else None
+    v = _G_DTYPES.get(t.dtype)
+    if v is None:
+        import torch
+        _G_DTYPES.update({torch.float32: G_F32, torch.bfloat16: G_BF16})
+        v = _G_DTYPES.get(t.dtype)
+        if v is None:
+            raise TypeError("float32 or bfloat16 expected")
+    return v
 
 
 class Gradients:
     """Owner of a dlm_gradients handle: n nodes' lists of parameter gradients.  Keeps the tensors alive."""
 
     def __init__(self, handle, n, tensors, keep):
-        self.handle, self.n, self.tensors, self.keep = handle, n, tensors, keep
+        self.handle, self.n, self.keep = handle, n, keep
+        po, c = ctypes.POINTER(_i64)(), _i64()
+        _check(_lib.gradients_layout(handle, ctypes.byref(po), ctypes.byref(c)), "gradients_layout")
+        self.offsets = [po[t] for t in range(tensors)]  # first column of each tensor in a stacked row
+        self.columns = c.value                          # width of a stacked row
 
     def __del__(self):
         try:
@@ -426,21 +433,6 @@ class Gradients:
             _lib.gradients_destroy(self.handle)
             self.handle = None
 
-    def _layout(self):
-        po, c = ctypes.POINTER(_i64)(), _i64()
-        _check(_lib.gradients_layout(self.handle, ctypes.byref(po), ctypes.byref(c)), "gradients_layout")
-        return po, c.value
-
-    @property
-    def offsets(self):
-        """First column of each tensor in a stacked row."""
-        po, _ = self._layout()
-        return [po[t] for t in range(self.tensors)]
-
-    @property
-    def columns(self):
-        """Width of a stacked row."""
-        return self._layout()[1]
 
 
 def gradients_build(nodes, offsets=None):
@@ -463,61 +455,67 @@ def gradients_build(nodes, offsets=None):
 
 
 def _check_norms(grads, norms):
-    import torch
-    assert norms.is_cuda and norms.dtype == torch.float32 and norms.is_contiguous() and norms.numel() == grads.n
+    assert norms.is_cuda and _dtype(norms) == G_F32 and norms.is_contiguous() and norms.numel() == grads.n
 
 
 def gradient_norm(grads, norms, kind=NORM_L2, stream=None):
     """norms[i] <- norm of node i's whole gradient (fp32 device tensor of n elements)."""
     _check_norms(grads, norms)
-    _check(_lib.gradient_norm(grads.handle, kind, _ptr(norms), _stream_ptr(stream)), "gradient_norm")
+    _check(_lib.gradient_norm(grads.handle, kind, norms.data_ptr(), _stream_ptr(stream)), "gradient_norm")
 
 
 def gradient_clip(grads, max_norm, norms, g=None, kind=NORM_L2, stream=None):
     """Clip every node's gradient to max_norm by its own norm (written to norms): in place, or (g [n, >= columns],
     fp32 or bf16) gathered into the stacked rows that the update rules read, the tensors left as they are."""
     _check_norms(grads, norms)
-    gd, ldg = G_F32, 0
+    pg, gd, ldg = None, G_F32, 0
     if g is not None:
-        assert g.is_cuda and g.dim() == 2 and g.shape[0] == grads.n and g.shape[1] >= grads.columns and g.stride(1) == 1
-        gd, ldg = _dtype(g), g.stride(0) if grads.n > 1 else max(g.stride(0), g.shape[1])
-    _check(_lib.gradient_clip(grads.handle, kind, max_norm, _ptr(norms), _ptr(g), gd, ldg, _stream_ptr(stream)), "gradient_clip")
+        n, width = g.shape
+        assert g.is_cuda and n == grads.n and width >= grads.columns and (g.stride(1) == 1 or width == 1)
+        pg, gd, ldg = g.data_ptr(), _dtype(g), g.stride(0) if n > 1 else width
+    _check(_lib.gradient_clip(grads.handle, kind, max_norm, norms.data_ptr(), pg, gd, ldg, _stream_ptr(stream)),
+           "gradient_clip")
 
 
-def _node_rows(t, like=None):
-    """Row stride of activations [n, rows, c] whose nodes follow one another."""
-    assert t.is_cuda and t.dim() == 3 and (like is None or (t.shape == like.shape and t.dtype == like.dtype))
-    n, rows, c = t.shape
-    assert t.stride(2) == 1 or c == 1, "unit column stride expected"
+def _node_rows(t, shape, dtype):
+    """Row stride of activations [n, rows, c] of this shape and type, whose nodes follow one another."""
+    assert t.is_cuda and t.dtype == dtype and t.shape == shape, "a CUDA tensor of the same shape and type is expected"
+    n, rows, c = shape
+    if t.is_contiguous():
+        return c
+    s0, s1, s2 = t.stride()
+    assert s2 == 1 or c == 1, "unit column stride expected"
     if rows == 1:
-        return max(c, t.stride(0)) if n > 1 else c
-    assert n <= 1 or rows == 0 or t.stride(0) == rows * t.stride(1), "the nodes' rows must be evenly spaced"
-    return t.stride(1)
+        return s0
+    assert n == 1 or s0 == rows * s1, "the nodes' rows must be evenly spaced"
+    return s1
 
 
-def _node_vectors(t, n, c, what):
+def _node_vectors(t, n, c):
     """(pointer, row stride) of per-node vectors [n, c] with unit column stride, or of None."""
     if t is None:
         return None, 0
-    assert t.is_cuda and t.shape == (n, c) and (t.stride(1) == 1 or c == 1), what
-    return _ptr(t), t.stride(0) if n > 1 else c
+    assert t.is_cuda and t.shape == (n, c), "per-node vectors [n, c] are expected"
+    s0, s1 = t.stride()
+    assert s1 == 1 or c == 1, "unit column stride expected"
+    return t.data_ptr(), s0 if n > 1 else c
 
 
-def _per_row(t, n, rows, dtype):
-    assert t.is_cuda and t.dtype == dtype and t.is_contiguous() and t.numel() == n * rows
-    return _ptr(t)
+def _per_row(t, count):
+    """Pointer of a contiguous fp32 tensor of one value per row."""
+    assert t.is_cuda and _dtype(t) == G_F32 and t.is_contiguous() and t.numel() == count, "fp32, one value per row"
+    return t.data_ptr()
 
 
 def layer_norm(x, weight, bias, eps, y, mean, rstd, stream=None):
     """y <- (x - mean) rstd weight + bias over the last axis of x [n, rows, c] (fp32 or bf16); weight, bias fp32 [n, c]
     (views of the stacked parameters, for instance; bias may be None); mean, rstd fp32 [n, rows] are written."""
-    import torch
-    n, rows, c = x.shape
-    ldx, ldy = _node_rows(x), _node_rows(y, x)
-    assert weight.dtype == torch.float32 and (bias is None or bias.dtype == torch.float32)
-    (pw, ldw), (pb, ldb) = _node_vectors(weight, n, c, "weight [n, c]"), _node_vectors(bias, n, c, "bias [n, c]")
-    _check(_lib.layer_norm(n, rows, c, _ptr(x), _dtype(x), ldx, pw, ldw, pb, ldb, eps, _ptr(y), ldy,
-                           _per_row(mean, n, rows, torch.float32), _per_row(rstd, n, rows, torch.float32),
+    shape, dtype = x.shape, x.dtype
+    n, rows, c = shape
+    assert _dtype(weight) == G_F32 and (bias is None or _dtype(bias) == G_F32)
+    (pw, ldw), (pb, ldb) = _node_vectors(weight, n, c), _node_vectors(bias, n, c)
+    _check(_lib.layer_norm(n, rows, c, x.data_ptr(), _dtype(x), _node_rows(x, shape, dtype), pw, ldw, pb, ldb, eps,
+                           y.data_ptr(), _node_rows(y, shape, dtype), _per_row(mean, n * rows), _per_row(rstd, n * rows),
                            _stream_ptr(stream)), "layer_norm")
 
 
@@ -532,16 +530,15 @@ def layer_norm_grad(x, dy, weight, mean, rstd, dx, dweight, dbias, workspace, st
     """Backward pass of layer_norm: dx of x's shape and type; dweight, dbias [n, c] fp32 or bf16 (views of the stacked
     gradient, for instance; dbias may be None) are overwritten; workspace: uint8 device tensor of at least
     layer_norm_grad_workspace_bytes(n, rows, c) bytes."""
-    import torch
-    n, rows, c = x.shape
-    ldx, lddy, lddx = _node_rows(x), _node_rows(dy, x), _node_rows(dx, x)
-    assert weight.dtype == torch.float32 and (dbias is None or dbias.dtype == dweight.dtype)
-    pw, ldw = _node_vectors(weight, n, c, "weight [n, c]")
-    (pgw, ldgw), (pgb, ldgb) = _node_vectors(dweight, n, c, "dweight [n, c]"), _node_vectors(dbias, n, c, "dbias [n, c]")
-    _check(_lib.layer_norm_grad(n, rows, c, _ptr(x), _dtype(x), ldx, _ptr(dy), lddy, pw, ldw,
-                                _per_row(mean, n, rows, torch.float32), _per_row(rstd, n, rows, torch.float32), _ptr(dx),
-                                lddx, pgw, ldgw, pgb, ldgb, _dtype(dweight), _ptr(workspace),
-                                workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "layer_norm_grad")
+    shape, dtype = x.shape, x.dtype
+    n, rows, c = shape
+    assert _dtype(weight) == G_F32 and (dbias is None or dbias.dtype == dweight.dtype) and workspace.is_cuda
+    pw, ldw = _node_vectors(weight, n, c)
+    (pgw, ldgw), (pgb, ldgb) = _node_vectors(dweight, n, c), _node_vectors(dbias, n, c)
+    _check(_lib.layer_norm_grad(n, rows, c, x.data_ptr(), _dtype(x), _node_rows(x, shape, dtype), dy.data_ptr(),
+                                _node_rows(dy, shape, dtype), pw, ldw, _per_row(mean, n * rows), _per_row(rstd, n * rows),
+                                dx.data_ptr(), _node_rows(dx, shape, dtype), pgw, ldgw, pgb, ldgb, _dtype(dweight),
+                                workspace.data_ptr(), workspace.nbytes, _stream_ptr(stream)), "layer_norm_grad")
 
 
 def policy_loss_workspace_bytes(n, rows, vocab):
@@ -558,16 +555,17 @@ def policy_loss_grad(logits, tokens, weight, advantage, old_logp, ref_logp, clip
     (of the logits' shape and type; None: no gradient; the logits themselves: in place).  workspace: uint8 device tensor
     of at least policy_loss_workspace_bytes(n, rows, vocab) bytes."""
     import torch
-    n, rows, vocab = logits.shape
-    f32 = torch.float32
-    ldl, ldd = _node_rows(logits), _node_rows(dlogits, logits) if dlogits is not None else 0
-    assert loss.is_cuda and loss.dtype == f32 and loss.is_contiguous() and loss.numel() == n
-    _check(_lib.policy_loss_grad(n, rows, vocab, _ptr(logits), _dtype(logits), ldl, _per_row(tokens, n, rows, torch.int64),
-                                 _per_row(weight, n, rows, f32), _per_row(advantage, n, rows, f32),
-                                 _per_row(old_logp, n, rows, f32), _per_row(ref_logp, n, rows, f32) if ref_logp is not None else None,
-                                 clip_low, clip_high, kl_coef, _ptr(loss), _per_row(logp, n, rows, f32), _ptr(dlogits), ldd,
-                                 _ptr(workspace), workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
-           "policy_loss_grad")
+    shape, dtype = logits.shape, logits.dtype
+    n, rows, vocab = shape
+    count = n * rows
+    assert tokens.is_cuda and tokens.dtype == torch.int64 and tokens.is_contiguous() and tokens.numel() == count
+    assert workspace.is_cuda
+    pd, ldd = (dlogits.data_ptr(), _node_rows(dlogits, shape, dtype)) if dlogits is not None else (None, 0)
+    _check(_lib.policy_loss_grad(n, rows, vocab, logits.data_ptr(), _dtype(logits), _node_rows(logits, shape, dtype),
+                                 tokens.data_ptr(), _per_row(weight, count), _per_row(advantage, count),
+                                 _per_row(old_logp, count), _per_row(ref_logp, count) if ref_logp is not None else None,
+                                 clip_low, clip_high, kl_coef, _per_row(loss, n), _per_row(logp, count), pd, ldd,
+                                 workspace.data_ptr(), workspace.nbytes, _stream_ptr(stream)), "policy_loss_grad")
 
 
 def launch_count():

@@ -249,7 +249,7 @@ int dlm_launch_gradient_norm(const dlm_gradients& list, int kind, float max_norm
         err = cudaGetLastError();
     } else {
         auto kern = kind == DLM_NORM_L2 ? gradient_norm_kernel<DLM_NORM_L2> : gradient_norm_kernel<DLM_NORM_MAX>;
-        err = launch_overlapped(kern, dim3((unsigned)(list.pieces * list.n)), dim3(kThreads), 0, s, list.d_pieces, list.pieces,
+        err = launch_overlapped(kern, dim3((unsigned)(list.pieces * list.n)), dim3(kThreads), 0, s, 1, list.d_pieces, list.pieces,
                                 list.d_partial, list.d_arrived, max_norm, norms, list.d_scale);
     }
     dlm_count_launch(1);
@@ -259,7 +259,7 @@ int dlm_launch_gradient_norm(const dlm_gradients& list, int kind, float max_norm
 int dlm_launch_gradient_scale(const dlm_gradients& list, void* g, int g_dtype, int64_t ldg, void* stream) {
     if (list.pieces == 0) return DLM_OK;
     cudaError_t err = launch_overlapped(gradient_scale_kernel, dim3((unsigned)(list.pieces * list.n)), dim3(kThreads), 0,
-                                        reinterpret_cast<cudaStream_t>(stream), list.d_pieces, list.pieces, list.d_scale, g,
+                                        reinterpret_cast<cudaStream_t>(stream), 1, list.d_pieces, list.pieces, list.d_scale, g,
                                         (int)(g_dtype == DLM_G_BF16), (long long)ldg);
     dlm_count_launch(1);
     return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;

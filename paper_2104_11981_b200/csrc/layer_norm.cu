@@ -379,7 +379,7 @@ int run_forward(const dlm_norm_args& a, cudaStream_t s) {
     const int64_t want = (a.rows + GROUPS - 1) / GROUPS;
     const int64_t cap = std::max<int64_t>(1, (int64_t)info.sms * (2048 / kBlock<TPR>) / a.n);
     cudaError_t err = launch_overlapped(layer_norm_kernel<T, LEN, RUNS, TPR>, dim3((unsigned)std::min(want, cap), a.n),
-                                        dim3(kBlock<TPR>), 0, s, a.rows, (int)a.c, static_cast<const T*>(a.x), a.ldx, a.weight,
+                                        dim3(kBlock<TPR>), 0, s, 1, a.rows, (int)a.c, static_cast<const T*>(a.x), a.ldx, a.weight,
                                         a.ldw, a.bias, a.ldb, a.eps, static_cast<T*>(a.y), a.ldy, a.mean, a.rstd);
     dlm_count_launch(1);
     return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
@@ -388,7 +388,7 @@ int run_forward(const dlm_norm_args& a, cudaStream_t s) {
 template <typename T, int LEN, int RUNS, int TPR>
 int run_backward(const dlm_norm_args& a, int ctas, cudaStream_t s) {
     cudaError_t err = launch_overlapped(layer_norm_grad_kernel<T, LEN, RUNS, TPR>, dim3((unsigned)ctas, a.n), dim3(kBlock<TPR>), 0,
-                                        s, a.rows, (int)a.c, static_cast<const T*>(a.x), a.ldx, static_cast<const T*>(a.dy), a.lddy,
+                                        s, 1, a.rows, (int)a.c, static_cast<const T*>(a.x), a.ldx, static_cast<const T*>(a.dy), a.lddy,
                                         a.weight, a.ldw, (const float*)a.mean, (const float*)a.rstd, static_cast<T*>(a.dx), a.lddx,
                                         a.partial);
     dlm_count_launch(1);
@@ -404,7 +404,7 @@ int forward(const dlm_norm_args& a, cudaStream_t s) {
         const DeviceInfo& info = device_info();
         if (!info.ok) return DLM_ERR_CUDA;
         const unsigned ctas = (unsigned)std::min<int64_t>(a.rows, std::max(1, 2 * info.sms / a.n));
-        cudaError_t err = launch_overlapped(layer_norm_wide_kernel<T>, dim3(ctas, a.n), dim3(1024), 0, s, a.rows, c,
+        cudaError_t err = launch_overlapped(layer_norm_wide_kernel<T>, dim3(ctas, a.n), dim3(1024), 0, s, 1, a.rows, c,
                                             static_cast<const T*>(a.x), a.ldx, a.weight, a.ldw, a.bias, a.ldb, a.eps,
                                             static_cast<T*>(a.y), a.ldy, a.mean, a.rstd);
         dlm_count_launch(1);
@@ -433,7 +433,7 @@ template <typename T>
 int backward(const dlm_norm_args& a, int ctas, cudaStream_t s) {
     const int64_t c = a.c;
     if (c > kMaxHeld / 2) {
-        cudaError_t err = launch_overlapped(layer_norm_grad_wide_kernel<T>, dim3((unsigned)ctas, a.n), dim3(1024), 0, s, a.rows, c,
+        cudaError_t err = launch_overlapped(layer_norm_grad_wide_kernel<T>, dim3((unsigned)ctas, a.n), dim3(1024), 0, s, 1, a.rows, c,
                                             static_cast<const T*>(a.x), a.ldx, static_cast<const T*>(a.dy), a.lddy, a.weight,
                                             a.ldw, (const float*)a.mean, (const float*)a.rstd, static_cast<T*>(a.dx), a.lddx,
                                             a.partial);
@@ -459,7 +459,7 @@ int backward(const dlm_norm_args& a, int ctas, cudaStream_t s) {
 
 template <typename G>
 cudaError_t join(const dlm_norm_args& a, int parts, cudaStream_t s) {
-    return launch_overlapped(layer_norm_join_kernel<G>, dim3((unsigned)((a.c + 31) / 32), a.n), dim3(256), 0, s, a.c, parts,
+    return launch_overlapped(layer_norm_join_kernel<G>, dim3((unsigned)((a.c + 31) / 32), a.n), dim3(256), 0, s, 1, a.c, parts,
                              (const float*)a.partial, static_cast<G*>(a.dweight), a.ldgw, static_cast<G*>(a.dbias), a.ldgb);
 }
 

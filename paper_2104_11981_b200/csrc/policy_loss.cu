@@ -5,6 +5,7 @@
 // The factor dl/dlogp depends on the row's own numbers alone, so loss and gradient take one kernel: a first sweep for
 // the maximum and the sum of exponentials, a second for the gradient.  Bound by memory: the logits read once, the
 // gradient written once.
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -20,6 +21,13 @@
 namespace {
 
 using namespace dlm;
+namespace cg = cooperative_groups;
+
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive_release() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+constexpr int kMaxCtas = 8;  // CTAs of a cluster: the most that every GPU of the architecture schedules
 
 // Exponents are kept to base 2: e^z = 2^{z L}, L = log2(e) in fp32, and sums are held as s 2^c with an integer c at or above
 // the largest exponent seen.  So an element takes one fused multiply-add, z L - c, rounded once; moving a sum to another
@@ -32,44 +40,37 @@ __device__ __forceinline__ float exp2_fast(float t) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));
     return r;
 }
+__device__ __forceinline__ float log2_fast(float t) {
+    float r;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));
+    return r;
+}
 
-// Running reference exponent and sum: total = s 2^c.  c = -inf: nothing but -inf so far.
+// Reference exponent and sum: total = s 2^c.  c = -inf: nothing but -inf so far.
 struct Tally {
     float c, s;
 };
 __device__ __forceinline__ float finite_ref(float c) { return c == -INFINITY ? 0.0f : c; }
-__device__ __forceinline__ Tally join(Tally a, Tally b) {
-    const float c = fmaxf(a.c, b.c), ref = finite_ref(c);
-    return {c, a.s * exp2_fast(a.c - ref) + b.s * exp2_fast(b.c - ref)};
+// Reference for values whose largest is m: an integer at or above their exponents.
+__device__ __forceinline__ float reference(float m) { return ceilf(m * kLog2E); }
+
+// The warp's total, the same in every lane.
+__device__ __forceinline__ Tally warp_total(Tally t) {
+    float c;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(c) : "f"(t.c));
+    return {c, warp_sum(t.s * exp2_fast(t.c - finite_ref(c)))};
 }
 
-template <int N>
-__device__ __forceinline__ void tally_values(Tally& t, const float* v) {
-    float m = v[0];
-#pragma unroll
-    for (int e = 1; e < N; ++e) m = fmaxf(m, v[e]);
-    m *= kLog2E;
-    if (m > t.c) {
-        m = ceilf(m);
-        t.s *= exp2_fast(t.c - m);
-        t.c = m;
-    }
-    const float ref = finite_ref(t.c);
-    float s = 0.0f;
-#pragma unroll
-    for (int e = 0; e < N; ++e) s += exp2_fast(fmaf(v[e], kLog2E, -ref));
-    t.s += s;
-}
-
-// What the row's scalars come to, the same for every thread.
+// What a row's scalars come to.  exp and log take the hardware's approximations, good to 2^-22 like the sum they follow;
+// the difference of two exponents of up to a few hundred is formed in double, where it costs nothing.
 struct RowOutcome {
     float logp, loss, slope;
 };
 __device__ __forceinline__ RowOutcome row_outcome(float zt, Tally t, float w, float adv, float old_logp, bool has_ref,
                                                   float ref_logp, float lo, float hi, float kl) {
-    const double logp = ((double)zt * (double)kLog2E - (double)t.c - (double)log2f(t.s)) * kLn2;
+    const double logp = (fma((double)zt, (double)kLog2E, -(double)t.c) - (double)log2_fast(t.s)) * kLn2;
     const float lp = logp > 0.0 ? 0.0f : (float)logp;  // rounding alone can take it above 0
-    const float r = expf(lp - old_logp);
+    const float r = exp2_fast((lp - old_logp) * kLog2E);
     const float held = fminf(fmaxf(r, 1.0f - lo), 1.0f + hi);
     const float a = r * adv, b = held * adv;
     float loss = -((a != a || a <= b) ? a : b);
@@ -77,143 +78,299 @@ __device__ __forceinline__ RowOutcome row_outcome(float zt, Tally t, float w, fl
     if (a != a) slope = a;
     if (has_ref) {
         const float far = ref_logp - lp;
-        const float grown = expm1f(far);
+        const float grown = exp2_fast(far * kLog2E) - 1.0f;
         loss += kl * (grown - far);
         slope -= kl * grown;
     }
     return {lp, w * loss, w * slope};
 }
 
-constexpr int kThreads = 512;
+// A row's 16-byte runs are dealt to the CTAS CTAs of a cluster in consecutive ranges, and within a CTA to TPR threads in
+// turn.  A thread copies its first kHold runs to its own slots of shared memory (asynchronous copies: they hold no
+// registers while in flight, and nobody else reads the slots, so no barrier is needed) and both sweeps read them there, so
+// that the logits cross the memory bus once; what a wider row has beyond that is read again, out of the L2.
+// TPR = 32: a warp per row, eight rows a CTA.
+constexpr int kHold = 8;
+template <int TPR>
+constexpr int kBlock = TPR < 128 ? 256 : TPR;
 
+__device__ __forceinline__ void copy_async(uint32_t smem, const void* p) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(p) : "memory");
+}
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+// Largest value of a run.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) policy_loss_kernel(dlm_policy_args a, int vec) {
+__device__ __forceinline__ float largest(const Words& q);
+template <>
+__device__ __forceinline__ float largest<float>(const Words& q) {
+    float v[4];
+    unpack<float>(q, v);
+    return fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
+}
+template <>
+__device__ __forceinline__ float largest<__nv_bfloat16>(const Words& q) {
+    __nv_bfloat162 p[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) p[k] = *reinterpret_cast<const __nv_bfloat162*>(&q.w[k]);
+    const __nv_bfloat162 m = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3]));
+    return fmaxf(__low2float(m), __high2float(m));
+}
+
+// Sum of a run's 2^(v L - ref).
+template <typename T>
+__device__ __forceinline__ float sum_exp(const Words& q, float ref) {
+    float v[kRun<T>];
+    unpack<T>(q, v);
+    float s = 0.0f;
+#pragma unroll
+    for (int e = 0; e < kRun<T>; ++e) s += exp2_fast(fmaf(v[e], kLog2E, -ref));
+    return s;
+}
+
+// A run of the gradient: k0 2^(v L - ref).
+template <typename T, bool VEC>
+__device__ __forceinline__ void put_run(T* d, const Words& q, float ref, float k0) {
     constexpr int R = kRun<T>;
-    constexpr int U = 4;
-    __shared__ Tally part[kThreads / 32];
+    float v[R];
+    unpack<T>(q, v);
+#pragma unroll
+    for (int e = 0; e < R; ++e) v[e] = k0 * exp2_fast(fmaf(v[e], kLog2E, -ref));
+    if constexpr (VEC) {
+        st_words(d, pack<T>(v));
+    } else {
+#pragma unroll
+        for (int e = 0; e < R; ++e) d[e] = narrow<T>(v[e]);
+    }
+}
+
+// What the second sweep needs of a row.
+struct Second {
+    float ref, k0, slope;
+};
+
+template <typename T, int TPR, bool CLUSTER>
+__global__ void __launch_bounds__(kBlock<TPR>, 1536 / kBlock<TPR>)
+    policy_loss_kernel(dlm_policy_args a, long long total_rows, int ctas, int dvec, float* row_loss) {
+    constexpr int R = kRun<T>;
+    constexpr int GROUPS = kBlock<TPR> / TPR, WARPS = TPR / 32;
+    extern __shared__ uint4 slots[];  // [kHold][block], as many rows of it as a thread has runs
+    __shared__ Tally part[WARPS];
+    __shared__ Tally peers[kMaxCtas];
+    __shared__ Second shared_second;
+    const int t = threadIdx.x % TPR, lane = threadIdx.x & 31;
+    const int rank = CLUSTER ? (int)(blockIdx.x % (unsigned)ctas) : 0;
+    const long long row = CLUSTER ? blockIdx.x / (unsigned)ctas : (long long)blockIdx.x * GROUPS + threadIdx.x / TPR;
     pdl_wait();
     pdl_release();
-    const long long row = blockIdx.x;
+    if (row >= total_rows) return;  // a whole warp of the TPR = 32 form
     const T* z = static_cast<const T*>(a.logits) + row * a.ldl;
     T* d = a.dlogits ? static_cast<T*>(a.dlogits) + row * a.ldd : nullptr;
-    const long long V = a.vocab;
+    const int V = (int)a.vocab;
     const long long token = a.tokens[row];
     const float w = a.weight[row];
     const bool kept = w != 0.0f && token >= 0 && token < V;
-    // elements before the first 16-byte boundary (both arrays share it when vec is set)
-    long long head = vec ? (long long)(((16u - ((uint32_t)(uintptr_t)z & 15u)) & 15u) / sizeof(T)) : V;
-    if (head > V) head = V;
-    const long long runs = (V - head) / R, tail = head + runs * R;
+    // elements before the first 16-byte boundary of the row, then runs, then the rest
+    const int head = min(V, (int)(((16u - ((uint32_t)(uintptr_t)z & 15u)) & 15u) / sizeof(T)));
+    const int runs = (V - head) / R, tail = head + runs * R;
+    const int share = CLUSTER ? (runs + ctas - 1) / ctas : runs;
+    const int first = rank * share, mine = min(runs - first, share) - t;  // this thread's runs are first + t + k TPR, k TPR < mine
+    const bool has_head = rank == 0 && t < head, has_tail = (!CLUSTER || rank == ctas - 1) && t < V - tail;
+    const T* zp = z + head + (long long)(first + t) * R;
+    T* dp = d + head + (long long)(first + t) * R;
     if (!kept) {  // contributes nothing, whatever its logits hold
         if (d) {
-            for (long long k = threadIdx.x; k < head; k += kThreads) d[k] = narrow<T>(0.0f);
-            for (long long r = threadIdx.x; r < runs; r += kThreads) st_words(d + head + r * R, Words{{0u, 0u, 0u, 0u}});
-            for (long long k = tail + threadIdx.x; k < V; k += kThreads) d[k] = narrow<T>(0.0f);
+            const float zeros[R] = {};
+            for (int r = 0; r < mine; r += TPR) {
+                T* to = dp + (long long)r * R;
+                if (dvec) {
+                    st_words(to, pack<T>(zeros));
+                } else {
+#pragma unroll
+                    for (int e = 0; e < R; ++e) to[e] = narrow<T>(0.0f);
+                }
+            }
+            if (has_head) d[t] = narrow<T>(0.0f);
+            if (has_tail) d[tail + t] = narrow<T>(0.0f);
         }
-        if (threadIdx.x == 0) {
+        if (rank == 0 && t == 0) {
             a.logp[row] = 0.0f;
-            a.row_loss[row] = 0.0f;
+            row_loss[row] = 0.0f;
         }
         return;
     }
+    if constexpr (CLUSTER) cluster_arrive_relaxed();
+    const int held = min(kHold, (mine + TPR - 1) / TPR);  // not above 0: none
+    const Words* hold = reinterpret_cast<const Words*>(slots + threadIdx.x);
+    {
+        uint32_t to = (uint32_t)__cvta_generic_to_shared(slots + threadIdx.x);
+        const T* from = zp;
+#pragma unroll 4
+        for (int u = 0; u < held; ++u, to += kBlock<TPR> * 16, from += TPR * R) copy_async(to, from);
+    }
     const float zt = widen(z[token]);
-    Tally t = {-INFINITY, 0.0f};
-    for (long long k = threadIdx.x; k < head; k += kThreads) {
-        const float v = widen(z[k]);
-        tally_values<1>(t, &v);
+    const float zh = has_head ? widen(z[t]) : -INFINITY, ze = has_tail ? widen(z[tail + t]) : -INFINITY;
+    copy_wait();
+    float m = fmaxf(zh, ze);
+#pragma unroll 4
+    for (int u = 0; u < held; ++u) m = fmaxf(m, largest<T>(hold[u * kBlock<TPR>]));
+    Tally sum = {reference(m), 0.0f};
+    {
+        const float ref = finite_ref(sum.c);
+        if (has_head) sum.s += exp2_fast(fmaf(zh, kLog2E, -ref));
+        if (has_tail) sum.s += exp2_fast(fmaf(ze, kLog2E, -ref));
+#pragma unroll 4
+        for (int u = 0; u < held; ++u) sum.s += sum_exp<T>(hold[u * kBlock<TPR>], ref);
     }
-    for (long long k = tail + threadIdx.x; k < V; k += kThreads) {
-        const float v = widen(z[k]);
-        tally_values<1>(t, &v);
+    for (int r = kHold * TPR; r < mine; r += TPR) {
+        const Words x = ld_words(zp + (long long)r * R);
+        const float c = reference(largest<T>(x));
+        if (c > sum.c) {
+            sum.s *= exp2_fast(sum.c - c);
+            sum.c = c;
+        }
+        sum.s += sum_exp<T>(x, finite_ref(sum.c));
     }
-    for (long long r0 = threadIdx.x; r0 < runs; r0 += U * kThreads) {
-        Words q[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (r0 + u * kThreads < runs) q[u] = ld_words(z + head + (r0 + u * kThreads) * R);
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (r0 + u * kThreads < runs) {
-                float v[R];
-                unpack<T>(q[u], v);
-                tally_values<R>(t, v);
-            }
+    sum = warp_total(sum);
+    if constexpr (TPR > 32) {
+        if (lane == 0) part[threadIdx.x >> 5] = sum;
+        __syncthreads();
+        if (threadIdx.x < 32) sum = warp_total(lane < WARPS ? part[lane] : Tally{-INFINITY, 0.0f});
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const Tally other = {__shfl_xor_sync(0xffffffffu, t.c, o), __shfl_xor_sync(0xffffffffu, t.s, o)};
-        t = join(t, other);
+    if constexpr (CLUSTER) {
+        // the first warp exchanges the totals; the others only take part in the barriers
+        cluster_wait();  // every CTA of the cluster runs: its shared memory may be written
+        if (threadIdx.x < 32) {
+            if (lane < ctas) cg::this_cluster().map_shared_rank(peers, lane)[rank] = sum;
+            cluster_arrive_release();
+            cluster_wait();
+            sum = warp_total(lane < ctas ? peers[lane] : Tally{-INFINITY, 0.0f});
+        } else {
+            cluster_arrive_relaxed();
+        }
     }
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = t;
-    __syncthreads();
-    t = part[0];
-    for (int k = 1; k < kThreads / 32; ++k) t = join(t, part[k]);
-    const RowOutcome o = row_outcome(zt, t, w, a.advantage[row], a.old_logp[row], a.ref_logp != nullptr,
-                                     a.ref_logp ? a.ref_logp[row] : 0.0f, a.lo, a.hi, a.kl);
-    if (threadIdx.x == 0) {
-        a.logp[row] = o.logp;
-        a.row_loss[row] = o.loss;
+    Second two = {0.0f, 0.0f, 0.0f};
+    if (TPR == 32 || threadIdx.x < 32) {
+        const RowOutcome o = row_outcome(zt, sum, w, a.advantage[row], a.old_logp[row], a.ref_logp != nullptr,
+                                         a.ref_logp ? a.ref_logp[row] : 0.0f, a.lo, a.hi, a.kl);
+        if (rank == 0 && t == 0) {
+            a.logp[row] = o.logp;
+            row_loss[row] = o.loss;
+        }
+        // 2^24 moved from the factor into the exponent: results below 2^-126 / |k0| leave exp2_fast as normal numbers
+        two = {finite_ref(sum.c) - 24.0f, -__fdividef(o.slope, sum.s) * 0x1p-24f, o.slope};
+        if (TPR > 32 && threadIdx.x == 0) shared_second = two;
     }
+    if constexpr (TPR > 32) {
+        __syncthreads();
+        two = shared_second;
+    }
+    if constexpr (CLUSTER)
+        if (threadIdx.x >= 32) cluster_wait();
     if (!d) return;
-    // 2^24 moved from the factor into the exponent: results below 2^-126 / |k0| leave exp2_fast as normal numbers
-    const float ref = finite_ref(t.c) - 24.0f, k0 = -o.slope / t.s * 0x1p-24f;
-    for (long long k = threadIdx.x; k < head; k += kThreads)
-        d[k] = narrow<T>(k0 * exp2_fast(fmaf(widen(z[k]), kLog2E, -ref)));
-    for (long long k = tail + threadIdx.x; k < V; k += kThreads)
-        d[k] = narrow<T>(k0 * exp2_fast(fmaf(widen(z[k]), kLog2E, -ref)));
-    for (long long r0 = threadIdx.x; r0 < runs; r0 += U * kThreads) {
-        Words q[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (r0 + u * kThreads < runs) q[u] = ld_words(z + head + (r0 + u * kThreads) * R);
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (r0 + u * kThreads < runs) {
-                float v[R];
-                unpack<T>(q[u], v);
-#pragma unroll
-                for (int e = 0; e < R; ++e) v[e] = k0 * exp2_fast(fmaf(v[e], kLog2E, -ref));
-                st_words(d + head + (r0 + u * kThreads) * R, pack<T>(v));
-            }
+    if (dvec) {
+#pragma unroll 4
+        for (int u = 0; u < held; ++u) put_run<T, true>(dp + u * TPR * R, hold[u * kBlock<TPR>], two.ref, two.k0);
+    } else {
+        for (int u = 0; u < held; ++u) put_run<T, false>(dp + u * TPR * R, hold[u * kBlock<TPR>], two.ref, two.k0);
     }
-    __syncthreads();  // the token's own element is written once more, after the sweep
-    if (threadIdx.x == 0) d[token] = narrow<T>(fmaf(k0, exp2_fast(fmaf(zt, kLog2E, -ref)), o.slope));
+    for (int r = kHold * TPR; r < mine; r += TPR)
+        if (dvec)
+            put_run<T, true>(dp + (long long)r * R, ld_words(zp + (long long)r * R), two.ref, two.k0);
+        else
+            put_run<T, false>(dp + (long long)r * R, ld_words(zp + (long long)r * R), two.ref, two.k0);
+    if (has_head) d[t] = narrow<T>(two.k0 * exp2_fast(fmaf(zh, kLog2E, -two.ref)));
+    if (has_tail) d[tail + t] = narrow<T>(two.k0 * exp2_fast(fmaf(ze, kLog2E, -two.ref)));
+    // the token's own element, once more by the thread that has just written it
+    const int at = (int)token - head, run = at / R - first;
+    const bool in_run = at >= 0 && (int)token < tail && run >= 0 && run - t < mine && run % TPR == t;
+    if (in_run || (has_head && token == t) || (has_tail && token == tail + t))
+        d[token] = narrow<T>(fmaf(two.k0, exp2_fast(fmaf(zt, kLog2E, -two.ref)), two.slope));
 }
 
-// loss_i = sum of the node's row losses, in a fixed order.
-__global__ void __launch_bounds__(256) policy_sum_kernel(long long rows, const float* row_loss, float* loss) {
-    __shared__ double part[8];
+// loss_i = sum of the node's row losses, in a fixed order: each of a cluster's CTAs sums a range, the first adds the parts.
+__global__ void __launch_bounds__(512) policy_sum_kernel(long long rows, const float* row_loss, float* loss) {
+    __shared__ double part[16];
+    __shared__ double parts[kMaxCtas];
+    cg::cluster_group cluster = cg::this_cluster();
+    const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int node = blockIdx.x / ctas;
+    const long long share = (rows + ctas - 1) / ctas;
+    const long long lo = rank * share, hi = min(rows, lo + share);
+    const float* mine = row_loss + node * rows;
     pdl_wait();
     pdl_release();
     double s = 0.0;
-    for (long long r = threadIdx.x; r < rows; r += 256) s += (double)row_loss[blockIdx.x * rows + r];
+#pragma unroll 8
+    for (long long r = lo + threadIdx.x; r < hi; r += 512) s += (double)mine[r];
     s = warp_sum(s);
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = s;
-    __syncthreads();
+    cluster.sync();
     if (threadIdx.x == 0) {
-        for (int k = 1; k < 8; ++k) s += part[k];
-        loss[blockIdx.x] = (float)s;
+        s = part[0];
+        for (int k = 1; k < 16; ++k) s += part[k];
+        *cluster.map_shared_rank(&parts[rank], 0) = s;
+    }
+    cluster.sync();
+    if (rank == 0 && threadIdx.x == 0) {
+        s = parts[0];
+        for (int k = 1; k < ctas; ++k) s += parts[k];
+        loss[node] = (float)s;
     }
 }
 
+template <typename T, int TPR, bool CLUSTER>
+cudaError_t run(const dlm_policy_args& a, int ctas, float* row_loss, cudaStream_t s) {
+    constexpr int GROUPS = kBlock<TPR> / TPR;
+    const long long rows = a.n * a.rows;
+    const bool dvec = a.dlogits && (uintptr_t)a.logits % 16 == (uintptr_t)a.dlogits % 16 &&
+                      (a.ldl * (int64_t)sizeof(T)) % 16 == (a.ldd * (int64_t)sizeof(T)) % 16;
+    const long long blocks = CLUSTER ? rows * ctas : (rows + GROUPS - 1) / GROUPS;
+    const int64_t share = (a.vocab / kRun<T> + ctas - 1) / ctas;
+    const size_t smem = (size_t)std::min<int64_t>(kHold, (share + TPR - 1) / TPR) * kBlock<TPR> * 16;
+    auto kern = policy_loss_kernel<T, TPR, CLUSTER>;
+    if (smem > 48 * 1024) {
+        const cudaError_t err = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (err != cudaSuccess) return err;
+    }
+    return launch_overlapped(kern, dim3((unsigned)blocks), dim3(kBlock<TPR>), smem, s, CLUSTER ? ctas : 1, a, rows, ctas,
+                             (int)dvec, row_loss);
+}
+
+template <typename T, int TPR>
+cudaError_t run_shared(const dlm_policy_args& a, int ctas, float* row_loss, cudaStream_t s) {
+    return ctas > 1 ? run<T, TPR, true>(a, ctas, row_loss, s) : run<T, TPR, false>(a, 1, row_loss, s);
+}
+
 template <typename T>
-cudaError_t launch(const dlm_policy_args& a, cudaStream_t s) {
-    // 16-byte runs need both arrays at the same distance from a 16-byte boundary in every row
-    const bool vec = !a.dlogits || ((uintptr_t)a.logits % 16 == (uintptr_t)a.dlogits % 16 &&
-                                    (a.ldl * (int64_t)sizeof(T)) % 16 == (a.ldd * (int64_t)sizeof(T)) % 16);
-    return launch_overlapped(policy_loss_kernel<T>, dim3((unsigned)(a.n * a.rows)), dim3(kThreads), 0, s, a, (int)vec);
+cudaError_t launch(const dlm_policy_args& a, float* row_loss, cudaStream_t s) {
+    const DeviceInfo& info = device_info();
+    if (!info.ok) return cudaErrorUnknown;
+    const int64_t runs = (a.vocab + kRun<T> - 1) / kRun<T>, rows = a.n * a.rows;
+    if (runs <= 32 * kHold && rows * 32 >= 128 * info.sms) return run<T, 32, false>(a, 1, row_loss, s);
+    // As few CTAs as hold the row in shared memory, and more while the rows leave SMs idle and a thread has more than one
+    // run.  Four nodes x 1024 rows x 131072, bf16: 8 CTAs 335 us, 4 of 512 threads 373, 1 that reads the row twice 409-472.
+    // 8 x 128 x 32768, bf16: 2 CTAs 26.9 us, 1 29.1, 4 30.8.  8 x 2000 x 4096, fp32: 1 CTA of 128 threads 79 us, of 256 91.
+    int ctas = 1;
+    while (ctas < kMaxCtas && (runs > (int64_t)ctas * 256 * kHold || (rows * ctas * 2 <= 2 * info.sms && runs > ctas * 256))) ctas *= 2;
+    if (runs <= 128 * kHold && ctas == 1) return run<T, 128, false>(a, 1, row_loss, s);
+    return run_shared<T, 256>(a, ctas, row_loss, s);
 }
 
 }  // namespace
 
 int dlm_launch_policy_loss(const dlm_policy_args& a, void* stream) {
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    // one row a node: its loss is the node's
+    float* row_loss = a.rows == 1 ? a.loss : a.row_loss;
     if (a.rows > 0) {
-        const cudaError_t err = a.dtype == DLM_G_BF16 ? launch<__nv_bfloat16>(a, s) : launch<float>(a, s);
+        const cudaError_t err = a.dtype == DLM_G_BF16 ? launch<__nv_bfloat16>(a, row_loss, s) : launch<float>(a, row_loss, s);
         dlm_count_launch(1);
         if (err != cudaSuccess) return DLM_ERR_CUDA;
     }
-    const cudaError_t err = launch_overlapped(policy_sum_kernel, dim3(a.n), dim3(256), 0, s, (long long)a.rows,
+    if (a.rows == 1) return DLM_OK;
+    const int ctas = a.rows > 8192 ? kMaxCtas : 1;
+    const cudaError_t err = launch_overlapped(policy_sum_kernel, dim3(a.n * ctas), dim3(512), 0, s, ctas, (long long)a.rows,
                                               (const float*)a.row_loss, a.loss);
     dlm_count_launch(1);
     return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
