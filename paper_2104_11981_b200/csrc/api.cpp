@@ -7,6 +7,7 @@
 #include <cmath>
 #include <cstdint>
 
+#include "dlm_gradients.h"
 #include "dlm_internal.h"
 
 int dlm_lsq_max_splits();
@@ -284,14 +285,16 @@ int dlm_set_tuning(int knob, int value) {
 
 int dlm_kernel_error(int* flag) {
     if (!flag) return DLM_ERR_NULL;
-    int step = 0, lsq = 0, shard = 0;
+    int step = 0, lsq = 0, shard = 0, gradients = 0;
     int rc = dlm_step_take_error(&step);
     if (rc != DLM_OK) return rc;
     rc = dlm_lsq_take_error(&lsq);
     if (rc != DLM_OK) return rc;
     rc = dlm_shard_take_error(&shard);
     if (rc != DLM_OK) return rc;
-    *flag = step != 0 ? step : lsq != 0 ? lsq : shard;
+    rc = dlm_gradient_take_error(&gradients);
+    if (rc != DLM_OK) return rc;
+    *flag = step != 0 ? step : lsq != 0 ? lsq : shard != 0 ? shard : gradients;
     return DLM_OK;
 }
 

@@ -15,12 +15,11 @@ namespace {
 
 int64_t element_bytes(int dtype) { return dtype == DLM_G_BF16 ? 2 : 4; }
 
-// Elements per piece.  A piece of 8192 elements gives each of the 256 threads of a CTA its 128 bytes (64 with bf16)
-// at once; lists too small to give every SM four CTAs of that size are cut finer, down to 1024.
-int piece_elements(int64_t total, int sms) {
-    int64_t want = total / (4 * (int64_t)std::max(1, sms));
-    int e = 8192;
-    while (e > 1024 && e > want) e /= 2;
+// Bytes per piece.  32 KB give each of the 256 threads of a CTA 128 bytes to ask for at once; lists too small to give every
+// SM four CTAs of that size are cut finer, down to 4 KB.
+int64_t piece_bytes(int64_t total, int sms) {
+    int64_t e = 32768;
+    while (e > 4096 && e * 4 * std::max(1, sms) > total) e /= 2;
     return e;
 }
 
@@ -34,6 +33,7 @@ int build(int n, int tensors, const int64_t* sizes, const int* dtypes, const voi
           dlm_gradients& list) {
     list.n = n;
     list.tensors = tensors;
+    list.types = dtypes[0];
     list.offsets.resize(tensors);
     int64_t total = 0;
     std::vector<std::pair<int64_t, int64_t>> spans;
@@ -44,11 +44,13 @@ int build(int n, int tensors, const int64_t* sizes, const int* dtypes, const voi
         list.offsets[t] = offsets ? offsets[t] : total;
         total += sizes[t];
         if (total > ((int64_t)1 << 42)) return DLM_ERR_SHAPE;
+        if (dtypes[t] != dtypes[0]) list.types = -1;
         if (sizes[t] > 0) {
             spans.push_back({list.offsets[t], list.offsets[t] + sizes[t]});
             list.columns = std::max(list.columns, list.offsets[t] + sizes[t]);
         }
     }
+    list.elements = total;
     std::sort(spans.begin(), spans.end());
     for (size_t k = 1; k < spans.size(); ++k)
         if (spans[k].first < spans[k - 1].second) return DLM_ERR_ALIAS;  // two tensors claim a column
@@ -72,25 +74,36 @@ int build(int n, int tensors, const int64_t* sizes, const int* dtypes, const voi
     if (cudaGetDevice(&list.device) != cudaSuccess) return DLM_ERR_CUDA;
     const dlm::DeviceInfo& info = dlm::device_info();
     if (!info.ok) return DLM_ERR_CUDA;
-    const int64_t step = piece_elements(total * n, info.sms);
     int64_t per_node = 0;
-    for (int t = 0; t < tensors; ++t) per_node += (sizes[t] + step - 1) / step;
-    if (per_node * n > 0x7fffffff) return DLM_ERR_UNSUPPORTED;
+    for (int t = 0; t < tensors; ++t) list.bytes += sizes[t] * element_bytes(dtypes[t]);
+    const int64_t step_bytes = piece_bytes(list.bytes * n, info.sms);
+    auto step_of = [&](int t) { return step_bytes / element_bytes(dtypes[t]); };
+    // Pieces are cut where the source's addresses are multiples of 16 bytes, so that all but a tensor's ends are whole
+    // 16-byte runs: a tensor that starts `skew` elements above such an address has its cuts that much earlier.  Every node
+    // gets the same number of pieces, of which the last may be empty.
+    auto most = [&](int t) { return 16 / element_bytes(dtypes[t]) - 1; };
+    for (int t = 0; t < tensors; ++t)
+        if (sizes[t] > 0) per_node += (sizes[t] + most(t) + step_of(t) - 1) / step_of(t);
+    if (per_node * n > 0x3fffffff) return DLM_ERR_UNSUPPORTED;
     list.pieces = (int)per_node;
     std::vector<dlm_piece> pieces;
     pieces.reserve((size_t)per_node * n);
     for (int i = 0; i < n; ++i)
-        for (int t = 0; t < tensors; ++t)
-            for (int64_t at = 0; at < sizes[t]; at += step)
-                pieces.push_back({static_cast<const char*>(data[(size_t)i * tensors + t]) + at * element_bytes(dtypes[t]),
-                                  list.offsets[t] + at, (int32_t)std::min(step, sizes[t] - at),
-                                  dtypes[t] == DLM_G_BF16});
-    std::vector<float> ones(n, 1.0f);
-    std::vector<unsigned> zeros(n, 0u);
-    if (!upload(&list.d_scale, ones) || !upload(&list.d_arrived, zeros)) return DLM_ERR_CUDA;
-    if (!pieces.empty()) {
-        if (!upload(&list.d_pieces, pieces)) return DLM_ERR_CUDA;
-        if (cudaMalloc((void**)&list.d_partial, pieces.size() * sizeof(double)) != cudaSuccess) return DLM_ERR_CUDA;
+        for (int t = 0; t < tensors; ++t) {
+            if (sizes[t] == 0) continue;
+            const char* src = static_cast<const char*>(data[(size_t)i * tensors + t]);
+            const int64_t e = element_bytes(dtypes[t]), step = step_of(t), skew = (int64_t)((uintptr_t)src % 16) / e;
+            const int64_t parts = (sizes[t] + most(t) + step - 1) / step;
+            for (int64_t k = 0; k < parts; ++k) {
+                const int64_t lo = std::min(sizes[t], std::max<int64_t>(0, k * step - skew)), hi = std::min(sizes[t], (k + 1) * step - skew);
+                pieces.push_back({src + lo * e, list.offsets[t] + lo, (int32_t)(hi - lo), dtypes[t] == DLM_G_BF16});
+            }
+        }
+    if (pieces.empty()) return DLM_OK;
+    if (!upload(&list.d_pieces, pieces)) return DLM_ERR_CUDA;
+    if (total > DLM_SMALL_NODE) {
+        if (cudaMalloc((void**)&list.d_scale, n * sizeof(float)) != cudaSuccess ||
+            cudaMalloc((void**)&list.d_partial, (size_t)n * DLM_CLIP_CTAS_PER_SM * info.sms * DLM_CLIP_WARPS * sizeof(double)) != cudaSuccess) return DLM_ERR_CUDA;
     }
     return DLM_OK;
 }
@@ -150,7 +163,6 @@ int gradients_destroy(dlm_gradients* list) {
     if (list->d_pieces) cudaFree(list->d_pieces);
     if (list->d_partial) cudaFree(list->d_partial);
     if (list->d_scale) cudaFree(list->d_scale);
-    if (list->d_arrived) cudaFree(list->d_arrived);
     delete list;
     return DLM_OK;
 }
@@ -158,7 +170,7 @@ int gradients_destroy(dlm_gradients* list) {
 int gradient_norm(dlm_gradients* list, int kind, float* norms, void* cuda_stream) {
     int rc = check_call(list, kind, norms);
     if (rc != DLM_OK) return rc;
-    return dlm_launch_gradient_norm(*list, kind, 1.0f, norms, cuda_stream);
+    return dlm_launch_gradients(*list, kind, 0.0f, norms, nullptr, DLM_G_F32, 0, cuda_stream);
 }
 
 int gradient_clip(dlm_gradients* list, int kind, float max_norm, float* norms, void* g, int g_dtype, int64_t ldg,
@@ -178,9 +190,7 @@ int gradient_clip(dlm_gradients* list, int kind, float max_norm, float* norms, v
             for (int i = 0; i < list->n; ++i)
                 if (meets_a_source(*list, lo + row * i, lo + row * i + width)) return DLM_ERR_ALIAS;
     }
-    rc = dlm_launch_gradient_norm(*list, kind, max_norm, norms, cuda_stream);
-    if (rc != DLM_OK) return rc;
-    return dlm_launch_gradient_scale(*list, g, g_dtype, ldg, cuda_stream);
+    return dlm_launch_gradients(*list, kind, max_norm, norms, g, g_dtype, ldg, cuda_stream);
 }
 
 }  // extern "C"

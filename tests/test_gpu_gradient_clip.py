@@ -91,7 +91,39 @@ def test_clip_mixed_types_and_order_of_columns():
     _check_clip(nodes, [16_384, 8, 32, 0, 24_000], 0.05, "f32")
 
 
-@pytest.mark.parametrize("n,sizes", [(1, [1]), (1, [2_000_003]), (64, [5]), (2, [0, 0]), (300, [17, 300]), (2, [3] * 500)])
+# nodes above 262144 elements take other kernels: fewer pieces than CTAs, many more, every type and misalignment
+@pytest.mark.parametrize("src,dst,shift", [("f32", "f32", 0), ("f32", "f32", 3), ("bf16", "bf16", 0), ("bf16", "bf16", 5),
+                                           ("bf16", "f32", 1), ("f32", "bf16", 2), ("bf16", "f32", 0), ("f32", "bf16", 0)])
+@pytest.mark.parametrize("n,sizes", [(1, [300_001]), (3, [1, 270_000, 0, 9, 20_001]), (2, [1_500_000, 3, 700_001]), (40, [262_145])])
+def test_clip_of_large_nodes(src, dst, shift, n, sizes):
+    nodes = _nodes(n, sizes, [src] * len(sizes), 21 + shift, shift)
+    for node in nodes[::2]:
+        for t in node:
+            t.mul_(0.01)
+    lst = _check_clip(nodes, None, 0.1, dst)
+    if src == dst:                                                     # the same in place
+        from paper_2104_11981_b200 import binding as B
+        norms, out = torch.empty(n, device=DEV), torch.empty((n, lst.columns), device=DEV, dtype=TYPE[dst])
+        B.gradient_clip(lst, 0.1, norms, out)
+        B.gradient_clip(lst, 0.1, norms)
+        assert all(torch.equal(torch.cat(node), row) for node, row in zip(nodes, out))
+
+
+def test_large_nodes_of_mixed_types():
+    from paper_2104_11981_b200 import binding as B
+    nodes = _nodes(3, [200_003, 17, 100_000, 64], ["bf16", "f32", "f32", "bf16"], 31, 1)
+    lst = _check_clip(nodes, [7, 400_000, 200_100, 300_200], 0.2, "f32")
+    _check_clip(nodes, None, 0.2, "bf16")
+    before, norms = [[to64(t) for t in node] for node in nodes], torch.empty(3, device=DEV)
+    B.gradient_clip(lst, 0.2, norms)
+    for node, old in zip(nodes, before):
+        s = min(1.0, 0.2 / (np.sqrt(sum((x ** 2).sum() for x in old)) + 1e-6))
+        for t, x, typ in zip(node, old, ["bf16", "f32", "f32", "bf16"]):
+            assert np.all(np.abs(to64(t) - s * x) <= np.abs(s * x) * 24 * U + half_unit(typ, s * x) + 1e-45)
+
+
+@pytest.mark.parametrize("n,sizes", [(1, [1]), (1, [2_000_003]), (64, [5]), (2, [0, 0]), (300, [17, 300]), (2, [3] * 500),
+                                     (5, [400_000, 7]), (700, [262_150])])
 def test_norm_over_shapes_and_kinds(n, sizes):
     from paper_2104_11981_b200 import binding as B
     nodes = _nodes(n, sizes, ["f32"] * len(sizes), 5)
@@ -148,10 +180,11 @@ def test_clip_of_views_of_the_stacked_rows():
     assert torch.isfinite(g).all()
 
 
-def test_norm_over_the_whole_range_of_fp32():
+@pytest.mark.parametrize("d", [20_000, 300_000])
+def test_norm_over_the_whole_range_of_fp32(d):
     """Squares that overflow or vanish in fp32 do not reach the norm; a NaN or an infinity does, in its node alone."""
     from paper_2104_11981_b200 import binding as B
-    n, d = 7, 20_000
+    n = 7
     g = torch.empty((n, d), device=DEV).normal_(generator=_gen(4))
     g[0] *= 1e30
     g[1] *= 1e-30
@@ -178,10 +211,11 @@ def test_norm_over_the_whole_range_of_fp32():
     assert got[3] == np.inf and np.isnan(got[4]) and got[0] == float(g[0].abs().max())
 
 
-def test_streams_and_graphs():
+@pytest.mark.parametrize("size", [70_000, 400_000])
+def test_streams_and_graphs(size):
     """On another stream than the current one, and captured: the replay follows the tensors' contents."""
     from paper_2104_11981_b200 import binding as B
-    nodes = _nodes(2, [70_000, 33], ["f32", "f32"], 8)
+    nodes = _nodes(2, [size, 33], ["f32", "f32"], 8)
     lst = B.gradients_build(nodes)
     norms, out = torch.empty(2, device=DEV), torch.empty((2, lst.columns), device=DEV)
     side = torch.cuda.Stream()
