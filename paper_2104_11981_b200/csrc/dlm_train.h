@@ -30,7 +30,7 @@ struct dlm_norm_args {
     int g_dtype;
     float* partial;
 };
-int dlm_norm_max_ctas(int n, int64_t rows);  // row blocks per node that the backward workspace is sized for
+int dlm_norm_max_ctas(int n, int64_t rows, int64_t c);  // row blocks per node that the backward workspace is sized for
 int dlm_launch_layer_norm(const dlm_norm_args& a, void* stream);
 int dlm_launch_layer_norm_grad(const dlm_norm_args& a, void* stream);
 

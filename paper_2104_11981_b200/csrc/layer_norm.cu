@@ -2,10 +2,11 @@
 //   mu = mean_c x ,  rstd = 1 / sqrt(mean_c (x - mu)^2 + eps) ,  y = (x - mu) rstd w + b ;
 // backward, with xh = (x - mu) rstd and v = w dy:
 //   dx = rstd (v - mean_c v - xh mean_c (v xh)) ,  dw = sum_rows dy xh ,  db = sum_rows dy.
-// Both directions are bound by memory: x is read once and y written once; x and dy are read once and dx written
-// once.  A row stays in the registers of the group of threads that owns it (a warp, or a whole CTA), which keep
-// the node's weights too, and, backward, the sums over their rows of dy xh and dy; these are joined by a second
-// kernel in a fixed order.
+// Both directions are bound by memory: x is read once and y written once; x and dy are read once and dx written once.
+// A group of threads (eight lanes of a warp up to a CTA) takes every G-th row of a node.  Rows come into shared memory by
+// asynchronous copies a few rows ahead, which hold no registers, in whole 16-byte chunks wherever the row starts.  A thread
+// keeps its columns' weights in registers, and backward its sums of dy xh and dy over the rows; a second kernel adds these
+// over the groups in a fixed order.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -21,68 +22,275 @@ namespace {
 
 using namespace dlm;
 
-// How a row of c elements is spread over its TPR threads: RUNS runs of LEN elements each, run u of thread t being
-// elements [(u TPR + t) LEN, ...).  LEN = 16 bytes' worth where every row is aligned and c a multiple of it, else 1.
-template <typename T, int LEN, int RUNS, int TPR>
-struct Slice {
-    static constexpr int E = LEN * RUNS;
-    static __device__ __forceinline__ int column(int t, int u) { return (u * TPR + t) * LEN; }
+template <int TPR>
+constexpr int kBlock = TPR < 64 ? 128 : TPR;
+// Rows on their way or in work per group: enough of the short ones to cover the latency.  The widest rows take fewer where
+// shared memory does not hold so many.
+template <int TPR>
+constexpr int kDepth = TPR <= 64 ? 4 : 3;
 
-    // Values of a row, held as they came.
-    struct Raw {
-        uint32_t w[LEN == 1 ? RUNS : RUNS * 4];
-    };
-    static __device__ __forceinline__ Raw load(const T* row, int t, int c) {
-        Raw r;
+// Columns of thread t of a group: E of them, in runs of LEN, run u being columns [(u TPR + t) LEN, ...).  LEN is 16 bytes'
+// worth where every row is aligned and c a multiple of it, else 1.
+template <int LEN, int TPR>
+__device__ __forceinline__ int column(int t, int u) { return (u * TPR + t) * LEN; }
+
+template <int TPR>
+__device__ __forceinline__ void group_barrier() {
+    if constexpr (TPR > 32)
+        __syncthreads();  // the group is the CTA
+    else
+        __syncwarp();
+}
+
+// Sum over the lanes of a warp that belong to the same group.
+template <int TPR>
+__device__ __forceinline__ float lane_sum(float v) {
 #pragma unroll
-        for (int u = 0; u < RUNS; ++u) {
-            const int at = column(t, u);
-            if constexpr (LEN == 1) {
-                r.w[u] = at < c ? __float_as_uint(widen(row[at])) : 0u;
-            } else {
-                Words v = {{0u, 0u, 0u, 0u}};
-                if (at < c) v = ld_words(row + at);
+    for (int o = (TPR < 32 ? TPR : 32) / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// Sum over the warps of a group of what lane 0 of each left in part[], the same in every thread.
+template <int WARPS>
+__device__ __forceinline__ float warps_sum(const float* part) {
+    float v = part[threadIdx.x & (WARPS - 1)];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) r.w[4 * u + k] = v.w[k];
-            }
-        }
-        return r;
+    for (int o = WARPS / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+// Two sums over a group at once: after one exchange each half of the lanes carries one of them.
+template <int TPR>
+__device__ __forceinline__ void pair_sum(float& a, float& b, float (*part)[TPR > 32 ? TPR / 32 : 1]) {
+    constexpr int H = (TPR < 32 ? TPR : 32) / 2, WARPS = TPR / 32;
+    const bool upper = threadIdx.x & H;
+    float v = (upper ? b : a) + __shfl_xor_sync(0xffffffffu, upper ? a : b, H);
+#pragma unroll
+    for (int o = H / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if constexpr (TPR > 32) {
+        if ((threadIdx.x & 15) == 0) part[upper][threadIdx.x >> 5] = v;
+        __syncthreads();
+        v = warps_sum<WARPS>(part[upper]);
     }
-    static __device__ __forceinline__ void values(const Raw& r, float* v) {
-        if constexpr (LEN == 1) {
+    const float w = __shfl_xor_sync(0xffffffffu, v, H);
+    a = upper ? w : v;
+    b = upper ? v : w;
+}
+
+// Bytes of shared memory for a row: its chunks, wherever it starts within the first.
+__host__ __device__ inline int row_bytes(int c, int esz) { return (c * esz + 30) / 16 * 16; }
+
+// A row's place in its buffer starts as many bytes into the first chunk as in memory.
+template <typename T>
+__device__ __forceinline__ int row_skew(const T* row) { return (int)((uintptr_t)row & 15u); }
+
+__device__ __forceinline__ void copy_chunk(uint32_t to, const void* from, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+// Starts the copy of a row into `buf`.  `array` is where the array begins: bytes before a row belong to it but for the
+// first row's, whose first chunk is then copied element by element.
+template <typename T, int LEN, int TPR>
+__device__ __forceinline__ void fetch_row(unsigned char* buf, const T* row, const T* array, int c, int t) {
+    const int skew = LEN > 1 ? 0 : row_skew(row), end = skew + c * (int)sizeof(T);
+    const unsigned char* from = reinterpret_cast<const unsigned char*>(row) - skew;
+    const uint32_t to = (uint32_t)__cvta_generic_to_shared(buf);
+    int at = t * 16;
+    if (LEN == 1 && from < reinterpret_cast<const unsigned char*>(array)) {
+        const int first = min(end, 16);
+        for (int b = skew + t * (int)sizeof(T); b < first; b += TPR * (int)sizeof(T))
+            *reinterpret_cast<T*>(buf + b) = *reinterpret_cast<const T*>(from + b);
+        at += 16;
+    }
+#pragma unroll 4
+    for (; at < end; at += TPR * 16) copy_chunk(to + at, from + at, min(16, end - at));
+}
+__device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
+// This thread's values of a row in shared memory; 0 beyond c.
+template <typename T, int LEN, int E, int TPR>
+__device__ __forceinline__ void row_values(const unsigned char* buf, int skew, int c, int t, float* v) {
+    const T* row = reinterpret_cast<const T*>(buf + (LEN > 1 ? 0 : skew));
 #pragma unroll
-            for (int u = 0; u < RUNS; ++u) v[u] = __uint_as_float(r.w[u]);
+    for (int u = 0; u < E / LEN; ++u) {
+        const int at = column<LEN, TPR>(t, u);
+        if constexpr (LEN > 1) {
+            Words a = {{0u, 0u, 0u, 0u}};
+            if (at < c) a = ld_words(row + at);
+            unpack<T>(a, v + u * LEN);
         } else {
-#pragma unroll
-            for (int u = 0; u < RUNS; ++u) {
-                Words a = {{r.w[4 * u], r.w[4 * u + 1], r.w[4 * u + 2], r.w[4 * u + 3]}};
-                unpack<T>(a, v + u * LEN);
-            }
+            v[u] = at < c ? widen(row[at]) : 0.0f;
         }
     }
-    static __device__ __forceinline__ void store(T* row, int t, int c, const float* v) {
+}
+// This thread's parameters.
+template <int LEN, int E, int TPR>
+__device__ __forceinline__ void params(const float* p, int c, int t, float* v) {
 #pragma unroll
-        for (int u = 0; u < RUNS; ++u) {
-            const int at = column(t, u);
-            if (at < c) {
-                if constexpr (LEN == 1)
-                    row[at] = narrow<T>(v[u]);
-                else
-                    st_words(row + at, pack<T>(v + u * LEN));
-            }
+    for (int u = 0; u < E / LEN; ++u)
+#pragma unroll
+        for (int k = 0; k < LEN; ++k) {
+            const int at = column<LEN, TPR>(t, u) + k;
+            v[u * LEN + k] = at < c ? p[at] : 0.0f;
+        }
+}
+// One run of the above.
+template <typename T, int LEN, int TPR>
+__device__ __forceinline__ void one_run(const unsigned char* buf, int skew, int c, int t, int u, float* v) {
+    const T* row = reinterpret_cast<const T*>(buf + (LEN > 1 ? 0 : skew));
+    const int at = column<LEN, TPR>(t, u);
+    if constexpr (LEN > 1) {
+        Words a = {{0u, 0u, 0u, 0u}};
+        if (at < c) a = ld_words(row + at);
+        unpack<T>(a, v);
+    } else {
+        v[0] = at < c ? widen(row[at]) : 0.0f;
+    }
+}
+// Results: straight to memory where rows are aligned, else into a buffer that lies like the row, which flush_row empties
+// after a barrier.
+template <typename T, int LEN, int E, int TPR>
+__device__ __forceinline__ void put_values(T* row, unsigned char* buf, int c, int t, const float* v) {
+    T* staged = reinterpret_cast<T*>(buf + (LEN > 1 ? 0 : row_skew(row)));
+#pragma unroll
+    for (int u = 0; u < E / LEN; ++u) {
+        const int at = column<LEN, TPR>(t, u);
+        if (at < c) {
+            if constexpr (LEN > 1)
+                st_words(row + at, pack<T>(v + u * LEN));
+            else
+                staged[at] = narrow<T>(v[u]);
         }
     }
-    // Parameters (fp32, any alignment): the columns this thread owns.
-    static __device__ __forceinline__ void params(const float* p, int t, int c, float* v) {
+}
+template <typename T, int TPR>
+__device__ __forceinline__ void flush_row(T* row, const unsigned char* buf, int c, int t) {
+    const int skew = row_skew(row), end = skew + c * (int)sizeof(T);
+    unsigned char* to = reinterpret_cast<unsigned char*>(row) - skew;
+    const int lo = skew ? 16 : 0, hi = end & ~15;  // whole chunks
+#pragma unroll 4
+    for (int at = lo + t * 16; at < hi; at += TPR * 16) st_words(to + at, ld_words(buf + at));
+    for (int at = skew + t * (int)sizeof(T); at < min(lo, end); at += TPR * (int)sizeof(T))
+        *reinterpret_cast<T*>(to + at) = *reinterpret_cast<const T*>(buf + at);
+    for (int at = max(hi, lo) + t * (int)sizeof(T); at < end; at += TPR * (int)sizeof(T))
+        *reinterpret_cast<T*>(to + at) = *reinterpret_cast<const T*>(buf + at);
+}
+
+// Columns of c that the lanes of this thread's warp (or group) own.
+template <int LEN, int E, int TPR>
+__device__ __forceinline__ int owned_columns(int c, int t) {
+    int n = 0;
 #pragma unroll
-        for (int u = 0; u < RUNS; ++u)
-#pragma unroll
-            for (int k = 0; k < LEN; ++k) {
-                const int at = column(t, u) + k;
-                v[u * LEN + k] = at < c ? __ldg(p + at) : 0.0f;
-            }
+    for (int u = 0; u < E / LEN; ++u) {
+        constexpr int lanes = TPR < 32 ? TPR : 32;
+        n += min(max(c - column<LEN, TPR>(t / lanes * lanes, u), 0), lanes * LEN);
     }
-};
+    return n;
+}
+
+template <typename T, int LEN, int E, int TPR, int D>
+__global__ void __launch_bounds__(kBlock<TPR>)
+    layer_norm_kernel(long long rows, int c, const T* x, long long ldx, const float* weight, long long ldw,
+                      const float* bias, long long ldb, float eps, T* y, long long ldy, float* mean, float* rstd) {
+    constexpr int GROUPS = kBlock<TPR> / TPR, WARPS = TPR / 32;
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ float part[2][2][TPR > 32 ? WARPS : 1];  // sum and squared deviations of each warp
+    const int node = blockIdx.y, t = threadIdx.x % TPR, group = threadIdx.x / TPR;
+    const int rb = row_bytes(c, sizeof(T));
+    unsigned char* in = smem + (size_t)group * (D + (LEN == 1)) * rb;
+    unsigned char* out = in + (size_t)D * rb;  // where rows are not aligned
+    const long long stride = (long long)gridDim.x * GROUPS;
+    const long long first = (long long)blockIdx.x * GROUPS + group, base = (long long)node * rows;
+    const T* fetch = x + (base + first) * ldx;  // the next row to ask for
+    const T* row = fetch;
+    T* to = y + (base + first) * ldy;
+    long long asked = first;
+    pdl_wait();
+    pdl_release();
+#pragma unroll
+    for (int k = 0; k < D - 1; ++k) {
+        if (asked < rows) fetch_row<T, LEN, TPR>(in + k * rb, fetch, x, c, t);
+        commit_copies();
+        asked += stride;
+        fetch += stride * ldx;
+    }
+    float w[E], b[E];
+    params<LEN, E, TPR>(weight + node * ldw, c, t, w);
+#pragma unroll
+    for (int e = 0; e < E; ++e) b[e] = 0.0f;
+    if (bias) params<LEN, E, TPR>(bias + node * ldb, c, t, b);
+    const float inv_c = 1.0f / (float)c;
+    const float owned = (float)owned_columns<LEN, E, TPR>(c, t);
+    const float inv_owned = owned > 0.0f ? 1.0f / owned : 0.0f;
+    // the share of the warp whose sums this lane takes between the warps
+    const int other = (threadIdx.x & (WARPS > 1 ? WARPS - 1 : 0)) * 32;
+    const float their = WARPS > 1 ? (float)owned_columns<LEN, E, TPR>(c, other) : 0.0f, inv_their = their > 0.0f ? 1.0f / their : 0.0f;
+    int slot = 0, side = 0;
+    // groups of a warp leave together: the loop counts the rows of its first group
+    long long r = first;
+    for (long long lead = TPR < 32 ? first - group % (32 / (TPR < 32 ? TPR : 32)) : first; lead < rows; lead += stride) {
+        const int next = slot == 0 ? D - 1 : slot - 1;
+        if (asked < rows) fetch_row<T, LEN, TPR>(in + next * rb, fetch, x, c, t);
+        commit_copies();
+        asked += stride;
+        fetch += stride * ldx;
+        wait_copies<D - 1>();
+        group_barrier<TPR>();
+        const bool live = r < rows;
+        float v[E];
+        row_values<T, LEN, E, TPR>(in + slot * rb, row_skew(row), live ? c : 0, t, v);
+        float sum = 0.0f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum += v[e];
+        sum = lane_sum<TPR>(sum);
+        // deviations from the warp's own mean first: one exchange between the warps instead of two
+        const float near = sum * inv_owned;
+        float sq = 0.0f;
+#pragma unroll
+        for (int u = 0; u < E / LEN; ++u)
+            if (column<LEN, TPR>(t, u) < c)
+#pragma unroll
+                for (int k = 0; k < LEN; ++k) {
+                    const float dev = v[u * LEN + k] - near;
+                    sq = fmaf(dev, dev, sq);
+                }
+        sq = lane_sum<TPR>(sq);
+        float mu = near;
+        if constexpr (TPR > 32) {
+            // and then sum_w [sq_w + n_w (mean_w - mu)^2]
+            if ((threadIdx.x & 31) == 0) {
+                part[side][0][threadIdx.x >> 5] = sum;
+                part[side][1][threadIdx.x >> 5] = sq;
+            }
+            __syncthreads();
+            const float ws = part[side][0][threadIdx.x & (WARPS - 1)];
+            float total = ws;
+#pragma unroll
+            for (int o = WARPS / 2; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+            mu = total * inv_c;
+            const float off = fmaf(ws, inv_their, -mu);
+            sq = fmaf(their * off, off, part[side][1][threadIdx.x & (WARPS - 1)]);
+#pragma unroll
+            for (int o = WARPS / 2; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
+            side ^= 1;
+        }
+        const float rs = rsqrtf(fmaf(sq, inv_c, eps));
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = fmaf((v[e] - mu) * rs, w[e], b[e]);
+        if (live) put_values<T, LEN, E, TPR>(to, out, c, t, v);
+        if (t == 0 && live) {
+            mean[base + r] = mu;
+            rstd[base + r] = rs;
+        }
+        group_barrier<TPR>();  // the slot may be filled again, and the results are in their buffer
+        if (LEN == 1 && live) flush_row<T, TPR>(to, out, c, t);
+        if (++slot == D) slot = 0;
+        r += stride;
+        row += stride * ldx;
+        to += stride * ldy;
+    }
+    wait_copies<0>();
+}
 
 // Sums over the TPR threads of a row's group, the same in each of them.  Groups of more than a warp use `part`
 // (two buffers, so that one barrier per call suffices); they are the whole CTA, so the barrier is uniform.
@@ -101,70 +309,6 @@ __device__ __forceinline__ void group_sum(float (&v)[N], float* part, int& turn)
         const int lane = threadIdx.x & 31;
 #pragma unroll
         for (int k = 0; k < N; ++k) v[k] = warp_sum(lane < W ? buf[k * W + lane] : 0.0f);
-    }
-}
-
-template <int TPR>
-constexpr int kBlock = TPR < 128 ? 128 : TPR;
-
-template <typename T, int LEN, int RUNS, int TPR>
-__global__ void __launch_bounds__(kBlock<TPR>)
-    layer_norm_kernel(long long rows, int c, const T* x, long long ldx, const float* weight, long long ldw,
-                      const float* bias, long long ldb, float eps, T* y, long long ldy, float* mean, float* rstd) {
-    using S = Slice<T, LEN, RUNS, TPR>;
-    constexpr int GROUPS = kBlock<TPR> / TPR;
-    __shared__ float part[TPR > 32 ? 2 * TPR / 32 : 1];
-    int turn = 0;
-    const int node = blockIdx.y;
-    const int t = threadIdx.x % TPR;
-    const long long stride = (long long)gridDim.x * GROUPS;
-    long long r = (long long)blockIdx.x * GROUPS + threadIdx.x / TPR;
-    pdl_wait();
-    pdl_release();
-    if (r >= rows) return;  // whole groups leave
-    x += (long long)node * rows * ldx;
-    y += (long long)node * rows * ldy;
-    typename S::Raw next = S::load(x + r * ldx, t, c);
-    float w[S::E], b[S::E];
-    S::params(weight + node * ldw, t, c, w);
-    if (bias) {
-        S::params(bias + node * ldb, t, c, b);
-    } else {
-#pragma unroll
-        for (int e = 0; e < S::E; ++e) b[e] = 0.0f;
-    }
-    const float inv_c = 1.0f / (float)c;
-    while (r < rows) {
-        float v[S::E];
-        S::values(next, v);
-        const long long here = r;
-        r += stride;
-        if (r < rows) next = S::load(x + r * ldx, t, c);
-        float sum[1] = {0.0f};
-#pragma unroll
-        for (int e = 0; e < S::E; ++e) sum[0] += v[e];
-        group_sum<TPR>(sum, part, turn);
-        const float mu = sum[0] * inv_c;
-        float sq[1] = {0.0f};
-#pragma unroll
-        for (int u = 0; u < RUNS; ++u) {
-            if (S::column(t, u) < c) {
-#pragma unroll
-                for (int k = 0; k < LEN; ++k) {
-                    const float dev = v[u * LEN + k] - mu;
-                    sq[0] = fmaf(dev, dev, sq[0]);
-                }
-            }
-        }
-        group_sum<TPR>(sq, part, turn);
-        const float rs = rsqrtf(fmaf(sq[0], inv_c, eps));
-#pragma unroll
-        for (int e = 0; e < S::E; ++e) v[e] = fmaf((v[e] - mu) * rs, w[e], b[e]);
-        S::store(y + here * ldy, t, c, v);
-        if (t == 0) {
-            mean[(long long)node * rows + here] = mu;
-            rstd[(long long)node * rows + here] = rs;
-        }
     }
 }
 
@@ -200,96 +344,174 @@ __global__ void __launch_bounds__(1024)
     }
 }
 
-// partial[((node G + cta) 2 + {0: dw, 1: db}) c + column]: the sums over the rows of one CTA.
-template <typename T, int LEN, int RUNS, int TPR>
+// partial[((node G + group) 2 + {0: dw, 1: db}) c + column]: the sums over the rows of one CTA.
+template <typename T, int LEN, int E, int TPR, int D>
 __global__ void __launch_bounds__(kBlock<TPR>)
     layer_norm_grad_kernel(long long rows, int c, const T* x, long long ldx, const T* dy, long long lddy,
                            const float* weight, long long ldw, const float* mean, const float* rstd, T* dx, long long lddx,
                            float* partial) {
-    using S = Slice<T, LEN, RUNS, TPR>;
     constexpr int GROUPS = kBlock<TPR> / TPR;
-    __shared__ float part[TPR > 32 ? 4 * TPR / 32 : 1];
-    __shared__ float joined[GROUPS > 1 ? (GROUPS - 1) * 32 * S::E : 1];
-    int turn = 0;
-    const int node = blockIdx.y;
-    const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
+    constexpr bool HOLD = E <= 16;  // the row's values stay in registers between the two sweeps, else they are read again
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ float part[2][2][TPR > 32 ? TPR / 32 : 1];
+    const int node = blockIdx.y, t = threadIdx.x % TPR, group = threadIdx.x / TPR;
+    const int rb = row_bytes(c, sizeof(T));
+    float* w = reinterpret_cast<float*>(smem) + t;  // weights that the registers do not hold: [E][TPR]
+    unsigned char* in = smem + (HOLD ? 0 : (size_t)E * TPR * 4) + (size_t)group * (2 * D + (LEN == 1)) * rb;
+    unsigned char* out = in + (size_t)2 * D * rb;  // where rows are not aligned
     const long long stride = (long long)gridDim.x * GROUPS;
-    long long r = (long long)blockIdx.x * GROUPS + group;
+    const long long first = (long long)blockIdx.x * GROUPS + group, base = (long long)node * rows;
+    const T *xf = x + (base + first) * ldx, *gf = dy + (base + first) * lddy;  // the next row to ask for
+    const T *xr = xf, *gr = gf;
+    T* to = dx + (base + first) * lddx;
+    long long asked = first;
+    mean += base;
+    rstd += base;
     pdl_wait();
     pdl_release();
-    const long long first = (long long)node * rows;
-    x += first * ldx;
-    dy += first * lddy;
-    dx += first * lddx;
-    mean += first;
-    rstd += first;
-    float w[S::E], dw[S::E], db[S::E];
-    S::params(weight + node * ldw, t, c, w);
 #pragma unroll
-    for (int e = 0; e < S::E; ++e) dw[e] = db[e] = 0.0f;
+    for (int k = 0; k < D - 1; ++k) {
+        if (asked < rows) {
+            fetch_row<T, LEN, TPR>(in + 2 * k * rb, xf, x, c, t);
+            fetch_row<T, LEN, TPR>(in + (2 * k + 1) * rb, gf, dy, c, t);
+        }
+        commit_copies();
+        asked += stride;
+        xf += stride * ldx;
+        gf += stride * lddy;
+    }
+    float wv[HOLD ? E : 1];
+    if constexpr (HOLD) {
+        params<LEN, E, TPR>(weight + node * ldw, c, t, wv);
+    } else {
+        float own[E];
+        params<LEN, E, TPR>(weight + node * ldw, c, t, own);
+#pragma unroll
+        for (int e = 0; e < E; ++e) w[e * TPR] = own[e];  // read back by this thread alone
+    }
+    float dw[E], db[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) dw[e] = db[e] = 0.0f;
     const float inv_c = 1.0f / (float)c;
-    typename S::Raw nx, ny;
+    int slot = 0, side = 0;
     float nmu = 0.0f, nrs = 0.0f;
-    if (r < rows) {
-        nx = S::load(x + r * ldx, t, c);
-        ny = S::load(dy + r * lddy, t, c);
-        nmu = mean[r];
-        nrs = rstd[r];
+    if (first < rows) {
+        nmu = mean[first];
+        nrs = rstd[first];
     }
-    while (r < rows) {
-        float xh[S::E], v[S::E];
-        S::values(nx, xh);
-        S::values(ny, v);
-        const float mu = nmu, rs = nrs;
-        const long long here = r;
-        r += stride;
-        if (r < rows) {
-            nx = S::load(x + r * ldx, t, c);
-            ny = S::load(dy + r * lddy, t, c);
-            nmu = mean[r];
-            nrs = rstd[r];
+    // groups of a warp leave together: the loop counts the rows of its first group
+    long long r = first;
+    for (long long lead = TPR < 32 ? first - group % (32 / (TPR < 32 ? TPR : 32)) : first; lead < rows; lead += stride) {
+        const int next = slot == 0 ? D - 1 : slot - 1;
+        if (asked < rows) {
+            fetch_row<T, LEN, TPR>(in + 2 * next * rb, xf, x, c, t);
+            fetch_row<T, LEN, TPR>(in + (2 * next + 1) * rb, gf, dy, c, t);
         }
+        commit_copies();
+        asked += stride;
+        xf += stride * ldx;
+        gf += stride * lddy;
+        const float mu = r < rows ? nmu : 0.0f, rs = r < rows ? nrs : 0.0f;
+        if (r + stride < rows) {
+            nmu = mean[r + stride];
+            nrs = rstd[r + stride];
+        }
+        wait_copies<D - 1>();
+        group_barrier<TPR>();
+        const bool live = r < rows;
+        const int live_c = live ? c : 0;
+        const unsigned char *xb = in + 2 * slot * rb, *gb = xb + rb;
+        const int xs = row_skew(xr), gs = row_skew(gr);
         float sums[2] = {0.0f, 0.0f};
+        float xh[HOLD ? E : LEN], v[HOLD ? E : LEN];
+        if constexpr (HOLD) {
+            row_values<T, LEN, E, TPR>(xb, xs, live_c, t, xh);
+            row_values<T, LEN, E, TPR>(gb, gs, live_c, t, v);
 #pragma unroll
-        for (int e = 0; e < S::E; ++e) {
-            xh[e] = (xh[e] - mu) * rs;
-            dw[e] = fmaf(v[e], xh[e], dw[e]);
-            db[e] += v[e];
-            v[e] *= w[e];  // columns beyond c have v = 0 and count nowhere
-            sums[0] += v[e];
-            sums[1] = fmaf(v[e], xh[e], sums[1]);
+            for (int e = 0; e < E; ++e) {
+                xh[e] = (xh[e] - mu) * rs;
+                dw[e] = fmaf(v[e], xh[e], dw[e]);
+                db[e] += v[e];
+                v[e] *= wv[e];  // 0 beyond c, where xh counts nowhere
+                sums[0] += v[e];
+                sums[1] = fmaf(v[e], xh[e], sums[1]);
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < E / LEN; ++u) {
+                one_run<T, LEN, TPR>(xb, xs, live_c, t, u, xh);
+                one_run<T, LEN, TPR>(gb, gs, live_c, t, u, v);
+#pragma unroll
+                for (int k = 0; k < LEN; ++k) {
+                    const float h = (xh[k] - mu) * rs, g = v[k], p = g * w[(u * LEN + k) * TPR];
+                    dw[u * LEN + k] = fmaf(g, h, dw[u * LEN + k]);
+                    db[u * LEN + k] += g;
+                    sums[0] += p;
+                    sums[1] = fmaf(p, h, sums[1]);
+                }
+            }
         }
-        group_sum<TPR>(sums, part, turn);
+        pair_sum<TPR>(sums[0], sums[1], part[side]);
+        side ^= 1;
         const float m0 = sums[0] * inv_c, m1 = sums[1] * inv_c;
+        if constexpr (HOLD) {
 #pragma unroll
-        for (int e = 0; e < S::E; ++e) v[e] = rs * (v[e] - m0 - xh[e] * m1);
-        S::store(dx + here * lddx, t, c, v);
+            for (int e = 0; e < E; ++e) v[e] = rs * fmaf(-xh[e], m1, v[e] - m0);
+            if (live) put_values<T, LEN, E, TPR>(to, out, c, t, v);
+        } else {
+#pragma unroll
+            for (int u = 0; u < E / LEN; ++u) {
+                one_run<T, LEN, TPR>(xb, xs, live_c, t, u, xh);
+                one_run<T, LEN, TPR>(gb, gs, live_c, t, u, v);
+#pragma unroll
+                for (int k = 0; k < LEN; ++k) v[k] = rs * (v[k] * w[(u * LEN + k) * TPR] - m0 - (xh[k] - mu) * rs * m1);
+                const int at = column<LEN, TPR>(t, u);
+                if (live && at < c) {
+                    if constexpr (LEN > 1)
+                        st_words(to + at, pack<T>(v));
+                    else
+                        reinterpret_cast<T*>(out + row_skew(to))[at] = narrow<T>(v[0]);
+                }
+            }
+        }
+        group_barrier<TPR>();  // the slot may be filled again, and the results are in their buffer
+        if (LEN == 1 && live) flush_row<T, TPR>(to, out, c, t);
+        if (++slot == D) slot = 0;
+        r += stride;
+        xr += stride * ldx;
+        gr += stride * lddy;
+        to += stride * lddx;
     }
-    // join the CTA's groups in order, dw then db
-    float* out = partial + ((long long)node * gridDim.x + blockIdx.x) * 2 * c;
+    wait_copies<0>();
+    // the CTA's groups join in order, in the rows' buffers: dw, then db
+    float* sum = partial + ((long long)node * gridDim.x + blockIdx.x) * 2 * c;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         float* acc = which == 0 ? dw : db;
         if constexpr (GROUPS > 1) {
+            float* joined = reinterpret_cast<float*>(smem);  // [GROUPS][c]
             __syncthreads();
-            if (group > 0)
 #pragma unroll
-                for (int e = 0; e < S::E; ++e) joined[((group - 1) * S::E + e) * 32 + t] = acc[e];
+            for (int u = 0; u < E / LEN; ++u)
+#pragma unroll
+                for (int k = 0; k < LEN; ++k)
+                    if (column<LEN, TPR>(t, u) + k < c) joined[group * c + column<LEN, TPR>(t, u) + k] = acc[u * LEN + k];
             __syncthreads();
-            if (group == 0)
+            for (int k = threadIdx.x; k < c; k += kBlock<TPR>) {
+                float s = joined[k];
+#pragma unroll 8
+                for (int q = 1; q < GROUPS; ++q) s += joined[q * c + k];
+                sum[which * c + k] = s;
+            }
+        } else {
 #pragma unroll
-                for (int e = 0; e < S::E; ++e)
-#pragma unroll
-                    for (int q = 0; q < GROUPS - 1; ++q) acc[e] += joined[(q * S::E + e) * 32 + t];
-        }
-        if (group == 0)
-#pragma unroll
-            for (int u = 0; u < RUNS; ++u)
+            for (int u = 0; u < E / LEN; ++u)
 #pragma unroll
                 for (int k = 0; k < LEN; ++k) {
-                    const int at = S::column(t, u) + k;
-                    if (at < c) out[which * c + at] = acc[u * LEN + k];
+                    const int at = column<LEN, TPR>(t, u) + k;
+                    if (at < c) sum[which * c + at] = acc[u * LEN + k];
                 }
+        }
     }
 }
 
@@ -362,100 +584,144 @@ __global__ void __launch_bounds__(256) layer_norm_join_kernel(long long c, int p
     }
 }
 
-// Widest row that fits the registers of a CTA.
-constexpr int64_t kMaxHeld = 32768;
+// Rows up to this many elements are held on chip; wider ones are swept from memory.
+constexpr int64_t kMaxHeld = 16384;
 
-// CTAs per node of the backward kernel: the SMs twice over, shared by the nodes.
-int grad_ctas(int n, int64_t rows, int64_t c, int sms) {
-    const int64_t groups = c <= 1024 ? 4 : 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>((rows + groups - 1) / groups, std::max(1, 2 * sms / n)));
-}
-
-template <typename T, int LEN, int RUNS, int TPR>
-int run_forward(const dlm_norm_args& a, cudaStream_t s) {
-    constexpr int GROUPS = kBlock<TPR> / TPR;
-    const DeviceInfo& info = device_info();
-    if (!info.ok) return DLM_ERR_CUDA;
-    const int64_t want = (a.rows + GROUPS - 1) / GROUPS;
-    const int64_t cap = std::max<int64_t>(1, (int64_t)info.sms * (2048 / kBlock<TPR>) / a.n);
-    cudaError_t err = launch_overlapped(layer_norm_kernel<T, LEN, RUNS, TPR>, dim3((unsigned)std::min(want, cap), a.n),
-                                        dim3(kBlock<TPR>), 0, s, 1, a.rows, (int)a.c, static_cast<const T*>(a.x), a.ldx, a.weight,
-                                        a.ldw, a.bias, a.ldb, a.eps, static_cast<T*>(a.y), a.ldy, a.mean, a.rstd);
-    dlm_count_launch(1);
-    return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
-}
-
-template <typename T, int LEN, int RUNS, int TPR>
-int run_backward(const dlm_norm_args& a, int ctas, cudaStream_t s) {
-    cudaError_t err = launch_overlapped(layer_norm_grad_kernel<T, LEN, RUNS, TPR>, dim3((unsigned)ctas, a.n), dim3(kBlock<TPR>), 0,
-                                        s, 1, a.rows, (int)a.c, static_cast<const T*>(a.x), a.ldx, static_cast<const T*>(a.dy), a.lddy,
-                                        a.weight, a.ldw, (const float*)a.mean, (const float*)a.rstd, static_cast<T*>(a.dx), a.lddx,
-                                        a.partial);
-    dlm_count_launch(1);
-    return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
-}
+// CALL(columns per thread, threads per row) of the narrowest group that holds c columns.  The backward kernel has twice the
+// sums to keep and takes more threads for it.
+#define DLM_NORM_SHAPES(CALL)            \
+    if (c <= 64) return CALL(8, 8);      \
+    if (c <= 128) return CALL(16, 8);    \
+    if (c <= 256) return CALL(32, 8);    \
+    if (c <= 512) return CALL(32, 16);   \
+    if (c <= 1024) return CALL(32, 32);  \
+    if (c <= 2048) return CALL(32, 64);  \
+    if (c <= 4096) return CALL(32, 128); \
+    if (c <= 8192) return CALL(32, 256); \
+    return CALL(32, 512);
+#define DLM_NORM_GRAD_SHAPES(CALL)       \
+    if (c <= 64) return CALL(8, 8);      \
+    if (c <= 128) return CALL(16, 8);    \
+    if (c <= 256) return CALL(16, 16);   \
+    if (c <= 512) return CALL(16, 32);   \
+    if (c <= 1024) return CALL(16, 64);  \
+    if (c <= 2048) return CALL(16, 128); \
+    if (c <= 4096) return CALL(16, 256); \
+    if (c <= 8192) return CALL(16, 512); \
+    return CALL(32, 512);
 
 bool rows_aligned(const void* p, int64_t ld, size_t esz) { return (uintptr_t)p % 16 == 0 && (ld * (int64_t)esz) % 16 == 0; }
+
+// CTAs per node: as many as the SMs hold at once, shared by the nodes, and no more than there are rows for.
+template <typename K>
+int resident_ctas(K kernel, int block, size_t smem, int n, int64_t rows, int groups) {
+    const DeviceInfo& info = device_info();
+    int per_sm = 0;
+    if (!info.ok || cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess ||
+        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, block, smem) != cudaSuccess || per_sm < 1)
+        return 0;
+    const int64_t cap = std::max<int64_t>(1, (int64_t)info.sms * per_sm / n);
+    return (int)std::min<int64_t>((rows + groups - 1) / groups, cap);
+}
+
+constexpr size_t kMostShared = 227 << 10;
+
+template <typename T>
+int wide_forward(const dlm_norm_args& a, cudaStream_t s) {
+    const DeviceInfo& info = device_info();
+    if (!info.ok) return DLM_ERR_CUDA;
+    const unsigned ctas = (unsigned)std::min<int64_t>(a.rows, std::max(1, 2 * info.sms / a.n));
+    cudaError_t err = launch_overlapped(layer_norm_wide_kernel<T>, dim3(ctas, a.n), dim3(1024), 0, s, 1, a.rows, a.c,
+                                        static_cast<const T*>(a.x), a.ldx, a.weight, a.ldw, a.bias, a.ldb, a.eps,
+                                        static_cast<T*>(a.y), a.ldy, a.mean, a.rstd);
+    dlm_count_launch(1);
+    return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
+}
+
+template <typename T, int LEN, int E, int TPR, int D = kDepth<TPR>>
+int run_forward(const dlm_norm_args& a, cudaStream_t s) {
+    constexpr int GROUPS = kBlock<TPR> / TPR;
+    const size_t smem = (size_t)GROUPS * (D + (LEN == 1)) * row_bytes((int)a.c, sizeof(T));
+    if (smem + 1024 > kMostShared) {
+        if constexpr (TPR == 512 && D > 1)
+            return run_forward<T, LEN, E, TPR, D - 1>(a, s);
+        else
+            return wide_forward<T>(a, s);
+    }
+    auto kern = layer_norm_kernel<T, LEN, E, TPR, D>;
+    const int ctas = resident_ctas(kern, kBlock<TPR>, smem, a.n, a.rows, GROUPS);
+    if (ctas < 1) return DLM_ERR_CUDA;
+    cudaError_t err = launch_overlapped(kern, dim3((unsigned)ctas, a.n), dim3(kBlock<TPR>), smem, s, 1, a.rows, (int)a.c,
+                                        static_cast<const T*>(a.x), a.ldx, a.weight, a.ldw, a.bias, a.ldb, a.eps,
+                                        static_cast<T*>(a.y), a.ldy, a.mean, a.rstd);
+    dlm_count_launch(1);
+    return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
+}
 
 template <typename T>
 int forward(const dlm_norm_args& a, cudaStream_t s) {
     const int64_t c = a.c;
-    if (c > kMaxHeld) {
-        const DeviceInfo& info = device_info();
-        if (!info.ok) return DLM_ERR_CUDA;
-        const unsigned ctas = (unsigned)std::min<int64_t>(a.rows, std::max(1, 2 * info.sms / a.n));
-        cudaError_t err = launch_overlapped(layer_norm_wide_kernel<T>, dim3(ctas, a.n), dim3(1024), 0, s, 1, a.rows, c,
-                                            static_cast<const T*>(a.x), a.ldx, a.weight, a.ldw, a.bias, a.ldb, a.eps,
-                                            static_cast<T*>(a.y), a.ldy, a.mean, a.rstd);
-        dlm_count_launch(1);
-        return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
+    if (c > kMaxHeld) return wide_forward<T>(a, s);
+#define DLM_VEC(E, TPR) run_forward<T, kRun<T>, E, TPR>(a, s)
+#define DLM_ONE(E, TPR) run_forward<T, 1, E, TPR>(a, s)
+    if (c % kRun<T> == 0 && rows_aligned(a.x, a.ldx, sizeof(T)) && rows_aligned(a.y, a.ldy, sizeof(T))) {
+        DLM_NORM_SHAPES(DLM_VEC)
     }
-    constexpr int R = kRun<T>;
-    if (c % R == 0 && rows_aligned(a.x, a.ldx, sizeof(T)) && rows_aligned(a.y, a.ldy, sizeof(T))) {
-        if (c <= 32 * R) return run_forward<T, R, 1, 32>(a, s);
-        if (c <= 32 * R * 2) return run_forward<T, R, 2, 32>(a, s);
-        if (c <= 32 * R * 4) return run_forward<T, R, 4, 32>(a, s);
-        if (c <= 256 * R) return run_forward<T, R, 1, 256>(a, s);
-        if (c <= 256 * R * 2) return run_forward<T, R, 2, 256>(a, s);
-        if (c <= 512 * R * 2) return run_forward<T, R, 2, 512>(a, s);
-        if (c <= 1024 * R * 2) return run_forward<T, R, 2, 1024>(a, s);
-        if (c <= 1024 * R * 4) return run_forward<T, R, 4, 1024>(a, s);
+    DLM_NORM_SHAPES(DLM_ONE)
+#undef DLM_VEC
+#undef DLM_ONE
+}
+
+// The backward launchers write the number of parts per node to *parts.
+template <typename T>
+int wide_backward(const dlm_norm_args& a, int* parts, cudaStream_t s) {
+    const DeviceInfo& info = device_info();
+    if (!info.ok) return DLM_ERR_CUDA;
+    *parts = (int)std::min<int64_t>(a.rows, std::min(std::max(1, 2 * info.sms / a.n), dlm_norm_max_ctas(a.n, a.rows, a.c)));
+    cudaError_t err = launch_overlapped(layer_norm_grad_wide_kernel<T>, dim3((unsigned)*parts, a.n), dim3(1024), 0, s, 1, a.rows, a.c,
+                                        static_cast<const T*>(a.x), a.ldx, static_cast<const T*>(a.dy), a.lddy, a.weight, a.ldw,
+                                        (const float*)a.mean, (const float*)a.rstd, static_cast<T*>(a.dx), a.lddx, a.partial);
+    dlm_count_launch(1);
+    return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
+}
+
+template <typename T, int LEN, int E, int TPR, int D = kDepth<TPR>>
+int run_backward(const dlm_norm_args& a, int* parts, cudaStream_t s) {
+    constexpr int GROUPS = kBlock<TPR> / TPR;
+    const size_t rows_smem = (size_t)GROUPS * (2 * D + (LEN == 1)) * row_bytes((int)a.c, sizeof(T));
+    const size_t smem = std::max((E > 16 ? (size_t)E * TPR * 4 : 0) + rows_smem, GROUPS > 1 ? (size_t)GROUPS * a.c * 4 : 0);
+    if (smem + 1024 > kMostShared) {
+        if constexpr (TPR == 512 && D > 1)
+            return run_backward<T, LEN, E, TPR, D - 1>(a, parts, s);
+        else
+            return wide_backward<T>(a, parts, s);
     }
-    if (c <= 32 * 4) return run_forward<T, 1, 4, 32>(a, s);
-    if (c <= 32 * 16) return run_forward<T, 1, 16, 32>(a, s);
-    if (c <= 256 * 8) return run_forward<T, 1, 8, 256>(a, s);
-    if (c <= 512 * 16) return run_forward<T, 1, 16, 512>(a, s);
-    if (c <= 1024 * 16) return run_forward<T, 1, 16, 1024>(a, s);
-    return run_forward<T, 1, 32, 1024>(a, s);
+    auto kern = layer_norm_grad_kernel<T, LEN, E, TPR, D>;
+    *parts = std::min(resident_ctas(kern, kBlock<TPR>, smem, a.n, a.rows, GROUPS), dlm_norm_max_ctas(a.n, a.rows, a.c));
+    if (*parts < 1) return DLM_ERR_CUDA;
+    cudaError_t err = launch_overlapped(kern, dim3((unsigned)*parts, a.n), dim3(kBlock<TPR>), smem, s, 1, a.rows, (int)a.c,
+                                        static_cast<const T*>(a.x), a.ldx, static_cast<const T*>(a.dy), a.lddy, a.weight, a.ldw,
+                                        (const float*)a.mean, (const float*)a.rstd, static_cast<T*>(a.dx), a.lddx, a.partial);
+    dlm_count_launch(1);
+    return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
 }
 
 template <typename T>
-int backward(const dlm_norm_args& a, int ctas, cudaStream_t s) {
+int backward(const dlm_norm_args& a, int* parts, cudaStream_t s) {
     const int64_t c = a.c;
-    if (c > kMaxHeld / 2) {
-        cudaError_t err = launch_overlapped(layer_norm_grad_wide_kernel<T>, dim3((unsigned)ctas, a.n), dim3(1024), 0, s, 1, a.rows, c,
-                                            static_cast<const T*>(a.x), a.ldx, static_cast<const T*>(a.dy), a.lddy, a.weight,
-                                            a.ldw, (const float*)a.mean, (const float*)a.rstd, static_cast<T*>(a.dx), a.lddx,
-                                            a.partial);
-        dlm_count_launch(1);
-        return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
-    }
-    constexpr int R = kRun<T>;
-    if (c % R == 0 && rows_aligned(a.x, a.ldx, sizeof(T)) && rows_aligned(a.dy, a.lddy, sizeof(T)) &&
+    if (c > kMaxHeld) return wide_backward<T>(a, parts, s);
+#define DLM_VEC(E, TPR) run_backward<T, kRun<T>, E, TPR>(a, parts, s)
+#define DLM_ONE(E, TPR) run_backward<T, 1, E, TPR>(a, parts, s)
+    if (c % kRun<T> == 0 && rows_aligned(a.x, a.ldx, sizeof(T)) && rows_aligned(a.dy, a.lddy, sizeof(T)) &&
         rows_aligned(a.dx, a.lddx, sizeof(T))) {
-        if (c <= 32 * R) return run_backward<T, R, 1, 32>(a, ctas, s);
-        if (c <= 32 * R * 2) return run_backward<T, R, 2, 32>(a, ctas, s);
-        if (c <= 256 * R) return run_backward<T, R, 1, 256>(a, ctas, s);
-        if (c <= 256 * R * 2) return run_backward<T, R, 2, 256>(a, ctas, s);
-        if (c <= 512 * R * 2) return run_backward<T, R, 2, 512>(a, ctas, s);
-        if (c <= 1024 * R * 2) return run_backward<T, R, 2, 1024>(a, ctas, s);
+        DLM_NORM_GRAD_SHAPES(DLM_VEC)
     }
-    if (c <= 32 * 4) return run_backward<T, 1, 4, 32>(a, ctas, s);
-    if (c <= 32 * 16) return run_backward<T, 1, 16, 32>(a, ctas, s);
-    if (c <= 256 * 8) return run_backward<T, 1, 8, 256>(a, ctas, s);
-    if (c <= 512 * 16) return run_backward<T, 1, 16, 512>(a, ctas, s);
-    return run_backward<T, 1, 16, 1024>(a, ctas, s);
+    DLM_NORM_GRAD_SHAPES(DLM_ONE)
+#undef DLM_VEC
+#undef DLM_ONE
 }
+#undef DLM_NORM_SHAPES
+#undef DLM_NORM_GRAD_SHAPES
 
 template <typename G>
 cudaError_t join(const dlm_norm_args& a, int parts, cudaStream_t s) {
@@ -465,8 +731,10 @@ cudaError_t join(const dlm_norm_args& a, int parts, cudaStream_t s) {
 
 }  // namespace
 
-// Bound on grad_ctas over all GPUs of this architecture, so that the workspace's size needs no device.
-int dlm_norm_max_ctas(int n, int64_t rows) { return (int)std::min<int64_t>(rows, std::max(1, 512 / n)); }
+// Bound on the row blocks per node, so that the workspace's size needs no device: a little over what the SMs hold at once.
+int dlm_norm_max_ctas(int n, int64_t rows, int64_t c) {
+    return (int)std::min<int64_t>(rows, std::max(1, (c <= 2048 ? 1024 : 448) / n));
+}
 
 int dlm_launch_layer_norm(const dlm_norm_args& a, void* stream) {
     if (a.rows == 0) return DLM_OK;
@@ -476,12 +744,9 @@ int dlm_launch_layer_norm(const dlm_norm_args& a, void* stream) {
 
 int dlm_launch_layer_norm_grad(const dlm_norm_args& a, void* stream) {
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    const DeviceInfo& info = device_info();
-    if (!info.ok) return DLM_ERR_CUDA;
     int parts = 0;
     if (a.rows > 0) {
-        parts = std::min(grad_ctas(a.n, a.rows, a.c, info.sms), dlm_norm_max_ctas(a.n, a.rows));
-        int rc = a.dtype == DLM_G_BF16 ? backward<__nv_bfloat16>(a, parts, s) : backward<float>(a, parts, s);
+        int rc = a.dtype == DLM_G_BF16 ? backward<__nv_bfloat16>(a, &parts, s) : backward<float>(a, &parts, s);
         if (rc != DLM_OK) return rc;
     }
     cudaError_t err = a.g_dtype == DLM_G_BF16 ? join<__nv_bfloat16>(a, parts, s) : join<float>(a, parts, s);

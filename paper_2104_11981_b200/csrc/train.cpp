@@ -92,7 +92,7 @@ int layer_norm(int n, int64_t rows, int64_t c, const void* x, int dtype, int64_t
 int64_t layer_norm_grad_workspace_bytes(int n, int64_t rows, int64_t c) {
     int rc = check_norm_shape(n, rows, c);
     if (rc != DLM_OK) return rc;
-    const int64_t bytes = (int64_t)n * dlm_norm_max_ctas(n, rows) * 2 * c * 4;
+    const int64_t bytes = (int64_t)n * dlm_norm_max_ctas(n, rows, c) * 2 * c * 4;
     return bytes > 256 ? bytes : 256;
 }
 
