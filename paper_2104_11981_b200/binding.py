@@ -194,10 +194,10 @@ def topology_build_periodic(kind, n, period, rowptr, col, val=None):
 
 def _stream_ptr(stream):
     if stream is not None:
-        return _vp(stream.cuda_stream)
+        return stream.cuda_stream
     import torch
     # the raw handle of the current stream: building a torch.cuda.Stream object for it costs 3.5 us a call
-    return _vp(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _state_args(x, m, g):

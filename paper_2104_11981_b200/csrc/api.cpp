@@ -9,6 +9,7 @@
 
 #include "dlm_gradients.h"
 #include "dlm_internal.h"
+#include "dlm_train.h"
 
 int dlm_lsq_max_splits();
 int dlm_step_take_error(int* flag);
@@ -285,7 +286,7 @@ int dlm_set_tuning(int knob, int value) {
 
 int dlm_kernel_error(int* flag) {
     if (!flag) return DLM_ERR_NULL;
-    int step = 0, lsq = 0, shard = 0, gradients = 0;
+    int step = 0, lsq = 0, shard = 0, gradients = 0, norm = 0;
     int rc = dlm_step_take_error(&step);
     if (rc != DLM_OK) return rc;
     rc = dlm_lsq_take_error(&lsq);
@@ -294,7 +295,9 @@ int dlm_kernel_error(int* flag) {
     if (rc != DLM_OK) return rc;
     rc = dlm_gradient_take_error(&gradients);
     if (rc != DLM_OK) return rc;
-    *flag = step != 0 ? step : lsq != 0 ? lsq : shard != 0 ? shard : gradients;
+    rc = dlm_norm_take_error(&norm);
+    if (rc != DLM_OK) return rc;
+    *flag = step != 0 ? step : lsq != 0 ? lsq : shard != 0 ? shard : gradients != 0 ? gradients : norm;
     return DLM_OK;
 }
 

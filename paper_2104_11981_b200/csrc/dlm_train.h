@@ -31,6 +31,7 @@ struct dlm_norm_args {
     float* partial;
 };
 int dlm_norm_max_ctas(int n, int64_t rows, int64_t c);  // row blocks per node that the backward workspace is sized for
+int dlm_norm_take_error(int* flag);
 int dlm_launch_layer_norm(const dlm_norm_args& a, void* stream);
 int dlm_launch_layer_norm_grad(const dlm_norm_args& a, void* stream);
 

@@ -13,6 +13,7 @@
 #include <algorithm>
 #include <cstdint>
 
+#include "dlm_device.cuh"
 #include "dlm_internal.h"
 #include "dlm_launch.h"
 #include "dlm_rows.cuh"
@@ -107,6 +108,28 @@ __device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_
 template <int LEFT>
 __device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
+// Aligned rows of a whole CTA come by bulk copies instead, one instruction of one thread each: 36 instructions a thread and
+// row fewer in the backward kernel, which the issue slots bound.
+template <int LEN, int TPR>
+constexpr bool kBulk = LEN > 1 && TPR >= 64;
+
+__device__ int g_norm_kernel_error = 0;  // set to a non-zero code if a bounded wait ran out
+
+__device__ __forceinline__ void bulk_row(unsigned char* buf, const void* row, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(buf)),
+                 "l"(row), "r"(bytes), "r"(bar)
+                 : "memory");
+}
+// Slots 0 .. count - 1, whose copies may be on their way, before a kernel that gave up leaves them.
+template <int D>
+__device__ __noinline__ void give_up(uint64_t (&full)[D], uint32_t parities) {
+    if (threadIdx.x == 0) {
+        atomicExch(&g_norm_kernel_error, 7);
+        for (int k = 0; k < D; ++k) mbar_wait(smem_u32(&full[k]), (parities >> k) & 1);
+    }
+    __syncthreads();
+}
+
 // This thread's values of a row in shared memory; 0 beyond c.
 template <typename T, int LEN, int E, int TPR>
 __device__ __forceinline__ void row_values(const unsigned char* buf, int skew, int c, int t, float* v) {
@@ -195,6 +218,9 @@ __global__ void __launch_bounds__(kBlock<TPR>)
     constexpr int GROUPS = kBlock<TPR> / TPR, WARPS = TPR / 32;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ float part[2][2][TPR > 32 ? WARPS : 1];  // sum and squared deviations of each warp
+    __shared__ uint64_t full[D];
+    constexpr bool BULK = kBulk<LEN, TPR>;
+    const uint32_t bytes = (uint32_t)c * sizeof(T);
     const int node = blockIdx.y, t = threadIdx.x % TPR, group = threadIdx.x / TPR;
     const int rb = row_bytes(c, sizeof(T));
     unsigned char* in = smem + (size_t)group * (D + (LEN == 1)) * rb;
@@ -205,15 +231,30 @@ __global__ void __launch_bounds__(kBlock<TPR>)
     const T* row = fetch;
     T* to = y + (base + first) * ldy;
     long long asked = first;
+    if constexpr (BULK) {
+        if (threadIdx.x == 0) {
+            for (int k = 0; k < D; ++k) mbar_init(smem_u32(&full[k]), 1);
+            mbar_init_fence();
+        }
+        __syncthreads();
+    }
     pdl_wait();
     pdl_release();
-#pragma unroll
-    for (int k = 0; k < D - 1; ++k) {
-        if (asked < rows) fetch_row<T, LEN, TPR>(in + k * rb, fetch, x, c, t);
-        commit_copies();
+    auto ask = [&](int k) {  // the next row, into slot k
+        if constexpr (BULK) {
+            if (threadIdx.x == 0 && asked < rows) {
+                mbar_expect_tx(smem_u32(&full[k]), bytes);
+                bulk_row(in + k * rb, fetch, bytes, smem_u32(&full[k]));
+            }
+        } else {
+            if (asked < rows) fetch_row<T, LEN, TPR>(in + k * rb, fetch, x, c, t);
+            commit_copies();
+        }
         asked += stride;
         fetch += stride * ldx;
-    }
+    };
+#pragma unroll
+    for (int k = 0; k < D - 1; ++k) ask(k);
     float w[E], b[E];
     params<LEN, E, TPR>(weight + node * ldw, c, t, w);
 #pragma unroll
@@ -226,17 +267,22 @@ __global__ void __launch_bounds__(kBlock<TPR>)
     const int other = (threadIdx.x & (WARPS > 1 ? WARPS - 1 : 0)) * 32;
     const float their = WARPS > 1 ? (float)owned_columns<LEN, E, TPR>(c, other) : 0.0f, inv_their = their > 0.0f ? 1.0f / their : 0.0f;
     int slot = 0, side = 0;
+    uint32_t parities = 0;  // of each slot's next phase
     // groups of a warp leave together: the loop counts the rows of its first group
     long long r = first;
     for (long long lead = TPR < 32 ? first - group % (32 / (TPR < 32 ? TPR : 32)) : first; lead < rows; lead += stride) {
-        const int next = slot == 0 ? D - 1 : slot - 1;
-        if (asked < rows) fetch_row<T, LEN, TPR>(in + next * rb, fetch, x, c, t);
-        commit_copies();
-        asked += stride;
-        fetch += stride * ldx;
-        wait_copies<D - 1>();
-        group_barrier<TPR>();
-        const bool live = r < rows;
+        ask(slot == 0 ? D - 1 : slot - 1);
+        if constexpr (BULK) {
+            if (!cta_wait(smem_u32(&full[slot]), (parities >> slot) & 1)) {
+                give_up(full, parities);
+                return;
+            }
+            parities ^= 1u << slot;
+        } else {
+            wait_copies<D - 1>();
+            group_barrier<TPR>();
+        }
+        const bool live = BULK || r < rows;
         float v[E];
         row_values<T, LEN, E, TPR>(in + slot * rb, row_skew(row), live ? c : 0, t, v);
         float sum = 0.0f;
@@ -282,6 +328,7 @@ __global__ void __launch_bounds__(kBlock<TPR>)
             mean[base + r] = mu;
             rstd[base + r] = rs;
         }
+        if constexpr (BULK) fence_before_refill();
         group_barrier<TPR>();  // the slot may be filled again, and the results are in their buffer
         if (LEN == 1 && live) flush_row<T, TPR>(to, out, c, t);
         if (++slot == D) slot = 0;
@@ -354,6 +401,9 @@ __global__ void __launch_bounds__(kBlock<TPR>)
     constexpr bool HOLD = E <= 16;  // the row's values stay in registers between the two sweeps, else they are read again
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ float part[2][2][TPR > 32 ? TPR / 32 : 1];
+    __shared__ uint64_t full[D];
+    constexpr bool BULK = kBulk<LEN, TPR>;
+    const uint32_t bytes = (uint32_t)c * sizeof(T);
     const int node = blockIdx.y, t = threadIdx.x % TPR, group = threadIdx.x / TPR;
     const int rb = row_bytes(c, sizeof(T));
     float* w = reinterpret_cast<float*>(smem) + t;  // weights that the registers do not hold: [E][TPR]
@@ -367,19 +417,36 @@ __global__ void __launch_bounds__(kBlock<TPR>)
     long long asked = first;
     mean += base;
     rstd += base;
+    if constexpr (BULK) {
+        if (threadIdx.x == 0) {
+            for (int k = 0; k < D; ++k) mbar_init(smem_u32(&full[k]), 1);
+            mbar_init_fence();
+        }
+        __syncthreads();
+    }
     pdl_wait();
     pdl_release();
-#pragma unroll
-    for (int k = 0; k < D - 1; ++k) {
-        if (asked < rows) {
-            fetch_row<T, LEN, TPR>(in + 2 * k * rb, xf, x, c, t);
-            fetch_row<T, LEN, TPR>(in + (2 * k + 1) * rb, gf, dy, c, t);
+    auto ask = [&](int k) {  // the next row, into slot k
+        unsigned char* buf = in + 2 * k * rb;
+        if constexpr (BULK) {
+            if (threadIdx.x == 0 && asked < rows) {
+                mbar_expect_tx(smem_u32(&full[k]), 2 * bytes);
+                bulk_row(buf, xf, bytes, smem_u32(&full[k]));
+                bulk_row(buf + rb, gf, bytes, smem_u32(&full[k]));
+            }
+        } else {
+            if (asked < rows) {
+                fetch_row<T, LEN, TPR>(buf, xf, x, c, t);
+                fetch_row<T, LEN, TPR>(buf + rb, gf, dy, c, t);
+            }
+            commit_copies();
         }
-        commit_copies();
         asked += stride;
         xf += stride * ldx;
         gf += stride * lddy;
-    }
+    };
+#pragma unroll
+    for (int k = 0; k < D - 1; ++k) ask(k);
     float wv[HOLD ? E : 1];
     if constexpr (HOLD) {
         params<LEN, E, TPR>(weight + node * ldw, c, t, wv);
@@ -394,6 +461,7 @@ __global__ void __launch_bounds__(kBlock<TPR>)
     for (int e = 0; e < E; ++e) dw[e] = db[e] = 0.0f;
     const float inv_c = 1.0f / (float)c;
     int slot = 0, side = 0;
+    uint32_t parities = 0;  // of each slot's next phase
     float nmu = 0.0f, nrs = 0.0f;
     if (first < rows) {
         nmu = mean[first];
@@ -402,23 +470,23 @@ __global__ void __launch_bounds__(kBlock<TPR>)
     // groups of a warp leave together: the loop counts the rows of its first group
     long long r = first;
     for (long long lead = TPR < 32 ? first - group % (32 / (TPR < 32 ? TPR : 32)) : first; lead < rows; lead += stride) {
-        const int next = slot == 0 ? D - 1 : slot - 1;
-        if (asked < rows) {
-            fetch_row<T, LEN, TPR>(in + 2 * next * rb, xf, x, c, t);
-            fetch_row<T, LEN, TPR>(in + (2 * next + 1) * rb, gf, dy, c, t);
-        }
-        commit_copies();
-        asked += stride;
-        xf += stride * ldx;
-        gf += stride * lddy;
+        ask(slot == 0 ? D - 1 : slot - 1);
         const float mu = r < rows ? nmu : 0.0f, rs = r < rows ? nrs : 0.0f;
         if (r + stride < rows) {
             nmu = mean[r + stride];
             nrs = rstd[r + stride];
         }
-        wait_copies<D - 1>();
-        group_barrier<TPR>();
-        const bool live = r < rows;
+        if constexpr (BULK) {
+            if (!cta_wait(smem_u32(&full[slot]), (parities >> slot) & 1)) {
+                give_up(full, parities);
+                return;
+            }
+            parities ^= 1u << slot;
+        } else {
+            wait_copies<D - 1>();
+            group_barrier<TPR>();
+        }
+        const bool live = BULK || r < rows;
         const int live_c = live ? c : 0;
         const unsigned char *xb = in + 2 * slot * rb, *gb = xb + rb;
         const int xs = row_skew(xr), gs = row_skew(gr);
@@ -456,7 +524,7 @@ __global__ void __launch_bounds__(kBlock<TPR>)
         const float m0 = sums[0] * inv_c, m1 = sums[1] * inv_c;
         if constexpr (HOLD) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) v[e] = rs * fmaf(-xh[e], m1, v[e] - m0);
+            for (int e = 0; e < E; ++e) v[e] = fmaf(v[e], rs, fmaf(xh[e], -m1 * rs, -m0 * rs));
             if (live) put_values<T, LEN, E, TPR>(to, out, c, t, v);
         } else {
 #pragma unroll
@@ -474,6 +542,7 @@ __global__ void __launch_bounds__(kBlock<TPR>)
                 }
             }
         }
+        if constexpr (BULK) fence_before_refill();
         group_barrier<TPR>();  // the slot may be filled again, and the results are in their buffer
         if (LEN == 1 && live) flush_row<T, TPR>(to, out, c, t);
         if (++slot == D) slot = 0;
@@ -612,15 +681,27 @@ constexpr int64_t kMaxHeld = 16384;
 
 bool rows_aligned(const void* p, int64_t ld, size_t esz) { return (uintptr_t)p % 16 == 0 && (ld * (int64_t)esz) % 16 == 0; }
 
-// CTAs per node: as many as the SMs hold at once, shared by the nodes, and no more than there are rows for.
+// CTAs per node: as many as the SMs hold at once, shared by the nodes, and no more than there are rows for.  What the runtime
+// says of a kernel is asked once per size and host thread: it costs as much as the launch.
 template <typename K>
 int resident_ctas(K kernel, int block, size_t smem, int n, int64_t rows, int groups) {
+    struct Known {
+        K kernel;
+        int device;
+        size_t smem;
+        int per_sm;
+    };
+    static thread_local Known known = {};
     const DeviceInfo& info = device_info();
-    int per_sm = 0;
-    if (!info.ok || cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess ||
-        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, block, smem) != cudaSuccess || per_sm < 1)
-        return 0;
-    const int64_t cap = std::max<int64_t>(1, (int64_t)info.sms * per_sm / n);
+    int device = 0;
+    if (!info.ok || cudaGetDevice(&device) != cudaSuccess) return 0;
+    if (known.kernel != kernel || known.device != device || known.smem != smem || known.per_sm < 1) {
+        known = {kernel, device, smem, 0};
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess ||
+            cudaOccupancyMaxActiveBlocksPerMultiprocessor(&known.per_sm, kernel, block, smem) != cudaSuccess || known.per_sm < 1)
+            return 0;
+    }
+    const int64_t cap = std::max<int64_t>(1, (int64_t)info.sms * known.per_sm / n);
     return (int)std::min<int64_t>((rows + groups - 1) / groups, cap);
 }
 
@@ -730,6 +811,17 @@ cudaError_t join(const dlm_norm_args& a, int parts, cudaStream_t s) {
 }
 
 }  // namespace
+
+int dlm_norm_take_error(int* flag) {
+    int v = 0;
+    if (cudaMemcpyFromSymbol(&v, g_norm_kernel_error, sizeof(int)) != cudaSuccess) return DLM_ERR_CUDA;
+    if (v != 0) {
+        int zero = 0;
+        if (cudaMemcpyToSymbol(g_norm_kernel_error, &zero, sizeof(int)) != cudaSuccess) return DLM_ERR_CUDA;
+    }
+    *flag = v;
+    return DLM_OK;
+}
 
 // Bound on the row blocks per node, so that the workspace's size needs no device: a little over what the SMs hold at once.
 int dlm_norm_max_ctas(int n, int64_t rows, int64_t c) {
