@@ -674,7 +674,7 @@ constexpr int64_t kMaxHeld = 16384;
     if (c <= 256) return CALL(16, 16);   \
     if (c <= 512) return CALL(16, 32);   \
     if (c <= 1024) return CALL(16, 64);  \
-    if (c <= 2048) return CALL(16, 128); \
+    if (c <= 2048) return CALL(8, 256);  \
     if (c <= 4096) return CALL(16, 256); \
     if (c <= 8192) return CALL(16, 512); \
     return CALL(32, 512);
