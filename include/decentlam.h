@@ -420,7 +420,8 @@ DLM_API int gradients_destroy(dlm_gradients* list);
  *           gathered into the stacked rows, as the update rules read them, and the tensors are left as they are.
  * The L2 norm is exact to fp32 rounding over the whole fp32 range (squares that overflow or vanish in fp32 are summed
  * again in double).  A NaN or infinity in a node's gradient shows in its norm; the scale is then NaN or 0 by the
- * formula.  Reads the list once for the norm, and once more for the copy.
+ * formula.  Reads the list once for the norm, and once more for the copy.  Nodes of up to 262144 elements take one launch,
+ * larger ones three (the norm alone two).
  * Errors: DLM_ERR_NULL, DLM_ERR_KIND, DLM_ERR_SHAPE, DLM_ERR_ALIGN, DLM_ERR_ALIAS (g's rows or norms overlapping a
  * tensor of the list), DLM_ERR_HYPER (max_norm not finite or <= 0), DLM_ERR_CUDA.
  */
@@ -444,7 +445,8 @@ DLM_API int gradient_clip(dlm_gradients* list, int kind, float max_norm, float* 
  *                stacked g, for instance.
  *   workspace  : device, layer_norm_grad_workspace_bytes(n, rows, c) bytes, 256-byte aligned, owned by the caller
  * rows may be 0 (the weight gradients are then 0).  Fast path: c a multiple of 16 bytes' worth and every activation row
- * 16-byte aligned; rows of up to 32768 (backward 16384) elements are held in registers, wider ones are read again.
+ * 16-byte aligned; other layouts take about twice the time on large arrays.  Rows of up to 16384 elements (fp32 rows that are
+ * not aligned: about 9500 backward, 11500 forward) are held on chip, wider ones are swept from the caches, which is slower.
  * Errors: DLM_ERR_NULL, DLM_ERR_SHAPE, DLM_ERR_KIND, DLM_ERR_ALIGN, DLM_ERR_ALIAS, DLM_ERR_HYPER, DLM_ERR_WORKSPACE,
  * DLM_ERR_UNSUPPORTED, DLM_ERR_CUDA.
  */

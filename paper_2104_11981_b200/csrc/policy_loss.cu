@@ -89,7 +89,8 @@ __device__ __forceinline__ RowOutcome row_outcome(float zt, Tally t, float w, fl
 // turn.  A thread copies its first kHold runs to its own slots of shared memory (asynchronous copies: they hold no
 // registers while in flight, and nobody else reads the slots, so no barrier is needed) and both sweeps read them there, so
 // that the logits cross the memory bus once; what a wider row has beyond that is read again, out of the L2.
-// TPR = 32: a warp per row, eight rows a CTA.
+// TPR = 32: a warp per row, eight rows a CTA.  kHold = 8 is 32 KB for 256 threads, six CTAs per SM; with 16 runs the widest
+// case below takes 351 to 367 us instead of 335.
 constexpr int kHold = 8;
 template <int TPR>
 constexpr int kBlock = TPR < 128 ? 256 : TPR;
@@ -205,21 +206,21 @@ __global__ void __launch_bounds__(kBlock<TPR>, 1536 / kBlock<TPR>)
     {
         uint32_t to = (uint32_t)__cvta_generic_to_shared(slots + threadIdx.x);
         const T* from = zp;
-#pragma unroll 4
+#pragma unroll 8
         for (int u = 0; u < held; ++u, to += kBlock<TPR> * 16, from += TPR * R) copy_async(to, from);
     }
     const float zt = widen(z[token]);
     const float zh = has_head ? widen(z[t]) : -INFINITY, ze = has_tail ? widen(z[tail + t]) : -INFINITY;
     copy_wait();
     float m = fmaxf(zh, ze);
-#pragma unroll 4
+#pragma unroll 8
     for (int u = 0; u < held; ++u) m = fmaxf(m, largest<T>(hold[u * kBlock<TPR>]));
     Tally sum = {reference(m), 0.0f};
     {
         const float ref = finite_ref(sum.c);
         if (has_head) sum.s += exp2_fast(fmaf(zh, kLog2E, -ref));
         if (has_tail) sum.s += exp2_fast(fmaf(ze, kLog2E, -ref));
-#pragma unroll 4
+#pragma unroll 8
         for (int u = 0; u < held; ++u) sum.s += sum_exp<T>(hold[u * kBlock<TPR>], ref);
     }
     for (int r = kHold * TPR; r < mine; r += TPR) {
@@ -269,7 +270,7 @@ __global__ void __launch_bounds__(kBlock<TPR>, 1536 / kBlock<TPR>)
         if (threadIdx.x >= 32) cluster_wait();
     if (!d) return;
     if (dvec) {
-#pragma unroll 4
+#pragma unroll 8
         for (int u = 0; u < held; ++u) put_run<T, true>(dp + u * TPR * R, hold[u * kBlock<TPR>], two.ref, two.k0);
     } else {
         for (int u = 0; u < held; ++u) put_run<T, false>(dp + u * TPR * R, hold[u * kBlock<TPR>], two.ref, two.k0);
