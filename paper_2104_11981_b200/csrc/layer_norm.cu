@@ -285,22 +285,29 @@ __global__ void __launch_bounds__(kBlock<TPR>)
         const bool live = BULK || r < rows;
         float v[E];
         row_values<T, LEN, E, TPR>(in + slot * rb, row_skew(row), live ? c : 0, t, v);
-        float sum = 0.0f;
+        float2 s2 = make_float2(0.0f, 0.0f);
 #pragma unroll
-        for (int e = 0; e < E; ++e) sum += v[e];
-        sum = lane_sum<TPR>(sum);
+        for (int e = 0; e < E; e += 2) s2 = __fadd2_rn(s2, make_float2(v[e], v[e + 1]));
+        const float sum = lane_sum<TPR>(s2.x + s2.y);
         // deviations from the warp's own mean first: one exchange between the warps instead of two
         const float near = sum * inv_owned;
         float sq = 0.0f;
+        s2 = make_float2(0.0f, 0.0f);
 #pragma unroll
         for (int u = 0; u < E / LEN; ++u)
-            if (column<LEN, TPR>(t, u) < c)
-#pragma unroll
-                for (int k = 0; k < LEN; ++k) {
-                    const float dev = v[u * LEN + k] - near;
+            if (column<LEN, TPR>(t, u) < c) {
+                if constexpr (LEN == 1) {
+                    const float dev = v[u] - near;
                     sq = fmaf(dev, dev, sq);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < LEN; k += 2) {
+                        const float2 dev = __fadd2_rn(make_float2(v[u * LEN + k], v[u * LEN + k + 1]), make_float2(-near, -near));
+                        s2 = __ffma2_rn(dev, dev, s2);
+                    }
                 }
-        sq = lane_sum<TPR>(sq);
+            }
+        sq = lane_sum<TPR>(LEN == 1 ? sq : s2.x + s2.y);
         float mu = near;
         if constexpr (TPR > 32) {
             // and then sum_w [sq_w + n_w (mean_w - mu)^2]
@@ -322,7 +329,12 @@ __global__ void __launch_bounds__(kBlock<TPR>)
         }
         const float rs = rsqrtf(fmaf(sq, inv_c, eps));
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = fmaf((v[e] - mu) * rs, w[e], b[e]);
+        for (int e = 0; e < E; e += 2) {
+            const float2 h = __fmul2_rn(__fadd2_rn(make_float2(v[e], v[e + 1]), make_float2(-mu, -mu)), make_float2(rs, rs));
+            const float2 o = __ffma2_rn(h, make_float2(w[e], w[e + 1]), make_float2(b[e], b[e + 1]));
+            v[e] = o.x;
+            v[e + 1] = o.y;
+        }
         if (live) put_values<T, LEN, E, TPR>(to, out, c, t, v);
         if (t == 0 && live) {
             mean[base + r] = mu;
@@ -493,17 +505,28 @@ __global__ void __launch_bounds__(kBlock<TPR>)
         float sums[2] = {0.0f, 0.0f};
         float xh[HOLD ? E : LEN], v[HOLD ? E : LEN];
         if constexpr (HOLD) {
+            float2 s0 = make_float2(0.0f, 0.0f), s1 = s0;
             row_values<T, LEN, E, TPR>(xb, xs, live_c, t, xh);
             row_values<T, LEN, E, TPR>(gb, gs, live_c, t, v);
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                xh[e] = (xh[e] - mu) * rs;
-                dw[e] = fmaf(v[e], xh[e], dw[e]);
-                db[e] += v[e];
-                v[e] *= wv[e];  // 0 beyond c, where xh counts nowhere
-                sums[0] += v[e];
-                sums[1] = fmaf(v[e], xh[e], sums[1]);
+            for (int e = 0; e < E; e += 2) {
+                float2 h = __fmul2_rn(__fadd2_rn(make_float2(xh[e], xh[e + 1]), make_float2(-mu, -mu)), make_float2(rs, rs));
+                float2 g = make_float2(v[e], v[e + 1]);
+                const float2 a = __ffma2_rn(g, h, make_float2(dw[e], dw[e + 1])), q = __fadd2_rn(make_float2(db[e], db[e + 1]), g);
+                dw[e] = a.x;
+                dw[e + 1] = a.y;
+                db[e] = q.x;
+                db[e + 1] = q.y;
+                g = __fmul2_rn(g, make_float2(wv[e], wv[e + 1]));  // 0 beyond c, where xh counts nowhere
+                s0 = __fadd2_rn(s0, g);
+                s1 = __ffma2_rn(g, h, s1);
+                xh[e] = h.x;
+                xh[e + 1] = h.y;
+                v[e] = g.x;
+                v[e + 1] = g.y;
             }
+            sums[0] = s0.x + s0.y;
+            sums[1] = s1.x + s1.y;
         } else {
 #pragma unroll
             for (int u = 0; u < E / LEN; ++u) {
@@ -524,7 +547,12 @@ __global__ void __launch_bounds__(kBlock<TPR>)
         const float m0 = sums[0] * inv_c, m1 = sums[1] * inv_c;
         if constexpr (HOLD) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) v[e] = fmaf(v[e], rs, fmaf(xh[e], -m1 * rs, -m0 * rs));
+            for (int e = 0; e < E; e += 2) {
+                const float2 f = __ffma2_rn(make_float2(xh[e], xh[e + 1]), make_float2(-m1 * rs, -m1 * rs), make_float2(-m0 * rs, -m0 * rs));
+                const float2 o = __ffma2_rn(make_float2(v[e], v[e + 1]), make_float2(rs, rs), f);
+                v[e] = o.x;
+                v[e + 1] = o.y;
+            }
             if (live) put_values<T, LEN, E, TPR>(to, out, c, t, v);
         } else {
 #pragma unroll
