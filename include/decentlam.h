@@ -445,8 +445,8 @@ DLM_API int gradient_clip(dlm_gradients* list, int kind, float max_norm, float* 
  *                stacked g, for instance.
  *   workspace  : device, layer_norm_grad_workspace_bytes(n, rows, c) bytes, 256-byte aligned, owned by the caller
  * rows may be 0 (the weight gradients are then 0).  Fast path: c a multiple of 16 bytes' worth and every activation row
- * 16-byte aligned; other layouts take about twice the time on large arrays.  Rows of up to 16384 elements (fp32 rows that are
- * not aligned: about 9500 backward, 11500 forward) are held on chip, wider ones are swept from the caches, which is slower.
+ * 16-byte aligned; other layouts take two to three times as long on large arrays.  Rows of up to 16384 elements (backward, fp32
+ * rows that are not aligned: 13800) are held on chip, wider ones are swept from the caches, which is slower.
  * Errors: DLM_ERR_NULL, DLM_ERR_SHAPE, DLM_ERR_KIND, DLM_ERR_ALIGN, DLM_ERR_ALIAS, DLM_ERR_HYPER, DLM_ERR_WORKSPACE,
  * DLM_ERR_UNSUPPORTED, DLM_ERR_CUDA.
  */

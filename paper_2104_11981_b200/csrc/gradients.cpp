@@ -140,7 +140,7 @@ int gradients_build(int n, int tensors, const int64_t* sizes, const int* dtypes,
     try {
         list = new dlm_gradients;
         rc = build(n, tensors, sizes, dtypes, data, offsets, *list);
-    } catch (const std::bad_alloc&) {
+    } catch (...) {  // no memory for the plan
         rc = DLM_ERR_CUDA;
     }
     if (rc != DLM_OK) {

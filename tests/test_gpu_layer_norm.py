@@ -88,7 +88,8 @@ def _check_backward(x, dy, w, mean, rstd, typ, bias=True, gtype="f32"):
 
 # widths on both sides of every variant's limit: a warp's registers, a CTA's, rows read again; odd ones take single elements
 WIDTHS = [1, 2, 7, 8, 64, 127, 128, 129, 256, 264, 500, 512, 513, 768, 1000, 1024, 1032, 2047, 2048, 4096, 4104, 5000, 8192, 8193,
-          10_240, 16_384, 16_385, 16_392, 32_768, 32_769, 40_000]
+          9001, 10_240, 12_288, 13_799, 13_900, 16_383, 16_384, 16_385,
+          16_392, 32_768, 32_769, 40_000]
 
 
 @pytest.mark.parametrize("typ", ["f32", "bf16"])
@@ -151,6 +152,35 @@ def test_in_place(c, typ):
     g = x.clone()
     r = _backward(g, dy, w, mean, rstd, dx=g)
     assert torch.equal(g, dx) and torch.equal(r[1], dw) and torch.equal(r[2], db)
+
+
+def test_calls_from_several_threads():
+    """Different widths of one kernel from two host threads, each on its own stream."""
+    import threading
+    from paper_2104_11981_b200 import binding as B
+    faults = []
+
+    def work(c, seed):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                x, w, b = _rand((2, 40, c), 1.0, seed), _rand((2, c), 1.0, seed + 1), _rand((2, c), 1.0, seed + 2)
+                first = None
+                for _ in range(30):
+                    y, mean, rstd = _forward(x, w, b)
+                    dx, dw, db = _backward(x, y, w, mean, rstd)
+                    first = first or (y, dx, dw, db)
+                    stream.synchronize()
+                    assert all(torch.equal(p, q) for p, q in zip(first, (y, dx, dw, db)))
+        except BaseException as e:  # noqa: BLE001
+            faults.append(e)
+
+    threads = [threading.Thread(target=work, args=(c, c)) for c in (4097, 8191, 9000, 16_384)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not faults and B.kernel_error() == 0
 
 
 def test_no_rows():
