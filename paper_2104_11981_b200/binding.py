@@ -1,4 +1,5 @@
-"""ctypes binding of libdecentlam.so: argument marshalling only.
+"""Binding of libdecentlam.so: argument marshalling only (ctypes; the training operators' calls, which have up to 22
+arguments, go through _calls, a C module that converts them in a tenth of the time).
 
 Every function mirrors the C entry point of the same name (include/decentlam.h).  Tensors are
 torch CUDA tensors used purely as device memory; only their data pointers, strides and the
@@ -33,6 +34,8 @@ if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} not found: build it with `python -m paper_2104_11981_b200.build` "
                       "(there is no CPU fallback)")
 _lib = ctypes.CDLL(LIB_PATH)
+
+from . import _calls  # noqa: E402  (linked to the library above)
 
 _i32p = ctypes.POINTER(ctypes.c_int32)
 _f32p = ctypes.POINTER(ctypes.c_float)
@@ -417,6 +420,7 @@ class Gradients:
 
     def __init__(self, handle, n, tensors, keep):
         self.handle, self.n, self.keep = handle, n, keep
+        self.address = handle.value
         po, c = ctypes.POINTER(_i64)(), _i64()
         _check(_lib.gradients_layout(handle, ctypes.byref(po), ctypes.byref(c)), "gradients_layout")
         self.offsets = [po[t] for t in range(tensors)]  # first column of each tensor in a stacked row
@@ -431,7 +435,7 @@ class Gradients:
     def destroy(self):
         if getattr(self, "handle", None):
             _lib.gradients_destroy(self.handle)
-            self.handle = None
+            self.handle = self.address = None
 
 
 
@@ -461,7 +465,7 @@ def _check_norms(grads, norms):
 def gradient_norm(grads, norms, kind=NORM_L2, stream=None):
     """norms[i] <- norm of node i's whole gradient (fp32 device tensor of n elements)."""
     _check_norms(grads, norms)
-    _check(_lib.gradient_norm(grads.handle, kind, norms.data_ptr(), _stream_ptr(stream)), "gradient_norm")
+    _check(_calls.gradient_norm(grads.address, kind, norms.data_ptr(), _stream_ptr(stream)), "gradient_norm")
 
 
 def gradient_clip(grads, max_norm, norms, g=None, kind=NORM_L2, stream=None):
@@ -473,7 +477,7 @@ def gradient_clip(grads, max_norm, norms, g=None, kind=NORM_L2, stream=None):
         n, width = g.shape
         assert g.is_cuda and n == grads.n and width >= grads.columns and (g.stride(1) == 1 or width == 1)
         pg, gd, ldg = g.data_ptr(), _dtype(g), g.stride(0) if n > 1 else width
-    _check(_lib.gradient_clip(grads.handle, kind, max_norm, norms.data_ptr(), pg, gd, ldg, _stream_ptr(stream)),
+    _check(_calls.gradient_clip(grads.address, kind, max_norm, norms.data_ptr(), pg, gd, ldg, _stream_ptr(stream)),
            "gradient_clip")
 
 
@@ -514,9 +518,9 @@ def layer_norm(x, weight, bias, eps, y, mean, rstd, stream=None):
     n, rows, c = shape
     assert _dtype(weight) == G_F32 and (bias is None or _dtype(bias) == G_F32)
     (pw, ldw), (pb, ldb) = _node_vectors(weight, n, c), _node_vectors(bias, n, c)
-    _check(_lib.layer_norm(n, rows, c, x.data_ptr(), _dtype(x), _node_rows(x, shape, dtype), pw, ldw, pb, ldb, eps,
-                           y.data_ptr(), _node_rows(y, shape, dtype), _per_row(mean, n * rows), _per_row(rstd, n * rows),
-                           _stream_ptr(stream)), "layer_norm")
+    _check(_calls.layer_norm(n, rows, c, x.data_ptr(), _dtype(x), _node_rows(x, shape, dtype), pw, ldw, pb, ldb, eps,
+                             y.data_ptr(), _node_rows(y, shape, dtype), _per_row(mean, n * rows), _per_row(rstd, n * rows),
+                             _stream_ptr(stream)), "layer_norm")
 
 
 def layer_norm_grad_workspace_bytes(n, rows, c):
@@ -535,10 +539,10 @@ def layer_norm_grad(x, dy, weight, mean, rstd, dx, dweight, dbias, workspace, st
     assert _dtype(weight) == G_F32 and (dbias is None or dbias.dtype == dweight.dtype) and workspace.is_cuda
     pw, ldw = _node_vectors(weight, n, c)
     (pgw, ldgw), (pgb, ldgb) = _node_vectors(dweight, n, c), _node_vectors(dbias, n, c)
-    _check(_lib.layer_norm_grad(n, rows, c, x.data_ptr(), _dtype(x), _node_rows(x, shape, dtype), dy.data_ptr(),
-                                _node_rows(dy, shape, dtype), pw, ldw, _per_row(mean, n * rows), _per_row(rstd, n * rows),
-                                dx.data_ptr(), _node_rows(dx, shape, dtype), pgw, ldgw, pgb, ldgb, _dtype(dweight),
-                                workspace.data_ptr(), workspace.nbytes, _stream_ptr(stream)), "layer_norm_grad")
+    _check(_calls.layer_norm_grad(n, rows, c, x.data_ptr(), _dtype(x), _node_rows(x, shape, dtype), dy.data_ptr(),
+                                  _node_rows(dy, shape, dtype), pw, ldw, _per_row(mean, n * rows), _per_row(rstd, n * rows),
+                                  dx.data_ptr(), _node_rows(dx, shape, dtype), pgw, ldgw, pgb, ldgb, _dtype(dweight),
+                                  workspace.data_ptr(), workspace.nbytes, _stream_ptr(stream)), "layer_norm_grad")
 
 
 def policy_loss_workspace_bytes(n, rows, vocab):
@@ -561,11 +565,11 @@ def policy_loss_grad(logits, tokens, weight, advantage, old_logp, ref_logp, clip
     assert tokens.is_cuda and tokens.dtype == torch.int64 and tokens.is_contiguous() and tokens.numel() == count
     assert workspace.is_cuda
     pd, ldd = (dlogits.data_ptr(), _node_rows(dlogits, shape, dtype)) if dlogits is not None else (None, 0)
-    _check(_lib.policy_loss_grad(n, rows, vocab, logits.data_ptr(), _dtype(logits), _node_rows(logits, shape, dtype),
-                                 tokens.data_ptr(), _per_row(weight, count), _per_row(advantage, count),
-                                 _per_row(old_logp, count), _per_row(ref_logp, count) if ref_logp is not None else None,
-                                 clip_low, clip_high, kl_coef, _per_row(loss, n), _per_row(logp, count), pd, ldd,
-                                 workspace.data_ptr(), workspace.nbytes, _stream_ptr(stream)), "policy_loss_grad")
+    _check(_calls.policy_loss_grad(n, rows, vocab, logits.data_ptr(), _dtype(logits), _node_rows(logits, shape, dtype),
+                                   tokens.data_ptr(), _per_row(weight, count), _per_row(advantage, count),
+                                   _per_row(old_logp, count), _per_row(ref_logp, count) if ref_logp is not None else None,
+                                   clip_low, clip_high, kl_coef, _per_row(loss, n), _per_row(logp, count), pd, ldd,
+                                   workspace.data_ptr(), workspace.nbytes, _stream_ptr(stream)), "policy_loss_grad")
 
 
 def launch_count():

@@ -1,4 +1,4 @@
-"""Build libdecentlam.so (CUDA kernels + C ABI) for sm_100a, in-tree.
+"""Build libdecentlam.so (CUDA kernels + C ABI) for sm_100a and _calls (its CPython entry points), in-tree.
 
 Usage: python -m paper_2104_11981_b200.build [--force] [--verbose]
 nvcc cross-compiles without a GPU; the runtime is linked statically so the library loads
@@ -8,6 +8,7 @@ compiled to an object of its own (in parallel, only when it or a header changed)
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -15,6 +16,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 OBJ = os.path.join(HERE, "_build")
 OUT = os.path.join(HERE, "libdecentlam.so")
+CALLS = os.path.join(HERE, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["api.cpp", "topology.cpp", "sharded.cpp", "step_kernels.cu", "step_merged.cu", "step_sharded.cu",
            "pmsgd_kernel.cu", "lsq_kernels.cu", "gradients.cpp", "gradient_kernels.cu", "train.cpp", "layer_norm.cu",
            "policy_loss.cu"]
@@ -50,8 +52,20 @@ def _compile(src: str, force: bool, verbose: bool) -> str:
     return obj
 
 
+def _build_calls(force: bool) -> None:
+    src = os.path.join(CSRC, "calls.c")
+    if not force and os.path.exists(CALLS) and all(os.path.getmtime(p) <= os.path.getmtime(CALLS)
+                                                   for p in (src, os.path.join(INCLUDE, "decentlam.h"))):
+        return
+    tmp = CALLS + ".tmp"
+    subprocess.run([os.environ.get("CC", "gcc"), "-O2", "-fPIC", "-shared", "-I", INCLUDE, "-I", sysconfig.get_paths()["include"],
+                    src, "-o", tmp, "-L", HERE, "-l:libdecentlam.so", "-Wl,-rpath,$ORIGIN"], check=True)
+    os.replace(tmp, CALLS)
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not _stale():
+        _build_calls(force)
         return OUT
     os.makedirs(OBJ, exist_ok=True)
     with ThreadPoolExecutor(max_workers=min(len(SOURCES), os.cpu_count() or 1)) as pool:
@@ -60,6 +74,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     tmp = OUT + ".tmp"
     subprocess.run([nvcc] + ARCH + ["-shared", "-Xcompiler", "-fPIC", "-cudart", "static"] + objs + ["-o", tmp], check=True)
     os.replace(tmp, OUT)
+    _build_calls(force)
     return OUT
 
 

@@ -118,3 +118,15 @@ def test_policy_loss_refusals():
     assert _policy(ws=0) == -10 and _policy(wb=255) == -10 and _policy(ws=0xa0080) == -10
     assert _policy(d=0x10004) == -4 and _policy(loss=0x30000) == -4 and _policy(logp=0x10000) == -4
     assert _policy(ws=0x20000) == -4 and _policy(d=0x10000, ldd=101) == -4
+
+
+def test_calls_convert_their_arguments():
+    from paper_2104_11981_b200 import _calls
+    none = [1, 1, 8, None, 0, 8, None, 8, None, 8, 1e-5, None, 8, None, None, 0]
+    assert _calls.layer_norm(*none) == B._lib.layer_norm(*none) == -1  # None is a null pointer in both
+    for bad in (none[:-1], none + [0], [None if k == 10 else v for k, v in enumerate(none)], ["1"] + none[1:]):
+        with pytest.raises(TypeError):
+            _calls.layer_norm(*bad)
+    with pytest.raises(OverflowError):
+        _calls.layer_norm(1, 1 << 64, *none[2:])
+    assert _calls.layer_norm(1, 1 << 62, *none[2:]) == B._lib.layer_norm(1, 1 << 62, *none[2:])  # 64-bit lengths arrive whole
