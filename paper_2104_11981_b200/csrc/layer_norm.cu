@@ -3,8 +3,8 @@
 // backward, with xh = (x - mu) rstd and v = w dy:
 //   dx = rstd (v - mean_c v - xh mean_c (v xh)) ,  dw = sum_rows dy xh ,  db = sum_rows dy.
 // Both directions read x (and dy) once and write y (dx) once.  8 x 2048 x 4096 bf16: forward 47 us (5.7 TB/s, memory-bound),
-// backward 81 us (5.0 TB/s; 23 instructions per element, bound by issue slots and the two barriers of a row as much as
-// by memory), 8192-wide fp32 rows 5.8 and 5.9 TB/s.  Rows of odd widths above 8192 keep one CTA per SM and run at a third of that.
+// backward 74 us (5.5 TB/s; 23 instructions per element, bound by issue slots and the barrier of a row as much as by
+// memory), 8192-wide fp32 rows 6.0 TB/s either way.  Rows of odd widths above 8192 keep one CTA per SM and run at a third of that.
 // A group of threads (eight lanes of a warp up to a CTA) takes every G-th row of a node.  Rows come into shared memory by
 // asynchronous copies a few rows ahead, which hold no registers, in whole 16-byte chunks wherever the row starts.  A thread
 // keeps its columns' weights in registers, and backward its sums of dy xh and dy over the rows; a second kernel adds these
@@ -61,9 +61,19 @@ __device__ __forceinline__ float warps_sum(const float* part) {
     for (int o = WARPS / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
-// Two sums over a group at once: after one exchange each half of the lanes carries one of them.
-template <int TPR>
-__device__ __forceinline__ void pair_sum(float& a, float& b, float (*part)[TPR > 32 ? TPR / 32 : 1]) {
+// The one barrier of a row that came by bulk copy: it joins the warps' sums, says to every thread whether the copy came for all
+// (`ok`), and frees the row's slot, since its values are in registers by then.  With a barrier for each: 81 us instead of 73 for
+// 8 x 2048 x 4096 bf16 backward.
+template <bool BULK>
+__device__ __forceinline__ bool sums_barrier(bool ok) {
+    if constexpr (BULK) return __syncthreads_and(ok);
+    __syncthreads();
+    return true;
+}
+// Two sums over a group at once: after one exchange each half of the lanes carries one of them.  Returns
+// sums_barrier's answer.
+template <int TPR, bool BULK>
+__device__ __forceinline__ bool pair_sum(float& a, float& b, float (*part)[TPR > 32 ? TPR / 32 : 1], bool ok) {
     constexpr int H = (TPR < 32 ? TPR : 32) / 2, WARPS = TPR / 32;
     const bool upper = threadIdx.x & H;
     float v = (upper ? b : a) + __shfl_xor_sync(0xffffffffu, upper ? a : b, H);
@@ -71,12 +81,13 @@ __device__ __forceinline__ void pair_sum(float& a, float& b, float (*part)[TPR >
     for (int o = H / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     if constexpr (TPR > 32) {
         if ((threadIdx.x & 15) == 0) part[upper][threadIdx.x >> 5] = v;
-        __syncthreads();
+        ok = sums_barrier<BULK>(ok);
         v = warps_sum<WARPS>(part[upper]);
     }
     const float w = __shfl_xor_sync(0xffffffffu, v, H);
     a = upper ? w : v;
     b = upper ? v : w;
+    return TPR <= 32 || ok;
 }
 
 // Bytes of shared memory for a row: its chunks, wherever it starts within the first.
@@ -275,12 +286,9 @@ __global__ void __launch_bounds__(kBlock<TPR>)
     long long r = first;
     for (long long lead = TPR < 32 ? first - group % (32 / (TPR < 32 ? TPR : 32)) : first; lead < rows; lead += stride) {
         ask(slot == 0 ? D - 1 : slot - 1);
+        bool ok = true;
         if constexpr (BULK) {
-            if (!cta_wait(smem_u32(&full[slot]), (parities >> slot) & 1)) {
-                give_up(full, parities);
-                return;
-            }
-            parities ^= 1u << slot;
+            ok = mbar_wait(smem_u32(&full[slot]), (parities >> slot) & 1);
         } else {
             wait_copies<D - 1>();
             group_barrier<TPR>();
@@ -310,6 +318,7 @@ __global__ void __launch_bounds__(kBlock<TPR>)
                     }
                 }
             }
+        if constexpr (BULK) fence_before_refill();
         sq = lane_sum<TPR>(LEN == 1 ? sq : s2.x + s2.y);
         float mu = near;
         if constexpr (TPR > 32) {
@@ -318,7 +327,10 @@ __global__ void __launch_bounds__(kBlock<TPR>)
                 part[side][0][threadIdx.x >> 5] = sum;
                 part[side][1][threadIdx.x >> 5] = sq;
             }
-            __syncthreads();
+            if (!sums_barrier<BULK>(ok)) {
+                give_up(full, parities);
+                return;
+            }
             const float ws = part[side][0][threadIdx.x & (WARPS - 1)];
             float total = ws;
 #pragma unroll
@@ -343,9 +355,9 @@ __global__ void __launch_bounds__(kBlock<TPR>)
             mean[base + r] = mu;
             rstd[base + r] = rs;
         }
-        if constexpr (BULK) fence_before_refill();
-        group_barrier<TPR>();  // the slot may be filled again, and the results are in their buffer
+        if constexpr (!BULK) group_barrier<TPR>();  // the slot may be filled again, and the results are in their buffer
         if (LEN == 1 && live) flush_row<T, TPR>(to, out, c, t);
+        parities ^= 1u << slot;
         if (++slot == D) slot = 0;
         r += stride;
         row += stride * ldx;
@@ -491,12 +503,9 @@ __global__ void __launch_bounds__(kBlock<TPR>)
             nmu = mean[r + stride];
             nrs = rstd[r + stride];
         }
+        bool ok = true;
         if constexpr (BULK) {
-            if (!cta_wait(smem_u32(&full[slot]), (parities >> slot) & 1)) {
-                give_up(full, parities);
-                return;
-            }
-            parities ^= 1u << slot;
+            ok = mbar_wait(smem_u32(&full[slot]), (parities >> slot) & 1);
         } else {
             wait_copies<D - 1>();
             group_barrier<TPR>();
@@ -545,7 +554,11 @@ __global__ void __launch_bounds__(kBlock<TPR>)
                 }
             }
         }
-        pair_sum<TPR>(sums[0], sums[1], part[side]);
+        if constexpr (BULK && HOLD) fence_before_refill();
+        if (!pair_sum<TPR, BULK>(sums[0], sums[1], part[side], ok)) {
+            give_up(full, parities);
+            return;
+        }
         side ^= 1;
         const float m0 = sums[0] * inv_c, m1 = sums[1] * inv_c;
         if constexpr (HOLD) {
@@ -573,9 +586,10 @@ __global__ void __launch_bounds__(kBlock<TPR>)
                 }
             }
         }
-        if constexpr (BULK) fence_before_refill();
-        group_barrier<TPR>();  // the slot may be filled again, and the results are in their buffer
+        if constexpr (BULK && !HOLD) fence_before_refill();
+        if constexpr (!BULK || !HOLD) group_barrier<TPR>();  // the slot may be filled again, and the results are in their buffer
         if (LEN == 1 && live) flush_row<T, TPR>(to, out, c, t);
+        parities ^= 1u << slot;
         if (++slot == D) slot = 0;
         r += stride;
         xr += stride * ldx;
@@ -652,36 +666,32 @@ __global__ void __launch_bounds__(1024)
 }
 
 // dw, db <- sums of the CTAs' parts in order.  32 columns by 8 slices of the CTAs; parts == 0 gives zeros.
-template <typename G>
-__global__ void __launch_bounds__(256) layer_norm_join_kernel(long long c, int parts, const float* partial, G* dweight,
-                                                               long long ldgw, G* dbias, long long ldgb) {
-    __shared__ float sums[8][2][32];
+// dw and db of a node from its CTAs' partial sums, 32 columns (of 2 c: dw's, then db's) to a CTA, each warp the sum of every
+// SLICES-th part.
+template <typename G, int SLICES>
+__global__ void __launch_bounds__(SLICES * 32) layer_norm_join_kernel(long long c, int parts, const float* partial, G* dweight,
+                                                                      long long ldgw, G* dbias, long long ldgb) {
+    __shared__ float sums[SLICES][32];
     const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
     const int node = blockIdx.y;
     const long long col = (long long)blockIdx.x * 32 + lane;
-    pdl_wait();
-    pdl_release();
-    float s0 = 0.0f, s1 = 0.0f;
-    if (col < c) {
+    pdl_wait();  // and no early release: CTAs of the next kernel that come between these cost it more than it gains by them (114 us
+                 // instead of 94 for 4 x 10000 x 1280 fp32, call after call)
+    float s = 0.0f;
+    if (col < 2 * c) {
         const float* p = partial + (long long)node * parts * 2 * c + col;
-#pragma unroll 4
-        for (int k = slice; k < parts; k += 8) {
-            s0 += p[(long long)k * 2 * c];
-            s1 += p[((long long)k * 2 + 1) * c];
-        }
+#pragma unroll 8
+        for (int k = slice; k < parts; k += SLICES) s += p[(long long)k * 2 * c];
     }
-    sums[slice][0][lane] = s0;
-    sums[slice][1][lane] = s1;
+    sums[slice][lane] = s;
     __syncthreads();
-    if (slice < 2 && col < c) {
-        float s = sums[0][slice][lane];
+    if (slice > 0 || col >= 2 * c) return;
 #pragma unroll
-        for (int k = 1; k < 8; ++k) s += sums[k][slice][lane];
-        if (slice == 0)
-            dweight[node * ldgw + col] = narrow<G>(s);
-        else if (dbias)
-            dbias[node * ldgb + col] = narrow<G>(s);
-    }
+    for (int k = 1; k < SLICES; ++k) s += sums[k][lane];
+    if (col < c)
+        dweight[node * ldgw + col] = narrow<G>(s);
+    else if (dbias)
+        dbias[node * ldgb + col - c] = narrow<G>(s);
 }
 
 // Rows up to this many elements are held on chip; wider ones are swept from memory.
@@ -715,10 +725,10 @@ bool rows_aligned(const void* p, int64_t ld, size_t esz) { return (uintptr_t)p %
 // Dynamic shared memory that every kernel here is allowed: an SM's, less room for the static part.
 constexpr size_t kMostShared = 226 << 10;
 
-// CTAs per node: as many as the SMs hold at once, shared by the nodes, and no more than there are rows for.  What the runtime
+// CTAs per node: as many as the SMs hold at once, `most` on each, shared by the nodes, and no more than there are rows for.  What the runtime
 // says of a kernel is asked once per size and host thread: it costs as much as the launch.
 template <typename K>
-int resident_ctas(K kernel, int block, size_t smem, int n, int64_t rows, int groups) {
+int resident_ctas(K kernel, int block, size_t smem, int most, int n, int64_t rows, int groups) {
     struct Known {
         K kernel;
         int device;
@@ -736,7 +746,7 @@ int resident_ctas(K kernel, int block, size_t smem, int n, int64_t rows, int gro
             cudaOccupancyMaxActiveBlocksPerMultiprocessor(&known.per_sm, kernel, block, smem) != cudaSuccess || known.per_sm < 1)
             return 0;
     }
-    const int64_t cap = std::max<int64_t>(1, (int64_t)info.sms * known.per_sm / n);
+    const int64_t cap = std::max<int64_t>(1, (int64_t)info.sms * std::min(known.per_sm, most) / n);
     return (int)std::min<int64_t>((rows + groups - 1) / groups, cap);
 }
 
@@ -759,7 +769,7 @@ int run_forward(const dlm_norm_args& a, cudaStream_t s) {
     if constexpr (TPR == 512 && D > 2)  // two rows fit whatever the type
         if (smem > kMostShared) return run_forward<T, LEN, E, TPR, D - 1>(a, s);
     auto kern = layer_norm_kernel<T, LEN, E, TPR, D>;
-    const int ctas = resident_ctas(kern, kBlock<TPR>, smem, a.n, a.rows, GROUPS);
+    const int ctas = resident_ctas(kern, kBlock<TPR>, smem, 32, a.n, a.rows, GROUPS);
     if (ctas < 1) return DLM_ERR_CUDA;
     cudaError_t err = launch_overlapped(kern, dim3((unsigned)ctas, a.n), dim3(kBlock<TPR>), smem, s, 1, a.rows, (int)a.c,
                                         static_cast<const T*>(a.x), a.ldx, a.weight, a.ldw, a.bias, a.ldb, a.eps,
@@ -807,7 +817,11 @@ int run_backward(const dlm_norm_args& a, int* parts, cudaStream_t s) {
             return wide_backward<T>(a, parts, s);
     }
     auto kern = layer_norm_grad_kernel<T, LEN, E, TPR, D>;
-    *parts = std::min(resident_ctas(kern, kBlock<TPR>, smem, a.n, a.rows, GROUPS), dlm_norm_max_ctas(a.n, a.rows, a.c));
+    // More than about 128 KB of rows on their way per SM is more than the memory wants, but two CTAs (8 x 2500 x 2048 fp32
+    // with four CTAs of 49 KB 87 us, with two 77; 4 x 8000 x 1536, four of 37 KB 101, three 91).  Narrow groups need their CTAs
+    // for the arithmetic (20833 x 768 fp32 with nine of 25 KB 35 us, with five 37).
+    const int most = TPR == 256 ? std::max(2, (int)((128 << 10) / smem)) : 32;
+    *parts = std::min(resident_ctas(kern, kBlock<TPR>, smem, most, a.n, a.rows, GROUPS), dlm_norm_max_ctas(a.n, a.rows, a.c));
     if (*parts < 1) return DLM_ERR_CUDA;
     cudaError_t err = launch_overlapped(kern, dim3((unsigned)*parts, a.n), dim3(kBlock<TPR>), smem, s, 1, a.rows, (int)a.c,
                                         static_cast<const T*>(a.x), a.ldx, static_cast<const T*>(a.dy), a.lddy, a.weight, a.ldw,
@@ -833,10 +847,20 @@ int backward(const dlm_norm_args& a, int* parts, cudaStream_t s) {
 #undef DLM_NORM_SHAPES
 #undef DLM_NORM_GRAD_SHAPES
 
+template <typename G, int SLICES>
+cudaError_t run_join(const dlm_norm_args& a, int parts, cudaStream_t s) {
+    return launch_overlapped(layer_norm_join_kernel<G, SLICES>, dim3((unsigned)((2 * a.c + 31) / 32), a.n), dim3(SLICES * 32), 0, s, 1,
+                             a.c, parts, (const float*)a.partial, static_cast<G*>(a.dweight), a.ldgw, static_cast<G*>(a.dbias), a.ldgb);
+}
+// As few slices as give each SM a thousand threads: 32 take 6.7 us where 8 took 23 (592 parts of 2 x 2048 columns), but 32 for eight
+// nodes' 4096 columns of 37 parts make the whole gradient 81 us instead of 74.
 template <typename G>
 cudaError_t join(const dlm_norm_args& a, int parts, cudaStream_t s) {
-    return launch_overlapped(layer_norm_join_kernel<G>, dim3((unsigned)((a.c + 31) / 32), a.n), dim3(256), 0, s, 1, a.c, parts,
-                             (const float*)a.partial, static_cast<G*>(a.dweight), a.ldgw, static_cast<G*>(a.dbias), a.ldgb);
+    const int64_t wanted = 1024ll * device_info().sms / (2 * a.c * a.n);
+    if (wanted < 4) return run_join<G, 4>(a, parts, s);
+    if (wanted < 8) return run_join<G, 8>(a, parts, s);
+    if (wanted < 16) return run_join<G, 16>(a, parts, s);
+    return run_join<G, 32>(a, parts, s);
 }
 
 }  // namespace
