@@ -2,7 +2,7 @@
 //   mu = mean_c x ,  rstd = 1 / sqrt(mean_c (x - mu)^2 + eps) ,  y = (x - mu) rstd w + b ;
 // backward, with xh = (x - mu) rstd and v = w dy:
 //   dx = rstd (v - mean_c v - xh mean_c (v xh)) ,  dw = sum_rows dy xh ,  db = sum_rows dy.
-// Both directions read x (and dy) once and write y (dx) once.  8 x 2048 x 4096 bf16: forward 47 us (5.7 TB/s, memory-bound),
+// Both directions read x (and dy) once and write y (dx) once.  8 x 2048 x 4096 bf16: forward 46 us (5.9 TB/s, memory-bound),
 // backward 74 us (5.5 TB/s; 23 instructions per element, bound by issue slots and the barrier of a row as much as by
 // memory), 8192-wide fp32 rows 6.0 TB/s either way.  Rows of odd widths above 8192 keep one CTA per SM and run at a third of that.
 // A group of threads (eight lanes of a warp up to a CTA) takes every G-th row of a node.  Rows come into shared memory by
@@ -762,7 +762,13 @@ int wide_forward(const dlm_norm_args& a, cudaStream_t s) {
     return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
 }
 
-template <typename T, int LEN, int E, int TPR, int D = kDepth<TPR>>
+// Two rows where three would be more than the memory wants beside the writes: 8 x 2048 x 4096 bf16 46 us instead of 50, 4 x 2000 x
+// 5120 fp32 52 instead of 59; but 2560 columns bf16 run at 73 % of the copy rate instead of 74.  Groups of 256 threads with bf16
+// rows have half the bytes on their way and keep three (8192 columns: 86 % instead of 81).
+template <typename T, int TPR>
+constexpr int kForwardDepth = TPR == 128 || (TPR == 256 && sizeof(T) == 4) ? 2 : kDepth<TPR>;
+
+template <typename T, int LEN, int E, int TPR, int D = kForwardDepth<T, TPR>>
 int run_forward(const dlm_norm_args& a, cudaStream_t s) {
     constexpr int GROUPS = kBlock<TPR> / TPR;
     const size_t smem = (size_t)GROUPS * (D + (LEN == 1)) * row_bytes((int)a.c, sizeof(T));
