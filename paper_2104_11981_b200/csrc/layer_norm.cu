@@ -3,7 +3,7 @@
 // backward, with xh = (x - mu) rstd and v = w dy:
 //   dx = rstd (v - mean_c v - xh mean_c (v xh)) ,  dw = sum_rows dy xh ,  db = sum_rows dy.
 // Both directions read x (and dy) once and write y (dx) once.  8 x 2048 x 4096 bf16: forward 46 us (5.9 TB/s, memory-bound),
-// backward 74 us (5.5 TB/s; 23 instructions per element, bound by issue slots and the barrier of a row as much as by
+// backward 74 us (5.5 TB/s; 17 instructions per element, bound by issue slots and latency within a row as much as by
 // memory), 8192-wide fp32 rows 6.0 TB/s either way.  Rows of odd widths above 8192 keep one CTA per SM and run at a third of that.
 // A group of threads (eight lanes of a warp up to a CTA) takes every G-th row of a node.  Rows come into shared memory by
 // asynchronous copies a few rows ahead, which hold no registers, in whole 16-byte chunks wherever the row starts.  A thread
