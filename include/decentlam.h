@@ -470,6 +470,8 @@ DLM_API int layer_norm_grad(int n, int64_t rows, int64_t c, const void* x, int d
  *   weight     : device fp32 [n * rows]: the mask and the normalisation in one (1 / tokens of the batch, for instance).  A row
  *                with weight 0, or whose token is outside [0, vocab), is masked: whatever its logits hold, it adds nothing
  *                to the loss, its logp is 0 and its gradient row is 0.
+ *                In a kept row logits may have any size: forbidden tokens may be marked by -inf, the type's lowest value or
+ *                any other, even where a row holds nothing else (finite marks alone: a uniform row; -inf alone: NaN, 0 / 0).
  *   advantage, old_logp, ref_logp : device fp32 [n * rows]; ref_logp may be NULL where kl_coef is 0
  *   loss       : device fp32 [n], written;  logp: device fp32 [n * rows], written
  *   dlogits    : device [n * rows, vocab] of dtype, row stride ldd, written; NULL: loss and logp only;

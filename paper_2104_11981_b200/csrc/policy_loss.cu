@@ -4,7 +4,7 @@
 //   dl/dlogp = w ( -A r [r A <= clip(r) A] + kl (1 - e^{ref - logp}) ) ,  dl/dz_v = dl/dlogp ([v = t] - e^{z_v} / sum).
 // The factor dl/dlogp depends on the row's own numbers alone, so loss and gradient take one kernel: a first sweep for
 // the maximum and the sum of exponentials, a second for the gradient.  The logits are read once, the gradient written once.
-// 4096 x 131072 bf16, a quarter masked: 334 us (5.6 TB/s); the exponentials keep their unit 62 % and the issue slots 62 % busy at
+// 4096 x 131072 bf16, a quarter masked: 339 us (5.5 TB/s); the exponentials keep their unit 62 % and the issue slots 62 % busy at
 // the same time.  16000 x 4096 fp32: 78 us (5.9 TB/s of what is not masked), memory-bound.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
@@ -30,11 +30,13 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 
 constexpr int kMaxCtas = 8;  // CTAs of a cluster: the most that every GPU of the architecture schedules
 
-// Exponents are kept to base 2: e^z = 2^{z L}, L = log2(e) in fp32, and sums are held as s 2^c with an integer c at or above
-// the largest exponent seen.  So an element takes one fused multiply-add, z L - c, rounded once; moving a sum to another
-// reference is exact; and L's own rounding changes an exponent z L by 1.4e-8 of itself, less than that one rounding.
+// Sums of exponentials are held as s e^m, m the largest logit seen, and an element adds 2^{(v - m) L}, L = log2(e) in fp32: 1 at
+// the largest and never more, whatever the logits' size (forbidden tokens are marked by anything from -1e4 to -inf, and may be
+// all that a thread sees).  With the exponent as v L - ceil(m L) in one multiply-add instead, its absolute error is that of m L, which
+// passes 128 from |m| = 3e9 on and makes 0 or infinity of the sum.  The two roundings change an exponent by 2^-23 of itself, L's
+// own by 1.4e-8.  Keeping the single multiply-add for rows whose largest logit is moderate gains 1.7 us of 341 (4096 x 131072 bf16).
 constexpr float kLog2E = 1.4426950408889634f;
-constexpr double kLn2 = 0.69314718055994530942;
+constexpr float kLn2 = 0.69314718055994531f;
 
 __device__ __forceinline__ float exp2_fast(float t) {
     float r;
@@ -47,30 +49,29 @@ __device__ __forceinline__ float log2_fast(float t) {
     return r;
 }
 
-// Reference exponent and sum: total = s 2^c.  c = -inf: nothing but -inf so far.
+// Largest value and sum: total = s e^m.  m = -inf: nothing but -inf so far.
 struct Tally {
-    float c, s;
+    float m, s;
 };
-__device__ __forceinline__ float finite_ref(float c) { return c == -INFINITY ? 0.0f : c; }
-// Reference for values whose largest is m: an integer at or above their exponents.
-__device__ __forceinline__ float reference(float m) { return ceilf(m * kLog2E); }
+__device__ __forceinline__ float finite_ref(float m) { return m == -INFINITY ? 0.0f : m; }
+// e^{v - ref}
+__device__ __forceinline__ float exp_from(float v, float ref) { return exp2_fast((v - ref) * kLog2E); }
 
 // The warp's total, the same in every lane.
 __device__ __forceinline__ Tally warp_total(Tally t) {
-    float c;
-    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(c) : "f"(t.c));
-    return {c, warp_sum(t.s * exp2_fast(t.c - finite_ref(c)))};
+    float m;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(t.m));
+    return {m, warp_sum(t.s * exp_from(t.m, finite_ref(m)))};
 }
 
-// What a row's scalars come to.  exp and log take the hardware's approximations, good to 2^-22 like the sum they follow;
-// the difference of two exponents of up to a few hundred is formed in double, where it costs nothing.
+// What a row's scalars come to.  exp and log take the hardware's approximations, good to 2^-22 like the sum they follow.
 struct RowOutcome {
     float logp, loss, slope;
 };
 __device__ __forceinline__ RowOutcome row_outcome(float zt, Tally t, float w, float adv, float old_logp, bool has_ref,
                                                   float ref_logp, float lo, float hi, float kl) {
-    const double logp = (fma((double)zt, (double)kLog2E, -(double)t.c) - (double)log2_fast(t.s)) * kLn2;
-    const float lp = logp > 0.0 ? 0.0f : (float)logp;  // rounding alone can take it above 0
+    const float logp = fmaf(-log2_fast(t.s), kLn2, zt - t.m);
+    const float lp = logp > 0.0f ? 0.0f : logp;  // rounding alone can take it above 0
     const float r = exp2_fast((lp - old_logp) * kLog2E);
     const float held = fminf(fmaxf(r, 1.0f - lo), 1.0f + hi);
     const float a = r * adv, b = held * adv;
@@ -119,25 +120,46 @@ __device__ __forceinline__ float largest<__nv_bfloat16>(const Words& q) {
     return fmaxf(__low2float(m), __high2float(m));
 }
 
-// Sum of a run's 2^(v L - ref).
+// (v - ref) L + shift of two elements.  bf16 as a pair (100000 x 1000: 82 us, one by one 86), fp32 one by one, which needs fewer
+// registers (1200 x 131072: 217 us, in pairs 219).
+template <typename T>
+__device__ __forceinline__ float2 exponents(float v0, float v1, float ref, float shift) {
+    if constexpr (sizeof(T) == 4)
+        return make_float2(fmaf(v0 - ref, kLog2E, shift), fmaf(v1 - ref, kLog2E, shift));
+    else
+        return __ffma2_rn(__fadd2_rn(make_float2(v0, v1), make_float2(-ref, -ref)), make_float2(kLog2E, kLog2E), make_float2(shift, shift));
+}
+// Sum of a run's e^{v - ref}.
 template <typename T>
 __device__ __forceinline__ float sum_exp(const Words& q, float ref) {
     float v[kRun<T>];
     unpack<T>(q, v);
     float s = 0.0f;
 #pragma unroll
-    for (int e = 0; e < kRun<T>; ++e) s += exp2_fast(fmaf(v[e], kLog2E, -ref));
+    for (int e = 0; e < kRun<T>; e += 2) {
+        const float2 t = exponents<T>(v[e], v[e + 1], ref, 0.0f);
+        s += exp2_fast(t.x);
+        s += exp2_fast(t.y);
+    }
     return s;
 }
 
-// A run of the gradient: k0 2^(v L - ref).
+// Gradients are formed as k0 2^24 e^{v - ref}: 2^24 moved from the factor into the exponent, so that results below 2^-126 / |k0| leave
+// exp2_fast as normal numbers.
+constexpr float kShift = 24.0f;
+__device__ __forceinline__ float grown_exp(float v, float ref) { return exp2_fast(fmaf(v - ref, kLog2E, kShift)); }
+// A run of the gradient.
 template <typename T, bool VEC>
 __device__ __forceinline__ void put_run(T* d, const Words& q, float ref, float k0) {
     constexpr int R = kRun<T>;
     float v[R];
     unpack<T>(q, v);
 #pragma unroll
-    for (int e = 0; e < R; ++e) v[e] = k0 * exp2_fast(fmaf(v[e], kLog2E, -ref));
+    for (int e = 0; e < R; e += 2) {
+        const float2 t = exponents<T>(v[e], v[e + 1], ref, kShift);
+        v[e] = k0 * exp2_fast(t.x);
+        v[e + 1] = k0 * exp2_fast(t.y);
+    }
     if constexpr (VEC) {
         st_words(d, pack<T>(v));
     } else {
@@ -216,22 +238,22 @@ __global__ void __launch_bounds__(kBlock<TPR>, 1536 / kBlock<TPR>)
     float m = fmaxf(zh, ze);
 #pragma unroll 8
     for (int u = 0; u < held; ++u) m = fmaxf(m, largest<T>(hold[u * kBlock<TPR>]));
-    Tally sum = {reference(m), 0.0f};
+    Tally sum = {m, 0.0f};
     {
-        const float ref = finite_ref(sum.c);
-        if (has_head) sum.s += exp2_fast(fmaf(zh, kLog2E, -ref));
-        if (has_tail) sum.s += exp2_fast(fmaf(ze, kLog2E, -ref));
+        const float ref = finite_ref(m);
+        if (has_head) sum.s += exp_from(zh, ref);
+        if (has_tail) sum.s += exp_from(ze, ref);
 #pragma unroll 8
         for (int u = 0; u < held; ++u) sum.s += sum_exp<T>(hold[u * kBlock<TPR>], ref);
     }
     for (int r = kHold * TPR; r < mine; r += TPR) {
         const Words x = ld_words(zp + (long long)r * R);
-        const float c = reference(largest<T>(x));
-        if (c > sum.c) {
-            sum.s *= exp2_fast(sum.c - c);
-            sum.c = c;
+        const float top = largest<T>(x);
+        if (top > sum.m) {
+            sum.s *= exp_from(sum.m, top);
+            sum.m = top;
         }
-        sum.s += sum_exp<T>(x, finite_ref(sum.c));
+        sum.s += sum_exp<T>(x, finite_ref(sum.m));
     }
     sum = warp_total(sum);
     if constexpr (TPR > 32) {
@@ -259,8 +281,7 @@ __global__ void __launch_bounds__(kBlock<TPR>, 1536 / kBlock<TPR>)
             a.logp[row] = o.logp;
             row_loss[row] = o.loss;
         }
-        // 2^24 moved from the factor into the exponent: results below 2^-126 / |k0| leave exp2_fast as normal numbers
-        two = {finite_ref(sum.c) - 24.0f, -__fdividef(o.slope, sum.s) * 0x1p-24f, o.slope};
+        two = {finite_ref(sum.m), -__fdividef(o.slope, sum.s) * 0x1p-24f, o.slope};
         if (TPR > 32 && threadIdx.x == 0) shared_second = two;
     }
     if constexpr (TPR > 32) {
@@ -281,13 +302,13 @@ __global__ void __launch_bounds__(kBlock<TPR>, 1536 / kBlock<TPR>)
             put_run<T, true>(dp + (long long)r * R, ld_words(zp + (long long)r * R), two.ref, two.k0);
         else
             put_run<T, false>(dp + (long long)r * R, ld_words(zp + (long long)r * R), two.ref, two.k0);
-    if (has_head) d[t] = narrow<T>(two.k0 * exp2_fast(fmaf(zh, kLog2E, -two.ref)));
-    if (has_tail) d[tail + t] = narrow<T>(two.k0 * exp2_fast(fmaf(ze, kLog2E, -two.ref)));
+    if (has_head) d[t] = narrow<T>(two.k0 * grown_exp(zh, two.ref));
+    if (has_tail) d[tail + t] = narrow<T>(two.k0 * grown_exp(ze, two.ref));
     // the token's own element, once more by the thread that has just written it
     const int at = (int)token - head, run = at / R - first;
     const bool in_run = at >= 0 && (int)token < tail && run >= 0 && run - t < mine && run % TPR == t;
     if (in_run || (has_head && token == t) || (has_tail && token == tail + t))
-        d[token] = narrow<T>(fmaf(two.k0, exp2_fast(fmaf(zt, kLog2E, -two.ref)), two.slope));
+        d[token] = narrow<T>(fmaf(two.k0, grown_exp(zt, two.ref), two.slope));
 }
 
 // loss_i = sum of the node's row losses, in a fixed order: each of a cluster's CTAs sums a range, the first adds the parts.
