@@ -34,6 +34,10 @@ inline const DeviceInfo& device_info() {
     return info[dev];
 }
 
+// Waits until the tables copied from pageable memory are on the device.  cudaMemcpy may return when it has staged them, and a call on a
+// stream that is not ordered behind the default one would then read what was there before.
+inline bool finish_uploads() { return cudaStreamSynchronize(cudaStreamLegacy) == cudaSuccess; }
+
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);

@@ -105,7 +105,7 @@ int build(int n, int tensors, const int64_t* sizes, const int* dtypes, const voi
         if (cudaMalloc((void**)&list.d_scale, n * sizeof(float)) != cudaSuccess ||
             cudaMalloc((void**)&list.d_partial, (size_t)n * DLM_CLIP_CTAS_PER_SM * info.sms * DLM_CLIP_WARPS * sizeof(double)) != cudaSuccess) return DLM_ERR_CUDA;
     }
-    return DLM_OK;
+    return dlm::finish_uploads() ? DLM_OK : DLM_ERR_CUDA;
 }
 
 bool meets_a_source(const dlm_gradients& list, uintptr_t lo, uintptr_t hi) {

@@ -15,6 +15,7 @@
 #include <new>
 
 #include "dlm_internal.h"
+#include "dlm_launch.h"
 
 namespace {
 
@@ -137,6 +138,7 @@ int topology_shard(const dlm_topology* topo, int rank, int ranks, dlm_shard** ou
         if ((rc = upload(loc.ent, &loc.d_ent)) != DLM_OK) break;
         if ((rc = upload(loc.order, &loc.d_order)) != DLM_OK) break;
     }
+    if (have_device && rc == DLM_OK && !dlm::finish_uploads()) rc = DLM_ERR_CUDA;
     if (rc != DLM_OK) {
         cudaGetLastError();
         topology_shard_destroy(sh);

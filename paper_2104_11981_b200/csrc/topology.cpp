@@ -9,6 +9,7 @@
 #include <new>
 
 #include "dlm_internal.h"
+#include "dlm_launch.h"
 
 namespace {
 
@@ -341,6 +342,7 @@ static int build_common(int kind, int n, int period, const int32_t* rowptr, cons
     if (rc == DLM_OK && !have_device) cudaGetLastError();
     if (have_device && cudaGetDevice(&t->device) != cudaSuccess) rc = DLM_ERR_CUDA;
     for (int slot = 0; have_device && slot < period && rc == DLM_OK; ++slot) rc = upload(t->slots[slot]);
+    if (have_device && rc == DLM_OK && !dlm::finish_uploads()) rc = DLM_ERR_CUDA;
     if (rc != DLM_OK) {
         cudaGetLastError();  // clear the error left by a failed runtime call
         topology_destroy(t);
