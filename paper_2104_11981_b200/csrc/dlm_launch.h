@@ -38,6 +38,13 @@ inline const DeviceInfo& device_info() {
 // stream that is not ordered behind the default one would then read what was there before.
 inline bool finish_uploads() { return cudaStreamSynchronize(cudaStreamLegacy) == cudaSuccess; }
 
+// For the end of an entry point: a runtime call that failed leaves its error behind, and the next step's launch would report it as
+// its own.
+inline int settled(int rc) {
+    if (rc == DLM_ERR_CUDA) cudaGetLastError();
+    return rc;
+}
+
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);

@@ -145,7 +145,7 @@ int gradients_build(int n, int tensors, const int64_t* sizes, const int* dtypes,
     }
     if (rc != DLM_OK) {
         gradients_destroy(list);
-        return rc;
+        return dlm::settled(rc);
     }
     *out = list;
     return DLM_OK;
@@ -170,7 +170,7 @@ int gradients_destroy(dlm_gradients* list) {
 int gradient_norm(dlm_gradients* list, int kind, float* norms, void* cuda_stream) {
     int rc = check_call(list, kind, norms);
     if (rc != DLM_OK) return rc;
-    return dlm_launch_gradients(*list, kind, 0.0f, norms, nullptr, DLM_G_F32, 0, cuda_stream);
+    return dlm::settled(dlm_launch_gradients(*list, kind, 0.0f, norms, nullptr, DLM_G_F32, 0, cuda_stream));
 }
 
 int gradient_clip(dlm_gradients* list, int kind, float max_norm, float* norms, void* g, int g_dtype, int64_t ldg,
@@ -190,7 +190,7 @@ int gradient_clip(dlm_gradients* list, int kind, float max_norm, float* norms, v
             for (int i = 0; i < list->n; ++i)
                 if (meets_a_source(*list, lo + row * i, lo + row * i + width)) return DLM_ERR_ALIAS;
     }
-    return dlm_launch_gradients(*list, kind, max_norm, norms, g, g_dtype, ldg, cuda_stream);
+    return dlm::settled(dlm_launch_gradients(*list, kind, max_norm, norms, g, g_dtype, ldg, cuda_stream));
 }
 
 }  // extern "C"

@@ -3,6 +3,7 @@
 #include <cstdint>
 
 #include "dlm_internal.h"
+#include "dlm_launch.h"
 #include "dlm_train.h"
 
 namespace {
@@ -86,7 +87,7 @@ int layer_norm(int n, int64_t rows, int64_t c, const void* x, int dtype, int64_t
     a.ldy = ldy;
     a.mean = mean;
     a.rstd = rstd;
-    return dlm_launch_layer_norm(a, cuda_stream);
+    return dlm::settled(dlm_launch_layer_norm(a, cuda_stream));
 }
 
 int64_t layer_norm_grad_workspace_bytes(int n, int64_t rows, int64_t c) {
@@ -147,7 +148,7 @@ int layer_norm_grad(int n, int64_t rows, int64_t c, const void* x, int dtype, in
     a.ldgb = ldgb;
     a.g_dtype = g_dtype;
     a.partial = static_cast<float*>(workspace);
-    return dlm_launch_layer_norm_grad(a, cuda_stream);
+    return dlm::settled(dlm_launch_layer_norm_grad(a, cuda_stream));
 }
 
 int64_t policy_loss_workspace_bytes(int n, int64_t rows, int64_t vocab) {
@@ -208,7 +209,7 @@ int policy_loss_grad(int n, int64_t rows, int64_t vocab, const void* logits, int
     a.dlogits = dlogits;
     a.ldd = ldd;
     a.row_loss = static_cast<float*>(workspace);
-    return dlm_launch_policy_loss(a, cuda_stream);
+    return dlm::settled(dlm_launch_policy_loss(a, cuda_stream));
 }
 
 }  // extern "C"

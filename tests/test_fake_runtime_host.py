@@ -53,3 +53,35 @@ def test_tables_have_reached_the_device_when_the_handle_is_handed_out(lib):
     assert rc == 0 and lib.fake_copies() > before and lib.fake_staged() == 0
     assert lib.topology_shard_destroy(shard) == 0 and lib.topology_destroy(topo) == 0
     assert lib.fake_blocks() == 0
+
+
+def test_a_build_that_runs_out_of_memory_leaves_nothing_behind(lib):
+    """Neither memory nor the runtime's last error, which the next step's launch would report as its own."""
+    for k in range(4):
+        lib.fake_mallocs_left(k)
+        rc, handle = _gradients(lib)
+        lib.fake_mallocs_left(-1)
+        assert (rc, bool(handle.value)) == ((-9, False) if k < 3 else (0, True))   # pieces, scales, partial sums
+        assert lib.fake_last_error() == 0
+        lib.gradients_destroy(handle)
+        assert lib.fake_blocks() == 0
+
+
+def test_a_launch_that_fails_leaves_no_error_behind(lib):
+    rc, handle = _gradients(lib)
+    assert rc == 0
+    flt, at = ctypes.c_float, lambda k: vp(k << 16)
+    calls = {
+        "gradient_norm": (handle, 0, vp(1 << 20), None),
+        "gradient_clip": (handle, 0, flt(1.0), vp(1 << 20), None, 0, i64(0), None),
+        "layer_norm": (2, i64(3), i64(8), at(1), 0, i64(8), at(2), i64(8), at(3), i64(8), flt(1e-5), at(4), i64(8), at(5), at(6), None),
+        "layer_norm_grad": (2, i64(3), i64(8), at(1), 0, i64(8), at(2), i64(8), at(3), i64(8), at(4), at(5), at(6), i64(8), at(7),
+                            i64(8), at(8), i64(8), 0, at(9), i64(1 << 14), None),
+        "policy_loss_grad": (2, i64(3), i64(100), at(1), 0, i64(100), at(2), at(3), at(4), at(5), at(6), flt(0.2), flt(0.2), flt(0.1),
+                             at(7), at(8), at(9), i64(100), at(10), i64(256), None)}
+    for fail in (1, 0):
+        lib.fake_launches_fail(fail)
+        for name, args in calls.items():
+            assert getattr(lib, name)(*args) == (-9 if fail else 0), name
+            assert lib.fake_last_error() == 0, name
+    lib.gradients_destroy(handle)
