@@ -423,7 +423,7 @@ DLM_API int gradients_destroy(dlm_gradients* list);
  * formula.  Reads the list once for the norm, and once more for the copy.  Nodes of up to 262144 elements take one launch,
  * larger ones three (the norm alone two).
  * Errors: DLM_ERR_NULL, DLM_ERR_KIND, DLM_ERR_SHAPE, DLM_ERR_ALIGN, DLM_ERR_ALIAS (g's rows or norms overlapping a
- * tensor of the list), DLM_ERR_HYPER (max_norm not finite or <= 0), DLM_ERR_CUDA.
+ * tensor of the list), DLM_ERR_HYPER (max_norm not finite or <= 0), DLM_ERR_UNSUPPORTED (n * ldg above 2^42), DLM_ERR_CUDA.
  */
 enum { DLM_NORM_L2 = 0, DLM_NORM_MAX = 1 };
 DLM_API int gradient_norm(dlm_gradients* list, int kind, float* norms, void* cuda_stream);

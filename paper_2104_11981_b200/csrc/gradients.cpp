@@ -13,6 +13,9 @@
 
 namespace {
 
+// Any array longer than this could not exist on the device; keeps the arithmetic of the checks in range.
+constexpr int64_t kMaxElements = (int64_t)1 << 42;
+
 int64_t element_bytes(int dtype) { return dtype == DLM_G_BF16 ? 2 : 4; }
 
 // Bytes per piece.  32 KB give each of the 256 threads of a CTA 128 bytes to ask for at once; lists too small to give every
@@ -39,11 +42,11 @@ int build(int n, int tensors, const int64_t* sizes, const int* dtypes, const voi
     std::vector<std::pair<int64_t, int64_t>> spans;
     for (int t = 0; t < tensors; ++t) {
         if (dtypes[t] != DLM_G_F32 && dtypes[t] != DLM_G_BF16) return DLM_ERR_KIND;
-        if (sizes[t] < 0 || sizes[t] > ((int64_t)1 << 42) || (offsets && (offsets[t] < 0 || offsets[t] > ((int64_t)1 << 42))))
+        if (sizes[t] < 0 || sizes[t] > kMaxElements || (offsets && (offsets[t] < 0 || offsets[t] > kMaxElements)))
             return DLM_ERR_SHAPE;
         list.offsets[t] = offsets ? offsets[t] : total;
         total += sizes[t];
-        if (total > ((int64_t)1 << 42)) return DLM_ERR_SHAPE;
+        if (total > kMaxElements) return DLM_ERR_SHAPE;
         if (dtypes[t] != dtypes[0]) list.types = -1;
         if (sizes[t] > 0) {
             spans.push_back({list.offsets[t], list.offsets[t] + sizes[t]});
@@ -181,6 +184,7 @@ int gradient_clip(dlm_gradients* list, int kind, float max_norm, float* norms, v
     if (g) {
         if (g_dtype != DLM_G_F32 && g_dtype != DLM_G_BF16) return DLM_ERR_KIND;
         if (ldg < list->columns) return DLM_ERR_SHAPE;
+        if (ldg > kMaxElements / list->n) return DLM_ERR_UNSUPPORTED;
         const size_t esz = g_dtype == DLM_G_BF16 ? 2 : 4;
         if ((uintptr_t)g % esz) return DLM_ERR_ALIGN;
         const uintptr_t lo = (uintptr_t)g, row = (uintptr_t)ldg * esz, width = (uintptr_t)list->columns * esz;

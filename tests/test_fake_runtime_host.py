@@ -85,3 +85,12 @@ def test_a_launch_that_fails_leaves_no_error_behind(lib):
             assert getattr(lib, name)(*args) == (-9 if fail else 0), name
             assert lib.fake_last_error() == 0, name
     lib.gradients_destroy(handle)
+
+
+def test_row_strides_of_the_gathered_rows_are_bounded(lib):
+    """A stride whose rows' addresses wrap would pass the overlap checks; none above 2^42 elements in all can exist."""
+    rc, handle = _gradients(lib)
+    assert rc == 0
+    for ldg, want in ((300_009, -2), (300_010, 0), (1 << 41, 0), ((1 << 41) + 1, -8), (1 << 61, -8), ((1 << 63) - 1, -8)):
+        assert lib.gradient_clip(handle, 0, ctypes.c_float(1.0), vp(1 << 20), vp(1 << 40), 0, i64(ldg), None) == want, ldg
+    lib.gradients_destroy(handle)
