@@ -451,7 +451,11 @@ __global__ void __launch_bounds__(kThreads + 32, 2) norm_kernel(const dlm_piece*
     for (int k = 0; k < count; ++k) {
         close_below((first + k * step) / per_node);
         const int s = take_buffer(ring, k);
-        if (s < 0) return;
+        if (s < 0) {
+            // the buffers that the filling warp may have asked for, before this CTA gives them up
+            for (int z = k; z < min(count, k + kRing); ++z) mbar_wait(smem_u32(&ring.full[z % kRing]), (z / kRing) & 1);
+            return;
+        }
         const Item item = ring.items[s];
         const uint32_t data = smem_u32(ring.data[s]);
         sum = both<KIND>(sum, item.piece.bf16 ? read_staged<__nv_bfloat16, KIND>(item, data) : read_staged<float, KIND>(item, data));
