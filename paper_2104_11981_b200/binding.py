@@ -35,7 +35,10 @@ if not os.path.exists(LIB_PATH):
                       "(there is no CPU fallback)")
 _lib = ctypes.CDLL(LIB_PATH)
 
-from . import _calls  # noqa: E402  (linked to the library above)
+try:
+    from . import _calls  # linked to the library above
+except ImportError:  # built for another Python, or where its headers are missing: ctypes makes the same calls, 1 to 2 us slower
+    _calls = _lib
 
 _i32p = ctypes.POINTER(ctypes.c_int32)
 _f32p = ctypes.POINTER(ctypes.c_float)

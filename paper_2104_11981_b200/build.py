@@ -57,6 +57,9 @@ def _build_calls(force: bool) -> None:
     if not force and os.path.exists(CALLS) and all(os.path.getmtime(p) <= os.path.getmtime(CALLS)
                                                    for p in (src, os.path.join(INCLUDE, "decentlam.h"))):
         return
+    if not os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h")):
+        print("Python.h not found: _calls is left out, the binding calls through ctypes", file=sys.stderr)
+        return
     tmp = CALLS + ".tmp"
     subprocess.run([os.environ.get("CC", "gcc"), "-O2", "-fPIC", "-shared", "-I", INCLUDE, "-I", sysconfig.get_paths()["include"],
                     src, "-o", tmp, "-L", HERE, "-l:libdecentlam.so", "-Wl,-rpath,$ORIGIN"], check=True)
