@@ -47,6 +47,15 @@ _i64 = ctypes.c_int64
 _int = ctypes.c_int
 _flt = ctypes.c_float
 
+
+class _held_int(ctypes.c_int):
+    """An int parameter whose argument is held to its range instead of cut to 32 bits: too large stays too large."""
+
+    @classmethod
+    def from_param(cls, v):
+        return _int(min(max(v, -(1 << 31)), (1 << 31) - 1))
+
+
 _lib.dlm_status_string.argtypes = [_int]
 _lib.dlm_status_string.restype = ctypes.c_char_p
 _lib.topology_build.argtypes = [_int, _int, _vp, _vp, _vp, ctypes.POINTER(_vp)]
@@ -82,16 +91,16 @@ _lib.gradients_build.argtypes = [_int, _int, ctypes.POINTER(_i64), ctypes.POINTE
                                  ctypes.POINTER(_i64), ctypes.POINTER(_vp)]
 _lib.gradients_layout.argtypes = [_vp, ctypes.POINTER(ctypes.POINTER(_i64)), ctypes.POINTER(_i64)]
 _lib.gradients_destroy.argtypes = [_vp]
-_lib.gradient_norm.argtypes = [_vp, _int, _vp, _vp]
-_lib.gradient_clip.argtypes = [_vp, _int, _flt, _vp, _vp, _int, _i64, _vp]
-_lib.layer_norm.argtypes = [_int, _i64, _i64, _vp, _int, _i64, _vp, _i64, _vp, _i64, _flt, _vp, _i64, _vp, _vp, _vp]
-_lib.layer_norm_grad_workspace_bytes.argtypes = [_int, _i64, _i64]
+_lib.gradient_norm.argtypes = [_vp, _held_int, _vp, _vp]
+_lib.gradient_clip.argtypes = [_vp, _held_int, _flt, _vp, _vp, _held_int, _i64, _vp]
+_lib.layer_norm.argtypes = [_held_int, _i64, _i64, _vp, _held_int, _i64, _vp, _i64, _vp, _i64, _flt, _vp, _i64, _vp, _vp, _vp]
+_lib.layer_norm_grad_workspace_bytes.argtypes = [_held_int, _i64, _i64]
 _lib.layer_norm_grad_workspace_bytes.restype = _i64
-_lib.layer_norm_grad.argtypes = [_int, _i64, _i64, _vp, _int, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _vp,
-                                 _i64, _int, _vp, _i64, _vp]
-_lib.policy_loss_workspace_bytes.argtypes = [_int, _i64, _i64]
+_lib.layer_norm_grad.argtypes = [_held_int, _i64, _i64, _vp, _held_int, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _vp,
+                                 _i64, _held_int, _vp, _i64, _vp]
+_lib.policy_loss_workspace_bytes.argtypes = [_held_int, _i64, _i64]
 _lib.policy_loss_workspace_bytes.restype = _i64
-_lib.policy_loss_grad.argtypes = [_int, _i64, _i64, _vp, _int, _i64, _vp, _vp, _vp, _vp, _vp, _flt, _flt, _flt, _vp, _vp, _vp,
+_lib.policy_loss_grad.argtypes = [_held_int, _i64, _i64, _vp, _held_int, _i64, _vp, _vp, _vp, _vp, _vp, _flt, _flt, _flt, _vp, _vp, _vp,
                                   _i64, _vp, _i64, _vp]
 _lib.dlm_launch_count.argtypes = []
 _lib.dlm_launch_count.restype = _i64

@@ -3,15 +3,18 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <limits.h>
 #include <stdint.h>
 
 #include "decentlam.h"
 
 /* Whole numbers and addresses; None is 0. */
 static int64_t whole(PyObject* o) { return o == Py_None ? 0 : (int64_t)PyLong_AsLongLong(o); }
+/* An int parameter: held to its range, so that what is too large stays so. */
+static int held(int64_t v) { return v > INT_MAX ? INT_MAX : v < INT_MIN ? INT_MIN : (int)v; }
 
 #define N(k) whole(args[k])
-#define I(k) ((int)whole(args[k]))
+#define I(k) held(whole(args[k]))
 #define P(k) ((void*)(uintptr_t)whole(args[k]))
 #define F(k) ((float)PyFloat_AsDouble(args[k]))
 
