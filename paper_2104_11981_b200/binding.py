@@ -553,7 +553,8 @@ def layer_norm_grad(x, dy, weight, mean, rstd, dx, dweight, dbias, workspace, st
     layer_norm_grad_workspace_bytes(n, rows, c) bytes."""
     shape, dtype = x.shape, x.dtype
     n, rows, c = shape
-    assert _dtype(weight) == G_F32 and (dbias is None or dbias.dtype == dweight.dtype) and workspace.is_cuda
+    assert _dtype(weight) == G_F32 and (dbias is None or dbias.dtype == dweight.dtype)
+    assert workspace.is_cuda and workspace.is_contiguous()
     pw, ldw = _node_vectors(weight, n, c)
     (pgw, ldgw), (pgb, ldgb) = _node_vectors(dweight, n, c), _node_vectors(dbias, n, c)
     _check(_calls.layer_norm_grad(n, rows, c, x.data_ptr(), _dtype(x), _node_rows(x, shape, dtype), dy.data_ptr(),
@@ -580,7 +581,7 @@ def policy_loss_grad(logits, tokens, weight, advantage, old_logp, ref_logp, clip
     n, rows, vocab = shape
     count = n * rows
     assert tokens.is_cuda and tokens.dtype == torch.int64 and tokens.is_contiguous() and tokens.numel() == count
-    assert workspace.is_cuda
+    assert workspace.is_cuda and workspace.is_contiguous()
     pd, ldd = (dlogits.data_ptr(), _node_rows(dlogits, shape, dtype)) if dlogits is not None else (None, 0)
     _check(_calls.policy_loss_grad(n, rows, vocab, logits.data_ptr(), _dtype(logits), _node_rows(logits, shape, dtype),
                                    tokens.data_ptr(), _per_row(weight, count), _per_row(advantage, count),
