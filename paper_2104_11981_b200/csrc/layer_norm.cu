@@ -698,7 +698,11 @@ __global__ void __launch_bounds__(SLICES * 32) layer_norm_join_kernel(long long 
 constexpr int64_t kMaxHeld = 16384;
 
 // CALL(columns per thread, threads per row) of the narrowest group that holds c columns.  The backward kernel has twice the
-// sums to keep and takes more threads for it.
+// sums to keep and takes more threads for it.  Its rows of 1025 to 2048 columns by the type: bf16 with 16 columns in 128 threads (8 x 2500
+// x 2048 50 us, 8 in 256 threads 56; 4 x 10000 x 1280 70 against 88; 8 x 2500 x 2047 90 against 116), fp32 the other way about (8 x 2500 x
+// 2048 77 us against 86; 4 x 8000 x 1536 91 against 99; 8 x 2500 x 2047 104 against 106, but 16 x 1000 x 1111 78 against 73).
+template <typename T>
+constexpr int kMidCols = sizeof(T) == 2 ? 16 : 8;
 #define DLM_NORM_SHAPES(CALL)            \
     if (c <= 64) return CALL(8, 8);      \
     if (c <= 128) return CALL(16, 8);    \
@@ -715,7 +719,7 @@ constexpr int64_t kMaxHeld = 16384;
     if (c <= 256) return CALL(16, 16);   \
     if (c <= 512) return CALL(16, 32);   \
     if (c <= 1024) return CALL(16, 64);  \
-    if (c <= 2048) return CALL(8, 256);  \
+    if (c <= 2048) return CALL(kMidCols<T>, 2048 / kMidCols<T>); \
     if (c <= 4096) return CALL(16, 256); \
     if (c <= 8192) return CALL(16, 512); \
     return CALL(32, 512);

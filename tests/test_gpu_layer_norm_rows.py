@@ -28,7 +28,8 @@ def _nodes_and_rows(c, typ):
     it has in flight."""
     size = (2 if typ == "bf16" else 4) * c
     ahead = next((t for top, t in ((256, 8), (512, 16), (1024, 32), (2048, 64), (4096, 128), (8192, 256)) if c <= top), 512)
-    back = next((t for top, t in ((128, 8), (256, 16), (512, 32), (1024, 64), (4096, 256)) if c <= top), 512)
+    middle = 128 if typ == "bf16" else 256
+    back = next((t for top, t in ((128, 8), (256, 16), (512, 32), (1024, 64), (2048, middle), (4096, 256)) if c <= top), 512)
     depth = 4 if ahead <= 64 else 3
     held = [_ctas(ahead, 4 if ahead <= 64 else 2, size), _ctas(back, 4 if back <= 64 else 3 if back < 512 else 1, 2 * size)]
     sms = torch.cuda.get_device_properties(0).multi_processor_count
