@@ -455,16 +455,16 @@ def gradients_build(nodes, offsets=None):
     """nodes: one list of gradient tensors per node, the same sizes and types in every node, each contiguous, all on the
     current CUDA device.  offsets: first column of each tensor in a node's stacked row (None: packed without gaps)."""
     n, tensors = len(nodes), len(nodes[0]) if nodes else 0
+    sizes, dtypes = [t.numel() for t in nodes[0]] if n else [], [_dtype(t) for t in nodes[0]] if n else []
     if tensors:
         import torch
         home = nodes[0][0].device
-        assert all(g.is_cuda and g.device == home for node in nodes for g in node), "gradients on one CUDA device are expected"
-        assert home.index == torch.cuda.current_device(), "the gradients' device has to be the current one"
-    sizes, dtypes = [t.numel() for t in nodes[0]] if n else [], [_dtype(t) for t in nodes[0]] if n else []
+        assert home.type == "cuda" and home.index == torch.cuda.current_device(), "gradients on the current CUDA device are expected"
     data = (_vp * max(1, n * tensors))()
     for i, node in enumerate(nodes):
         assert len(node) == tensors, "every node has the same tensors"
         for t, g in enumerate(node):
+            assert g.device == home, "gradients on one device are expected"
             assert g.is_contiguous() and g.numel() == sizes[t] and _dtype(g) == dtypes[t]
             data[i * tensors + t] = g.data_ptr()
     assert offsets is None or len(offsets) == tensors
