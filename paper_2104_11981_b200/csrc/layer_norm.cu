@@ -665,9 +665,8 @@ __global__ void __launch_bounds__(1024)
     }
 }
 
-// dw, db <- sums of the CTAs' parts in order.  32 columns by 8 slices of the CTAs; parts == 0 gives zeros.
 // dw and db of a node from its CTAs' partial sums, 32 columns (of 2 c: dw's, then db's) to a CTA, each warp the sum of every
-// SLICES-th part.
+// SLICES-th part, in a fixed order; parts == 0 gives zeros.
 template <typename G, int SLICES>
 __global__ void __launch_bounds__(SLICES * 32) layer_norm_join_kernel(long long c, int parts, const float* partial, G* dweight,
                                                                       long long ldgw, G* dbias, long long ldgb) {
