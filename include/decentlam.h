@@ -398,7 +398,8 @@ DLM_API int lsq_grad_gram(int n, int q, const float* H, const float* c, const fl
  *   offsets : host [tensors], first column of each tensor in a node's stacked row; NULL packs them without gaps.
  *             Columns that no tensor covers are never written.
  * The handle keeps the addresses: the buffers stay where they are while it is used (their contents change from step to
- * step); build another one when they move.  It owns device scratch, so calls with one handle are ordered (one stream,
+ * step); build another one when they move, which takes 0.4 ms for 8 nodes x 12 tensors and 3 ms for 64 x 62 (device memory, and a copy that
+ * is waited for), destroying the old one 0.3 to 0.6 ms.  It owns device scratch, so calls with one handle are ordered (one stream,
  * or events).  Without a CUDA device the handle is host-only and the calls below fail with DLM_ERR_CUDA.
  * Errors: DLM_ERR_NULL, DLM_ERR_SHAPE, DLM_ERR_KIND, DLM_ERR_ALIGN, DLM_ERR_ALIAS (two tensors sharing bytes, or
  * columns), DLM_ERR_UNSUPPORTED (n above DLM_MAX_NODES), DLM_ERR_CUDA.

@@ -323,7 +323,7 @@ __global__ void __launch_bounds__(kThreads) node_clip_kernel(const dlm_piece* pi
 // The norms: two CTAs per SM, each of which takes every G-th piece.  A CTA's pieces pass through a ring of shared-memory
 // buffers that one warp fills by bulk copies ahead of the others: they hold no registers, and up to 192 KB per SM are on
 // their way.  The other warps each wait for a buffer, take their share of it and give it back; no barrier holds them
-// together.  16 x 25.6M fp32: 225 us, 7.2 TB/s; with a CTA per piece that loads into registers 297.
+// together.  16 x 25.6M fp32: 227 us, 7.2 TB/s; with a CTA per piece that loads into registers 297.
 constexpr int kRing = 3;
 constexpr int kPieceBytes = 32768;
 constexpr int kWarps = kThreads / 32;
@@ -483,8 +483,9 @@ __global__ void __launch_bounds__(kThreads) close_kernel(const double* partial, 
 }
 
 // Half a piece per CTA, the last one first: what was read last is the likeliest to be in the L2 still.  Short CTAs that load
-// into registers, which the hardware deals out as SMs become free: 485 us for 16 x 25.6M fp32 (6.7 TB/s), a whole piece per
-// CTA 502; CTAs that stay and take pieces through the ring above, which is best where nothing is written, 558.
+// into registers, which the hardware deals out as SMs become free: 496 us for 16 x 25.6M fp32 packed without gaps (6.6 TB/s), 483 where
+// source and destination are aligned.  A whole piece per CTA takes 3 % more; CTAs that stay and take pieces through the ring above, which
+// is best where nothing is written, 15 %.
 template <int TYPES>
 __global__ void __launch_bounds__(kThreads) scale_kernel(const dlm_piece* pieces, int per_node, const float* scale, Target to) {
     const unsigned b = gridDim.x - 1 - blockIdx.x;

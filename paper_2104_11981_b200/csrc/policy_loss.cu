@@ -4,7 +4,7 @@
 //   dl/dlogp = w ( -A r [r A <= clip(r) A] + kl (1 - e^{ref - logp}) ) ,  dl/dz_v = dl/dlogp ([v = t] - e^{z_v} / sum).
 // The factor dl/dlogp depends on the row's own numbers alone, so loss and gradient take one kernel: a first sweep for
 // the maximum and the sum of exponentials, a second for the gradient.  The logits are read once, the gradient written once.
-// 4096 x 131072 bf16, a quarter masked: 329 us (5.7 TB/s); the exponentials keep their unit 62 % and the issue slots 62 % busy at
+// 4096 x 131072 bf16, a quarter masked: 329 us (5.7 TB/s); the exponentials keep their unit 61 % and the issue slots 64 % busy at
 // the same time.  16000 x 4096 fp32: 78 us (5.9 TB/s of what is not masked), memory-bound.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
@@ -109,7 +109,7 @@ __device__ __forceinline__ RowOutcome row_outcome(float zt, Tally t, float w, fl
 // registers while in flight, and nobody else reads the slots, so no barrier is needed) and both sweeps read them there, so
 // that the logits cross the memory bus once; what a wider row has beyond that is read again, out of the L2.
 // TPR = 32: a warp per row, eight rows a CTA.  kHold = 8 is 32 KB for 256 threads, six CTAs per SM; with 16 runs the widest
-// case below takes 351 to 367 us instead of 335.
+// case below takes 5 to 10 % more.
 constexpr int kHold = 8;
 template <int TPR>
 constexpr int kBlock = TPR < 128 ? 256 : TPR;
@@ -385,8 +385,8 @@ cudaError_t launch(const dlm_policy_args& a, float* row_loss, cudaStream_t s) {
     const int64_t runs = (a.vocab + kRun<T> - 1) / kRun<T>, rows = a.n * a.rows;
     if (runs <= 32 * kHold && rows * 32 >= 128 * info.sms) return run<T, 32, false>(a, 1, row_loss, s);
     // As few CTAs as hold the row in shared memory, and more while the rows leave SMs idle and a thread has more than one
-    // run.  Four nodes x 1024 rows x 131072, bf16: 8 CTAs 335 us, 4 of 512 threads 373, 1 that reads the row twice 409-472.
-    // 8 x 128 x 32768, bf16: 2 CTAs 26.9 us, 1 29.1, 4 30.8.  8 x 2000 x 4096, fp32: 1 CTA of 128 threads 79 us, of 256 91.
+    // run.  Four nodes x 1024 rows x 131072, bf16: 8 CTAs 329 us, 4 of 512 threads 11 % more, 1 that reads the row twice
+    // 22 to 41 %.  8 x 128 x 32768, bf16: 2 CTAs 26.3 us, 1 8 % more, 4 15 %.  8 x 2000 x 4096, fp32: 1 CTA of 128 threads 79 us, of 256 91.
     int ctas = 1;
     while (ctas < kMaxCtas && (runs > (int64_t)ctas * 256 * kHold || (rows * ctas * 2 <= 2 * info.sms && runs > ctas * 256))) ctas *= 2;
     if (runs <= 128 * kHold && ctas == 1) return run<T, 128, false>(a, 1, row_loss, s);

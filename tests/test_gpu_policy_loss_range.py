@@ -148,3 +148,12 @@ def test_rows_of_minus_infinity(typ):
     bad[0, 1] = True
     assert torch.equal(torch.isnan(logp), bad) and torch.equal(torch.isnan(d).all(-1), bad) and torch.equal(torch.isnan(d).any(-1), bad)
     assert bool(torch.isnan(loss[0])) and bool(torch.isfinite(loss[1]))
+
+
+@pytest.mark.parametrize("typ", ["f32", "bf16"])
+def test_no_rows(typ):
+    z = torch.empty((3, 0, 500), device=DEV, dtype=TYPE[typ])
+    none = torch.empty((3, 0), device=DEV)
+    s = dict(z=z, tok=none.long(), old=none, ref=none, adv=none, w=none, kl=0.1)
+    loss, logp, d = _call(s)
+    assert bool((loss == 0).all()) and logp.shape == (3, 0) and d.shape == z.shape
