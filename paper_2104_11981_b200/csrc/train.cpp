@@ -173,7 +173,7 @@ int policy_loss_grad(int n, int64_t rows, int64_t vocab, const void* logits, int
         !aligned(advantage, 4) || !aligned(old_logp, 4) || !aligned(ref_logp, 4) || !aligned(logp, 4))
         return DLM_ERR_ALIGN;
     if (!std::isfinite(clip_low) || !(clip_low >= 0.0f) || !std::isfinite(clip_high) || !(clip_high >= 0.0f) ||
-        !std::isfinite(kl_coef) || !(kl_coef >= 0.0f) || (kl_coef > 0.0f && !ref_logp))
+        !std::isfinite(kl_coef) || !(kl_coef >= 0.0f) || (kl_coef > 0.0f && rows > 0 && !ref_logp))
         return DLM_ERR_HYPER;
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < need) return DLM_ERR_WORKSPACE;
     const Rows none = {0, 0, 0, 0};

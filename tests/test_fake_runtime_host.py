@@ -94,3 +94,15 @@ def test_row_strides_of_the_gathered_rows_are_bounded(lib):
     for ldg, want in ((300_009, -2), (300_010, 0), (1 << 41, 0), ((1 << 41) + 1, -8), (1 << 61, -8), ((1 << 63) - 1, -8)):
         assert lib.gradient_clip(handle, 0, ctypes.c_float(1.0), vp(1 << 20), vp(1 << 40), 0, i64(ldg), None) == want, ldg
     lib.gradients_destroy(handle)
+
+
+def test_a_policy_loss_without_rows_needs_no_reference(lib):
+    """Tensors without elements have no address, the reference's among them."""
+    lib.fake_launches_fail(0)
+    flt, none = ctypes.c_float, vp(None)
+
+    def call(rows, ref):
+        at = (lambda k: vp(k << 16)) if rows else (lambda k: none)
+        return lib.policy_loss_grad(2, i64(rows), i64(100), at(1), 0, i64(100), at(2), at(3), at(4), at(5), ref, flt(0.2), flt(0.2), flt(0.1),
+                                    vp(7 << 16), at(8), at(9), i64(100), vp(10 << 16), i64(256), None)
+    assert call(3, vp(6 << 16)) == 0 and call(3, none) == -5 and call(0, none) == 0
