@@ -488,6 +488,120 @@ DLM_API int policy_loss_grad(int n, int64_t rows, int64_t vocab, const void* log
                              const float* ref_logp, float clip_low, float clip_high, float kl_coef, float* loss, float* logp,
                              void* dlogits, int64_t ldd, void* workspace, int64_t workspace_bytes, void* cuda_stream);
 
+/* ------------------------------------------------------------------------------------
+ * Operators between a model's tokens and its logits, in the same stacking and with the same rules as the training operators
+ * above: enqueue-only, capturable, arithmetic in fp32 (one rounding at the end), bitwise the same result every time.
+ * ------------------------------------------------------------------------------------ */
+
+/*
+ * Embedding of n nodes' tokens, each node with its own table, and its gradient:
+ *   y_r = scale table_i[token_r] ;   dtable_i[v] = scale sum_{r : token_r = v} dy_r
+ *   table      : device [n, vocab, c] of t_dtype, a node's rows following one another, ldt >= vocab c elements from one node to
+ *                the next (a column range of the stacked x, for instance)
+ *   tokens     : device int64 [n * rows].  A token outside [0, vocab) stands for none: its row of y is 0 and its row of dy is not read.
+ *   y, dy      : device [n * rows, c] of dtype, row strides ldy, lddy
+ *   scale      : finite
+ *   dtable     : device [n, vocab, c] of g_dtype, ldgt >= vocab c elements from one node to the next.  accumulate = 0: overwritten,
+ *                rows without tokens by 0.  accumulate = 1: added to (a table that the output head shares, further batches); rows
+ *                without tokens are left as they are.
+ *   workspace  : device, embedding_grad_workspace_bytes(n, rows, vocab, c) bytes, 256-byte aligned, owned by the caller
+ * rows may be 0.  The gradient sorts the tokens and adds their rows in the order of the text (of a token that fills blocks of 64
+ * places of the sorted text, block by block).  Fast path: c a multiple of 16 bytes' worth of the narrower type, arrays and strides
+ * 16-byte aligned.
+ * Errors: DLM_ERR_NULL, DLM_ERR_SHAPE, DLM_ERR_KIND, DLM_ERR_ALIGN, DLM_ERR_ALIAS, DLM_ERR_HYPER, DLM_ERR_WORKSPACE,
+ * DLM_ERR_UNSUPPORTED, DLM_ERR_CUDA.
+ */
+DLM_API int embedding(int n, int64_t rows, int64_t vocab, int64_t c, const void* table, int t_dtype, int64_t ldt,
+                      const int64_t* tokens, float scale, void* y, int dtype, int64_t ldy, void* cuda_stream);
+DLM_API int64_t embedding_grad_workspace_bytes(int n, int64_t rows, int64_t vocab, int64_t c); /* negative dlm_status on bad sizes */
+DLM_API int embedding_grad(int n, int64_t rows, int64_t vocab, int64_t c, const int64_t* tokens, const void* dy, int dtype,
+                           int64_t lddy, float scale, int accumulate, void* dtable, int g_dtype, int64_t ldgt, void* workspace,
+                           int64_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Root-mean-square norm of n nodes' activations, each node with its own weight w_i, after the residual's addition:
+ *   h = x + residual ;  rstd = 1 / sqrt(sum_c h^2 / c + eps) ;  y = h rstd w_i
+ *   x          : device [n * rows, c] of dtype, row stride ldx
+ *   residual   : as x with stride ldr, or NULL (h = x)
+ *   weight     : device fp32 [n, c], row stride ldw (a column range of the stacked x, for instance)
+ *   h          : device [n * rows, c] of dtype, written (the residual stream that goes on, and what the backward pass reads), or
+ *                NULL.  y is computed from the sum before it is rounded for h.
+ *   y          : device [n * rows, c] of dtype, written; NULL where y8 is given and nothing else is wanted
+ *   y8, scales : device [n * rows, c] bytes with row stride ld8 and fp32 [n * rows], written, or both NULL: the 8-bit output
+ *                y8 = e4m3(h w_i 448 / top), scale = top rstd / 448, top = max_c |h w_i|, so that y8 scale = y up to y8's rounding (to
+ *                nearest even).  A row of zeros has scale 0; the scale of a row with a NaN or an infinity is NaN.
+ *   rstd       : device fp32 [n * rows], written; the backward pass reads it
+ *   eps        : finite, >= 0
+ * h and y may each be x or residual (same stride), but not one another.  Squares are summed in fp32: rows above 1e19 have rstd 0.
+ * rms_norm_grad, with xh = h rstd and v = w_i dy:
+ *   dh = dresidual + rstd (v - xh sum_c (v xh) / c) ;  dweight_i = sum_rows dy xh
+ *   dh is the gradient of x and of residual alike.
+ *   dresidual  : device [n * rows, c] of dtype: the gradient that reaches h along the residual stream; NULL: none
+ *   dy, dh     : device [n * rows, c] of dtype; dh may be h, dy or dresidual (same stride)
+ *   dweight    : device [n, c] of g_dtype, row stride ldgw, overwritten (in a column range of the stacked g, for instance)
+ *   workspace  : device, rms_norm_grad_workspace_bytes(n, rows, c) bytes, 256-byte aligned, owned by the caller
+ * rows may be 0 (the weight's gradient is then 0).  Fast path: c a multiple of 16 bytes' worth and every activation row 16-byte
+ * aligned (y8: 8-byte with bf16 rows, 4-byte with fp32 rows).
+ * Errors: DLM_ERR_NULL, DLM_ERR_SHAPE, DLM_ERR_KIND, DLM_ERR_ALIGN, DLM_ERR_ALIAS, DLM_ERR_HYPER, DLM_ERR_WORKSPACE,
+ * DLM_ERR_UNSUPPORTED, DLM_ERR_CUDA.
+ */
+DLM_API int rms_norm(int n, int64_t rows, int64_t c, const void* x, int dtype, int64_t ldx, const void* residual, int64_t ldr,
+                     const float* weight, int64_t ldw, float eps, void* h, int64_t ldh, void* y, int64_t ldy, void* y8, int64_t ld8,
+                     float* scales, float* rstd, void* cuda_stream);
+DLM_API int64_t rms_norm_grad_workspace_bytes(int n, int64_t rows, int64_t c); /* negative dlm_status on bad sizes */
+DLM_API int rms_norm_grad(int n, int64_t rows, int64_t c, const void* h, int dtype, int64_t ldh, const void* dy, int64_t lddy,
+                          const void* dresidual, int64_t lddr, const float* weight, int64_t ldw, const float* rstd, void* dh,
+                          int64_t lddh, void* dweight, int64_t ldgw, int g_dtype, void* workspace, int64_t workspace_bytes,
+                          void* cuda_stream);
+
+/*
+ * Dropout from a counter-based generator; no mask is stored:
+ *   y_e = residual_e + (u_e >= limit ? x_e 65536 / (65536 - limit) : 0) ,   limit = floor(65536 p + 1/2)
+ * e counts the elements of [n, rows, c] in order, whatever the strides.  u_e are 16 bits of Philox4x32-10 (Salmon et al., SC 2011):
+ * block number floor(e / 8) (64 bits, the counter's first two words), the low 32 bits of `step` and `site` (its third and fourth),
+ * `seed` as key (low word first); elements 8b, 8b + 1 take the low and the high half of the block's first word, and so on.
+ *   x, residual, y : device [n * rows, c] of dtype; residual may be NULL; y == x or y == residual (same stride) is allowed
+ *   p          : probability of an element to be dropped, 0 <= p <= 65535/65536; it is rounded to a multiple of 2^-16, and the scale
+ *                goes by the rounded one
+ *   state      : device int64 [2]: seed and step.  They are read by the kernel, so a captured call draws anew when they change.
+ *   site       : 0 .. 2^32 - 1: which of the model's dropouts this is
+ * The backward pass is the same call on dy (without residual): the same state and site give the same mask.  A dropped element gives 0 (or
+ * the residual) whatever x holds.  Ranks of a sharded run need seeds of their own.
+ * Errors: DLM_ERR_NULL, DLM_ERR_SHAPE, DLM_ERR_KIND, DLM_ERR_ALIGN, DLM_ERR_ALIAS, DLM_ERR_HYPER (p, site), DLM_ERR_UNSUPPORTED,
+ * DLM_ERR_CUDA.
+ */
+DLM_API int dropout(int n, int64_t rows, int64_t c, const void* x, int dtype, int64_t ldx, const void* residual, int64_t ldr, float p,
+                    const int64_t* state, int64_t site, void* y, int64_t ldy, void* cuda_stream);
+
+/*
+ * Adjustment of logits before a token is drawn or its log-probability taken, and the way back to the logits.  For element v of row r
+ * of node i, with z its logit and k how often the row's text has v:
+ *   z1 = k > 0 ? (z > 0 ? z / repetition_r : z repetition_r) - frequency_r k - presence_r : z
+ *   out = (z1 + bias_iv) / temperature_r ;   -inf where the mask forbids v, whatever z and the bias hold
+ *   dlogits = dout / temperature_r (k > 0 ? (z > 0 ? 1 / repetition_r : repetition_r) : 1) ;   0 where the mask forbids v
+ *   logits, out, dout, dlogits : device [n * rows, vocab] of dtype; out == logits, dlogits == dout, dlogits == logits (same
+ *                stride) are allowed
+ *   bias       : device fp32 [n, vocab], row stride ldb, or NULL
+ *   allowed    : device 32-bit words, bit v % 32 of word v / 32 of a row allows v; rows ldm >= ceil(vocab / 32) words apart, or
+ *                ldm = 0: one row for all.  NULL: all allowed.  A row that allows nothing is all -inf.
+ *   history, history_length, history_start : device int64 [history_length], its length, and device int64 [n * rows + 1]: row r's
+ *                text is history[history_start_r .. history_start_{r+1}) (held to [0, history_length)); tokens outside [0, vocab)
+ *                count nowhere.  history_start NULL: no texts, and then no penalties either.
+ *   repetition, frequency, presence, temperature : device fp32 [n * rows], or NULL (1, 0, 0, 1)
+ * The gradient needs `logits` (as they were before the adjustment) only with `repetition`; without it NULL is allowed.  The bias is a
+ * constant to it.  rows may be 0.
+ * Errors: DLM_ERR_NULL, DLM_ERR_SHAPE, DLM_ERR_KIND, DLM_ERR_ALIGN, DLM_ERR_ALIAS, DLM_ERR_UNSUPPORTED (n * rows or vocab above
+ * 2^31 - 1), DLM_ERR_CUDA.
+ */
+DLM_API int logits_adjust(int n, int64_t rows, int64_t vocab, const void* logits, int dtype, int64_t ldl, const float* bias,
+                          int64_t ldb, const uint32_t* allowed, int64_t ldm, const int64_t* history, int64_t history_length,
+                          const int64_t* history_start, const float* repetition, const float* frequency, const float* presence,
+                          const float* temperature, void* out, int64_t ldo, void* cuda_stream);
+DLM_API int logits_adjust_grad(int n, int64_t rows, int64_t vocab, const void* dout, int dtype, int64_t lddo, const void* logits,
+                               int64_t ldl, const uint32_t* allowed, int64_t ldm, const int64_t* history, int64_t history_length,
+                               const int64_t* history_start, const float* repetition, const float* temperature, void* dlogits,
+                               int64_t ldd, void* cuda_stream);
+
 /* Kernel launches issued by this library in the calling process so far (all entry points). */
 DLM_API int64_t dlm_launch_count(void);
 

@@ -102,6 +102,22 @@ _lib.policy_loss_workspace_bytes.argtypes = [_held_int, _i64, _i64]
 _lib.policy_loss_workspace_bytes.restype = _i64
 _lib.policy_loss_grad.argtypes = [_held_int, _i64, _i64, _vp, _held_int, _i64, _vp, _vp, _vp, _vp, _vp, _flt, _flt, _flt, _vp, _vp, _vp,
                                   _i64, _vp, _i64, _vp]
+_lib.embedding.argtypes = [_held_int, _i64, _i64, _i64, _vp, _held_int, _i64, _vp, _flt, _vp, _held_int, _i64, _vp]
+_lib.embedding_grad_workspace_bytes.argtypes = [_held_int, _i64, _i64, _i64]
+_lib.embedding_grad_workspace_bytes.restype = _i64
+_lib.embedding_grad.argtypes = [_held_int, _i64, _i64, _i64, _vp, _vp, _held_int, _i64, _flt, _held_int, _vp, _held_int, _i64, _vp,
+                                _i64, _vp]
+_lib.rms_norm.argtypes = [_held_int, _i64, _i64, _vp, _held_int, _i64, _vp, _i64, _vp, _i64, _flt, _vp, _i64, _vp, _i64, _vp, _i64, _vp,
+                          _vp, _vp]
+_lib.rms_norm_grad_workspace_bytes.argtypes = [_held_int, _i64, _i64]
+_lib.rms_norm_grad_workspace_bytes.restype = _i64
+_lib.rms_norm_grad.argtypes = [_held_int, _i64, _i64, _vp, _held_int, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _i64,
+                               _held_int, _vp, _i64, _vp]
+_lib.dropout.argtypes = [_held_int, _i64, _i64, _vp, _held_int, _i64, _vp, _i64, _flt, _vp, _i64, _vp, _i64, _vp]
+_lib.logits_adjust.argtypes = [_held_int, _i64, _i64, _vp, _held_int, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp,
+                               _vp, _i64, _vp]
+_lib.logits_adjust_grad.argtypes = [_held_int, _i64, _i64, _vp, _held_int, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp,
+                                    _i64, _vp]
 _lib.dlm_launch_count.argtypes = []
 _lib.dlm_launch_count.restype = _i64
 _lib.dlm_kernel_error.argtypes = [ctypes.POINTER(_int)]
@@ -113,7 +129,9 @@ EXPORTS = ["dlm_status_string", "topology_build", "topology_build_periodic", "to
            "decentlam_step_sharded", "dmsgd_local_sharded", "partial_average_sharded",
            "lsq_grad_workspace_bytes", "lsq_grad", "lsq_grad_static", "lsq_gram_build", "lsq_grad_gram",
            "gradients_build", "gradients_layout", "gradients_destroy", "gradient_norm", "gradient_clip", "layer_norm",
-           "layer_norm_grad_workspace_bytes", "layer_norm_grad", "policy_loss_workspace_bytes", "policy_loss_grad", "dlm_launch_count", "dlm_kernel_error", "dlm_set_tuning"]
+           "layer_norm_grad_workspace_bytes", "layer_norm_grad", "policy_loss_workspace_bytes", "policy_loss_grad",
+           "embedding", "embedding_grad_workspace_bytes", "embedding_grad", "rms_norm", "rms_norm_grad_workspace_bytes",
+           "rms_norm_grad", "dropout", "logits_adjust", "logits_adjust_grad", "dlm_launch_count", "dlm_kernel_error", "dlm_set_tuning"]
 
 
 def _check(rc, where):
@@ -588,6 +606,180 @@ def policy_loss_grad(logits, tokens, weight, advantage, old_logp, ref_logp, clip
                                    _per_row(old_logp, count), _per_row(ref_logp, count) if ref_logp is not None else None,
                                    clip_low, clip_high, kl_coef, _per_row(loss, n), _per_row(logp, count), pd, ldd,
                                    workspace.data_ptr(), workspace.nbytes, _stream_ptr(stream)), "policy_loss_grad")
+
+
+def _at_home(*tensors):
+    """The tensors (None among them) are on the current device, on which the call runs."""
+    import torch
+    home = torch._C._cuda_getDevice()
+    for t in tensors:
+        assert t is None or t.get_device() == home, "tensors on the current CUDA device are expected"
+
+
+def _tables(t):
+    """Elements from one node's table to the next one's, of tables [n, vocab, c] whose rows follow one another."""
+    n, vocab, c = t.shape
+    s0, s1, s2 = t.stride()
+    assert t.is_cuda and (s2 == 1 or c == 1) and (s1 == c or vocab == 1), "a node's rows follow one another"
+    return s0 if n > 1 else vocab * c
+
+
+def _tokens(t, count):
+    import torch
+    assert t.is_cuda and t.dtype == torch.int64 and t.is_contiguous() and t.numel() == count, "int64, one token per row"
+    return t.data_ptr()
+
+
+def embedding(table, tokens, y, scale=1.0, stream=None):
+    """y[i, r] <- scale table[i, tokens[i, r]] (0 where the token is outside [0, vocab)): table [n, vocab, c] fp32 or bf16 (a view of
+    the stacked parameters, for instance), tokens int64 [n, rows], y [n, rows, c] fp32 or bf16."""
+    _at_home(table, tokens, y)
+    n, vocab, c = table.shape
+    rows = tokens.shape[1]
+    shape = y.shape
+    assert shape == (n, rows, c), "y [n, rows, c] is expected"
+    _check(_calls.embedding(n, rows, vocab, c, table.data_ptr(), _dtype(table), _tables(table), _tokens(tokens, n * rows), scale,
+                            y.data_ptr(), _dtype(y), _node_rows(y, shape, y.dtype), _stream_ptr(stream)), "embedding")
+
+
+def embedding_grad_workspace_bytes(n, rows, vocab, c):
+    v = _lib.embedding_grad_workspace_bytes(n, rows, vocab, c)
+    if v < 0:
+        raise DecentlamError(v, "embedding_grad_workspace_bytes")
+    return int(v)
+
+
+def embedding_grad(tokens, dy, dtable, workspace, scale=1.0, accumulate=False, stream=None):
+    """Gradient of embedding's table: dtable [n, vocab, c] fp32 or bf16 (a view of the stacked gradient, for instance) is overwritten, or
+    added to (accumulate); workspace: uint8 device tensor of at least embedding_grad_workspace_bytes(n, rows, vocab, c) bytes."""
+    _at_home(tokens, dy, dtable, workspace)
+    n, vocab, c = dtable.shape
+    shape = dy.shape
+    rows = shape[1]
+    assert shape == (n, rows, c) and workspace.is_cuda and workspace.is_contiguous()
+    _check(_calls.embedding_grad(n, rows, vocab, c, _tokens(tokens, n * rows), dy.data_ptr(), _dtype(dy),
+                                 _node_rows(dy, shape, dy.dtype), scale, int(accumulate), dtable.data_ptr(), _dtype(dtable),
+                                 _tables(dtable), workspace.data_ptr(), workspace.nbytes, _stream_ptr(stream)), "embedding_grad")
+
+
+def _maybe_rows(t, shape, dtype):
+    """(pointer, row stride) of activations, or of None."""
+    return (t.data_ptr(), _node_rows(t, shape, dtype)) if t is not None else (None, 0)
+
+
+def rms_norm(x, weight, eps, y, rstd, residual=None, h=None, y8=None, scales=None, stream=None):
+    """h <- x + residual; y <- h rstd weight over the last axis of x [n, rows, c] (fp32 or bf16); weight fp32 [n, c] (a view of the
+    stacked parameters, for instance); rstd fp32 [n, rows] is written.  residual and h (of x's shape and type) may be None.  y8
+    (float8_e4m3fn of x's shape) and scales (fp32 [n, rows]): the output in 8 bits, beside y or in its place (y None)."""
+    _at_home(x, weight, y, rstd, residual, h, y8, scales)
+    shape, dtype = x.shape, x.dtype
+    n, rows, c = shape
+    assert _dtype(weight) == G_F32
+    (pr, ldr), (ph, ldh), (py, ldy) = (_maybe_rows(t, shape, dtype) for t in (residual, h, y))
+    pw, ldw = _node_vectors(weight, n, c)
+    p8, ld8, ps = None, 0, None
+    if y8 is not None:
+        import torch
+        p8, ld8, ps = y8.data_ptr(), _node_rows(y8, shape, torch.float8_e4m3fn), _per_row(scales, n * rows)
+    _check(_calls.rms_norm(n, rows, c, x.data_ptr(), _dtype(x), _node_rows(x, shape, dtype), pr, ldr, pw, ldw, eps, ph, ldh, py, ldy,
+                           p8, ld8, ps, _per_row(rstd, n * rows), _stream_ptr(stream)), "rms_norm")
+
+
+def rms_norm_grad_workspace_bytes(n, rows, c):
+    v = _lib.rms_norm_grad_workspace_bytes(n, rows, c)
+    if v < 0:
+        raise DecentlamError(v, "rms_norm_grad_workspace_bytes")
+    return int(v)
+
+
+def rms_norm_grad(h, dy, weight, rstd, dh, dweight, workspace, dresidual=None, stream=None):
+    """Backward pass of rms_norm: dh (of h's shape and type) is the gradient of x and of residual alike, dresidual (or None) what
+    reaches h along the residual stream; dweight [n, c] fp32 or bf16 (a view of the stacked gradient, for instance) is overwritten;
+    workspace: uint8 device tensor of at least rms_norm_grad_workspace_bytes(n, rows, c) bytes."""
+    _at_home(h, dy, weight, rstd, dh, dweight, workspace, dresidual)
+    shape, dtype = h.shape, h.dtype
+    n, rows, c = shape
+    assert _dtype(weight) == G_F32 and workspace.is_cuda and workspace.is_contiguous()
+    pr, lddr = _maybe_rows(dresidual, shape, dtype)
+    (pw, ldw), (pgw, ldgw) = _node_vectors(weight, n, c), _node_vectors(dweight, n, c)
+    _check(_calls.rms_norm_grad(n, rows, c, h.data_ptr(), _dtype(h), _node_rows(h, shape, dtype), dy.data_ptr(),
+                                _node_rows(dy, shape, dtype), pr, lddr, pw, ldw, _per_row(rstd, n * rows), dh.data_ptr(),
+                                _node_rows(dh, shape, dtype), pgw, ldgw, _dtype(dweight), workspace.data_ptr(), workspace.nbytes,
+                                _stream_ptr(stream)), "rms_norm_grad")
+
+
+def dropout(x, p, state, y, site=0, residual=None, stream=None):
+    """y <- residual + dropout(x) (residual may be None) of x [n, rows, c] fp32 or bf16, with probability p of an element to be
+    dropped.  state: int64 device tensor (seed, step); site: which of the model's dropouts.  The same call on dy is the backward
+    pass."""
+    _at_home(x, state, y, residual)
+    import torch
+    shape, dtype = x.shape, x.dtype
+    n, rows, c = shape
+    assert state.is_cuda and state.dtype == torch.int64 and state.is_contiguous() and state.numel() == 2, "state: int64 (seed, step)"
+    pr, ldr = _maybe_rows(residual, shape, dtype)
+    _check(_calls.dropout(n, rows, c, x.data_ptr(), _dtype(x), _node_rows(x, shape, dtype), pr, ldr, p, state.data_ptr(), site,
+                          y.data_ptr(), _node_rows(y, shape, dtype), _stream_ptr(stream)), "dropout")
+
+
+def _mask_rows(allowed, n, rows, vocab):
+    """(pointer, words between rows) of a bit mask int32 [n, rows, words]; expanded from one row: 0 words."""
+    if allowed is None:
+        return None, 0
+    import torch
+    words = (vocab + 31) // 32
+    assert allowed.is_cuda and allowed.dtype == torch.int32 and allowed.dim() == 3 and allowed.shape[:2] == (n, rows), \
+        "a bit mask int32 [n, rows, words] is expected"
+    assert allowed.shape[2] >= words and (allowed.stride(2) == 1 or allowed.shape[2] == 1), "a bit for each token is expected"
+    if allowed.stride(0) == 0 and allowed.stride(1) == 0:
+        return allowed.data_ptr(), 0
+    return allowed.data_ptr(), _node_rows(allowed, allowed.shape, torch.int32)
+
+
+def _texts(history, history_start, count):
+    if history_start is None:
+        assert history is None, "a text needs its bounds"
+        return None, 0, None
+    import torch
+    assert history_start.is_cuda and history_start.dtype == torch.int64 and history_start.is_contiguous()
+    assert history_start.numel() == count + 1, "bounds of every row's text are expected"
+    return _tokens(history, history.numel()), history.numel(), history_start.data_ptr()
+
+
+def logits_adjust(logits, out, bias=None, allowed=None, history=None, history_start=None, repetition=None, frequency=None,
+                  presence=None, temperature=None, stream=None):
+    """out <- (penalties(logits) + bias) / temperature, -inf where the mask forbids: logits, out [n, rows, vocab] fp32 or bf16 (out
+    may be the logits themselves); bias fp32 [n, vocab]; allowed int32 [n, rows, >= ceil(vocab / 32)], bit v % 32 of word v / 32;
+    history int64, all rows' texts one after another, and history_start int64 [n * rows + 1] their bounds; repetition, frequency,
+    presence, temperature fp32 [n, rows].  Each may be None."""
+    _at_home(logits, out, bias, allowed, history, history_start, repetition, frequency, presence, temperature)
+    shape, dtype = logits.shape, logits.dtype
+    n, rows, vocab = shape
+    count = n * rows
+    assert bias is None or _dtype(bias) == G_F32
+    (pb, ldb), (pm, ldm) = _node_vectors(bias, n, vocab), _mask_rows(allowed, n, rows, vocab)
+    pt, length, ps = _texts(history, history_start, count)
+    rep, freq, pres, temp = (_per_row(t, count) if t is not None else None for t in (repetition, frequency, presence, temperature))
+    _check(_calls.logits_adjust(n, rows, vocab, logits.data_ptr(), _dtype(logits), _node_rows(logits, shape, dtype), pb, ldb, pm, ldm,
+                                pt, length, ps, rep, freq, pres, temp, out.data_ptr(), _node_rows(out, shape, dtype),
+                                _stream_ptr(stream)), "logits_adjust")
+
+
+def logits_adjust_grad(dout, dlogits, logits=None, allowed=None, history=None, history_start=None, repetition=None,
+                       temperature=None, stream=None):
+    """Backward pass of logits_adjust: dlogits of dout's shape and type (dout itself: in place); logits: as they were before the
+    adjustment, needed with repetition; the others as there (biases, frequency and presence have no slope)."""
+    _at_home(dout, dlogits, logits, allowed, history, history_start, repetition, temperature)
+    shape, dtype = dout.shape, dout.dtype
+    n, rows, vocab = shape
+    count = n * rows
+    pz, ldl = _maybe_rows(logits, shape, dtype)
+    pm, ldm = _mask_rows(allowed, n, rows, vocab)
+    pt, length, ps = _texts(history, history_start, count)
+    rep, temp = (_per_row(t, count) if t is not None else None for t in (repetition, temperature))
+    _check(_calls.logits_adjust_grad(n, rows, vocab, dout.data_ptr(), _dtype(dout), _node_rows(dout, shape, dtype), pz, ldl, pm, ldm,
+                                     pt, length, ps, rep, temp, dlogits.data_ptr(), _node_rows(dlogits, shape, dtype),
+                                     _stream_ptr(stream)), "logits_adjust_grad")
 
 
 def launch_count():

@@ -19,7 +19,7 @@ OUT = os.path.join(HERE, "libdecentlam.so")
 CALLS = os.path.join(HERE, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["api.cpp", "topology.cpp", "sharded.cpp", "step_kernels.cu", "step_merged.cu", "step_sharded.cu",
            "pmsgd_kernel.cu", "lsq_kernels.cu", "gradients.cpp", "gradient_kernels.cu", "train.cpp", "layer_norm.cu",
-           "policy_loss.cu"]
+           "policy_loss.cu", "model.cpp", "embedding.cu", "rms_norm.cu", "dropout.cu", "logits.cu"]
 ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]
 
 

@@ -77,8 +77,66 @@ CALL(policy_loss_grad, 21, {
                             stream))
 })
 
+CALL(embedding, 13, {
+    int n = I(0), t_dtype = I(5), dtype = I(10);
+    int64_t rows = N(1), vocab = N(2), c = N(3), ldt = N(6), ldy = N(11);
+    void *table = P(4), *tokens = P(7), *y = P(9), *stream = P(12);
+    float scale = F(8);
+    LAUNCH(embedding(n, rows, vocab, c, table, t_dtype, ldt, tokens, scale, y, dtype, ldy, stream))
+})
+
+CALL(embedding_grad, 16, {
+    int n = I(0), dtype = I(6), accumulate = I(9), g_dtype = I(11);
+    int64_t rows = N(1), vocab = N(2), c = N(3), lddy = N(7), ldgt = N(12), bytes = N(14);
+    void *tokens = P(4), *dy = P(5), *dtable = P(10), *work = P(13), *stream = P(15);
+    float scale = F(8);
+    LAUNCH(embedding_grad(n, rows, vocab, c, tokens, dy, dtype, lddy, scale, accumulate, dtable, g_dtype, ldgt, work, bytes, stream))
+})
+
+CALL(rms_norm, 20, {
+    int n = I(0), dtype = I(4);
+    int64_t rows = N(1), c = N(2), ldx = N(5), ldr = N(7), ldw = N(9), ldh = N(12), ldy = N(14), ld8 = N(16);
+    void *x = P(3), *res = P(6), *w = P(8), *h = P(11), *y = P(13), *y8 = P(15), *scales = P(17), *rstd = P(18), *stream = P(19);
+    float eps = F(10);
+    LAUNCH(rms_norm(n, rows, c, x, dtype, ldx, res, ldr, w, ldw, eps, h, ldh, y, ldy, y8, ld8, scales, rstd, stream))
+})
+
+CALL(rms_norm_grad, 21, {
+    int n = I(0), dtype = I(4), g_dtype = I(17);
+    int64_t rows = N(1), c = N(2), ldh = N(5), lddy = N(7), lddr = N(9), ldw = N(11), lddh = N(14), ldgw = N(16), bytes = N(19);
+    void *h = P(3), *dy = P(6), *dres = P(8), *w = P(10), *rstd = P(12), *dh = P(13), *gw = P(15), *work = P(18), *stream = P(20);
+    LAUNCH(rms_norm_grad(n, rows, c, h, dtype, ldh, dy, lddy, dres, lddr, w, ldw, rstd, dh, lddh, gw, ldgw, g_dtype, work, bytes,
+                         stream))
+})
+
+CALL(dropout, 14, {
+    int n = I(0), dtype = I(4);
+    int64_t rows = N(1), c = N(2), ldx = N(5), ldr = N(7), site = N(10), ldy = N(12);
+    void *x = P(3), *res = P(6), *state = P(9), *y = P(11), *stream = P(13);
+    float p = F(8);
+    LAUNCH(dropout(n, rows, c, x, dtype, ldx, res, ldr, p, state, site, y, ldy, stream))
+})
+
+CALL(logits_adjust, 20, {
+    int n = I(0), dtype = I(4);
+    int64_t rows = N(1), vocab = N(2), ldl = N(5), ldb = N(7), ldm = N(9), length = N(11), ldo = N(18);
+    void *z = P(3), *bias = P(6), *allowed = P(8), *text = P(10), *start = P(12), *rep = P(13), *freq = P(14), *pres = P(15),
+         *temp = P(16), *out = P(17), *stream = P(19);
+    LAUNCH(logits_adjust(n, rows, vocab, z, dtype, ldl, bias, ldb, allowed, ldm, text, length, start, rep, freq, pres, temp, out, ldo,
+                         stream))
+})
+
+CALL(logits_adjust_grad, 18, {
+    int n = I(0), dtype = I(4);
+    int64_t rows = N(1), vocab = N(2), lddo = N(5), ldl = N(7), ldm = N(9), length = N(11), ldd = N(16);
+    void *g = P(3), *z = P(6), *allowed = P(8), *text = P(10), *start = P(12), *rep = P(13), *temp = P(14), *d = P(15),
+         *stream = P(17);
+    LAUNCH(logits_adjust_grad(n, rows, vocab, g, dtype, lddo, z, ldl, allowed, ldm, text, length, start, rep, temp, d, ldd, stream))
+})
+
 #define ENTRY(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {ENTRY(gradient_norm), ENTRY(gradient_clip), ENTRY(layer_norm), ENTRY(layer_norm_grad),
-                                ENTRY(policy_loss_grad), {NULL, NULL, 0, NULL}};
+                                ENTRY(policy_loss_grad), ENTRY(embedding), ENTRY(embedding_grad), ENTRY(rms_norm),
+                                ENTRY(rms_norm_grad), ENTRY(dropout), ENTRY(logits_adjust), ENTRY(logits_adjust_grad), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", NULL, -1, methods, NULL, NULL, NULL, NULL};
 PyMODINIT_FUNC PyInit__calls(void) { return PyModule_Create(&module); }
