@@ -498,15 +498,15 @@ DLM_API int policy_loss_grad(int n, int64_t rows, int64_t vocab, const void* log
  *   y_r = scale table_i[token_r] ;   dtable_i[v] = scale sum_{r : token_r = v} dy_r
  *   table      : device [n, vocab, c] of t_dtype, a node's rows following one another, ldt >= vocab c elements from one node to
  *                the next (a column range of the stacked x, for instance)
- *   tokens     : device int64 [n * rows].  A token outside [0, vocab) stands for none: its row of y is 0 and its row of dy is not read.
+ *   tokens     : device int64 [n * rows].  A token outside [0, vocab) stands for none: its row of y is 0 and its row of dy does not count.
  *   y, dy      : device [n * rows, c] of dtype, row strides ldy, lddy
  *   scale      : finite
  *   dtable     : device [n, vocab, c] of g_dtype, ldgt >= vocab c elements from one node to the next.  accumulate = 0: overwritten,
  *                rows without tokens by 0.  accumulate = 1: added to (a table that the output head shares, further batches); rows
  *                without tokens are left as they are.
  *   workspace  : device, embedding_grad_workspace_bytes(n, rows, vocab, c) bytes, 256-byte aligned, owned by the caller
- * rows may be 0.  The gradient sorts the tokens and adds their rows in the order of the text (of a token that fills blocks of 64
- * places of the sorted text, block by block).  Fast path: c a multiple of 16 bytes' worth of the narrower type, arrays and strides
+ * rows may be 0.  The gradient sorts the tokens and adds their rows in the order of the text (of a token that
+ * occurs often, in shares of up to 32).  Fast path: c a multiple of 16 bytes' worth of the narrower type, arrays and strides
  * 16-byte aligned.
  * Errors: DLM_ERR_NULL, DLM_ERR_SHAPE, DLM_ERR_KIND, DLM_ERR_ALIGN, DLM_ERR_ALIAS, DLM_ERR_HYPER, DLM_ERR_WORKSPACE,
  * DLM_ERR_UNSUPPORTED, DLM_ERR_CUDA.

@@ -1,9 +1,9 @@
 // Embedding of n nodes' tokens, each node with its own table in its row of the stacked parameters, and its gradient:
 //   y_r = scale table_i[token_r] ,   dtable_i[v] = scale sum_{r : token_r = v} dy_r   (0 for a token outside [0, vocab)).
-// The gradient is a gather, not a scatter: a node's tokens are sorted (stably, in chunks that one CTA's shared memory holds), every row
-// of the table then finds its places in the sorted chunks and adds their rows of dy in the order of the text, so the sums have a
-// fixed order, no atomics, and every byte of the gradient is written once.  Where a token is so common that it fills whole aligned
-// blocks of kBlockItems sorted places, the blocks' sums are taken by CTAs of their own first.
+// The gradient is a gather, not a scatter: a node's tokens are sorted (stably, in chunks that one CTA's shared memory holds, then
+// merged by rank), groups of threads walk equal shares of the sorted places and add rows of dy in the order of the text, and other CTAs
+// clear the rows that no token names.  The sums have a fixed order, no atomics, common tokens are shared between many groups (whose
+// parts a last kernel joins), and every byte of the gradient is written once.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -97,48 +97,54 @@ int forward(const dlm_embed_args& a, cudaStream_t s) {
 
 // ------------------------------------------------------------------------------------------------ backward: sorting
 constexpr int kSortThreads = 1024, kSortWarps = 32;
-constexpr int kTileRows = 64;    // rows of the table that one CTA of the last kernel writes
-constexpr int kBlockItems = 64;  // sorted places whose sum is taken at once where they hold one token
-
 // Chunks of up to 16384 places: two copies of keys and places fit a CTA's shared memory.
 template <int ITEMS>
 constexpr int kChunk = kSortThreads * ITEMS;
 constexpr int kSmallItems = 2, kLargeItems = 16;
 constexpr size_t sort_smem(int items) { return (size_t)kSortThreads * items * 12 + kSortWarps * 256 * 2 + 1024; }
-int chunk_places(int64_t rows) { return rows <= kChunk<kSmallItems> ? kChunk<kSmallItems> : kChunk<kLargeItems>; }
+
+constexpr int kTileItems = 32;  // sorted places that one group of threads sums
 
 struct Sorted {  // the workspace
-    uint32_t* keys;    // [n rows] tokens, sorted within each chunk; vocab for those outside [0, vocab)
+    uint32_t* keys;    // [n rows] tokens, sorted; vocab for those outside [0, vocab)
     uint32_t* places;  // [n rows] rows of the node
-    int* starts;       // [n chunks][tiles + 1] first place of each tile's rows in the chunk
-    float* sums;       // [n chunks][blocks][c] of the blocks that hold one token
-    int chunk, chunks, tiles, blocks;
+    uint32_t* chunk_keys;    // as above, each chunk sorted by itself; the same arrays where a node is one chunk
+    uint32_t* chunk_places;
+    float* parts;  // [n tiles][2][c] sums of a tile's first and last token, where they go on in the tiles before and behind
+    int chunk, chunks, tiles;
     size_t bytes;
 };
-Sorted sorted_layout(int n, int64_t rows, int64_t vocab, int64_t c, void* workspace) {
+Sorted sorted_layout(int n, int64_t rows, int64_t c, void* workspace) {
     Sorted w = {};
-    w.chunk = chunk_places(rows);
-    w.chunks = (int)std::max<int64_t>(1, (rows + w.chunk - 1) / w.chunk);
-    w.tiles = (int)((vocab + kTileRows - 1) / kTileRows);
-    w.blocks = (int)(std::min<int64_t>(rows, w.chunk) / kBlockItems);
-    auto up = [](int64_t b) { return (b + 255) / 256 * 256; };
+    w.chunk = rows <= kChunk<kSmallItems> ? kChunk<kSmallItems> : kChunk<kLargeItems>;
+    w.chunks = (int)((rows + w.chunk - 1) / w.chunk);
+    w.tiles = (int)((rows + kTileItems - 1) / kTileItems);
+    const int64_t keys = (n * rows * 4 + 255) / 256 * 256;
     char* p = static_cast<char*>(workspace);
-    const int64_t keys = up(n * rows * 4), starts = up((int64_t)n * w.chunks * (w.tiles + 1) * 4);
-    w.keys = reinterpret_cast<uint32_t*>(p);
-    w.places = reinterpret_cast<uint32_t*>(p + keys);
-    w.starts = reinterpret_cast<int*>(p + 2 * keys);
-    w.sums = reinterpret_cast<float*>(p + 2 * keys + starts);
-    w.bytes = (size_t)(2 * keys + starts + (int64_t)n * w.chunks * w.blocks * c * 4);
+    auto take = [&](int64_t bytes) {
+        char* at = p + w.bytes;
+        w.bytes += (size_t)bytes;
+        return at;
+    };
+    w.chunk_keys = w.keys = reinterpret_cast<uint32_t*>(take(keys));
+    w.chunk_places = w.places = reinterpret_cast<uint32_t*>(take(keys));
+    if (w.chunks > 1) {
+        w.chunk_keys = reinterpret_cast<uint32_t*>(take(keys));
+        w.chunk_places = reinterpret_cast<uint32_t*>(take(keys));
+    }
+    w.parts = reinterpret_cast<float*>(take((int64_t)n * w.tiles * 2 * c * 4));
     return w;
 }
 
-__device__ __forceinline__ int lower_bound(const uint32_t* keys, int lo, int hi, uint32_t v) {
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
+// Places of keys below v, among keys[0 .. count).
+__device__ __forceinline__ int lower_bound(const uint32_t* keys, int count, uint32_t v) {
+    int lo = 0;
+    while (lo < count) {
+        const int mid = (lo + count) >> 1;
         if (keys[mid] < v)
             lo = mid + 1;
         else
-            hi = mid;
+            count = mid;
     }
     return lo;
 }
@@ -195,6 +201,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(long long rows, uint
         // first place of every digit, and within it of every warp
         uint32_t total = 0;
         if (threadIdx.x < 256) {
+#pragma unroll
             for (int k = 0; k < kSortWarps; ++k) {
                 const uint32_t v = counts[k * 256 + threadIdx.x];
                 counts[k * 256 + threadIdx.x] = (uint16_t)total;
@@ -232,111 +239,199 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(long long rows, uint
     const uint32_t* kin = keys + from * CH;
     const uint16_t* pin = places + from * CH;
     for (int k = threadIdx.x; k < len; k += kSortThreads) {
-        w.keys[base + k] = kin[k];
-        w.places[base + k] = (uint32_t)(chunk * CH + pin[k]);
+        w.chunk_keys[base + k] = kin[k];
+        w.chunk_places[base + k] = (uint32_t)(chunk * CH + pin[k]);
     }
-    int* starts = w.starts + (long long)blockIdx.x * (w.tiles + 1);
-    for (int k = threadIdx.x; k <= w.tiles; k += kSortThreads)
-        starts[k] = lower_bound(kin, 0, len, min(vocab, (uint32_t)k * kTileRows));
+}
+
+// Every key's place among all chunks of its node: its own, and in each other chunk the number of keys before it (equal ones of earlier
+// chunks among them).
+__global__ void __launch_bounds__(256) merge_kernel(long long rows, Sorted w) {
+    const int node = blockIdx.y;
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x, base = (long long)node * rows;
+    pdl_wait();
+    pdl_release();
+    if (i >= rows) return;
+    const uint32_t* keys = w.chunk_keys + base;
+    const int own = (int)(i / w.chunk);
+    const uint32_t key = keys[i];
+    long long to = i - (long long)own * w.chunk;
+    for (int k = 0; k < w.chunks; ++k)
+        if (k != own) to += lower_bound(keys + (long long)k * w.chunk, (int)min((long long)w.chunk, rows - (long long)k * w.chunk), key + (k < own));
+    w.keys[base + to] = key;
+    w.places[base + to] = w.chunk_places[base + i];
 }
 
 // ------------------------------------------------------------------------------------------------ backward: sums
-// Blocks of kBlockItems places with one token.
+// Adds to, or overwrites, a run of the gradient.
+template <typename G, int LEN>
+__device__ __forceinline__ void put_sum(G* to, const float* sum, float scale, int accumulate) {
+    float v[LEN] = {};
+    if (accumulate) load_run<G, LEN>(to, v);
+#pragma unroll
+    for (int e = 0; e < LEN; ++e) v[e] = fmaf(sum[e], scale, v[e]);
+    store_run<G, LEN>(to, v);
+}
+
+// A run of one row of dy as it is loaded.
 template <typename T, int LEN>
-__global__ void __launch_bounds__(128) block_sums_kernel(long long rows, uint32_t vocab, long long c, const T* dy, long long ldy, Sorted w) {
-    const int which = blockIdx.x / w.blocks, block = blockIdx.x % w.blocks;  // of all chunks
-    const int node = which / w.chunks, chunk = which % w.chunks;
-    const long long at = (long long)node * rows + (long long)chunk * w.chunk + block * kBlockItems;
-    pdl_wait();
-    pdl_release();
-    if ((long long)chunk * w.chunk + (block + 1) * kBlockItems > rows) return;
-    const uint32_t token = w.keys[at];
-    if (token != w.keys[at + kBlockItems - 1] || token >= vocab) return;
-    const long long col = ((long long)blockIdx.y * 128 + threadIdx.x) * LEN;
-    if (col >= c) return;
-    float sum[LEN] = {};
-    const T* from = dy + (long long)node * rows * ldy + col;
-#pragma unroll 8
-    for (int k = 0; k < kBlockItems; ++k) {
+struct Raw {
+    Words w[LEN / kRun<T>];
+    __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+        for (int k = 0; k < LEN / kRun<T>; ++k) w[k] = ld_words(p + k * kRun<T>);
+    }
+    __device__ __forceinline__ void add(float* sum) const {
         float v[LEN];
-        load_run<T, LEN>(from + (long long)w.places[at + k] * ldy, v);
+#pragma unroll
+        for (int k = 0; k < LEN / kRun<T>; ++k) unpack<T>(w[k], v + k * kRun<T>);
 #pragma unroll
         for (int e = 0; e < LEN; ++e) sum[e] += v[e];
     }
-    float* to = w.sums + ((long long)which * w.blocks + block) * c + col;
-    store_run<float, LEN>(to, sum);
-}
+};
+template <typename T>
+struct Raw<T, 1> {
+    T v;
+    __device__ __forceinline__ void load(const T* p) { v = *p; }
+    __device__ __forceinline__ void add(float* sum) const { sum[0] += widen(v); }
+};
 
-// A warp to a row of the table, U runs a lane; a CTA kTileRows rows and 32 U LEN columns.
-template <typename T, typename G, int LEN, int U>
-__global__ void __launch_bounds__(256) embedding_grad_kernel(long long rows, uint32_t vocab, long long c, const T* dy, long long ldy,
-                                                             float scale, int accumulate, G* dtable, long long ldgt, Sorted w) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int node = blockIdx.x / w.tiles, tile = blockIdx.x % w.tiles;
-    const long long col0 = (long long)blockIdx.y * 32 * U * LEN + lane * LEN;
-    pdl_wait();
-    pdl_release();
-    const T* from = dy + (long long)node * rows * ldy;
-    const uint32_t end = min(vocab, (uint32_t)(tile + 1) * kTileRows);
-    for (uint32_t v = (uint32_t)tile * kTileRows + warp; v < end; v += 8) {
-        float sum[U][LEN];
+struct GradShape {
+    long long rows, c, ldy, ldgt;
+    uint32_t vocab;
+    int n, accumulate, lanes, strips, zero_rows, zero_ctas;  // zero_ctas: a node's
+    float scale;
+    unsigned sum_ctas;
+};
+
+// Sums over kTileItems sorted places: `lanes` threads take a tile and a strip of lanes LEN columns, walk the places in order and write
+// a token's sum at its end; what goes on in another tile is left in parts.
+template <typename T, typename G, int LEN>
+__device__ __forceinline__ void sum_tiles(const GradShape& s, unsigned cta, const T* dy, G* dtable, const Sorted& w) {
+    constexpr int BATCH = 8;
+    const long long tile_at = (long long)(cta / s.strips) * (256 / s.lanes) + threadIdx.x / s.lanes;
+    const long long col = ((long long)(cta % s.strips) * s.lanes + threadIdx.x % s.lanes) * LEN;
+    if (tile_at >= (long long)s.n * w.tiles || col >= s.c) return;
+    const int node = (int)(tile_at / w.tiles), tile = (int)(tile_at % w.tiles);
+    const long long first = (long long)tile * kTileItems, base = (long long)node * s.rows;
+    const uint32_t *keys = w.keys + base + first, *places = w.places + base + first;
+    const int len = (int)min((long long)kTileItems, s.rows - first);
+    const T* from = dy + base * s.ldy + col;
+    G* to = dtable + node * s.ldgt + col;
+    float* part = w.parts + tile_at * 2 * s.c + col;
+    uint32_t key = keys[0];
+    bool before = first > 0 && keys[-1] == key;  // the run at hand began in an earlier tile
+    float sum[LEN] = {};
+    for (int b = 0; b < len && key < s.vocab; b += BATCH) {
+        Raw<T, LEN> raw[BATCH];
+        uint32_t next[BATCH];  // key behind each place
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int e = 0; e < LEN; ++e) sum[u][e] = 0.0f;
-        bool any = false;
-        for (int c0 = 0; c0 < w.chunks && rows > 0; c0 += 32) {
-            int lo = 0, hi = 0;  // of the lane's chunk
-            if (c0 + lane < w.chunks) {
-                const long long which = (long long)node * w.chunks + c0 + lane;
-                const int* starts = w.starts + which * (w.tiles + 1) + tile;
-                const uint32_t* keys = w.keys + (long long)node * rows + (long long)(c0 + lane) * w.chunk;
-                hi = starts[1];
-                lo = lower_bound(keys, starts[0], hi, v);
-                hi = lower_bound(keys, lo, hi, v + 1);
+        for (int k = 0; k < BATCH; ++k)
+            if (b + k < len) {
+                next[k] = first + b + k + 1 < s.rows ? keys[b + k + 1] : 0xffffffffu;
+                raw[k].load(from + (long long)places[b + k] * s.ldy);
             }
-            uint32_t found = __ballot_sync(0xffffffffu, lo < hi);
-            any |= found != 0;
-            for (; found; found &= found - 1) {
-                const int k = __ffs(found) - 1;
-                const int b = __shfl_sync(0xffffffffu, hi, k);
-                int i = __shfl_sync(0xffffffffu, lo, k);
-                const uint32_t* places = w.places + (long long)node * rows + (long long)(c0 + k) * w.chunk;
-                const float* sums = w.sums + ((long long)node * w.chunks + c0 + k) * w.blocks * c;
-                while (i < b) {
-                    const bool whole = i % kBlockItems == 0 && i + kBlockItems <= b;
-                    const T* row = from + (whole ? 0 : (long long)places[i] * ldy);
 #pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        const long long col = col0 + u * 32 * LEN;
-                        if (col < c) {
-                            float x[LEN];
-                            if (whole)
-                                load_run<float, LEN>(sums + (long long)(i / kBlockItems) * c + col, x);
-                            else
-                                load_run<T, LEN>(row + col, x);
+        for (int k = 0; k < BATCH; ++k) {
+            if (b + k >= len || key >= s.vocab) break;
+            raw[k].add(sum);
+            const bool last = b + k + 1 == len;
+            if (next[k] != key || last) {
+                const bool beyond = next[k] == key;
+                if (before)
+                    store_run<float, LEN>(part, sum);
+                else if (beyond)
+                    store_run<float, LEN>(part + s.c, sum);
+                else
+                    put_sum<G, LEN>(to + (long long)key * s.c, sum, s.scale, s.accumulate);
+                before = false;
 #pragma unroll
-                            for (int e = 0; e < LEN; ++e) sum[u][e] += x[e];
-                        }
-                    }
-                    i += whole ? kBlockItems : 1;
-                }
+                for (int e = 0; e < LEN; ++e) sum[e] = 0.0f;
             }
-        }
-        if (accumulate && !any) continue;
-        G* to = dtable + node * ldgt + (long long)v * c;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const long long col = col0 + u * 32 * LEN;
-            if (col < c) {
-                float old[LEN] = {};
-                if (accumulate) load_run<G, LEN>(to + col, old);
-#pragma unroll
-                for (int e = 0; e < LEN; ++e) sum[u][e] = fmaf(sum[u][e], scale, old[e]);
-                store_run<G, LEN>(to + col, sum[u]);
-            }
+            key = next[k];
         }
     }
+}
+
+// Rows without tokens: a CTA clears those among zero_rows rows of a node's table, in 16-byte chunks wherever they start.
+template <typename G>
+__device__ __forceinline__ void clear_rows(const GradShape& s, unsigned cta, G* dtable, const Sorted& w) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    uint32_t* touched = reinterpret_cast<uint32_t*>(smem);  // a bit for each row
+    __shared__ int bounds[2];
+    const int node = cta / s.zero_ctas;
+    const uint32_t v0 = (cta % s.zero_ctas) * (uint32_t)s.zero_rows, count = min((uint32_t)s.zero_rows, s.vocab - v0);
+    for (uint32_t k = threadIdx.x; k < (count + 31) / 32; k += 256) touched[k] = 0;
+    const uint32_t* keys = w.keys + (long long)node * s.rows;
+    if (threadIdx.x < 2) bounds[threadIdx.x] = lower_bound(keys, (int)s.rows, threadIdx.x ? v0 + count : v0);
+    __syncthreads();
+    for (int k = bounds[0] + threadIdx.x; k < bounds[1]; k += 256) {
+        const uint32_t v = keys[k] - v0;
+        atomicOr(&touched[v >> 5], 1u << (v & 31));
+    }
+    __syncthreads();
+    G* table = dtable + node * s.ldgt + (long long)v0 * s.c;
+    const long long row_bytes = s.c * (long long)sizeof(G), bytes = count * row_bytes;
+    const int skew = (int)((uintptr_t)table & 15);  // chunks lie on 16-byte boundaries; the first may begin before the table
+    char* chunks = reinterpret_cast<char*>(table) - skew;
+    const long long step = 256 * 16;
+    const long long rows_per_step = step / row_bytes, rest = step % row_bytes;
+    long long at = threadIdx.x * 16ll - skew;  // of this thread's chunk within the rows
+    long long row = at < 0 ? -1 : at / row_bytes, in_row = at - row * row_bytes;
+    auto is_touched = [&](long long r) { return (touched[r >> 5] >> (r & 31)) & 1u; };
+    for (; at < bytes; at += step) {
+        if (in_row >= 0 && in_row + 16 <= row_bytes) {
+            if (!is_touched(row)) *reinterpret_cast<uint4*>(chunks + skew + at) = make_uint4(0, 0, 0, 0);
+        } else {
+            for (long long b = max(at, 0ll); b < min(at + 16, bytes); b += sizeof(G))
+                if (!is_touched(b / row_bytes)) table[b / sizeof(G)] = narrow<G>(0.0f);
+        }
+        row += rows_per_step;
+        in_row += rest;
+        if (in_row >= row_bytes) {
+            ++row;
+            in_row -= row_bytes;
+        }
+    }
+}
+
+template <typename T, typename G, int LEN>
+__global__ void __launch_bounds__(256) embedding_grad_kernel(GradShape s, const T* dy, G* dtable, Sorted w) {
+    pdl_wait();
+    pdl_release();
+    if (blockIdx.x < s.sum_ctas)
+        sum_tiles<T, G, LEN>(s, blockIdx.x, dy, dtable, w);
+    else
+        clear_rows<G>(s, blockIdx.x - s.sum_ctas, dtable, w);
+}
+
+// Tokens that go on beyond their first tile: its part, then those of the tiles that follow.
+template <typename G, int LEN>
+__global__ void __launch_bounds__(256) embedding_grad_join_kernel(GradShape s, G* dtable, Sorted w) {
+    const long long tile_at = (long long)(blockIdx.x / s.strips) * (256 / s.lanes) + threadIdx.x / s.lanes;
+    const long long col = ((long long)(blockIdx.x % s.strips) * s.lanes + threadIdx.x % s.lanes) * LEN;
+    pdl_wait();
+    pdl_release();
+    if (tile_at >= (long long)s.n * w.tiles || col >= s.c) return;
+    const int node = (int)(tile_at / w.tiles), tile = (int)(tile_at % w.tiles);
+    const long long end = (long long)(tile + 1) * kTileItems;
+    if (end >= s.rows) return;
+    const uint32_t* keys = w.keys + (long long)node * s.rows;
+    const uint32_t key = keys[end - 1];
+    if (key >= s.vocab || keys[end] != key) return;
+    if (end > kTileItems && keys[end - kTileItems - 1] == key) return;  // an earlier tile has its beginning
+    const int last = (int)((end + lower_bound(keys + end, (int)(s.rows - end), key + 1) - 1) / kTileItems);
+    float sum[LEN];
+    const float* part = w.parts + tile_at * 2 * s.c + col;
+    load_run<float, LEN>(part + s.c, sum);
+#pragma unroll 8
+    for (int k = 1; k <= last - tile; ++k) {
+        float v[LEN];
+        load_run<float, LEN>(part + (long long)k * 2 * s.c, v);
+#pragma unroll
+        for (int e = 0; e < LEN; ++e) sum[e] += v[e];
+    }
+    put_sum<G, LEN>(dtable + node * s.ldgt + (long long)key * s.c + col, sum, s.scale, s.accumulate);
 }
 
 template <int ITEMS>
@@ -349,32 +444,52 @@ int run_sort(const dlm_embed_args& a, const Sorted& w, cudaStream_t s) {
     cudaError_t err = launch_overlapped(sort_kernel<ITEMS>, dim3((unsigned)(a.n * w.chunks)), dim3(kSortThreads), sort_smem(ITEMS), s, 1,
                                         a.rows, (uint32_t)a.vocab, a.tokens, passes, (bits + passes - 1) / passes, w);
     dlm_count_launch(1);
+    if (err == cudaSuccess && w.chunks > 1) {
+        err = launch_overlapped(merge_kernel, dim3((unsigned)((a.rows + 255) / 256), a.n), dim3(256), 0, s, 1, a.rows, w);
+        dlm_count_launch(1);
+    }
     return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
 }
 
 template <typename T, typename G, int LEN>
 int run_backward(const dlm_embed_args& a, const Sorted& w, cudaStream_t s) {
-    constexpr int U = LEN == 1 ? 8 : 4;
-    cudaError_t err = cudaSuccess;
-    if (w.blocks > 0) {
-        err = launch_overlapped(block_sums_kernel<T, LEN>, dim3((unsigned)(a.n * w.chunks * w.blocks), (unsigned)((a.c + 128 * LEN - 1) / (128 * LEN))),
-                                dim3(128), 0, s, 1, a.rows, (uint32_t)a.vocab, a.c, static_cast<const T*>(a.dy), a.ldy, w);
-        dlm_count_launch(1);
-        if (err != cudaSuccess) return DLM_ERR_CUDA;
-    }
-    err = launch_overlapped(embedding_grad_kernel<T, G, LEN, U>,
-                            dim3((unsigned)(a.n * w.tiles), (unsigned)((a.c + 32 * U * LEN - 1) / (32 * U * LEN))), dim3(256), 0, s, 1,
-                            a.rows, (uint32_t)a.vocab, a.c, static_cast<const T*>(a.dy), a.ldy, a.scale, a.accumulate,
-                            static_cast<G*>(a.dtable), a.ldgt, w);
+    GradShape g = {};
+    g.rows = a.rows;
+    g.c = a.c;
+    g.ldy = a.ldy;
+    g.ldgt = a.ldgt;
+    g.vocab = (uint32_t)a.vocab;
+    g.n = a.n;
+    g.accumulate = a.accumulate;
+    g.scale = a.scale;
+    const int64_t runs = (a.c + LEN - 1) / LEN;
+    g.lanes = 8;
+    while (g.lanes < 256 && g.lanes < runs) g.lanes *= 2;
+    g.strips = (int)((runs + g.lanes - 1) / g.lanes);
+    const int64_t tiles = (int64_t)a.n * w.tiles, sum_ctas = (tiles + 256 / g.lanes - 1) / (256 / g.lanes) * g.strips;
+    // about 256 KB of the gradient to a CTA
+    g.zero_rows = (int)std::min<int64_t>(a.vocab, std::max<int64_t>(1, (256 << 10) / (a.c * (int64_t)sizeof(G))));
+    g.zero_ctas = (int)((a.vocab + g.zero_rows - 1) / g.zero_rows);
+    const int64_t zero_ctas = a.accumulate ? 0 : (int64_t)a.n * g.zero_ctas;
+    if (sum_ctas + zero_ctas > 0x7fffffff) return DLM_ERR_UNSUPPORTED;
+    if (sum_ctas + zero_ctas == 0) return DLM_OK;
+    g.sum_ctas = (unsigned)sum_ctas;
+    cudaError_t err = launch_overlapped(embedding_grad_kernel<T, G, LEN>, dim3((unsigned)(sum_ctas + zero_ctas)), dim3(256),
+                                        (size_t)((g.zero_rows + 31) / 32 * 4), s, 1, g, static_cast<const T*>(a.dy),
+                                        static_cast<G*>(a.dtable), w);
     dlm_count_launch(1);
+    if (err == cudaSuccess && w.tiles > 1) {
+        err = launch_overlapped(embedding_grad_join_kernel<G, LEN>, dim3((unsigned)sum_ctas), dim3(256), 0, s, 1, g,
+                                static_cast<G*>(a.dtable), w);
+        dlm_count_launch(1);
+    }
     return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
 }
 
 template <typename T, typename G>
 int backward(const dlm_embed_args& a, cudaStream_t s) {
-    const Sorted w = sorted_layout(a.n, a.rows, a.vocab, a.c, a.workspace);
-    if ((int64_t)a.n * w.tiles > 0x7fffffff || (int64_t)a.n * w.chunks * std::max(1, w.blocks) > 0x7fffffff || a.c > 65535 * 32 * 8)
-        return DLM_ERR_UNSUPPORTED;
+    const Sorted w = sorted_layout(a.n, a.rows, a.c, a.workspace);
+    if ((int64_t)a.n * w.chunks > 0x7fffffff) return DLM_ERR_UNSUPPORTED;
     if (a.rows > 0) {
         const int rc = w.chunk == kChunk<kSmallItems> ? run_sort<kSmallItems>(a, w, s) : run_sort<kLargeItems>(a, w, s);
         if (rc != DLM_OK) return rc;
@@ -388,7 +503,7 @@ int backward(const dlm_embed_args& a, cudaStream_t s) {
 }  // namespace
 
 int64_t dlm_embedding_workspace(int n, int64_t rows, int64_t vocab, int64_t c) {
-    return (int64_t)sorted_layout(n, rows, vocab, c, nullptr).bytes;
+    return (int64_t)sorted_layout(n, rows, c, nullptr).bytes;
 }
 
 int dlm_launch_embedding(const dlm_embed_args& a, void* stream) {
