@@ -116,7 +116,7 @@ struct Sorted {  // the workspace
 };
 Sorted sorted_layout(int n, int64_t rows, int64_t c, void* workspace) {
     Sorted w = {};
-    w.chunk = rows <= kChunk<kSmallItems> ? kChunk<kSmallItems> : kChunk<kLargeItems>;
+    w.chunk = rows <= 32 * kChunk<kSmallItems> ? kChunk<kSmallItems> : kChunk<kLargeItems>;
     w.chunks = (int)((rows + w.chunk - 1) / w.chunk);
     w.tiles = (int)((rows + kTileItems - 1) / kTileItems);
     const int64_t keys = (n * rows * 4 + 255) / 256 * 256;
@@ -135,6 +135,8 @@ Sorted sorted_layout(int n, int64_t rows, int64_t c, void* workspace) {
     w.parts = reinterpret_cast<float*>(take((int64_t)n * w.tiles * 2 * c * 4));
     return w;
 }
+
+// Small chunks sort in 9 us where large ones take 39, but every key is looked for in all chunks: they are for texts of up to 32 of them.
 
 // Places of keys below v, among keys[0 .. count).
 __device__ __forceinline__ int lower_bound(const uint32_t* keys, int count, uint32_t v) {
@@ -245,19 +247,23 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(long long rows, uint
 }
 
 // Every key's place among all chunks of its node: its own, and in each other chunk the number of keys before it (equal ones of earlier
-// chunks among them).
+// chunks among them).  Sixteen lanes to a key share the chunks.
+constexpr int kMergeLanes = 16;
 __global__ void __launch_bounds__(256) merge_kernel(long long rows, Sorted w) {
-    const int node = blockIdx.y;
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x, base = (long long)node * rows;
+    const int node = blockIdx.y, lane = threadIdx.x % kMergeLanes;
+    const long long i = min(rows - 1, ((long long)blockIdx.x * 256 + threadIdx.x) / kMergeLanes), base = (long long)node * rows;
+    pdl_release();  // the next kernel clears rows meanwhile, and waits where it needs the order
     pdl_wait();
-    pdl_release();
-    if (i >= rows) return;
     const uint32_t* keys = w.chunk_keys + base;
     const int own = (int)(i / w.chunk);
     const uint32_t key = keys[i];
-    long long to = i - (long long)own * w.chunk;
-    for (int k = 0; k < w.chunks; ++k)
-        if (k != own) to += lower_bound(keys + (long long)k * w.chunk, (int)min((long long)w.chunk, rows - (long long)k * w.chunk), key + (k < own));
+    int before = 0;
+    for (int k = lane; k < w.chunks; k += kMergeLanes)
+        if (k != own) before += lower_bound(keys + (long long)k * w.chunk, (int)min((long long)w.chunk, rows - (long long)k * w.chunk), key + (k < own));
+#pragma unroll
+    for (int o = kMergeLanes / 2; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
+    if (lane != 0) return;
+    const long long to = i - (long long)own * w.chunk + before;
     w.keys[base + to] = key;
     w.places[base + to] = w.chunk_places[base + i];
 }
@@ -301,16 +307,22 @@ struct GradShape {
     uint32_t vocab;
     int n, accumulate, lanes, strips, zero_rows, zero_ctas;  // zero_ctas: a node's
     float scale;
-    unsigned sum_ctas;
+    int scan;  // rows without tokens are found in the text
+    unsigned lead, sum_ctas;
 };
 
-// Sums over kTileItems sorted places: `lanes` threads take a tile and a strip of lanes LEN columns, walk the places in order and write
+// Runs of columns of a thread, `lanes` runs apart: four single elements share the work of a place that one run of 16 bytes has to itself.
+template <int LEN>
+constexpr int kRuns = LEN == 1 ? 4 : 1;
+
+// Sums over kTileItems sorted places: `lanes` threads take a tile and a strip of its columns, walk the places in order and write
 // a token's sum at its end; what goes on in another tile is left in parts.
 template <typename T, typename G, int LEN>
 __device__ __forceinline__ void sum_tiles(const GradShape& s, unsigned cta, const T* dy, G* dtable, const Sorted& w) {
-    constexpr int BATCH = 8;
+    constexpr int BATCH = 8, U = kRuns<LEN>;
     const long long tile_at = (long long)(cta / s.strips) * (256 / s.lanes) + threadIdx.x / s.lanes;
-    const long long col = ((long long)(cta % s.strips) * s.lanes + threadIdx.x % s.lanes) * LEN;
+    const long long col = ((long long)(cta % s.strips) * s.lanes * U + threadIdx.x % s.lanes) * LEN;
+    const int apart = s.lanes * LEN;
     if (tile_at >= (long long)s.n * w.tiles || col >= s.c) return;
     const int node = (int)(tile_at / w.tiles), tile = (int)(tile_at % w.tiles);
     const long long first = (long long)tile * kTileItems, base = (long long)node * s.rows;
@@ -321,117 +333,188 @@ __device__ __forceinline__ void sum_tiles(const GradShape& s, unsigned cta, cons
     float* part = w.parts + tile_at * 2 * s.c + col;
     uint32_t key = keys[0];
     bool before = first > 0 && keys[-1] == key;  // the run at hand began in an earlier tile
-    float sum[LEN] = {};
+    float sum[U][LEN] = {};
     for (int b = 0; b < len && key < s.vocab; b += BATCH) {
-        Raw<T, LEN> raw[BATCH];
+        Raw<T, LEN> raw[BATCH][U];
         uint32_t next[BATCH];  // key behind each place
 #pragma unroll
         for (int k = 0; k < BATCH; ++k)
             if (b + k < len) {
                 next[k] = first + b + k + 1 < s.rows ? keys[b + k + 1] : 0xffffffffu;
-                raw[k].load(from + (long long)places[b + k] * s.ldy);
+                const T* row = from + (long long)places[b + k] * s.ldy;
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (u == 0 || col + u * apart < s.c) raw[k][u].load(row + u * apart);
             }
 #pragma unroll
         for (int k = 0; k < BATCH; ++k) {
             if (b + k >= len || key >= s.vocab) break;
-            raw[k].add(sum);
+#pragma unroll
+            for (int u = 0; u < U; ++u) raw[k][u].add(sum[u]);
             const bool last = b + k + 1 == len;
             if (next[k] != key || last) {
                 const bool beyond = next[k] == key;
-                if (before)
-                    store_run<float, LEN>(part, sum);
-                else if (beyond)
-                    store_run<float, LEN>(part + s.c, sum);
-                else
-                    put_sum<G, LEN>(to + (long long)key * s.c, sum, s.scale, s.accumulate);
-                before = false;
 #pragma unroll
-                for (int e = 0; e < LEN; ++e) sum[e] = 0.0f;
+                for (int u = 0; u < U; ++u) {
+                    if (u > 0 && col + u * apart >= s.c) break;
+                    if (before)
+                        store_run<float, LEN>(part + u * apart, sum[u]);
+                    else if (beyond)
+                        store_run<float, LEN>(part + s.c + u * apart, sum[u]);
+                    else
+                        put_sum<G, LEN>(to + (long long)key * s.c + u * apart, sum[u], s.scale, s.accumulate);
+#pragma unroll
+                    for (int e = 0; e < LEN; ++e) sum[u][e] = 0.0f;
+                }
+                before = false;
             }
             key = next[k];
         }
     }
 }
 
-// Rows without tokens: a CTA clears those among zero_rows rows of a node's table, in 16-byte chunks wherever they start.
+// Rows without tokens: a CTA clears those among zero_rows rows of a node's table, in 16-byte chunks wherever they start.  It finds
+// them by itself, from the text as it stands, while the tokens are sorted; or, where texts are long beside the table, from the
+// sorted ones.
 template <typename G>
-__device__ __forceinline__ void clear_rows(const GradShape& s, unsigned cta, G* dtable, const Sorted& w) {
+__device__ __forceinline__ void clear_rows(const GradShape& s, unsigned cta, const int64_t* tokens, G* dtable, const Sorted& w) {
     extern __shared__ __align__(16) unsigned char smem[];
     uint32_t* touched = reinterpret_cast<uint32_t*>(smem);  // a bit for each row
     __shared__ int bounds[2];
     const int node = cta / s.zero_ctas;
     const uint32_t v0 = (cta % s.zero_ctas) * (uint32_t)s.zero_rows, count = min((uint32_t)s.zero_rows, s.vocab - v0);
     for (uint32_t k = threadIdx.x; k < (count + 31) / 32; k += 256) touched[k] = 0;
-    const uint32_t* keys = w.keys + (long long)node * s.rows;
-    if (threadIdx.x < 2) bounds[threadIdx.x] = lower_bound(keys, (int)s.rows, threadIdx.x ? v0 + count : v0);
-    __syncthreads();
-    for (int k = bounds[0] + threadIdx.x; k < bounds[1]; k += 256) {
-        const uint32_t v = keys[k] - v0;
-        atomicOr(&touched[v >> 5], 1u << (v & 31));
+    if (s.scan) {
+        __syncthreads();
+        const int64_t* text = tokens + (long long)node * s.rows;
+#pragma unroll 8
+        for (int k = threadIdx.x; k < (int)s.rows; k += 256) {
+            const uint64_t v = (uint64_t)text[k] - v0;
+            if (v < count) atomicOr(&touched[v >> 5], 1u << (v & 31));
+        }
+    } else {
+        pdl_wait();
+        const uint32_t* keys = w.keys + (long long)node * s.rows;
+        if (threadIdx.x < 2) bounds[threadIdx.x] = lower_bound(keys, (int)s.rows, threadIdx.x ? v0 + count : v0);
+        __syncthreads();
+        for (int k = bounds[0] + threadIdx.x; k < bounds[1]; k += 256) {
+            const uint32_t v = keys[k] - v0;
+            atomicOr(&touched[v >> 5], 1u << (v & 31));
+        }
     }
     __syncthreads();
+    auto is_touched = [&](uint32_t r) { return (touched[r >> 5] >> (r & 31)) & 1u; };
     G* table = dtable + node * s.ldgt + (long long)v0 * s.c;
-    const long long row_bytes = s.c * (long long)sizeof(G), bytes = count * row_bytes;
-    const int skew = (int)((uintptr_t)table & 15);  // chunks lie on 16-byte boundaries; the first may begin before the table
+    const long long row_bytes = s.c * (long long)sizeof(G);
+    if (row_bytes >= 512) {  // a warp to a row
+        const int lane = threadIdx.x & 31;
+        for (uint32_t r = threadIdx.x >> 5; r < count; r += 8) {
+            if (is_touched(r)) continue;
+            char* row = reinterpret_cast<char*>(table) + r * row_bytes;
+            char* end = row + row_bytes;
+            char* body = row + (-(uintptr_t)row & 15);
+            char* tail = end - ((uintptr_t)end & 15);
+            if (row + lane * sizeof(G) < body) reinterpret_cast<G*>(row)[lane] = narrow<G>(0.0f);  // at most 7 elements on either side
+            if (tail + lane * sizeof(G) < end) reinterpret_cast<G*>(tail)[lane] = narrow<G>(0.0f);
+#pragma unroll 4
+            for (char* p = body + lane * 16; p < tail; p += 512) *reinterpret_cast<uint4*>(p) = make_uint4(0, 0, 0, 0);
+        }
+        return;
+    }
+    // narrow rows: all of them as one stretch
+    const long long bytes = count * row_bytes;
+    const int skew = (int)((uintptr_t)table & 15);  // the first chunk may begin before the table
     char* chunks = reinterpret_cast<char*>(table) - skew;
-    const long long step = 256 * 16;
-    const long long rows_per_step = step / row_bytes, rest = step % row_bytes;
+    constexpr int kStep = 256 * 16;
+    const int rows_per_step = kStep / (int)row_bytes, rest = kStep % (int)row_bytes;
     long long at = threadIdx.x * 16ll - skew;  // of this thread's chunk within the rows
-    long long row = at < 0 ? -1 : at / row_bytes, in_row = at - row * row_bytes;
-    auto is_touched = [&](long long r) { return (touched[r >> 5] >> (r & 31)) & 1u; };
-    for (; at < bytes; at += step) {
-        if (in_row >= 0 && in_row + 16 <= row_bytes) {
-            if (!is_touched(row)) *reinterpret_cast<uint4*>(chunks + skew + at) = make_uint4(0, 0, 0, 0);
-        } else {
+    int row = at < 0 ? -1 : (int)(at / row_bytes), in_row = (int)(at - row * row_bytes);
+    for (; at < bytes; at += kStep) {
+        if (at >= 0 && at + 16 <= bytes && row_bytes >= 16) {  // one row or two
+            const int left = (int)row_bytes - in_row;  // bytes of the first
+            const uint32_t a = is_touched(row), b = left >= 16 ? a : is_touched(row + 1);
+            if (!(a | b))
+                *reinterpret_cast<uint4*>(chunks + skew + at) = make_uint4(0, 0, 0, 0);
+            else if (a != b)
+                for (int k = a ? left : 0; k < (a ? 16 : left); k += sizeof(G)) table[(at + k) / (long long)sizeof(G)] = narrow<G>(0.0f);
+        } else {  // the ends, and tables a few columns wide
             for (long long b = max(at, 0ll); b < min(at + 16, bytes); b += sizeof(G))
-                if (!is_touched(b / row_bytes)) table[b / sizeof(G)] = narrow<G>(0.0f);
+                if (!is_touched((uint32_t)(b / row_bytes))) table[b / (long long)sizeof(G)] = narrow<G>(0.0f);
         }
         row += rows_per_step;
         in_row += rest;
         if (in_row >= row_bytes) {
             ++row;
-            in_row -= row_bytes;
+            in_row -= (int)row_bytes;
         }
     }
 }
 
+// CTAs [lead, lead + sum_ctas) add, the others clear: the first of them have work until the tokens are sorted.
 template <typename T, typename G, int LEN>
-__global__ void __launch_bounds__(256) embedding_grad_kernel(GradShape s, const T* dy, G* dtable, Sorted w) {
-    pdl_wait();
-    pdl_release();
-    if (blockIdx.x < s.sum_ctas)
-        sum_tiles<T, G, LEN>(s, blockIdx.x, dy, dtable, w);
-    else
-        clear_rows<G>(s, blockIdx.x - s.sum_ctas, dtable, w);
+__global__ void __launch_bounds__(256) embedding_grad_kernel(GradShape s, const int64_t* tokens, const T* dy, G* dtable, Sorted w) {
+    pdl_release();  // the join waits for all of this
+    const unsigned cta = blockIdx.x;
+    if (cta >= s.lead && cta < s.lead + s.sum_ctas) {
+        pdl_wait();
+        sum_tiles<T, G, LEN>(s, cta - s.lead, dy, dtable, w);
+    } else {
+        clear_rows<G>(s, cta < s.lead ? cta : cta - s.sum_ctas, tokens, dtable, w);
+    }
 }
 
 // Tokens that go on beyond their first tile: its part, then those of the tiles that follow.
 template <typename G, int LEN>
 __global__ void __launch_bounds__(256) embedding_grad_join_kernel(GradShape s, G* dtable, Sorted w) {
     const long long tile_at = (long long)(blockIdx.x / s.strips) * (256 / s.lanes) + threadIdx.x / s.lanes;
-    const long long col = ((long long)(blockIdx.x % s.strips) * s.lanes + threadIdx.x % s.lanes) * LEN;
+    constexpr int U = kRuns<LEN>;
+    const long long col = ((long long)(blockIdx.x % s.strips) * s.lanes * U + threadIdx.x % s.lanes) * LEN;
+    const int apart = s.lanes * LEN;
     pdl_wait();
     pdl_release();
     if (tile_at >= (long long)s.n * w.tiles || col >= s.c) return;
-    const int node = (int)(tile_at / w.tiles), tile = (int)(tile_at % w.tiles);
+    const int node = (int)(tile_at / w.tiles);
+    int tile = (int)(tile_at % w.tiles);
     const long long end = (long long)(tile + 1) * kTileItems;
     if (end >= s.rows) return;
     const uint32_t* keys = w.keys + (long long)node * s.rows;
-    const uint32_t key = keys[end - 1];
-    if (key >= s.vocab || keys[end] != key) return;
-    if (end > kTileItems && keys[end - kTileItems - 1] == key) return;  // an earlier tile has its beginning
-    const int last = (int)((end + lower_bound(keys + end, (int)(s.rows - end), key + 1) - 1) / kTileItems);
-    float sum[LEN];
+    const uint32_t key = keys[end - 1], behind = keys[end], ahead = end > kTileItems ? keys[end - kTileItems - 1] : 0xffffffffu;
+    if (key >= s.vocab || behind != key || ahead == key) return;  // the last: an earlier tile has its beginning
     const float* part = w.parts + tile_at * 2 * s.c + col;
-    load_run<float, LEN>(part + s.c, sum);
-#pragma unroll 8
-    for (int k = 1; k <= last - tile; ++k) {
-        float v[LEN];
-        load_run<float, LEN>(part + (long long)k * 2 * s.c, v);
+    float sum[U][LEN];
 #pragma unroll
-        for (int e = 0; e < LEN; ++e) sum[e] += v[e];
+    for (int u = 0; u < U; ++u)
+        if (u == 0 || col + u * apart < s.c) load_run<float, LEN>(part + s.c + u * apart, sum[u]);
+    constexpr int BATCH = 8;
+    for (bool on = true; on;) {  // the parts of the next tiles come with the keys that say whether they count
+        float v[BATCH][U][LEN];
+        uint32_t head[BATCH];
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+            ++tile;
+            part += 2 * s.c;
+            head[k] = 0xffffffffu;
+            if (tile < w.tiles) {
+                head[k] = keys[(long long)tile * kTileItems];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (u == 0 || col + u * apart < s.c) load_run<float, LEN>(part + u * apart, v[k][u]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+            on = on && head[k] == key;
+            if (on)
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int e = 0; e < LEN; ++e) sum[u][e] += v[k][u][e];
+        }
     }
-    put_sum<G, LEN>(dtable + node * s.ldgt + (long long)key * s.c + col, sum, s.scale, s.accumulate);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (u == 0 || col + u * apart < s.c)
+            put_sum<G, LEN>(dtable + node * s.ldgt + (long long)key * s.c + col + u * apart, sum[u], s.scale, s.accumulate);
 }
 
 template <int ITEMS>
@@ -445,7 +528,8 @@ int run_sort(const dlm_embed_args& a, const Sorted& w, cudaStream_t s) {
                                         a.rows, (uint32_t)a.vocab, a.tokens, passes, (bits + passes - 1) / passes, w);
     dlm_count_launch(1);
     if (err == cudaSuccess && w.chunks > 1) {
-        err = launch_overlapped(merge_kernel, dim3((unsigned)((a.rows + 255) / 256), a.n), dim3(256), 0, s, 1, a.rows, w);
+        err = launch_overlapped(merge_kernel, dim3((unsigned)((a.rows * kMergeLanes + 255) / 256), a.n), dim3(256), 0, s,
+                                1, a.rows, w);
         dlm_count_launch(1);
     }
     return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
@@ -462,20 +546,27 @@ int run_backward(const dlm_embed_args& a, const Sorted& w, cudaStream_t s) {
     g.n = a.n;
     g.accumulate = a.accumulate;
     g.scale = a.scale;
-    const int64_t runs = (a.c + LEN - 1) / LEN;
+    const int64_t runs = (a.c + LEN * kRuns<LEN> - 1) / (LEN * kRuns<LEN>);
     g.lanes = 8;
     while (g.lanes < 256 && g.lanes < runs) g.lanes *= 2;
     g.strips = (int)((runs + g.lanes - 1) / g.lanes);
     const int64_t tiles = (int64_t)a.n * w.tiles, sum_ctas = (tiles + 256 / g.lanes - 1) / (256 / g.lanes) * g.strips;
-    // about 256 KB of the gradient to a CTA
-    g.zero_rows = (int)std::min<int64_t>(a.vocab, std::max<int64_t>(1, (256 << 10) / (a.c * (int64_t)sizeof(G))));
+    // 256 KB of the gradient to a CTA, or more: at least four times what it reads of the text (8 bytes a token, out of the L2).  Where
+    // texts are long and that leaves less than two CTAs to an SM, the sorted tokens tell.
+    const int64_t row_bytes = a.c * (int64_t)sizeof(G), sms = device_info().sms;
+    auto share = [&](int64_t bytes) { return (int)std::min<int64_t>(a.vocab, std::max<int64_t>(1, bytes / row_bytes)); };
+    g.zero_rows = share(std::max<int64_t>(256 << 10, 32 * a.rows));
+    g.scan = a.rows > 0 && (a.rows <= 4096 || (a.vocab / g.zero_rows * a.n >= 2 * sms));
+    if (!g.scan) g.zero_rows = share(256 << 10);
+    g.zero_rows = std::min(g.zero_rows, 1 << 17);  // 16 KB of bits
     g.zero_ctas = (int)((a.vocab + g.zero_rows - 1) / g.zero_rows);
     const int64_t zero_ctas = a.accumulate ? 0 : (int64_t)a.n * g.zero_ctas;
     if (sum_ctas + zero_ctas > 0x7fffffff) return DLM_ERR_UNSUPPORTED;
     if (sum_ctas + zero_ctas == 0) return DLM_OK;
     g.sum_ctas = (unsigned)sum_ctas;
+    g.lead = (unsigned)std::min<int64_t>(zero_ctas, g.scan ? 8 * sms : 0);
     cudaError_t err = launch_overlapped(embedding_grad_kernel<T, G, LEN>, dim3((unsigned)(sum_ctas + zero_ctas)), dim3(256),
-                                        (size_t)((g.zero_rows + 31) / 32 * 4), s, 1, g, static_cast<const T*>(a.dy),
+                                        (size_t)((g.zero_rows + 31) / 32 * 4), s, 1, g, a.tokens, static_cast<const T*>(a.dy),
                                         static_cast<G*>(a.dtable), w);
     dlm_count_launch(1);
     if (err == cudaSuccess && w.tiles > 1) {
