@@ -14,16 +14,23 @@
 #include "dlm_launch.h"
 #include "dlm_model.h"
 #include "dlm_rows.cuh"
+#include "dlm_staged_rows.cuh"
 
 namespace {
 
 using namespace dlm;
 
-// LEN consecutive elements: 16 bytes of fp32 or bf16, or one.
+// LEN consecutive elements: one, 8 bytes, or a multiple of 16.
 template <typename T, int LEN>
 __device__ __forceinline__ void load_run(const T* p, float* v) {
     if constexpr (LEN == 1) {
         v[0] = widen(*p);
+    } else if constexpr (LEN * sizeof(T) == 8) {
+        const uint2 a = *reinterpret_cast<const uint2*>(p);
+        float w[kRun<T>];
+        unpack<T>({{a.x, a.y, 0u, 0u}}, w);
+#pragma unroll
+        for (int k = 0; k < LEN; ++k) v[k] = w[k];
     } else {
 #pragma unroll
         for (int k = 0; k < LEN; k += kRun<T>) unpack<T>(ld_words(p + k), v + k);
@@ -33,6 +40,9 @@ template <typename T, int LEN>
 __device__ __forceinline__ void store_run(T* p, const float* v) {
     if constexpr (LEN == 1) {
         *p = narrow<T>(v[0]);
+    } else if constexpr (LEN * sizeof(T) == 8) {
+        static_assert(LEN == 4 && sizeof(T) == 2);
+        *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
     } else {
 #pragma unroll
         for (int k = 0; k < LEN; k += kRun<T>) st_words(p + k, pack<T>(v + k));
@@ -85,12 +95,10 @@ int run_forward(const dlm_embed_args& a, cudaStream_t s) {
     dlm_count_launch(1);
     return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
 }
-bool aligned_rows(const void* p, int64_t ld, size_t esz) { return (uintptr_t)p % 16 == 0 && (ld * (int64_t)esz) % 16 == 0; }
-
 template <typename S, typename T>
 int forward(const dlm_embed_args& a, cudaStream_t s) {
     constexpr int LEN = kCommonRun<S, T>;
-    if (a.c % LEN == 0 && aligned_rows(a.table, a.ldt, sizeof(S)) && aligned_rows(a.y, a.ldy, sizeof(T)))
+    if (a.c % LEN == 0 && rows_aligned(a.table, a.ldt, sizeof(S)) && rows_aligned(a.y, a.ldy, sizeof(T)))
         return run_forward<S, T, LEN>(a, s);
     return run_forward<S, T, 1>(a, s);
 }
@@ -136,8 +144,6 @@ Sorted sorted_layout(int n, int64_t rows, int64_t c, void* workspace) {
     return w;
 }
 
-// Small chunks sort in 9 us where large ones take 39, but every key is looked for in all chunks: they are for texts of up to 32 of them.
-
 // Places of keys below v, among keys[0 .. count).
 __device__ __forceinline__ int lower_bound(const uint32_t* keys, int count, uint32_t v) {
     int lo = 0;
@@ -168,10 +174,22 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(long long rows, uint
     const long long base = (long long)node * rows + (long long)chunk * CH;
     pdl_wait();
     pdl_release();
-    for (int k = threadIdx.x; k < len; k += kSortThreads) {
-        const int64_t t = tokens[base + k];
-        keys[k] = t >= 0 && t < (int64_t)vocab ? (uint32_t)t : vocab;
-        places[k] = (uint16_t)k;
+    constexpr int AHEAD = ITEMS < 8 ? ITEMS : 8;
+    for (int r = 0; r < ITEMS; r += AHEAD) {
+        int64_t t[AHEAD];
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q) {
+            const int k = (r + q) * kSortThreads + threadIdx.x;
+            if (k < len) t[q] = tokens[base + k];
+        }
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q) {
+            const int k = (r + q) * kSortThreads + threadIdx.x;
+            if (k < len) {
+                keys[k] = t[q] >= 0 && t[q] < (int64_t)vocab ? (uint32_t)t[q] : vocab;
+                places[k] = (uint16_t)k;
+            }
+        }
     }
     const int rounds = (len + kSortThreads - 1) / kSortThreads;  // of a warp's lanes over its stretch
     const int first = warp * rounds * 32;
@@ -190,12 +208,19 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(long long rows, uint
         for (int r = 0; r < ITEMS; ++r) {
             if (r >= rounds) break;
             const int at = first + r * 32 + lane;
-            const uint32_t digit = at < len ? (kin[at] >> shift) & mask : 256u + lane;
-            const uint32_t peers = __match_any_sync(0xffffffffu, digit);
+            const bool live = at < len;
+            const uint32_t digit = live ? (kin[at] >> shift) & mask : 0;
+            // lanes with the same digit, a vote for each of its bits (a match instruction takes five times as long)
+            uint32_t peers = __ballot_sync(0xffffffffu, live);
+            for (int q = 0; q < bits; ++q) {
+                const bool set = (digit >> q) & 1;
+                const uint32_t votes = __ballot_sync(0xffffffffu, set);
+                peers &= set ? votes : ~votes;
+            }
             const int before = __popc(peers & ((1u << lane) - 1));
-            const uint32_t old = digit < 256 ? mine[digit] : 0;
+            const uint32_t old = mine[digit];
             __syncwarp();
-            if (before == 0 && digit < 256) mine[digit] = (uint16_t)(old + __popc(peers));
+            if (live && before == 0) mine[digit] = (uint16_t)(old + __popc(peers));
             __syncwarp();
             rank[r] = (uint16_t)(old + before);
         }
@@ -203,11 +228,13 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(long long rows, uint
         // first place of every digit, and within it of every warp
         uint32_t total = 0;
         if (threadIdx.x < 256) {
+            uint16_t v[kSortWarps];
+#pragma unroll
+            for (int k = 0; k < kSortWarps; ++k) v[k] = counts[k * 256 + threadIdx.x];
 #pragma unroll
             for (int k = 0; k < kSortWarps; ++k) {
-                const uint32_t v = counts[k * 256 + threadIdx.x];
                 counts[k * 256 + threadIdx.x] = (uint16_t)total;
-                total += v;
+                total += v[k];
             }
             uint32_t sum = total;
 #pragma unroll
@@ -247,130 +274,145 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(long long rows, uint
 }
 
 // Every key's place among all chunks of its node: its own, and in each other chunk the number of keys before it (equal ones of earlier
-// chunks among them).  Sixteen lanes to a key share the chunks.
-constexpr int kMergeLanes = 16;
+// chunks among them).  A CTA takes 32 neighbouring keys of one chunk, whose searches touch the same lines; its warps share the chunks.
 __global__ void __launch_bounds__(256) merge_kernel(long long rows, Sorted w) {
-    const int node = blockIdx.y, lane = threadIdx.x % kMergeLanes;
-    const long long i = min(rows - 1, ((long long)blockIdx.x * 256 + threadIdx.x) / kMergeLanes), base = (long long)node * rows;
+    __shared__ int counts[8][32];
+    const int node = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long i = min(rows - 1, (long long)blockIdx.x * 32 + lane), base = (long long)node * rows;
     pdl_release();  // the next kernel clears rows meanwhile, and waits where it needs the order
     pdl_wait();
     const uint32_t* keys = w.chunk_keys + base;
     const int own = (int)(i / w.chunk);
     const uint32_t key = keys[i];
     int before = 0;
-    for (int k = lane; k < w.chunks; k += kMergeLanes)
+    for (int k = warp; k < w.chunks; k += 8)
         if (k != own) before += lower_bound(keys + (long long)k * w.chunk, (int)min((long long)w.chunk, rows - (long long)k * w.chunk), key + (k < own));
+    counts[warp][lane] = before;
+    __syncthreads();
+    if (warp > 0 || (long long)blockIdx.x * 32 + lane >= rows) return;
 #pragma unroll
-    for (int o = kMergeLanes / 2; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
-    if (lane != 0) return;
+    for (int k = 1; k < 8; ++k) before += counts[k][lane];
     const long long to = i - (long long)own * w.chunk + before;
     w.keys[base + to] = key;
     w.places[base + to] = w.chunk_places[base + i];
 }
 
 // ------------------------------------------------------------------------------------------------ backward: sums
-// Adds to, or overwrites, a run of the gradient.
-template <typename G, int LEN>
-__device__ __forceinline__ void put_sum(G* to, const float* sum, float scale, int accumulate) {
-    float v[LEN] = {};
-    if (accumulate) load_run<G, LEN>(to, v);
+// Adds to, or overwrites, the runs of a row of the gradient that lie within `columns`, `apart` elements apart.
+template <typename G, int LEN, int U>
+__device__ __forceinline__ void put_sums(G* to, const float (&sum)[U][LEN], float scale, int accumulate, int columns, int apart) {
+    float v[U][LEN] = {};
+    if (accumulate) {
 #pragma unroll
-    for (int e = 0; e < LEN; ++e) v[e] = fmaf(sum[e], scale, v[e]);
-    store_run<G, LEN>(to, v);
+        for (int u = 0; u < U; ++u)
+            if (u * apart < columns) load_run<G, LEN>(to + u * apart, v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int e = 0; e < LEN; ++e) v[u][e] = fmaf(sum[u][e], scale, v[u][e]);
+        if (u * apart < columns) store_run<G, LEN>(to + u * apart, v[u]);
+    }
 }
-
-// A run of one row of dy as it is loaded.
-template <typename T, int LEN>
-struct Raw {
-    Words w[LEN / kRun<T>];
-    __device__ __forceinline__ void load(const T* p) {
-#pragma unroll
-        for (int k = 0; k < LEN / kRun<T>; ++k) w[k] = ld_words(p + k * kRun<T>);
-    }
-    __device__ __forceinline__ void add(float* sum) const {
-        float v[LEN];
-#pragma unroll
-        for (int k = 0; k < LEN / kRun<T>; ++k) unpack<T>(w[k], v + k * kRun<T>);
-#pragma unroll
-        for (int e = 0; e < LEN; ++e) sum[e] += v[e];
-    }
-};
-template <typename T>
-struct Raw<T, 1> {
-    T v;
-    __device__ __forceinline__ void load(const T* p) { v = *p; }
-    __device__ __forceinline__ void add(float* sum) const { sum[0] += widen(v); }
-};
 
 struct GradShape {
     long long rows, c, ldy, ldgt;
     uint32_t vocab;
-    int n, accumulate, lanes, strips, zero_rows, zero_ctas;  // zero_ctas: a node's
+    int n, accumulate, strips, zero_rows, zero_ctas;  // zero_ctas: a node's
     float scale;
     int scan;  // rows without tokens are found in the text
     unsigned lead, sum_ctas;
 };
 
-// Runs of columns of a thread, `lanes` runs apart: four single elements share the work of a place that one run of 16 bytes has to itself.
-template <int LEN>
-constexpr int kRuns = LEN == 1 ? 4 : 1;
+// A warp's strip of a row: kStripBytes of dy.  Where rows are aligned a lane has kRun<T> columns of every 512 bytes, else single columns 32
+// apart.
+constexpr int kStripBytes = 1024, kSlots = 8, kSlotBytes = kStripBytes + 16;
+template <typename T>
+constexpr int kStrip = kStripBytes / (int)sizeof(T);
+template <typename T, int LEN>
+constexpr int kRuns = kStrip<T> / (32 * LEN);
 
-// Sums over kTileItems sorted places: `lanes` threads take a tile and a strip of its columns, walk the places in order and write
-// a token's sum at its end; what goes on in another tile is left in parts.
+// Sums over kTileItems sorted places: a warp takes a tile and a strip of its columns, walks the places in order and writes a token's sum at
+// its end; what goes on in another tile is left in parts.  Rows of dy are on their way into the warp's slots kSlots - 1 places ahead: 8 KB
+// a warp, which hold no registers.
 template <typename T, typename G, int LEN>
 __device__ __forceinline__ void sum_tiles(const GradShape& s, unsigned cta, const T* dy, G* dtable, const Sorted& w) {
-    constexpr int BATCH = 8, U = kRuns<LEN>;
-    const long long tile_at = (long long)(cta / s.strips) * (256 / s.lanes) + threadIdx.x / s.lanes;
-    const long long col = ((long long)(cta % s.strips) * s.lanes * U + threadIdx.x % s.lanes) * LEN;
-    const int apart = s.lanes * LEN;
-    if (tile_at >= (long long)s.n * w.tiles || col >= s.c) return;
+    constexpr int U = kRuns<T, LEN>;
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int lane = threadIdx.x & 31;
+    const long long task = (long long)cta * 8 + (threadIdx.x >> 5), tile_at = task / s.strips;
+    if (tile_at >= (long long)s.n * w.tiles) return;
+    const long long col0 = task % s.strips * kStrip<T>;
+    const int columns = (int)min((long long)kStrip<T>, s.c - col0);
     const int node = (int)(tile_at / w.tiles), tile = (int)(tile_at % w.tiles);
     const long long first = (long long)tile * kTileItems, base = (long long)node * s.rows;
-    const uint32_t *keys = w.keys + base + first, *places = w.places + base + first;
     const int len = (int)min((long long)kTileItems, s.rows - first);
-    const T* from = dy + base * s.ldy + col;
-    G* to = dtable + node * s.ldgt + col;
-    float* part = w.parts + tile_at * 2 * s.c + col;
-    uint32_t key = keys[0];
-    bool before = first > 0 && keys[-1] == key;  // the run at hand began in an earlier tile
-    float sum[U][LEN] = {};
-    for (int b = 0; b < len && key < s.vocab; b += BATCH) {
-        Raw<T, LEN> raw[BATCH][U];
-        uint32_t next[BATCH];  // key behind each place
-#pragma unroll
-        for (int k = 0; k < BATCH; ++k)
-            if (b + k < len) {
-                next[k] = first + b + k + 1 < s.rows ? keys[b + k + 1] : 0xffffffffu;
-                const T* row = from + (long long)places[b + k] * s.ldy;
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (u == 0 || col + u * apart < s.c) raw[k][u].load(row + u * apart);
-            }
-#pragma unroll
-        for (int k = 0; k < BATCH; ++k) {
-            if (b + k >= len || key >= s.vocab) break;
-#pragma unroll
-            for (int u = 0; u < U; ++u) raw[k][u].add(sum[u]);
-            const bool last = b + k + 1 == len;
-            if (next[k] != key || last) {
-                const bool beyond = next[k] == key;
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    if (u > 0 && col + u * apart >= s.c) break;
-                    if (before)
-                        store_run<float, LEN>(part + u * apart, sum[u]);
-                    else if (beyond)
-                        store_run<float, LEN>(part + s.c + u * apart, sum[u]);
-                    else
-                        put_sum<G, LEN>(to + (long long)key * s.c + u * apart, sum[u], s.scale, s.accumulate);
-#pragma unroll
-                    for (int e = 0; e < LEN; ++e) sum[u][e] = 0.0f;
-                }
-                before = false;
-            }
-            key = next[k];
-        }
+    unsigned char* slots = smem + (threadIdx.x >> 5) * kSlots * kSlotBytes;
+    // a lane's place and the key there; the keys on both sides of the tile
+    uint32_t key = 0xffffffffu, place = 0;
+    if (lane < len) {
+        key = w.keys[base + first + lane];
+        place = w.places[base + first + lane];
     }
+    const uint32_t ahead = first > 0 ? w.keys[base + first - 1] : 0xffffffffu, behind = first + len < s.rows ? w.keys[base + first + len] : 0xffffffffu;
+    const int known = __popc(__ballot_sync(0xffffffffu, key < s.vocab));  // tokens that stand for none come last
+    const T* from = dy + base * s.ldy + col0;
+    G* to = dtable + node * s.ldgt + col0 + lane * LEN;
+    float* part = w.parts + tile_at * 2 * s.c + col0 + lane * LEN;
+    bool before = __shfl_sync(0xffffffffu, key, 0) == ahead;  // the run at hand began in an earlier tile
+    float sum[U][LEN] = {};
+    const int mine = columns - lane * LEN;  // the lane's runs begin before this
+    const bool whole_strip = columns == kStrip<T>;
+    const uint32_t low = (uint32_t)(uintptr_t)from, pitch = (uint32_t)(s.ldy * (long long)sizeof(T));  // for a row's place within 16 bytes
+    const uint32_t slots_at = smem_u32(slots) + lane * 16;
+    auto ask = [&](int i) {
+        if (i < known) {
+            const uint32_t at = __shfl_sync(0xffffffffu, place, i);
+            const T* row = from + (long long)at * s.ldy;
+            if (LEN > 1 || !whole_strip || (uintptr_t)row < (uintptr_t)dy + 16) {
+                fetch_row<T, LEN, 32>(slots + i % kSlots * kSlotBytes, row, dy, columns, lane);
+            } else {  // 64 chunks, and the first bytes of another one where the row does not start on a chunk
+                const uint32_t skew = (low + at * pitch) & 15, to_slot = slots_at + i % kSlots * kSlotBytes;
+                const char* chunks = reinterpret_cast<const char*>(row) - skew + lane * 16;
+                copy_chunk(to_slot, chunks, 16);
+                copy_chunk(to_slot + 512, chunks + 512, 16);
+                if (lane == 0 && skew > 0) copy_chunk(to_slot + 1024, chunks + 1024, (int)skew);
+            }
+        }
+        commit_copies();
+    };
+    for (int i = 0; i < kSlots - 1; ++i) ask(i);
+    for (int i = 0; i < known; ++i) {
+        ask(i + kSlots - 1);
+        wait_copies<kSlots - 1>();
+        const unsigned char* slot = slots + i % kSlots * kSlotBytes;
+        if constexpr (LEN == 1) {
+            __syncwarp();
+            slot += (low + __shfl_sync(0xffffffffu, place, i) * pitch) & 15;
+        }
+        const T* row = reinterpret_cast<const T*>(slot) + lane * LEN;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {  // whatever the slot holds beyond the strip's columns: those sums go nowhere
+            float v[LEN];
+            load_run<T, LEN>(row + u * 32 * LEN, v);
+#pragma unroll
+            for (int e = 0; e < LEN; ++e) sum[u][e] += v[e];
+        }
+        const uint32_t here = __shfl_sync(0xffffffffu, key, i), next = i + 1 < len ? __shfl_sync(0xffffffffu, key, i + 1) : behind;
+        if (next != here || i + 1 == len) {
+            if (before || next == here)
+                put_sums<float, LEN, U>(before ? part : part + s.c, sum, 1.0f, 0, mine, 32 * LEN);
+            else
+                put_sums<G, LEN, U>(to + (long long)here * s.c, sum, s.scale, s.accumulate, mine, 32 * LEN);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int e = 0; e < LEN; ++e) sum[u][e] = 0.0f;
+            before = false;
+        }
+        __syncwarp();  // the slot may be filled again
+    }
+    wait_copies<0>();
 }
 
 // Rows without tokens: a CTA clears those among zero_rows rows of a node's table, in 16-byte chunks wherever they start.  It finds
@@ -403,49 +445,31 @@ __device__ __forceinline__ void clear_rows(const GradShape& s, unsigned cta, con
         }
     }
     __syncthreads();
-    auto is_touched = [&](uint32_t r) { return (touched[r >> 5] >> (r & 31)) & 1u; };
-    G* table = dtable + node * s.ldgt + (long long)v0 * s.c;
-    const long long row_bytes = s.c * (long long)sizeof(G);
-    if (row_bytes >= 512) {  // a warp to a row
-        const int lane = threadIdx.x & 31;
-        for (uint32_t r = threadIdx.x >> 5; r < count; r += 8) {
-            if (is_touched(r)) continue;
-            char* row = reinterpret_cast<char*>(table) + r * row_bytes;
-            char* end = row + row_bytes;
-            char* body = row + (-(uintptr_t)row & 15);
+    // a warp takes up to 32 rows, about 32 KB, and clears the stretches between touched ones
+    const int lane = threadIdx.x & 31;
+    const long long line = s.c * (long long)sizeof(G);
+    char* table = reinterpret_cast<char*>(dtable + node * s.ldgt + (long long)v0 * s.c);
+    const uint32_t group = line >= (16 << 10) ? 1 : line >= (4 << 10) ? 4 : 32;
+    for (uint32_t r0 = (threadIdx.x >> 5) * group; r0 < count; r0 += 8 * group) {
+        const uint32_t rows = min(group, count - r0);
+        uint32_t left = ~(touched[r0 >> 5] >> (r0 & 31)) & (0xffffffffu >> (32 - rows));  // rows to clear
+        while (left) {
+            const int from = __ffs(left) - 1;
+            const uint32_t run = ~(left >> from);  // its lowest bit: where the stretch ends
+            const int length = run ? __ffs(run) - 1 : 32;
+            left &= length + from >= 32 ? 0u : ~0u << (from + length);
+            char* begin = table + (r0 + from) * line;
+            char* end = begin + length * line;
+            char* body = begin + (-(uintptr_t)begin & 15);
             char* tail = end - ((uintptr_t)end & 15);
-            if (row + lane * sizeof(G) < body) reinterpret_cast<G*>(row)[lane] = narrow<G>(0.0f);  // at most 7 elements on either side
+            if (body >= tail) {  // a few elements
+                for (char* p = begin + lane * sizeof(G); p < end; p += 32 * sizeof(G)) *reinterpret_cast<G*>(p) = narrow<G>(0.0f);
+                continue;
+            }
+            if (begin + lane * sizeof(G) < body) reinterpret_cast<G*>(begin)[lane] = narrow<G>(0.0f);  // at most 7 elements on either side
             if (tail + lane * sizeof(G) < end) reinterpret_cast<G*>(tail)[lane] = narrow<G>(0.0f);
-#pragma unroll 4
+#pragma unroll 8
             for (char* p = body + lane * 16; p < tail; p += 512) *reinterpret_cast<uint4*>(p) = make_uint4(0, 0, 0, 0);
-        }
-        return;
-    }
-    // narrow rows: all of them as one stretch
-    const long long bytes = count * row_bytes;
-    const int skew = (int)((uintptr_t)table & 15);  // the first chunk may begin before the table
-    char* chunks = reinterpret_cast<char*>(table) - skew;
-    constexpr int kStep = 256 * 16;
-    const int rows_per_step = kStep / (int)row_bytes, rest = kStep % (int)row_bytes;
-    long long at = threadIdx.x * 16ll - skew;  // of this thread's chunk within the rows
-    int row = at < 0 ? -1 : (int)(at / row_bytes), in_row = (int)(at - row * row_bytes);
-    for (; at < bytes; at += kStep) {
-        if (at >= 0 && at + 16 <= bytes && row_bytes >= 16) {  // one row or two
-            const int left = (int)row_bytes - in_row;  // bytes of the first
-            const uint32_t a = is_touched(row), b = left >= 16 ? a : is_touched(row + 1);
-            if (!(a | b))
-                *reinterpret_cast<uint4*>(chunks + skew + at) = make_uint4(0, 0, 0, 0);
-            else if (a != b)
-                for (int k = a ? left : 0; k < (a ? 16 : left); k += sizeof(G)) table[(at + k) / (long long)sizeof(G)] = narrow<G>(0.0f);
-        } else {  // the ends, and tables a few columns wide
-            for (long long b = max(at, 0ll); b < min(at + 16, bytes); b += sizeof(G))
-                if (!is_touched((uint32_t)(b / row_bytes))) table[b / (long long)sizeof(G)] = narrow<G>(0.0f);
-        }
-        row += rows_per_step;
-        in_row += rest;
-        if (in_row >= row_bytes) {
-            ++row;
-            in_row -= (int)row_bytes;
         }
     }
 }
@@ -463,13 +487,12 @@ __global__ void __launch_bounds__(256) embedding_grad_kernel(GradShape s, const 
     }
 }
 
-// Tokens that go on beyond their first tile: its part, then those of the tiles that follow.
+// Tokens that go on beyond their first tile: its part, then those of the tiles that follow.  A warp to a tile and a strip of 32 LEN columns.
 template <typename G, int LEN>
 __global__ void __launch_bounds__(256) embedding_grad_join_kernel(GradShape s, G* dtable, Sorted w) {
-    const long long tile_at = (long long)(blockIdx.x / s.strips) * (256 / s.lanes) + threadIdx.x / s.lanes;
-    constexpr int U = kRuns<LEN>;
-    const long long col = ((long long)(blockIdx.x % s.strips) * s.lanes * U + threadIdx.x % s.lanes) * LEN;
-    const int apart = s.lanes * LEN;
+    const int strips = (int)((s.c + 32 * LEN - 1) / (32 * LEN));
+    const long long task = (long long)blockIdx.x * 8 + (threadIdx.x >> 5), tile_at = task / strips;
+    const long long col = (task % strips * 32 + (threadIdx.x & 31)) * LEN;
     pdl_wait();
     pdl_release();
     if (tile_at >= (long long)s.n * w.tiles || col >= s.c) return;
@@ -481,13 +504,11 @@ __global__ void __launch_bounds__(256) embedding_grad_join_kernel(GradShape s, G
     const uint32_t key = keys[end - 1], behind = keys[end], ahead = end > kTileItems ? keys[end - kTileItems - 1] : 0xffffffffu;
     if (key >= s.vocab || behind != key || ahead == key) return;  // the last: an earlier tile has its beginning
     const float* part = w.parts + tile_at * 2 * s.c + col;
-    float sum[U][LEN];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-        if (u == 0 || col + u * apart < s.c) load_run<float, LEN>(part + s.c + u * apart, sum[u]);
-    constexpr int BATCH = 8;
+    float sum[1][LEN];
+    load_run<float, LEN>(part + s.c, sum[0]);
+    constexpr int BATCH = 16;
     for (bool on = true; on;) {  // the parts of the next tiles come with the keys that say whether they count
-        float v[BATCH][U][LEN];
+        float v[BATCH][LEN];
         uint32_t head[BATCH];
 #pragma unroll
         for (int k = 0; k < BATCH; ++k) {
@@ -496,9 +517,7 @@ __global__ void __launch_bounds__(256) embedding_grad_join_kernel(GradShape s, G
             head[k] = 0xffffffffu;
             if (tile < w.tiles) {
                 head[k] = keys[(long long)tile * kTileItems];
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (u == 0 || col + u * apart < s.c) load_run<float, LEN>(part + u * apart, v[k][u]);
+                load_run<float, LEN>(part, v[k]);
             }
         }
 #pragma unroll
@@ -506,15 +525,10 @@ __global__ void __launch_bounds__(256) embedding_grad_join_kernel(GradShape s, G
             on = on && head[k] == key;
             if (on)
 #pragma unroll
-                for (int u = 0; u < U; ++u)
-#pragma unroll
-                    for (int e = 0; e < LEN; ++e) sum[u][e] += v[k][u][e];
+                for (int e = 0; e < LEN; ++e) sum[0][e] += v[k][e];
         }
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-        if (u == 0 || col + u * apart < s.c)
-            put_sum<G, LEN>(dtable + node * s.ldgt + (long long)key * s.c + col + u * apart, sum[u], s.scale, s.accumulate);
+    put_sums<G, LEN, 1>(dtable + node * s.ldgt + (long long)key * s.c + col, sum, s.scale, s.accumulate, 1, 0);
 }
 
 template <int ITEMS>
@@ -528,8 +542,7 @@ int run_sort(const dlm_embed_args& a, const Sorted& w, cudaStream_t s) {
                                         a.rows, (uint32_t)a.vocab, a.tokens, passes, (bits + passes - 1) / passes, w);
     dlm_count_launch(1);
     if (err == cudaSuccess && w.chunks > 1) {
-        err = launch_overlapped(merge_kernel, dim3((unsigned)((a.rows * kMergeLanes + 255) / 256), a.n), dim3(256), 0, s,
-                                1, a.rows, w);
+        err = launch_overlapped(merge_kernel, dim3((unsigned)((a.rows + 31) / 32), a.n), dim3(256), 0, s, 1, a.rows, w);
         dlm_count_launch(1);
     }
     return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
@@ -546,18 +559,17 @@ int run_backward(const dlm_embed_args& a, const Sorted& w, cudaStream_t s) {
     g.n = a.n;
     g.accumulate = a.accumulate;
     g.scale = a.scale;
-    const int64_t runs = (a.c + LEN * kRuns<LEN> - 1) / (LEN * kRuns<LEN>);
-    g.lanes = 8;
-    while (g.lanes < 256 && g.lanes < runs) g.lanes *= 2;
-    g.strips = (int)((runs + g.lanes - 1) / g.lanes);
-    const int64_t tiles = (int64_t)a.n * w.tiles, sum_ctas = (tiles + 256 / g.lanes - 1) / (256 / g.lanes) * g.strips;
+    g.strips = (int)((a.c + kStrip<T> - 1) / kStrip<T>);
+    const int64_t tiles = (int64_t)a.n * w.tiles, sum_ctas = (tiles * g.strips + 7) / 8;
     // 256 KB of the gradient to a CTA, or more: at least four times what it reads of the text (8 bytes a token, out of the L2).  Where
     // texts are long and that leaves less than two CTAs to an SM, the sorted tokens tell.
-    const int64_t row_bytes = a.c * (int64_t)sizeof(G), sms = device_info().sms;
-    auto share = [&](int64_t bytes) { return (int)std::min<int64_t>(a.vocab, std::max<int64_t>(1, bytes / row_bytes)); };
-    g.zero_rows = share(std::max<int64_t>(256 << 10, 32 * a.rows));
+    const int64_t line = a.c * (int64_t)sizeof(G), sms = device_info().sms;
+    // (small tables: four CTAs to an SM, but no less than 8 KB)
+    const int64_t grain = std::min<int64_t>(256 << 10, std::max<int64_t>(8 << 10, a.n * a.vocab * line / (4 * sms)));
+    auto share = [&](int64_t bytes) { return (int)std::min<int64_t>(a.vocab, std::max<int64_t>(1, bytes / line)); };
+    g.zero_rows = share(std::max<int64_t>(grain, 32 * a.rows));
     g.scan = a.rows > 0 && (a.rows <= 4096 || (a.vocab / g.zero_rows * a.n >= 2 * sms));
-    if (!g.scan) g.zero_rows = share(256 << 10);
+    if (!g.scan) g.zero_rows = share(grain);
     g.zero_rows = std::min(g.zero_rows, 1 << 17);  // 16 KB of bits
     g.zero_ctas = (int)((a.vocab + g.zero_rows - 1) / g.zero_rows);
     const int64_t zero_ctas = a.accumulate ? 0 : (int64_t)a.n * g.zero_ctas;
@@ -565,12 +577,18 @@ int run_backward(const dlm_embed_args& a, const Sorted& w, cudaStream_t s) {
     if (sum_ctas + zero_ctas == 0) return DLM_OK;
     g.sum_ctas = (unsigned)sum_ctas;
     g.lead = (unsigned)std::min<int64_t>(zero_ctas, g.scan ? 8 * sms : 0);
-    cudaError_t err = launch_overlapped(embedding_grad_kernel<T, G, LEN>, dim3((unsigned)(sum_ctas + zero_ctas)), dim3(256),
-                                        (size_t)((g.zero_rows + 31) / 32 * 4), s, 1, g, a.tokens, static_cast<const T*>(a.dy),
-                                        static_cast<G*>(a.dtable), w);
+    const size_t smem = std::max<size_t>(sum_ctas > 0 ? 8 * kSlots * kSlotBytes : 0, (g.zero_rows + 31) / 32 * 4);
+    auto kern = embedding_grad_kernel<T, G, LEN>;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 8 * kSlots * kSlotBytes) != cudaSuccess)
+        return DLM_ERR_CUDA;
+    cudaError_t err = launch_overlapped(kern, dim3((unsigned)(sum_ctas + zero_ctas)), dim3(256), smem, s, 1, g, a.tokens,
+                                        static_cast<const T*>(a.dy), static_cast<G*>(a.dtable), w);
     dlm_count_launch(1);
     if (err == cudaSuccess && w.tiles > 1) {
-        err = launch_overlapped(embedding_grad_join_kernel<G, LEN>, dim3((unsigned)sum_ctas), dim3(256), 0, s, 1, g,
+        constexpr int RUN = LEN == 1 ? 1 : 4;
+        const int64_t ctas = (tiles * ((a.c + 32 * RUN - 1) / (32 * RUN)) + 7) / 8;
+        if (ctas > 0x7fffffff) return DLM_ERR_UNSUPPORTED;
+        err = launch_overlapped(embedding_grad_join_kernel<G, RUN>, dim3((unsigned)ctas), dim3(256), 0, s, 1, g,
                                 static_cast<G*>(a.dtable), w);
         dlm_count_launch(1);
     }
@@ -585,8 +603,8 @@ int backward(const dlm_embed_args& a, cudaStream_t s) {
         const int rc = w.chunk == kChunk<kSmallItems> ? run_sort<kSmallItems>(a, w, s) : run_sort<kLargeItems>(a, w, s);
         if (rc != DLM_OK) return rc;
     }
-    constexpr int LEN = kCommonRun<T, G>;
-    if (a.c % LEN == 0 && (a.rows == 0 || aligned_rows(a.dy, a.ldy, sizeof(T))) && aligned_rows(a.dtable, a.ldgt, sizeof(G)))
+    constexpr int LEN = kRun<T>;
+    if (a.c % LEN == 0 && (a.rows == 0 || rows_aligned(a.dy, a.ldy, sizeof(T))) && rows_aligned(a.dtable, a.ldgt, sizeof(G)))
         return run_backward<T, G, LEN>(a, w, s);
     return run_backward<T, G, 1>(a, w, s);
 }
