@@ -326,93 +326,194 @@ struct GradShape {
 
 // A warp's strip of a row: kStripBytes of dy.  Where rows are aligned a lane has kRun<T> columns of every 512 bytes, else single columns 32
 // apart.
-constexpr int kStripBytes = 1024, kSlots = 8, kSlotBytes = kStripBytes + 16;
+constexpr int kStripBytes = 1024, kAtOnce = 4, kSlots = 2 * kAtOnce, kSlotBytes = kStripBytes + 16;
 template <typename T>
 constexpr int kStrip = kStripBytes / (int)sizeof(T);
 template <typename T, int LEN>
 constexpr int kRuns = kStrip<T> / (32 * LEN);
 
-// Sums over kTileItems sorted places: a warp takes a tile and a strip of its columns, walks the places in order and writes a token's sum at
-// its end; what goes on in another tile is left in parts.  Rows of dy are on their way into the warp's slots kSlots - 1 places ahead: 8 KB
-// a warp, which hold no registers.
+// Sums over a tile of sorted places, of which lane i of a warp has the i-th and its key: the warp takes a strip of its columns, walks the places
+// in order and writes a token's sum at its end; what goes on in another tile (`ahead`, `behind`: the keys there) is left in part[0 ..] and
+// part[gap ..].  Rows of dy come into the warp's slots by asynchronous copies, four while the four before them are added: 4 to 8 KB on their way for each
+// warp, which hold no registers.
+// from, to: the node's gradients and table at the strip's first column.
+template <typename T, typename G, int LEN>
+__device__ __forceinline__ void walk_tile(const GradShape& s, const T* dy, const T* from, G* to, int columns, uint32_t key, uint32_t place,
+                                          int len, uint32_t ahead, uint32_t behind, unsigned char* slots, float* part, long long gap) {
+    constexpr int U = kRuns<T, LEN>;
+    const int lane = threadIdx.x & 31;
+    const int known = __popc(__ballot_sync(0xffffffffu, key < s.vocab));  // tokens that stand for none come last
+    to += lane * LEN;
+    part += lane * LEN;
+    // bit i: the i-th place is the last of its run here
+    const uint32_t next = __shfl_down_sync(0xffffffffu, key, 1);
+    const uint32_t ends = __ballot_sync(0xffffffffu, lane < known && (lane + 1 == len || next != key));
+    const bool goes_on = known == len && len > 0 && __shfl_sync(0xffffffffu, key, (len - 1) & 31) == behind;
+    bool before = __shfl_sync(0xffffffffu, key, 0) == ahead;  // the run at hand began in an earlier tile
+    float sum[U][LEN] = {};
+    const int mine = columns - lane * LEN;  // the lane's runs begin before this
+    const bool whole_strip = columns == kStrip<T>;
+    // where a lane's place starts within 16 bytes
+    const uint32_t skews = ((uint32_t)(uintptr_t)from + place * (uint32_t)(s.ldy * (long long)sizeof(T))) & 15;
+    auto ask = [&](int i) {
+        if (i >= known) return;
+        const T* row = from + (long long)__shfl_sync(0xffffffffu, place, i) * s.ldy;
+        unsigned char* slot = slots + i % kSlots * kSlotBytes;
+        if (LEN > 1 || !whole_strip || (uintptr_t)row < (uintptr_t)dy + 16) {
+            fetch_row<T, LEN, 32>(slot, row, dy, columns, lane);
+        } else {  // 64 chunks, and the first bytes of another one where the row does not start on a chunk
+            const int skew = (int)__shfl_sync(0xffffffffu, skews, i);
+            const uint32_t to_slot = smem_u32(slot) + lane * 16;
+            const char* chunks = reinterpret_cast<const char*>(row) - skew + lane * 16;
+            copy_chunk(to_slot, chunks, 16);
+            copy_chunk(to_slot + 512, chunks + 512, 16);
+            if (lane == 0 && skew > 0) copy_chunk(to_slot + 1024, chunks + 1024, skew);
+        }
+    };
+    for (int q = 0; q < kAtOnce; ++q) ask(q);
+    commit_copies();
+    for (int i = 0; i < known; i += kAtOnce) {
+        for (int q = 0; q < kAtOnce; ++q) ask(i + kAtOnce + q);
+        commit_copies();
+        wait_copies<1>();
+        __syncwarp();
+        constexpr int HOLD = LEN > 1 ? kAtOnce : 2;  // places whose elements are in registers at once
+#pragma unroll
+        for (int h = 0; h < kAtOnce; h += HOLD) {
+            // whatever the slots hold beyond the strip's columns or the last place: those sums go nowhere
+            constexpr int W = LEN > 1 ? 4 : 1;
+            uint32_t raw[HOLD][U][W];
+#pragma unroll
+            for (int q = 0; q < HOLD; ++q) {
+                const int at = i + h + q;
+                const unsigned char* slot = slots + at % kSlots * kSlotBytes;
+                if constexpr (LEN == 1) slot += __shfl_sync(0xffffffffu, skews, at & 31);
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const unsigned char* p = slot + (u * 32 + lane) * LEN * sizeof(T);
+                    if constexpr (LEN > 1) {
+                        const Words a = ld_words(p);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) raw[q][u][k] = a.w[k];
+                    } else if constexpr (sizeof(T) == 2) {
+                        raw[q][u][0] = (uint32_t)*reinterpret_cast<const uint16_t*>(p) << 16;
+                    } else {
+                        raw[q][u][0] = *reinterpret_cast<const uint32_t*>(p);
+                    }
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < HOLD; ++q) {
+                const int at = i + h + q;
+                if (at >= known) break;
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    float v[LEN];
+                    if constexpr (LEN > 1)
+                        unpack<T>({{raw[q][u][0], raw[q][u][1], raw[q][u][2], raw[q][u][3]}}, v);
+                    else
+                        v[0] = __uint_as_float(raw[q][u][0]);
+#pragma unroll
+                    for (int e = 0; e < LEN; ++e) sum[u][e] += v[e];
+                }
+                if ((ends >> at) & 1) {
+                    const bool beyond = goes_on && at + 1 == len;
+                    if (before || beyond)
+                        put_sums<float, LEN, U>(before ? part : part + gap, sum, 1.0f, 0, mine, 32 * LEN);
+                    else
+                        put_sums<G, LEN, U>(to + (long long)__shfl_sync(0xffffffffu, key, at) * s.c, sum, s.scale, s.accumulate, mine, 32 * LEN);
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+#pragma unroll
+                        for (int e = 0; e < LEN; ++e) sum[u][e] = 0.0f;
+                    before = false;
+                }
+            }
+        }
+        __syncwarp();  // the slots may be filled again
+    }
+    wait_copies<0>();
+}
+
 template <typename T, typename G, int LEN>
 __device__ __forceinline__ void sum_tiles(const GradShape& s, unsigned cta, const T* dy, G* dtable, const Sorted& w) {
-    constexpr int U = kRuns<T, LEN>;
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 31;
     const long long task = (long long)cta * 8 + (threadIdx.x >> 5), tile_at = task / s.strips;
     if (tile_at >= (long long)s.n * w.tiles) return;
     const long long col0 = task % s.strips * kStrip<T>;
-    const int columns = (int)min((long long)kStrip<T>, s.c - col0);
     const int node = (int)(tile_at / w.tiles), tile = (int)(tile_at % w.tiles);
     const long long first = (long long)tile * kTileItems, base = (long long)node * s.rows;
     const int len = (int)min((long long)kTileItems, s.rows - first);
-    unsigned char* slots = smem + (threadIdx.x >> 5) * kSlots * kSlotBytes;
-    // a lane's place and the key there; the keys on both sides of the tile
     uint32_t key = 0xffffffffu, place = 0;
     if (lane < len) {
         key = w.keys[base + first + lane];
         place = w.places[base + first + lane];
     }
     const uint32_t ahead = first > 0 ? w.keys[base + first - 1] : 0xffffffffu, behind = first + len < s.rows ? w.keys[base + first + len] : 0xffffffffu;
-    const int known = __popc(__ballot_sync(0xffffffffu, key < s.vocab));  // tokens that stand for none come last
-    const T* from = dy + base * s.ldy + col0;
-    G* to = dtable + node * s.ldgt + col0 + lane * LEN;
-    float* part = w.parts + tile_at * 2 * s.c + col0 + lane * LEN;
-    bool before = __shfl_sync(0xffffffffu, key, 0) == ahead;  // the run at hand began in an earlier tile
-    float sum[U][LEN] = {};
-    const int mine = columns - lane * LEN;  // the lane's runs begin before this
-    const bool whole_strip = columns == kStrip<T>;
-    const uint32_t low = (uint32_t)(uintptr_t)from, pitch = (uint32_t)(s.ldy * (long long)sizeof(T));  // for a row's place within 16 bytes
-    const uint32_t slots_at = smem_u32(slots) + lane * 16;
-    auto ask = [&](int i) {
-        if (i < known) {
-            const uint32_t at = __shfl_sync(0xffffffffu, place, i);
-            const T* row = from + (long long)at * s.ldy;
-            if (LEN > 1 || !whole_strip || (uintptr_t)row < (uintptr_t)dy + 16) {
-                fetch_row<T, LEN, 32>(slots + i % kSlots * kSlotBytes, row, dy, columns, lane);
-            } else {  // 64 chunks, and the first bytes of another one where the row does not start on a chunk
-                const uint32_t skew = (low + at * pitch) & 15, to_slot = slots_at + i % kSlots * kSlotBytes;
-                const char* chunks = reinterpret_cast<const char*>(row) - skew + lane * 16;
-                copy_chunk(to_slot, chunks, 16);
-                copy_chunk(to_slot + 512, chunks + 512, 16);
-                if (lane == 0 && skew > 0) copy_chunk(to_slot + 1024, chunks + 1024, (int)skew);
-            }
-        }
-        commit_copies();
-    };
-    for (int i = 0; i < kSlots - 1; ++i) ask(i);
-    for (int i = 0; i < known; ++i) {
-        ask(i + kSlots - 1);
-        wait_copies<kSlots - 1>();
-        const unsigned char* slot = slots + i % kSlots * kSlotBytes;
-        if constexpr (LEN == 1) {
-            __syncwarp();
-            slot += (low + __shfl_sync(0xffffffffu, place, i) * pitch) & 15;
-        }
-        const T* row = reinterpret_cast<const T*>(slot) + lane * LEN;
+    walk_tile<T, G, LEN>(s, dy, dy + base * s.ldy + col0, dtable + node * s.ldgt + col0, (int)min((long long)kStrip<T>, s.c - col0), key, place,
+                         len, ahead, behind, smem + (threadIdx.x >> 5) * kSlots * kSlotBytes, w.parts + tile_at * 2 * s.c + col0, s.c);
+}
+
+// Short texts: a CTA sorts a node's tokens by itself (each counts those before it), its warps walk their tiles of a strip, and what goes
+// on between tiles is joined in shared memory.
+constexpr int kShortText = 256;
+template <typename T, typename G, int LEN>
+__device__ __forceinline__ void sum_short_text(const GradShape& s, unsigned cta, const int64_t* tokens, const T* dy, G* dtable) {
+    constexpr int U = kRuns<T, LEN>;
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ __align__(16) uint32_t text[kShortText], keys[kShortText + 1];
+    __shared__ uint32_t places[kShortText];
+    float* parts = reinterpret_cast<float*>(smem + 8 * kSlots * kSlotBytes);  // [8 tiles][2][strip]
+    const int lane = threadIdx.x & 31, tile = threadIdx.x >> 5;
+    const int node = cta / s.strips, rows = (int)s.rows;
+    const long long col0 = (long long)(cta % s.strips) * kStrip<T>;
+    uint32_t key = 0xffffffffu;  // behind the text's end
+    if ((int)threadIdx.x < rows) {
+        const int64_t token = tokens[(long long)node * rows + threadIdx.x];
+        key = token >= 0 && token < (int64_t)s.vocab ? (uint32_t)token : s.vocab;
+    }
+    text[threadIdx.x] = key;
+    __syncthreads();
+    int rank = 0;
+    for (int k = 0; k < rows; k += 4) {
+        const uint4 other = *reinterpret_cast<const uint4*>(text + k);
+        rank += (other.x < key || (other.x == key && k < (int)threadIdx.x)) + (other.y < key || (other.y == key && k + 1 < (int)threadIdx.x)) +
+                (other.z < key || (other.z == key && k + 2 < (int)threadIdx.x)) + (other.w < key || (other.w == key && k + 3 < (int)threadIdx.x));
+    }
+    if ((int)threadIdx.x < rows) {
+        keys[rank] = key;
+        places[rank] = threadIdx.x;
+    }
+    if ((int)threadIdx.x >= rows || threadIdx.x == 0) keys[threadIdx.x == 0 ? kShortText : threadIdx.x] = 0xffffffffu;
+    __syncthreads();
+    const T* from = dy + (long long)node * rows * s.ldy + col0;
+    G* to = dtable + node * s.ldgt + col0;
+    const int columns = (int)min((long long)kStrip<T>, s.c - col0), items = min(kTileItems, (rows + 31) / 32 * 4);  // places to a warp
+    const int first = tile * items, len = max(0, min(items, rows - first));
+    const uint32_t mine = lane < len ? keys[first + lane] : 0xffffffffu, place = lane < len ? places[first + lane] : 0;
+    const uint32_t ahead = tile > 0 ? keys[first - 1] : 0xffffffffu, behind = keys[first + items];
+    walk_tile<T, G, LEN>(s, dy, from, to, columns, mine, place, len, ahead, behind, smem + tile * kSlots * kSlotBytes,
+                         parts + tile * 2 * kStrip<T>, kStrip<T>);
+    __syncthreads();
+    const uint32_t last = __shfl_sync(0xffffffffu, mine, items - 1);
+    if (last >= s.vocab || last != behind || last == ahead) return;
+    float sum[U][LEN];
+    const float* part = parts + tile * 2 * kStrip<T> + kStrip<T> + lane * LEN;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {  // whatever the slot holds beyond the strip's columns: those sums go nowhere
+    for (int u = 0; u < U; ++u) load_run<float, LEN>(part + u * 32 * LEN, sum[u]);
+    part -= kStrip<T>;
+    for (int k = tile + 1; k < 8 && keys[k * items] == last; ++k) {
+        part += 2 * kStrip<T>;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
             float v[LEN];
-            load_run<T, LEN>(row + u * 32 * LEN, v);
+            load_run<float, LEN>(part + u * 32 * LEN, v);
 #pragma unroll
             for (int e = 0; e < LEN; ++e) sum[u][e] += v[e];
         }
-        const uint32_t here = __shfl_sync(0xffffffffu, key, i), next = i + 1 < len ? __shfl_sync(0xffffffffu, key, i + 1) : behind;
-        if (next != here || i + 1 == len) {
-            if (before || next == here)
-                put_sums<float, LEN, U>(before ? part : part + s.c, sum, 1.0f, 0, mine, 32 * LEN);
-            else
-                put_sums<G, LEN, U>(to + (long long)here * s.c, sum, s.scale, s.accumulate, mine, 32 * LEN);
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int e = 0; e < LEN; ++e) sum[u][e] = 0.0f;
-            before = false;
-        }
-        __syncwarp();  // the slot may be filled again
     }
-    wait_copies<0>();
+    put_sums<G, LEN, U>(to + (long long)last * s.c + lane * LEN, sum, s.scale, s.accumulate, columns - lane * LEN, 32 * LEN);
 }
 
 // Rows without tokens: a CTA clears those among zero_rows rows of a node's table, in 16-byte chunks wherever they start.  It finds
@@ -485,6 +586,16 @@ __global__ void __launch_bounds__(256) embedding_grad_kernel(GradShape s, const 
     } else {
         clear_rows<G>(s, cta < s.lead ? cta : cta - s.sum_ctas, tokens, dtable, w);
     }
+}
+
+template <typename T, typename G, int LEN>
+__global__ void __launch_bounds__(256) embedding_grad_short_kernel(GradShape s, const int64_t* tokens, const T* dy, G* dtable) {
+    pdl_wait();
+    pdl_release();
+    if (blockIdx.x < s.sum_ctas)
+        sum_short_text<T, G, LEN>(s, blockIdx.x, tokens, dy, dtable);
+    else
+        clear_rows<G>(s, blockIdx.x - s.sum_ctas, tokens, dtable, Sorted());
 }
 
 // Tokens that go on beyond their first tile: its part, then those of the tiles that follow.  A warp to a tile and a strip of 32 LEN columns.
@@ -560,7 +671,10 @@ int run_backward(const dlm_embed_args& a, const Sorted& w, cudaStream_t s) {
     g.accumulate = a.accumulate;
     g.scale = a.scale;
     g.strips = (int)((a.c + kStrip<T> - 1) / kStrip<T>);
-    const int64_t tiles = (int64_t)a.n * w.tiles, sum_ctas = (tiles * g.strips + 7) / 8;
+    const bool brief = a.rows > 0 && a.rows <= kShortText;
+    const int64_t tiles = (int64_t)a.n * w.tiles, sum_ctas = brief ? (int64_t)a.n * g.strips : (tiles * g.strips + 7) / 8;
+    constexpr int RUN = LEN == 1 ? 1 : 4;
+    const int64_t join_ctas = (tiles * ((a.c + 32 * RUN - 1) / (32 * RUN)) + 7) / 8;
     // 256 KB of the gradient to a CTA, or more: at least four times what it reads of the text (8 bytes a token, out of the L2).  Where
     // texts are long and that leaves less than two CTAs to an SM, the sorted tokens tell.
     const int64_t line = a.c * (int64_t)sizeof(G), sms = device_info().sms;
@@ -573,23 +687,32 @@ int run_backward(const dlm_embed_args& a, const Sorted& w, cudaStream_t s) {
     g.zero_rows = std::min(g.zero_rows, 1 << 17);  // 16 KB of bits
     g.zero_ctas = (int)((a.vocab + g.zero_rows - 1) / g.zero_rows);
     const int64_t zero_ctas = a.accumulate ? 0 : (int64_t)a.n * g.zero_ctas;
-    if (sum_ctas + zero_ctas > 0x7fffffff) return DLM_ERR_UNSUPPORTED;
+    if (sum_ctas + zero_ctas > 0x7fffffff || join_ctas > 0x7fffffff) return DLM_ERR_UNSUPPORTED;
     if (sum_ctas + zero_ctas == 0) return DLM_OK;
     g.sum_ctas = (unsigned)sum_ctas;
     g.lead = (unsigned)std::min<int64_t>(zero_ctas, g.scan ? 8 * sms : 0);
-    const size_t smem = std::max<size_t>(sum_ctas > 0 ? 8 * kSlots * kSlotBytes : 0, (g.zero_rows + 31) / 32 * 4);
+    constexpr size_t kRing = 8 * kSlots * kSlotBytes, kParts = 8 * 2 * kStrip<T> * 4;
+    const size_t smem = std::max<size_t>(sum_ctas == 0 ? 0 : brief ? kRing + kParts : kRing, (g.zero_rows + 31) / 32 * 4);
+    const dim3 grid((unsigned)(sum_ctas + zero_ctas));
+    const T* dy = static_cast<const T*>(a.dy);
+    G* dtable = static_cast<G*>(a.dtable);
+    if (brief) {
+        auto kern = embedding_grad_short_kernel<T, G, LEN>;
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kRing + kParts)) != cudaSuccess) return DLM_ERR_CUDA;
+        const cudaError_t err = launch_overlapped(kern, grid, dim3(256), smem, s, 1, g, a.tokens, dy, dtable);
+        dlm_count_launch(1);
+        return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
+    }
+    if (a.rows > 0) {
+        const int rc = w.chunk == kChunk<kSmallItems> ? run_sort<kSmallItems>(a, w, s) : run_sort<kLargeItems>(a, w, s);
+        if (rc != DLM_OK) return rc;
+    }
     auto kern = embedding_grad_kernel<T, G, LEN>;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 8 * kSlots * kSlotBytes) != cudaSuccess)
-        return DLM_ERR_CUDA;
-    cudaError_t err = launch_overlapped(kern, dim3((unsigned)(sum_ctas + zero_ctas)), dim3(256), smem, s, 1, g, a.tokens,
-                                        static_cast<const T*>(a.dy), static_cast<G*>(a.dtable), w);
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRing) != cudaSuccess) return DLM_ERR_CUDA;
+    cudaError_t err = launch_overlapped(kern, grid, dim3(256), smem, s, 1, g, a.tokens, dy, dtable, w);
     dlm_count_launch(1);
     if (err == cudaSuccess && w.tiles > 1) {
-        constexpr int RUN = LEN == 1 ? 1 : 4;
-        const int64_t ctas = (tiles * ((a.c + 32 * RUN - 1) / (32 * RUN)) + 7) / 8;
-        if (ctas > 0x7fffffff) return DLM_ERR_UNSUPPORTED;
-        err = launch_overlapped(embedding_grad_join_kernel<G, RUN>, dim3((unsigned)ctas), dim3(256), 0, s, 1, g,
-                                static_cast<G*>(a.dtable), w);
+        err = launch_overlapped(embedding_grad_join_kernel<G, RUN>, dim3((unsigned)join_ctas), dim3(256), 0, s, 1, g, dtable, w);
         dlm_count_launch(1);
     }
     return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
@@ -599,10 +722,6 @@ template <typename T, typename G>
 int backward(const dlm_embed_args& a, cudaStream_t s) {
     const Sorted w = sorted_layout(a.n, a.rows, a.c, a.workspace);
     if ((int64_t)a.n * w.chunks > 0x7fffffff) return DLM_ERR_UNSUPPORTED;
-    if (a.rows > 0) {
-        const int rc = w.chunk == kChunk<kSmallItems> ? run_sort<kSmallItems>(a, w, s) : run_sort<kLargeItems>(a, w, s);
-        if (rc != DLM_OK) return rc;
-    }
     constexpr int LEN = kRun<T>;
     if (a.c % LEN == 0 && (a.rows == 0 || rows_aligned(a.dy, a.ldy, sizeof(T))) && rows_aligned(a.dtable, a.ldgt, sizeof(G)))
         return run_backward<T, G, LEN>(a, w, s);

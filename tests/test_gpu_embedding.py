@@ -225,3 +225,14 @@ def test_captured_calls_see_new_tokens_and_share_a_workspace():
             s["tokens"].copy_(_tokens(*s["tokens"].shape, vocab, turn, "text"))
             s["graph"].replay()
             assert torch.equal(s["g"], _backward(s["tokens"], s["dy"], vocab, "f32"))
+
+
+@pytest.mark.parametrize("typ,gtype", [("f32", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("rows", [2, 31, 32, 33, 200, 255, 256, 257])
+@pytest.mark.parametrize("c", [40, 1001, 1200])
+def test_gradient_of_short_texts(rows, c, typ, gtype):
+    """Around the sizes where a CTA has the whole text; tokens that fill several tiles, in one strip of columns and in several."""
+    for vocab, kind in ((3, "uniform"), (900, "text"), (5, "stray")):
+        tokens, dy = _tokens(2, rows, vocab, rows, kind), _rand((2, rows, c), 1.0, c, typ)
+        _check_backward(tokens, dy, vocab, gtype, 1.5)
+        _check_backward(tokens, dy, vocab, gtype, 1.5, add=_rand((2, vocab, c), 1.0, 9, gtype))
