@@ -46,6 +46,180 @@ __device__ __forceinline__ float warp_max(float v) {
     return v;
 }
 
+// A sum, and (TOP) a maximum, over the group of a row; returns whether all threads had `ok`.  One barrier, which also frees the row's
+// slot where rows come by bulk copies, since its values are in registers by then.
+template <int TPR, bool BULK, bool TOP>
+__device__ __forceinline__ bool sum_and_top(float& sum, float& top, float (*part)[TPR > 32 ? TPR / 32 : 1], bool ok) {
+    constexpr int WARPS = TPR / 32;
+    sum = lane_sum<TPR>(sum);
+    if constexpr (TOP) {
+#pragma unroll
+        for (int o = (TPR < 32 ? TPR : 32) / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    }
+    if constexpr (TPR > 32) {
+        if ((threadIdx.x & 31) == 0) {
+            part[0][threadIdx.x >> 5] = sum;
+            if (TOP) part[1][threadIdx.x >> 5] = top;
+        }
+        ok = sums_barrier<BULK>(ok);
+        sum = warps_sum<WARPS>(part[0]);
+        if constexpr (TOP) {
+            top = part[1][threadIdx.x & (WARPS - 1)];
+#pragma unroll
+            for (int o = WARPS / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        }
+    }
+    return TPR <= 32 || ok;
+}
+
+// LEN elements in 8 bits.
+template <int LEN>
+__device__ __forceinline__ void put_e4m3(unsigned char* to, const float* v) {
+    if constexpr (LEN == 8)
+        *reinterpret_cast<uint2*>(to) = make_uint2(e4m3_pair(v[0], v[1]) | (uint32_t)e4m3_pair(v[2], v[3]) << 16,
+                                                   e4m3_pair(v[4], v[5]) | (uint32_t)e4m3_pair(v[6], v[7]) << 16);
+    else if constexpr (LEN == 4)
+        *reinterpret_cast<uint32_t*>(to) = e4m3_pair(v[0], v[1]) | (uint32_t)e4m3_pair(v[2], v[3]) << 16;
+    else
+        *to = e4m3_one(v[0]);
+}
+
+// Groups of TPR threads take every G-th row of a node; x and the residual come D - 1 rows ahead.  EIGHT: the 8-bit output, too.
+template <typename T, int LEN, int E, int TPR, int D, bool EIGHT>
+__global__ void __launch_bounds__(kBlock<TPR>)
+    rms_norm_kernel(long long rows, int c, const T* x, long long ldx, const T* residual, long long ldr, const float* weight, long long ldw,
+                    float eps, T* h, long long ldh, T* y, long long ldy, unsigned char* y8, long long ld8, float* scales, float* rstd) {
+    constexpr int GROUPS = kBlock<TPR> / TPR, WARPS = TPR / 32;
+    constexpr bool BULK = kBulk<LEN, TPR>;
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ float part[2][2][TPR > 32 ? WARPS : 1];
+    __shared__ uint64_t full[D];
+    const uint32_t bytes = (uint32_t)c * sizeof(T);
+    const int node = blockIdx.y, t = threadIdx.x % TPR, group = threadIdx.x / TPR;
+    const int rb = row_bytes(c, sizeof(T)), slot_bytes = residual ? 2 * rb : rb;
+    unsigned char* in = smem + (size_t)group * (D * slot_bytes + (LEN == 1 ? 2 * rb : 0));
+    unsigned char* out = in + (size_t)D * slot_bytes;  // where rows are not aligned: h, then y
+    const long long stride = (long long)gridDim.x * GROUPS;
+    const long long first = (long long)blockIdx.x * GROUPS + group, base = (long long)node * rows;
+    const T *fetch = x + (base + first) * ldx, *fetch_r = residual + (base + first) * ldr;  // the next row to ask for
+    const T *row = fetch, *row_r = fetch_r;
+    long long asked = first;
+    if constexpr (BULK) {
+        if (threadIdx.x == 0) {
+            for (int k = 0; k < D; ++k) mbar_init(smem_u32(&full[k]), 1);
+            mbar_init_fence();
+        }
+        __syncthreads();
+    }
+    pdl_wait();
+    pdl_release();
+    auto ask = [&](int k) {  // the next row, into slot k
+        unsigned char* buf = in + k * slot_bytes;
+        if constexpr (BULK) {
+            if (threadIdx.x == 0 && asked < rows) {
+                mbar_expect_tx(smem_u32(&full[k]), residual ? 2 * bytes : bytes);
+                bulk_row(buf, fetch, bytes, smem_u32(&full[k]));
+                if (residual) bulk_row(buf + rb, fetch_r, bytes, smem_u32(&full[k]));
+            }
+        } else {
+            if (asked < rows) {
+                fetch_row<T, LEN, TPR>(buf, fetch, x, c, t);
+                if (residual) fetch_row<T, LEN, TPR>(buf + rb, fetch_r, residual, c, t);
+            }
+            commit_copies();
+        }
+        asked += stride;
+        fetch += stride * ldx;
+        fetch_r += stride * ldr;
+    };
+#pragma unroll
+    for (int k = 0; k < D - 1; ++k) ask(k);
+    float w[E];
+    params<LEN, E, TPR>(weight + node * ldw, c, t, w);
+    const float inv_c = 1.0f / (float)c;
+    int slot = 0, side = 0;
+    uint32_t parities = 0;  // of each slot's next phase
+    // groups of a warp leave together: the loop counts the rows of its first group
+    long long r = first;
+    for (long long lead = TPR < 32 ? first - group % (32 / (TPR < 32 ? TPR : 32)) : first; lead < rows; lead += stride) {
+        ask(slot == 0 ? D - 1 : slot - 1);
+        bool ok = true;
+        if constexpr (BULK) {
+            ok = mbar_wait(smem_u32(&full[slot]), (parities >> slot) & 1);
+        } else {
+            wait_copies<D - 1>();
+            group_barrier<TPR>();
+        }
+        const bool live = BULK || r < rows;
+        const int live_c = live ? c : 0;
+        const unsigned char* buf = in + slot * slot_bytes;
+        float v[E];
+        row_values<T, LEN, E, TPR>(buf, row_skew(row), live_c, t, v);
+        if (residual) {
+            const int skew = row_skew(row_r);
+#pragma unroll
+            for (int u = 0; u < E / LEN; ++u) {
+                float a[LEN];
+                one_run<T, LEN, TPR>(buf + rb, skew, live_c, t, u, a);
+#pragma unroll
+                for (int k = 0; k < LEN; ++k) v[u * LEN + k] += a[k];
+            }
+        }
+        float2 s2 = make_float2(0.0f, 0.0f);
+        float top = 0.0f;
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+            s2 = __ffma2_rn(make_float2(v[e], v[e + 1]), make_float2(v[e], v[e + 1]), s2);
+            if constexpr (EIGHT) top = fmaxf(top, fmaxf(fabsf(v[e] * w[e]), fabsf(v[e + 1] * w[e + 1])));
+        }
+        float sum = s2.x + s2.y;
+        if constexpr (BULK) fence_before_refill();
+        if (!sum_and_top<TPR, BULK, EIGHT>(sum, top, part[side], ok)) {
+            give_up(&g_rms_kernel_error, full, parities);
+            return;
+        }
+        side ^= 1;
+        const float rs = rsqrtf(fmaf(sum, inv_c, eps));
+        const long long at = base + r;
+        if (h && live) put_values<T, LEN, E, TPR>(h + at * ldh, out, c, t, v);
+        if constexpr (EIGHT) {
+            const ToE4M3 map(top);
+            if (live) {
+#pragma unroll
+                for (int u = 0; u < E / LEN; ++u) {
+                    float q[LEN];
+#pragma unroll
+                    for (int k = 0; k < LEN; ++k) q[k] = map(v[u * LEN + k] * w[u * LEN + k]);
+                    const int col = column<LEN, TPR>(t, u);
+                    if (col < c) put_e4m3<LEN>(y8 + at * ld8 + col, q);
+                }
+                if (t == 0) scales[at] = top * rs / kE4M3Max;
+            }
+        }
+        if (!EIGHT || y) {
+#pragma unroll
+            for (int e = 0; e < E; e += 2) {
+                const float2 o = __fmul2_rn(__fmul2_rn(make_float2(v[e], v[e + 1]), make_float2(rs, rs)), make_float2(w[e], w[e + 1]));
+                v[e] = o.x;
+                v[e + 1] = o.y;
+            }
+            if (live) put_values<T, LEN, E, TPR>(y + at * ldy, out + rb, c, t, v);
+        }
+        if (t == 0 && live) rstd[at] = rs;
+        if constexpr (!BULK) group_barrier<TPR>();  // the slot may be filled again, and the results are in their buffers
+        if (LEN == 1 && live) {
+            if (h) flush_row<T, TPR>(h + at * ldh, out, c, t);
+            if (!EIGHT || y) flush_row<T, TPR>(y + at * ldy, out + rb, c, t);
+        }
+        parities ^= 1u << slot;
+        if (++slot == D) slot = 0;
+        r += stride;
+        row += stride * ldx;
+        row_r += stride * ldr;
+    }
+    wait_copies<0>();
+}
+
 // Rows of any width, two sweeps each, the second out of the caches.
 template <typename T>
 __global__ void __launch_bounds__(1024)
@@ -92,7 +266,205 @@ __global__ void __launch_bounds__(1024)
     }
 }
 
-// partial[(node G + group) c + column]: the sum over the rows of one CTA.
+// As forward, with h, dy and the residual's gradient; partial[(node G + CTA) c + column]: the sums over the rows of one CTA.
+template <typename T, int LEN, int E, int TPR, int D>
+__global__ void __launch_bounds__(kBlock<TPR>)
+    rms_norm_grad_kernel(long long rows, int c, const T* h, long long ldh, const T* dy, long long lddy, const T* dres, long long lddr,
+                         const float* weight, long long ldw, const float* rstd, T* dh, long long lddh, float* partial) {
+    constexpr int GROUPS = kBlock<TPR> / TPR;
+    constexpr bool BULK = kBulk<LEN, TPR>;
+    constexpr bool HOLD = E <= 16;  // the row's values stay in registers between the two sweeps, else they are read again
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ float part[2][2][TPR > 32 ? TPR / 32 : 1];
+    __shared__ uint64_t full[D];
+    const uint32_t bytes = (uint32_t)c * sizeof(T);
+    const int node = blockIdx.y, t = threadIdx.x % TPR, group = threadIdx.x / TPR;
+    const int rb = row_bytes(c, sizeof(T)), slot_bytes = (dres ? 3 : 2) * rb;
+    unsigned char* in = smem + (size_t)group * (D * slot_bytes + (LEN == 1 ? rb : 0));
+    unsigned char* out = in + (size_t)D * slot_bytes;  // where rows are not aligned
+    const long long stride = (long long)gridDim.x * GROUPS;
+    const long long first = (long long)blockIdx.x * GROUPS + group, base = (long long)node * rows;
+    const T *hf = h + (base + first) * ldh, *gf = dy + (base + first) * lddy, *ef = dres + (base + first) * lddr;  // the next row to ask for
+    const T *hr = hf, *gr = gf, *er = ef;
+    T* to = dh + (base + first) * lddh;
+    const float* w = weight + node * ldw;
+    long long asked = first;
+    rstd += base;
+    if constexpr (BULK) {
+        if (threadIdx.x == 0) {
+            for (int k = 0; k < D; ++k) mbar_init(smem_u32(&full[k]), 1);
+            mbar_init_fence();
+        }
+        __syncthreads();
+    }
+    pdl_wait();
+    pdl_release();
+    auto ask = [&](int k) {  // the next row, into slot k
+        unsigned char* buf = in + k * slot_bytes;
+        if constexpr (BULK) {
+            if (threadIdx.x == 0 && asked < rows) {
+                mbar_expect_tx(smem_u32(&full[k]), (dres ? 3 : 2) * bytes);
+                bulk_row(buf, hf, bytes, smem_u32(&full[k]));
+                bulk_row(buf + rb, gf, bytes, smem_u32(&full[k]));
+                if (dres) bulk_row(buf + 2 * rb, ef, bytes, smem_u32(&full[k]));
+            }
+        } else {
+            if (asked < rows) {
+                fetch_row<T, LEN, TPR>(buf, hf, h, c, t);
+                fetch_row<T, LEN, TPR>(buf + rb, gf, dy, c, t);
+                if (dres) fetch_row<T, LEN, TPR>(buf + 2 * rb, ef, dres, c, t);
+            }
+            commit_copies();
+        }
+        asked += stride;
+        hf += stride * ldh;
+        gf += stride * lddy;
+        ef += stride * lddr;
+    };
+#pragma unroll
+    for (int k = 0; k < D - 1; ++k) ask(k);
+    float wv[HOLD ? E : 1];
+    if constexpr (HOLD) params<LEN, E, TPR>(w, c, t, wv);
+    float dw[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) dw[e] = 0.0f;
+    const float inv_c = 1.0f / (float)c;
+    int slot = 0, side = 0;
+    uint32_t parities = 0;  // of each slot's next phase
+    float nrs = first < rows ? rstd[first] : 0.0f;
+    // groups of a warp leave together: the loop counts the rows of its first group
+    long long r = first;
+    for (long long lead = TPR < 32 ? first - group % (32 / (TPR < 32 ? TPR : 32)) : first; lead < rows; lead += stride) {
+        ask(slot == 0 ? D - 1 : slot - 1);
+        const float rs = r < rows ? nrs : 0.0f;
+        if (r + stride < rows) nrs = rstd[r + stride];
+        bool ok = true;
+        if constexpr (BULK) {
+            ok = mbar_wait(smem_u32(&full[slot]), (parities >> slot) & 1);
+        } else {
+            wait_copies<D - 1>();
+            group_barrier<TPR>();
+        }
+        const bool live = BULK || r < rows;
+        const int live_c = live ? c : 0;
+        const unsigned char *hb = in + slot * slot_bytes, *gb = hb + rb, *eb = gb + rb;
+        const int hs = row_skew(hr), gs = row_skew(gr), es = row_skew(er);
+        float sum = 0.0f, none = 0.0f;
+        float xh[HOLD ? E : LEN], v[HOLD ? E : LEN], more[HOLD ? E : LEN];
+        if constexpr (HOLD) {
+            float2 s2 = make_float2(0.0f, 0.0f);
+            row_values<T, LEN, E, TPR>(hb, hs, live_c, t, xh);
+            row_values<T, LEN, E, TPR>(gb, gs, live_c, t, v);
+            if (dres) {
+                row_values<T, LEN, E, TPR>(eb, es, live_c, t, more);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) more[e] = 0.0f;
+            }
+#pragma unroll
+            for (int e = 0; e < E; e += 2) {
+                const float2 x = __fmul2_rn(make_float2(xh[e], xh[e + 1]), make_float2(rs, rs)), g = make_float2(v[e], v[e + 1]);
+                const float2 a = __ffma2_rn(g, x, make_float2(dw[e], dw[e + 1])), p = __fmul2_rn(g, make_float2(wv[e], wv[e + 1]));
+                s2 = __ffma2_rn(p, x, s2);
+                dw[e] = a.x;
+                dw[e + 1] = a.y;
+                xh[e] = x.x;
+                xh[e + 1] = x.y;
+                v[e] = p.x;
+                v[e + 1] = p.y;
+            }
+            sum = s2.x + s2.y;
+        } else {
+#pragma unroll
+            for (int u = 0; u < E / LEN; ++u) {
+                one_run<T, LEN, TPR>(hb, hs, live_c, t, u, xh);
+                one_run<T, LEN, TPR>(gb, gs, live_c, t, u, v);
+#pragma unroll
+                for (int k = 0; k < LEN; ++k) {
+                    const int at = column<LEN, TPR>(t, u) + k;
+                    const float x = xh[k] * rs;
+                    dw[u * LEN + k] = fmaf(v[k], x, dw[u * LEN + k]);
+                    if (at < c) sum = fmaf(v[k] * w[at], x, sum);
+                }
+            }
+        }
+        if constexpr (BULK && HOLD) fence_before_refill();
+        if (!sum_and_top<TPR, BULK, false>(sum, none, part[side], ok)) {
+            give_up(&g_rms_kernel_error, full, parities);
+            return;
+        }
+        side ^= 1;
+        const float m = sum * inv_c;
+        if constexpr (HOLD) {
+#pragma unroll
+            for (int e = 0; e < E; e += 2) {
+                const float2 d = __ffma2_rn(make_float2(xh[e], xh[e + 1]), make_float2(-m, -m), make_float2(v[e], v[e + 1]));
+                const float2 o = __ffma2_rn(d, make_float2(rs, rs), make_float2(more[e], more[e + 1]));
+                v[e] = o.x;
+                v[e + 1] = o.y;
+            }
+            if (live) put_values<T, LEN, E, TPR>(to, out, c, t, v);
+        } else {
+#pragma unroll
+            for (int u = 0; u < E / LEN; ++u) {
+                const int at = column<LEN, TPR>(t, u);
+                one_run<T, LEN, TPR>(hb, hs, live_c, t, u, xh);
+                one_run<T, LEN, TPR>(gb, gs, live_c, t, u, v);
+                if (dres) one_run<T, LEN, TPR>(eb, es, live_c, t, u, more);
+#pragma unroll
+                for (int k = 0; k < LEN; ++k) {
+                    const float d = fmaf(xh[k] * rs, -m, at + k < c ? v[k] * w[at + k] : 0.0f);
+                    v[k] = fmaf(d, rs, dres ? more[k] : 0.0f);
+                }
+                if (live && at < c) {
+                    if constexpr (LEN > 1)
+                        st_words(to + at, pack<T>(v));
+                    else
+                        reinterpret_cast<T*>(out + row_skew(to))[at] = narrow<T>(v[0]);
+                }
+            }
+        }
+        if constexpr (BULK && !HOLD) fence_before_refill();
+        if constexpr (!BULK || !HOLD) group_barrier<TPR>();  // the slot may be filled again, and the results are in their buffer
+        if (LEN == 1 && live) flush_row<T, TPR>(to, out, c, t);
+        parities ^= 1u << slot;
+        if (++slot == D) slot = 0;
+        r += stride;
+        hr += stride * ldh;
+        gr += stride * lddy;
+        er += stride * lddr;
+        to += stride * lddh;
+    }
+    wait_copies<0>();
+    // the CTA's groups join in order, in the rows' buffers
+    float* total = partial + ((long long)node * gridDim.x + blockIdx.x) * c;
+    if constexpr (GROUPS > 1) {
+        float* joined = reinterpret_cast<float*>(smem);  // [GROUPS][c]
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < E / LEN; ++u)
+#pragma unroll
+            for (int k = 0; k < LEN; ++k)
+                if (column<LEN, TPR>(t, u) + k < c) joined[group * c + column<LEN, TPR>(t, u) + k] = dw[u * LEN + k];
+        __syncthreads();
+        for (int k = threadIdx.x; k < c; k += kBlock<TPR>) {
+            float s = joined[k];
+#pragma unroll 8
+            for (int q = 1; q < GROUPS; ++q) s += joined[q * c + k];
+            total[k] = s;
+        }
+    } else {
+#pragma unroll
+        for (int u = 0; u < E / LEN; ++u)
+#pragma unroll
+            for (int k = 0; k < LEN; ++k) {
+                const int at = column<LEN, TPR>(t, u) + k;
+                if (at < c) total[at] = dw[u * LEN + k];
+            }
+    }
+}
+
+// partial[(node G + CTA) c + column]: the sum over the rows of one CTA.
 template <typename T>
 __global__ void __launch_bounds__(1024)
     rms_norm_grad_wide_kernel(long long rows, long long c, const T* h, long long ldh, const T* dy, long long lddy, const T* dres,
@@ -164,6 +536,58 @@ int wide_forward(const dlm_rms_args& a, cudaStream_t s) {
     return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
 }
 
+// Rows up to this many elements are held on chip; wider ones are swept from memory.
+constexpr int64_t kMaxHeld = 16384;
+
+// CALL(columns per thread, threads per row) of the narrowest group that holds c columns.
+#define DLM_RMS_SHAPES(CALL)             \
+    if (c <= 64) return CALL(8, 8);      \
+    if (c <= 128) return CALL(16, 8);    \
+    if (c <= 256) return CALL(16, 16);   \
+    if (c <= 512) return CALL(16, 32);   \
+    if (c <= 1024) return CALL(16, 64);  \
+    if (c <= 2048) return CALL(16, 128); \
+    if (c <= 4096) return CALL(16, 256); \
+    if (c <= 8192) return CALL(16, 512); \
+    return CALL(32, 512);
+
+template <typename T, int LEN, int E, int TPR, bool EIGHT, int D = kDepth<TPR>>
+int run_forward(const dlm_rms_args& a, cudaStream_t s) {
+    constexpr int GROUPS = kBlock<TPR> / TPR;
+    const size_t smem = (size_t)GROUPS * (D * (a.residual ? 2 : 1) + (LEN == 1 ? 2 : 0)) * row_bytes((int)a.c, sizeof(T));
+    if (smem > kMostShared) {
+        if constexpr (TPR == 512 && D > 1)
+            return run_forward<T, LEN, E, TPR, EIGHT, D - 1>(a, s);
+        else
+            return wide_forward<T>(a, s);
+    }
+    auto kern = rms_norm_kernel<T, LEN, E, TPR, D, EIGHT>;
+    const int ctas = resident_ctas(kern, kBlock<TPR>, smem, 32, a.n, a.rows, GROUPS);
+    if (ctas < 1) return DLM_ERR_CUDA;
+    cudaError_t err = launch_overlapped(kern, dim3((unsigned)ctas, a.n), dim3(kBlock<TPR>), smem, s, 1, a.rows, (int)a.c,
+                                        static_cast<const T*>(a.x), a.ldx, static_cast<const T*>(a.residual), a.ldr, a.weight, a.ldw,
+                                        a.eps, static_cast<T*>(a.h), a.ldh, static_cast<T*>(a.y), a.ldy,
+                                        static_cast<unsigned char*>(a.y8), a.ld8, a.scales, a.rstd);
+    dlm_count_launch(1);
+    return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
+}
+
+template <typename T, bool EIGHT>
+int forward(const dlm_rms_args& a, cudaStream_t s) {
+    const int64_t c = a.c;
+    if (c > kMaxHeld) return wide_forward<T>(a, s);
+#define DLM_VEC(E, TPR) run_forward<T, kRun<T>, E, TPR, EIGHT>(a, s)
+#define DLM_ONE(E, TPR) run_forward<T, 1, E, TPR, EIGHT>(a, s)
+    if (c % kRun<T> == 0 && rows_aligned(a.x, a.ldx, sizeof(T)) && (!a.residual || rows_aligned(a.residual, a.ldr, sizeof(T))) &&
+        (!a.h || rows_aligned(a.h, a.ldh, sizeof(T))) && (!a.y || rows_aligned(a.y, a.ldy, sizeof(T))) &&
+        (!EIGHT || ((uintptr_t)a.y8 % kRun<T> == 0 && a.ld8 % kRun<T> == 0))) {
+        DLM_RMS_SHAPES(DLM_VEC)
+    }
+    DLM_RMS_SHAPES(DLM_ONE)
+#undef DLM_VEC
+#undef DLM_ONE
+}
+
 // The backward launchers write the number of parts per node to *parts.
 template <typename T>
 int wide_backward(const dlm_rms_args& a, int* parts, cudaStream_t s) {
@@ -177,6 +601,44 @@ int wide_backward(const dlm_rms_args& a, int* parts, cudaStream_t s) {
     dlm_count_launch(1);
     return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
 }
+
+template <typename T, int LEN, int E, int TPR, int D = kDepth<TPR>>
+int run_backward(const dlm_rms_args& a, int* parts, cudaStream_t s) {
+    constexpr int GROUPS = kBlock<TPR> / TPR;
+    const size_t smem = std::max((size_t)GROUPS * (D * (a.residual ? 3 : 2) + (LEN == 1)) * row_bytes((int)a.c, sizeof(T)),
+                                 GROUPS > 1 ? (size_t)GROUPS * a.c * 4 : 0);
+    if (smem > kMostShared) {
+        if constexpr (TPR == 512 && D > 1)
+            return run_backward<T, LEN, E, TPR, D - 1>(a, parts, s);
+        else
+            return wide_backward<T>(a, parts, s);
+    }
+    auto kern = rms_norm_grad_kernel<T, LEN, E, TPR, D>;
+    *parts = std::min(resident_ctas(kern, kBlock<TPR>, smem, 32, a.n, a.rows, GROUPS), dlm_rms_max_ctas(a.n, a.rows, a.c));
+    if (*parts < 1) return DLM_ERR_CUDA;
+    cudaError_t err = launch_overlapped(kern, dim3((unsigned)*parts, a.n), dim3(kBlock<TPR>), smem, s, 1, a.rows, (int)a.c,
+                                        static_cast<const T*>(a.x), a.ldx, static_cast<const T*>(a.dy), a.lddy,
+                                        static_cast<const T*>(a.residual), a.ldr, a.weight, a.ldw, (const float*)a.rstd,
+                                        static_cast<T*>(a.dh), a.lddh, a.partial);
+    dlm_count_launch(1);
+    return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
+}
+
+template <typename T>
+int backward(const dlm_rms_args& a, int* parts, cudaStream_t s) {
+    const int64_t c = a.c;
+    if (c > kMaxHeld) return wide_backward<T>(a, parts, s);
+#define DLM_VEC(E, TPR) run_backward<T, kRun<T>, E, TPR>(a, parts, s)
+#define DLM_ONE(E, TPR) run_backward<T, 1, E, TPR>(a, parts, s)
+    if (c % kRun<T> == 0 && rows_aligned(a.x, a.ldx, sizeof(T)) && rows_aligned(a.dy, a.lddy, sizeof(T)) &&
+        rows_aligned(a.dh, a.lddh, sizeof(T)) && (!a.residual || rows_aligned(a.residual, a.ldr, sizeof(T)))) {
+        DLM_RMS_SHAPES(DLM_VEC)
+    }
+    DLM_RMS_SHAPES(DLM_ONE)
+#undef DLM_VEC
+#undef DLM_ONE
+}
+#undef DLM_RMS_SHAPES
 
 template <typename G, int SLICES>
 cudaError_t run_join(const dlm_rms_args& a, int parts, cudaStream_t s) {
@@ -213,14 +675,15 @@ int dlm_rms_max_ctas(int n, int64_t rows, int64_t c) {
 
 int dlm_launch_rms_norm(const dlm_rms_args& a, void* stream) {
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    return a.dtype == DLM_G_BF16 ? wide_forward<__nv_bfloat16>(a, s) : wide_forward<float>(a, s);
+    if (a.y8) return a.dtype == DLM_G_BF16 ? forward<__nv_bfloat16, true>(a, s) : forward<float, true>(a, s);
+    return a.dtype == DLM_G_BF16 ? forward<__nv_bfloat16, false>(a, s) : forward<float, false>(a, s);
 }
 
 int dlm_launch_rms_norm_grad(const dlm_rms_args& a, void* stream) {
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     int parts = 0;
     if (a.rows > 0) {
-        int rc = a.dtype == DLM_G_BF16 ? wide_backward<__nv_bfloat16>(a, &parts, s) : wide_backward<float>(a, &parts, s);
+        int rc = a.dtype == DLM_G_BF16 ? backward<__nv_bfloat16>(a, &parts, s) : backward<float>(a, &parts, s);
         if (rc != DLM_OK) return rc;
     }
     cudaError_t err = a.g_dtype == DLM_G_BF16 ? join<__nv_bfloat16>(a, parts, s) : join<float>(a, parts, s);
