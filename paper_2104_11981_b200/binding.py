@@ -608,38 +608,88 @@ def policy_loss_grad(logits, tokens, weight, advantage, old_logp, ref_logp, clip
                                    workspace.data_ptr(), workspace.nbytes, _stream_ptr(stream)), "policy_loss_grad")
 
 
-def _at_home(*tensors):
-    """The tensors (None among them) are on the current device, on which the call runs."""
+# The operators between tokens and logits are called on single tokens as well, where reading a tensor's attributes takes longer than
+# the kernel: these helpers ask for each once.  Filled on first use, so that importing this module does not import torch.
+_current_device = _current_stream = _f32 = _bf16 = _i32 = _i64_t = _e4m3 = None
+
+
+def _torch_names():
+    global _current_device, _current_stream, _f32, _bf16, _i32, _i64_t, _e4m3
     import torch
-    home = torch._C._cuda_getDevice()
-    for t in tensors:
-        assert t is None or t.get_device() == home, "tensors on the current CUDA device are expected"
+    _f32, _bf16, _i32, _i64_t, _e4m3 = torch.float32, torch.bfloat16, torch.int32, torch.int64, torch.float8_e4m3fn
+    _current_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
-def _tables(t):
-    """Elements from one node's table to the next one's, of tables [n, vocab, c] whose rows follow one another."""
-    n, vocab, c = t.shape
-    s0, s1, s2 = t.stride()
-    assert t.is_cuda and (s2 == 1 or c == 1) and (s1 == c or vocab == 1), "a node's rows follow one another"
-    return s0 if n > 1 else vocab * c
+def _home():
+    """The current device, on which the call runs and its tensors have to be."""
+    if _current_device is None:
+        _torch_names()
+    return _current_device()
 
 
-def _tokens(t, count):
-    import torch
-    assert t.is_cuda and t.dtype == torch.int64 and t.is_contiguous() and t.numel() == count, "int64, one token per row"
+def _kind(dtype):
+    if dtype is _f32:
+        return G_F32
+    if dtype is _bf16:
+        return G_BF16
+    raise TypeError("float32 or bfloat16 expected")
+
+
+def _rows(t, shape, dtype, home):
+    """(pointer, row stride) of activations [n, rows, c] of this shape and type, or of None."""
+    if t is None:
+        return None, 0
+    if t.dtype is not dtype or t.get_device() != home or t.shape != shape:
+        raise AssertionError("a tensor of the same shape and type on the current CUDA device is expected")
+    return t.data_ptr(), shape[2] if t.is_contiguous() else _node_rows(t, shape, dtype)
+
+
+def _vectors(t, n, c, home):
+    """(pointer, row stride) of fp32 per-node vectors [n, c] with unit column stride, or of None."""
+    if t is None:
+        return None, 0
+    if t.dtype is not _f32 or t.get_device() != home:
+        raise AssertionError("fp32 on the current CUDA device is expected")
+    return _node_vectors(t, n, c)
+
+
+def _flat(t, count, dtype, home):
+    """Pointer of a contiguous tensor of this many elements, or of None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != home or t.numel() != count or not t.is_contiguous():
+        raise AssertionError(f"a contiguous {dtype} tensor of {count} elements on the current CUDA device is expected")
     return t.data_ptr()
+
+
+def _scratch(t, home):
+    if t.get_device() != home or not t.is_contiguous():
+        raise AssertionError("a contiguous workspace on the current CUDA device is expected")
+    return t.data_ptr(), t.nbytes
+
+
+def _tables(t, home):
+    """Pointer of tables [n, vocab, c] whose rows follow one another, and the elements from one node's to the next one's."""
+    n, vocab, c = t.shape
+    if t.get_device() != home:
+        raise AssertionError("tables on the current CUDA device are expected")
+    if n == 1 and t.is_contiguous():
+        return t.data_ptr(), vocab * c
+    s0, s1, s2 = t.stride()
+    assert (s2 == 1 or c == 1) and (s1 == c or vocab == 1), "a node's rows follow one another"
+    return t.data_ptr(), s0 if n > 1 else vocab * c
 
 
 def embedding(table, tokens, y, scale=1.0, stream=None):
     """y[i, r] <- scale table[i, tokens[i, r]] (0 where the token is outside [0, vocab)): table [n, vocab, c] fp32 or bf16 (a view of
     the stacked parameters, for instance), tokens int64 [n, rows], y [n, rows, c] fp32 or bf16."""
-    _at_home(table, tokens, y)
+    home, shape, dtype = _home(), y.shape, y.dtype
     n, vocab, c = table.shape
-    rows = tokens.shape[1]
-    shape = y.shape
-    assert shape == (n, rows, c), "y [n, rows, c] is expected"
-    _check(_calls.embedding(n, rows, vocab, c, table.data_ptr(), _dtype(table), _tables(table), _tokens(tokens, n * rows), scale,
-                            y.data_ptr(), _dtype(y), _node_rows(y, shape, y.dtype), _stream_ptr(stream)), "embedding")
+    rows = shape[1]
+    assert shape[0] == n and shape[2] == c and len(shape) == 3, "y [n, rows, c] is expected"
+    (pt, ldt), (py, ldy) = _tables(table, home), _rows(y, shape, dtype, home)
+    _check(_calls.embedding(n, rows, vocab, c, pt, _kind(table.dtype), ldt, _flat(tokens, n * rows, _i64_t, home), scale, py,
+                            _kind(dtype), ldy, _current_stream(home) if stream is None else stream.cuda_stream), "embedding")
 
 
 def embedding_grad_workspace_bytes(n, rows, vocab, c):
@@ -652,37 +702,32 @@ def embedding_grad_workspace_bytes(n, rows, vocab, c):
 def embedding_grad(tokens, dy, dtable, workspace, scale=1.0, accumulate=False, stream=None):
     """Gradient of embedding's table: dtable [n, vocab, c] fp32 or bf16 (a view of the stacked gradient, for instance) is overwritten, or
     added to (accumulate); workspace: uint8 device tensor of at least embedding_grad_workspace_bytes(n, rows, vocab, c) bytes."""
-    _at_home(tokens, dy, dtable, workspace)
+    home, shape, dtype = _home(), dy.shape, dy.dtype
     n, vocab, c = dtable.shape
-    shape = dy.shape
     rows = shape[1]
-    assert shape == (n, rows, c) and workspace.is_cuda and workspace.is_contiguous()
-    _check(_calls.embedding_grad(n, rows, vocab, c, _tokens(tokens, n * rows), dy.data_ptr(), _dtype(dy),
-                                 _node_rows(dy, shape, dy.dtype), scale, int(accumulate), dtable.data_ptr(), _dtype(dtable),
-                                 _tables(dtable), workspace.data_ptr(), workspace.nbytes, _stream_ptr(stream)), "embedding_grad")
-
-
-def _maybe_rows(t, shape, dtype):
-    """(pointer, row stride) of activations, or of None."""
-    return (t.data_ptr(), _node_rows(t, shape, dtype)) if t is not None else (None, 0)
+    assert shape[0] == n and shape[2] == c and len(shape) == 3, "dy [n, rows, c] is expected"
+    (pt, ldt), (py, ldy), (pw, nbytes) = _tables(dtable, home), _rows(dy, shape, dtype, home), _scratch(workspace, home)
+    _check(_calls.embedding_grad(n, rows, vocab, c, _flat(tokens, n * rows, _i64_t, home), py, _kind(dtype), ldy, scale,
+                                 1 if accumulate else 0, pt, _kind(dtable.dtype), ldt, pw, nbytes,
+                                 _current_stream(home) if stream is None else stream.cuda_stream), "embedding_grad")
 
 
 def rms_norm(x, weight, eps, y, rstd, residual=None, h=None, y8=None, scales=None, stream=None):
     """h <- x + residual; y <- h rstd weight over the last axis of x [n, rows, c] (fp32 or bf16); weight fp32 [n, c] (a view of the
     stacked parameters, for instance); rstd fp32 [n, rows] is written.  residual and h (of x's shape and type) may be None.  y8
     (float8_e4m3fn of x's shape) and scales (fp32 [n, rows]): the output in 8 bits, beside y or in its place (y None)."""
-    _at_home(x, weight, y, rstd, residual, h, y8, scales)
-    shape, dtype = x.shape, x.dtype
+    home, shape, dtype = _home(), x.shape, x.dtype
     n, rows, c = shape
-    assert _dtype(weight) == G_F32
-    (pr, ldr), (ph, ldh), (py, ldy) = (_maybe_rows(t, shape, dtype) for t in (residual, h, y))
-    pw, ldw = _node_vectors(weight, n, c)
-    p8, ld8, ps = None, 0, None
-    if y8 is not None:
-        import torch
-        p8, ld8, ps = y8.data_ptr(), _node_rows(y8, shape, torch.float8_e4m3fn), _per_row(scales, n * rows)
-    _check(_calls.rms_norm(n, rows, c, x.data_ptr(), _dtype(x), _node_rows(x, shape, dtype), pr, ldr, pw, ldw, eps, ph, ldh, py, ldy,
-                           p8, ld8, ps, _per_row(rstd, n * rows), _stream_ptr(stream)), "rms_norm")
+    px, ldx = _rows(x, shape, dtype, home)
+    pr, ldr = _rows(residual, shape, dtype, home)
+    ph, ldh = _rows(h, shape, dtype, home)
+    py, ldy = _rows(y, shape, dtype, home)
+    p8, ld8 = _rows(y8, shape, _e4m3, home)
+    pw, ldw = _vectors(weight, n, c, home)
+    count = n * rows
+    _check(_calls.rms_norm(n, rows, c, px, _kind(dtype), ldx, pr, ldr, pw, ldw, eps, ph, ldh, py, ldy, p8, ld8,
+                           _flat(scales, count, _f32, home), _flat(rstd, count, _f32, home),
+                           _current_stream(home) if stream is None else stream.cuda_stream), "rms_norm")
 
 
 def rms_norm_grad_workspace_bytes(n, rows, c):
@@ -696,54 +741,55 @@ def rms_norm_grad(h, dy, weight, rstd, dh, dweight, workspace, dresidual=None, s
     """Backward pass of rms_norm: dh (of h's shape and type) is the gradient of x and of residual alike, dresidual (or None) what
     reaches h along the residual stream; dweight [n, c] fp32 or bf16 (a view of the stacked gradient, for instance) is overwritten;
     workspace: uint8 device tensor of at least rms_norm_grad_workspace_bytes(n, rows, c) bytes."""
-    _at_home(h, dy, weight, rstd, dh, dweight, workspace, dresidual)
-    shape, dtype = h.shape, h.dtype
+    home, shape, dtype = _home(), h.shape, h.dtype
     n, rows, c = shape
-    assert _dtype(weight) == G_F32 and workspace.is_cuda and workspace.is_contiguous()
-    pr, lddr = _maybe_rows(dresidual, shape, dtype)
-    (pw, ldw), (pgw, ldgw) = _node_vectors(weight, n, c), _node_vectors(dweight, n, c)
-    _check(_calls.rms_norm_grad(n, rows, c, h.data_ptr(), _dtype(h), _node_rows(h, shape, dtype), dy.data_ptr(),
-                                _node_rows(dy, shape, dtype), pr, lddr, pw, ldw, _per_row(rstd, n * rows), dh.data_ptr(),
-                                _node_rows(dh, shape, dtype), pgw, ldgw, _dtype(dweight), workspace.data_ptr(), workspace.nbytes,
-                                _stream_ptr(stream)), "rms_norm_grad")
+    px, ldx = _rows(h, shape, dtype, home)
+    py, ldy = _rows(dy, shape, dtype, home)
+    pr, ldr = _rows(dresidual, shape, dtype, home)
+    pd, ldd = _rows(dh, shape, dtype, home)
+    pw, ldw = _vectors(weight, n, c, home)
+    assert dweight.get_device() == home, "dweight on the current CUDA device is expected"
+    pg, ldg = _node_vectors(dweight, n, c)
+    ps, nbytes = _scratch(workspace, home)
+    _check(_calls.rms_norm_grad(n, rows, c, px, _kind(dtype), ldx, py, ldy, pr, ldr, pw, ldw, _flat(rstd, n * rows, _f32, home), pd, ldd,
+                                pg, ldg, _kind(dweight.dtype), ps, nbytes,
+                                _current_stream(home) if stream is None else stream.cuda_stream), "rms_norm_grad")
 
 
 def dropout(x, p, state, y, site=0, residual=None, stream=None):
     """y <- residual + dropout(x) (residual may be None) of x [n, rows, c] fp32 or bf16, with probability p of an element to be
     dropped.  state: int64 device tensor (seed, step); site: which of the model's dropouts.  The same call on dy is the backward
     pass."""
-    _at_home(x, state, y, residual)
-    import torch
-    shape, dtype = x.shape, x.dtype
+    home, shape, dtype = _home(), x.shape, x.dtype
     n, rows, c = shape
-    assert state.is_cuda and state.dtype == torch.int64 and state.is_contiguous() and state.numel() == 2, "state: int64 (seed, step)"
-    pr, ldr = _maybe_rows(residual, shape, dtype)
-    _check(_calls.dropout(n, rows, c, x.data_ptr(), _dtype(x), _node_rows(x, shape, dtype), pr, ldr, p, state.data_ptr(), site,
-                          y.data_ptr(), _node_rows(y, shape, dtype), _stream_ptr(stream)), "dropout")
+    (px, ldx), (pr, ldr), (py, ldy) = (_rows(x, shape, dtype, home), _rows(residual, shape, dtype, home),
+                                       _rows(y, shape, dtype, home))
+    _check(_calls.dropout(n, rows, c, px, _kind(dtype), ldx, pr, ldr, p, _flat(state, 2, _i64_t, home), site, py, ldy,
+                          _current_stream(home) if stream is None else stream.cuda_stream), "dropout")
 
 
-def _mask_rows(allowed, n, rows, vocab):
+def _mask_rows(allowed, n, rows, vocab, home):
     """(pointer, words between rows) of a bit mask int32 [n, rows, words]; expanded from one row: 0 words."""
     if allowed is None:
         return None, 0
-    import torch
-    words = (vocab + 31) // 32
-    assert allowed.is_cuda and allowed.dtype == torch.int32 and allowed.dim() == 3 and allowed.shape[:2] == (n, rows), \
-        "a bit mask int32 [n, rows, words] is expected"
-    assert allowed.shape[2] >= words and (allowed.stride(2) == 1 or allowed.shape[2] == 1), "a bit for each token is expected"
-    if allowed.stride(0) == 0 and allowed.stride(1) == 0:
-        return allowed.data_ptr(), 0
-    return allowed.data_ptr(), _node_rows(allowed, allowed.shape, torch.int32)
+    shape = allowed.shape
+    assert allowed.dtype is _i32 and allowed.get_device() == home and shape[:2] == (n, rows) and len(shape) == 3, \
+        "a bit mask int32 [n, rows, words] on the current CUDA device is expected"
+    words = shape[2]
+    assert words * 32 >= vocab, "a bit for each token is expected"
+    if allowed.is_contiguous():
+        return allowed.data_ptr(), words
+    s0, s1, s2 = allowed.stride()
+    assert s2 == 1 or words == 1, "unit stride of the words is expected"
+    return allowed.data_ptr(), 0 if s0 == 0 and s1 == 0 else _node_rows(allowed, shape, _i32)
 
 
-def _texts(history, history_start, count):
+def _texts(history, history_start, count, home):
     if history_start is None:
         assert history is None, "a text needs its bounds"
         return None, 0, None
-    import torch
-    assert history_start.is_cuda and history_start.dtype == torch.int64 and history_start.is_contiguous()
-    assert history_start.numel() == count + 1, "bounds of every row's text are expected"
-    return _tokens(history, history.numel()), history.numel(), history_start.data_ptr()
+    length = history.numel()
+    return _flat(history, length, _i64_t, home), length, _flat(history_start, count + 1, _i64_t, home)
 
 
 def logits_adjust(logits, out, bias=None, allowed=None, history=None, history_start=None, repetition=None, frequency=None,
@@ -752,34 +798,32 @@ def logits_adjust(logits, out, bias=None, allowed=None, history=None, history_st
     may be the logits themselves); bias fp32 [n, vocab]; allowed int32 [n, rows, >= ceil(vocab / 32)], bit v % 32 of word v / 32;
     history int64, all rows' texts one after another, and history_start int64 [n * rows + 1] their bounds; repetition, frequency,
     presence, temperature fp32 [n, rows].  Each may be None."""
-    _at_home(logits, out, bias, allowed, history, history_start, repetition, frequency, presence, temperature)
-    shape, dtype = logits.shape, logits.dtype
+    home, shape, dtype = _home(), logits.shape, logits.dtype
     n, rows, vocab = shape
     count = n * rows
-    assert bias is None or _dtype(bias) == G_F32
-    (pb, ldb), (pm, ldm) = _node_vectors(bias, n, vocab), _mask_rows(allowed, n, rows, vocab)
-    pt, length, ps = _texts(history, history_start, count)
-    rep, freq, pres, temp = (_per_row(t, count) if t is not None else None for t in (repetition, frequency, presence, temperature))
-    _check(_calls.logits_adjust(n, rows, vocab, logits.data_ptr(), _dtype(logits), _node_rows(logits, shape, dtype), pb, ldb, pm, ldm,
-                                pt, length, ps, rep, freq, pres, temp, out.data_ptr(), _node_rows(out, shape, dtype),
-                                _stream_ptr(stream)), "logits_adjust")
+    (pz, ldl), (po, ldo) = _rows(logits, shape, dtype, home), _rows(out, shape, dtype, home)
+    (pb, ldb), (pm, ldm) = _vectors(bias, n, vocab, home), _mask_rows(allowed, n, rows, vocab, home)
+    pt, length, ps = _texts(history, history_start, count, home)
+    _check(_calls.logits_adjust(n, rows, vocab, pz, _kind(dtype), ldl, pb, ldb, pm, ldm, pt, length, ps,
+                                _flat(repetition, count, _f32, home), _flat(frequency, count, _f32, home),
+                                _flat(presence, count, _f32, home), _flat(temperature, count, _f32, home), po, ldo,
+                                _current_stream(home) if stream is None else stream.cuda_stream), "logits_adjust")
 
 
 def logits_adjust_grad(dout, dlogits, logits=None, allowed=None, history=None, history_start=None, repetition=None,
                        temperature=None, stream=None):
     """Backward pass of logits_adjust: dlogits of dout's shape and type (dout itself: in place); logits: as they were before the
     adjustment, needed with repetition; the others as there (biases, frequency and presence have no slope)."""
-    _at_home(dout, dlogits, logits, allowed, history, history_start, repetition, temperature)
-    shape, dtype = dout.shape, dout.dtype
+    home, shape, dtype = _home(), dout.shape, dout.dtype
     n, rows, vocab = shape
     count = n * rows
-    pz, ldl = _maybe_rows(logits, shape, dtype)
-    pm, ldm = _mask_rows(allowed, n, rows, vocab)
-    pt, length, ps = _texts(history, history_start, count)
-    rep, temp = (_per_row(t, count) if t is not None else None for t in (repetition, temperature))
-    _check(_calls.logits_adjust_grad(n, rows, vocab, dout.data_ptr(), _dtype(dout), _node_rows(dout, shape, dtype), pz, ldl, pm, ldm,
-                                     pt, length, ps, rep, temp, dlogits.data_ptr(), _node_rows(dlogits, shape, dtype),
-                                     _stream_ptr(stream)), "logits_adjust_grad")
+    (pg, ldg), (pd, ldd) = _rows(dout, shape, dtype, home), _rows(dlogits, shape, dtype, home)
+    pz, ldl = _rows(logits, shape, dtype, home)
+    pm, ldm = _mask_rows(allowed, n, rows, vocab, home)
+    pt, length, ps = _texts(history, history_start, count, home)
+    _check(_calls.logits_adjust_grad(n, rows, vocab, pg, _kind(dtype), ldg, pz, ldl, pm, ldm, pt, length, ps,
+                                     _flat(repetition, count, _f32, home), _flat(temperature, count, _f32, home), pd, ldd,
+                                     _current_stream(home) if stream is None else stream.cuda_stream), "logits_adjust_grad")
 
 
 def launch_count():
