@@ -28,7 +28,7 @@ int check_table(int n, int64_t rows, int64_t vocab, int64_t c) {
 }
 int check_logits(int n, int64_t rows, int64_t vocab) {
     if (n < 1 || rows < 0 || vocab < 1) return DLM_ERR_SHAPE;
-    if (n > DLM_MAX_NODES || !fits(rows, n) || rows * n > 0x7fffffff || vocab > 0x7fffffff) return DLM_ERR_UNSUPPORTED;
+    if (n > DLM_MAX_NODES || !fits(rows, n) || rows * n > 0x7fffffff || vocab > (1 << 30)) return DLM_ERR_UNSUPPORTED;
     return DLM_OK;
 }
 // An output may lie on an input only row by row.
