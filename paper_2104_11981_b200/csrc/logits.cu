@@ -2,7 +2,7 @@
 // the row's text has v, rho, f, p the row's penalties and T its temperature:
 //   z1 = k > 0 ? (z > 0 ? z / rho : z rho) - f k - p : z ,   out = (z1 + bias_v) / T ,   -inf where the mask forbids v ;
 //   dlogits = dout / T (k > 0 ? (z > 0 ? 1 / rho : rho) : 1) ,   0 where the mask forbids v.
-// A CTA takes a tile of a row: its elements are on their way into registers while it counts the row's text in shared memory
+// A CTA takes a tile of a row: its elements are on their way into registers while it marks and counts the row's text in shared memory
 // (whole numbers: the order of the additions does not matter).  One read and one write of the logits.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -19,136 +19,149 @@ namespace {
 
 using namespace dlm;
 
+// What a row's elements are mapped by.
 struct Adjust {
-    float repetition, frequency, presence, cooling;  // cooling = 1 / T
+    float up, down, frequency, presence, cooling;  // repetition and its reciprocal, 1 / T
+    const float* bias;
 };
 
-// An element without bias, temperature and mask: d is mapped (the logit z itself, or the gradient).
+// An element d (the logit, or the gradient): `marked`: the text has it, `count` times; `positive`: its logit is above 0.
 template <bool GRAD>
-__device__ __forceinline__ float penalised(const Adjust& a, float d, float z, int count) {
-    d = z > 0.0f ? d / a.repetition : d * a.repetition;
-    if constexpr (!GRAD) d = d - a.frequency * (float)count - a.presence;
-    return d;
+__device__ __forceinline__ float penalised(const Adjust& a, float d, bool positive, int count) {
+    d *= positive ? a.down : a.up;
+    return GRAD ? d : d - fmaf(a.frequency, (float)count, a.presence);
 }
 
 // A row lies in memory as chunks of LEN elements (16 bytes wherever the row starts, or one element); the first begins `skew` elements
-// before the row.  A CTA takes THREADS U chunks: U a thread, THREADS apart.
-template <typename T, bool GRAD, int LEN, int THREADS, int U>
+// before the row.  A CTA takes THREADS U chunks: U a thread, THREADS apart.  Chunks and masks are on their way into registers while the
+// CTA marks the row's text in a bit map, and (COUNTS) counts it: counts of marked elements alone are cleared, added to and read.  For the
+// gradient, whoever marks an element first fetches its logit and notes the sign, all of them at once; asking for it where the element is
+// mapped would let nearly every warp wait for memory a second time.
+template <typename T, bool GRAD, bool COUNTS, int LEN, int THREADS, int U>
 __global__ void __launch_bounds__(THREADS) logits_kernel(dlm_logits_args a, int tiles) {
-    constexpr int TILE = THREADS * U * LEN;
-    extern __shared__ __align__(16) int counts[];  // [TILE] where there are texts
+    constexpr int TILE = THREADS * U * LEN, WORDS = (TILE + 31) / 32;
+    extern __shared__ int counts[];  // [TILE]
+    __shared__ uint32_t marks[WORDS], positives[GRAD ? WORDS : 1];
     const long long row = blockIdx.x / tiles, node = row / a.rows;
     const T* in = static_cast<const T*>(a.in) + row * a.ldi;
     T* out = static_cast<T*>(a.out) + row * a.ldo;
     const int skew = LEN > 1 ? (int)((uintptr_t)in & 15) / (int)sizeof(T) : 0;
-    const long long tile0 = (long long)(blockIdx.x % tiles) * TILE - skew;  // the tile's first element
     const int vocab = (int)a.vocab;
+    const int tile0 = (int)((blockIdx.x % tiles) * TILE) - skew;  // the tile's first element
+    auto chunk_at = [&](int u) { return tile0 + (u * THREADS + (int)threadIdx.x) * LEN; };
+    auto whole = [&](int v) { return v >= 0 && v + LEN <= vocab; };
     pdl_wait();
     pdl_release();
-    Words raw[U];  // LEN > 1: the chunk; else one element
-    auto chunk_at = [&](int u) { return (int)(tile0 + (long long)(u * THREADS + (int)threadIdx.x) * LEN); };
+    long long from = 0, to = 0;
+    if (a.history_start) {
+        from = max(0ll, (long long)a.history_start[row]);
+        to = min((long long)a.history_length, (long long)a.history_start[row + 1]);
+    }
+    Adjust how;
+    how.up = a.repetition ? a.repetition[row] : 1.0f;
+    how.frequency = a.frequency ? a.frequency[row] : 0.0f;
+    how.presence = a.presence ? a.presence[row] : 0.0f;
+    how.cooling = a.temperature ? a.temperature[row] : 1.0f;
+    how.bias = !GRAD && a.bias ? a.bias + node * a.ldb : nullptr;
+    const uint32_t* allowed = a.allowed ? a.allowed + row * a.ldm : nullptr;
+    // bit k: element v + k is allowed
+    auto allowed_bits = [&](int v) {
+        const int shift = v & 31;
+        uint32_t b = allowed[v >> 5] >> shift;
+        if (LEN > 1 && shift > 32 - LEN) b |= allowed[(v >> 5) + 1] << (32 - shift);
+        return b;
+    };
+    Words raw[U];      // LEN > 1: the chunk; else one element
+    uint32_t bits[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int v = chunk_at(u);
-        if constexpr (LEN > 1) {
-            if (v >= 0 && v + LEN <= vocab) {
+        bits[u] = 0xffffffffu;
+        if (whole(v)) {
+            if constexpr (LEN > 1)
                 raw[u] = ld_words(in + v);
-            } else {
-                float e[LEN];
-#pragma unroll
-                for (int k = 0; k < LEN; ++k) e[k] = v + k >= 0 && v + k < vocab ? widen(in[v + k]) : 0.0f;
-                raw[u] = pack<T>(e);
-            }
-        } else {
-            raw[u].w[0] = v < vocab ? __float_as_uint(widen(in[v])) : 0u;
+            else
+                raw[u].w[0] = __float_as_uint(widen(in[v]));
+            if (allowed) bits[u] = allowed_bits(v);
         }
     }
-    Adjust how;
-    how.repetition = a.repetition ? a.repetition[row] : 1.0f;
-    how.frequency = a.frequency ? a.frequency[row] : 0.0f;
-    how.presence = a.presence ? a.presence[row] : 0.0f;
-    how.cooling = a.temperature ? 1.0f / a.temperature[row] : 1.0f;
-    bool texts = false;
-    if (a.history_start) {
-        const long long from = max(0ll, (long long)a.history_start[row]), to = min((long long)a.history_length, (long long)a.history_start[row + 1]);
-        texts = from < to;
-        if (texts) {
-#pragma unroll
-            for (int k = 0; k < U * LEN; k += 4 <= LEN ? 4 : 1) {
-                if constexpr (LEN >= 4)
-                    *reinterpret_cast<int4*>(counts + (k / 4 * THREADS + threadIdx.x) * 4) = make_int4(0, 0, 0, 0);
-                else
-                    counts[k * THREADS + threadIdx.x] = 0;
-            }
-            __syncthreads();
+    how.down = 1.0f / how.up;
+    how.cooling = 1.0f / how.cooling;
+    const bool texts = a.history_start != nullptr;
+    if (texts) {
+        for (int k = threadIdx.x; k < WORDS; k += THREADS) {
+            marks[k] = 0;
+            if (GRAD) positives[k] = 0;
+        }
+        __syncthreads();
+        const T* z = GRAD ? static_cast<const T*>(a.logits) + row * a.ldl + tile0 : nullptr;
+        auto each = [&](auto&& f) {
 #pragma unroll 4
             for (long long k = from + threadIdx.x; k < to; k += THREADS) {
                 const int64_t token = a.history[k], at = token - tile0;
-                if (token >= 0 && token < vocab && at >= 0 && at < TILE) atomicAdd(&counts[at], 1);
+                if (token >= 0 && token < vocab && at >= 0 && at < TILE) f((int)at);
             }
+        };
+        each([&](int at) {
+            const uint32_t bit = 1u << (at & 31), old = atomicOr(&marks[at >> 5], bit);
+            if (GRAD && !(old & bit) && widen(z[at]) > 0.0f) atomicOr(&positives[at >> 5], bit);
+            if (COUNTS) counts[at] = 0;
+        });
+        __syncthreads();
+        if constexpr (COUNTS) {
+            each([&](int at) { atomicAdd(&counts[at], 1); });
             __syncthreads();
         }
     }
-    const uint32_t* allowed = a.allowed ? a.allowed + row * a.ldm : nullptr;
-    const float* bias = !GRAD && a.bias ? a.bias + node * a.ldb : nullptr;
-    const T* z = GRAD && a.logits ? static_cast<const T*>(a.logits) + row * a.ldl : nullptr;
+    constexpr uint32_t ALL = (uint32_t)((1ull << LEN) - 1);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int v = chunk_at(u);
-        if (v >= vocab) break;
+        if (!whole(v)) continue;
         float d[LEN];
         if constexpr (LEN > 1)
             unpack<T>(raw[u], d);
         else
             d[0] = __uint_as_float(raw[u].w[0]);
         if (texts) {
-            int count[LEN], any = 0;
-            const int* mine = counts + (u * THREADS + threadIdx.x) * LEN;
-#pragma unroll
-            for (int k = 0; k < LEN; k += 4 <= LEN ? 4 : 1) {
-                if constexpr (LEN >= 4) {
-                    const int4 c = *reinterpret_cast<const int4*>(mine + k);
-                    count[k] = c.x;
-                    count[k + 1] = c.y;
-                    count[k + 2] = c.z;
-                    count[k + 3] = c.w;
-                    any |= c.x | c.y | c.z | c.w;
-                } else {
-                    any = count[k] = mine[k];
-                }
-            }
-            if (any) {
+            const int at = (u * THREADS + (int)threadIdx.x) * LEN;  // LEN divides 32: a chunk's marks are in one word
+            const uint32_t marked = marks[at >> 5] >> (at & 31) & ALL;
+            if (marked) {
+                const uint32_t positive = GRAD ? positives[at >> 5] >> (at & 31) : 0;
 #pragma unroll
                 for (int k = 0; k < LEN; ++k)
-                    if (count[k] > 0) d[k] = penalised<GRAD>(how, d[k], GRAD && z ? widen(z[v + k]) : d[k], count[k]);
+                    if ((marked >> k) & 1) d[k] = penalised<GRAD>(how, d[k], GRAD ? (positive >> k) & 1 : d[k] > 0.0f, COUNTS ? counts[at + k] : 1);
             }
         }
-        if (bias) {
+        if (how.bias) {
+#pragma unroll
+            for (int k = 0; k < LEN; ++k) d[k] += how.bias[v + k];
+        }
+#pragma unroll
+        for (int k = 0; k < LEN; ++k) d[k] *= how.cooling;
+        if ((bits[u] & ALL) != ALL) {
 #pragma unroll
             for (int k = 0; k < LEN; ++k)
-                if (v + k >= 0 && v + k < vocab) d[k] += bias[v + k];
+                if (!((bits[u] >> k) & 1)) d[k] = GRAD ? 0.0f : -INFINITY;
         }
-        uint32_t bits = 0xffffffffu;  // bit k: element k is allowed
-        if (allowed) {
-            const int first = max(v, 0), shift = first & 31;
-            bits = allowed[first >> 5] >> shift;
-            if (LEN > 1 && shift > 32 - LEN && (first | 31) + 1 < vocab) bits |= allowed[(first >> 5) + 1] << (32 - shift);
-            if (v < 0) bits <<= -v;
-        }
-#pragma unroll
-        for (int k = 0; k < LEN; ++k) d[k] = (bits >> k) & 1 ? d[k] * how.cooling : GRAD ? 0.0f : -INFINITY;
-        if constexpr (LEN > 1) {
-            if (v >= 0 && v + LEN <= vocab) {
-                st_words(out + v, pack<T>(d));
-            } else {
-#pragma unroll
-                for (int k = 0; k < LEN; ++k)
-                    if (v + k >= 0 && v + k < vocab) out[v + k] = narrow<T>(d[k]);
-            }
-        } else {
+        if constexpr (LEN > 1)
+            st_words(out + v, pack<T>(d));
+        else
             out[v] = narrow<T>(d[0]);
-        }
     }
+    if (LEN == 1 || (int)threadIdx.x >= 2 * LEN) return;
+    // elements of the row's first and last chunk that are not whole
+    const int last = vocab - (vocab + skew) % LEN;  // where that chunk begins
+    const int v = (int)threadIdx.x < LEN ? (skew > 0 ? (int)threadIdx.x - skew : -1) : max(last, 0) + (int)threadIdx.x - LEN;
+    const int at = v - tile0;
+    if (v < 0 || v >= vocab || at < 0 || at >= TILE || ((int)threadIdx.x >= LEN && v + skew < LEN && skew > 0)) return;
+    float d = widen(in[v]);
+    if (texts && (marks[at >> 5] >> (at & 31) & 1))
+        d = penalised<GRAD>(how, d, GRAD ? positives[at >> 5] >> (at & 31) & 1 : d > 0.0f, COUNTS ? counts[at] : 1);
+    if (how.bias) d += how.bias[v];
+    d *= how.cooling;
+    if (allowed && !(allowed[v >> 5] >> (v & 31) & 1)) d = GRAD ? 0.0f : -INFINITY;
+    out[v] = narrow<T>(d);
 }
 
 template <typename T, bool GRAD, int LEN, int THREADS, int U>
@@ -157,8 +170,15 @@ int run(const dlm_logits_args& a, cudaStream_t s) {
     const int tiles = (int)((a.vocab + (LEN - 1) + TILE - 1) / TILE);  // a row may begin anywhere in its first chunk
     const int64_t ctas = a.n * a.rows * tiles;
     if (ctas > 0x7fffffff) return DLM_ERR_UNSUPPORTED;
-    cudaError_t err = launch_overlapped(logits_kernel<T, GRAD, LEN, THREADS, U>, dim3((unsigned)ctas), dim3(THREADS),
-                                        a.history_start ? TILE * sizeof(int) : 0, s, 1, a, tiles);
+    const bool counted = !GRAD && a.history_start && a.frequency;  // the other penalties only ask whether
+    auto kern = logits_kernel<T, GRAD, false, LEN, THREADS, U>;
+    if constexpr (!GRAD) {
+        if (counted) kern = logits_kernel<T, GRAD, true, LEN, THREADS, U>;
+        if (counted && TILE * sizeof(int) > (48 << 10) - 8192 &&
+            cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, TILE * sizeof(int)) != cudaSuccess)
+            return DLM_ERR_CUDA;
+    }
+    cudaError_t err = launch_overlapped(kern, dim3((unsigned)ctas), dim3(THREADS), counted ? TILE * sizeof(int) : 0, s, 1, a, tiles);
     dlm_count_launch(1);
     return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
 }
