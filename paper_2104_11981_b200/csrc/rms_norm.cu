@@ -46,6 +46,109 @@ __device__ __forceinline__ float warp_max(float v) {
     return v;
 }
 
+// Where rows do not start on 16 bytes (SKEW), but all arrays' rows do so alike, a group takes rows that start at the same place of their
+// first chunk: every P-th row, P <= 8.  Chunks of memory are then the same columns in each of its rows, and a thread copies, keeps and
+// writes whole chunks of its own as elsewhere; the elements of the first and last chunk that belong to other rows are masked.
+// A thread's first column in run u.
+template <int LEN, int TPR>
+__device__ __forceinline__ int run_column(int t, int u, int skew) { return column<LEN, TPR>(t, u) - skew; }
+
+// The thread's chunks of a row into the slot, zeros behind its end.  Nothing is read before the array or beyond the row.
+template <typename T, int LEN, int E, int TPR>
+__device__ __forceinline__ void fetch_chunks(unsigned char* buf, const T* row, const T* array, int skew, int c, int t) {
+    const uint32_t to = (uint32_t)__cvta_generic_to_shared(buf) + t * 16;
+    int at = t * LEN - skew;
+    row += at;
+#pragma unroll
+    for (int u = 0; u < E / LEN; ++u) {
+        if (at < c) {
+            if (u == 0 && row < array)  // the first row of all: its bytes alone
+#pragma unroll 1
+                for (int k = skew; k < min(LEN, c + skew); ++k) reinterpret_cast<T*>(buf)[k] = row[k];
+            else
+                copy_chunk(to + u * TPR * 16, row + u * TPR * LEN, min(LEN, c - at) * (int)sizeof(T));
+        }
+        at += TPR * LEN;
+    }
+}
+// Where a row ends within its chunks.
+template <typename T, int LEN>
+struct Ends {
+    int skew, rest, last;  // elements of another row before it, its own in a last chunk that is not whole, and that chunk
+    __device__ __forceinline__ Ends(int skew, int c) : skew(skew), rest((c + skew) % LEN), last((c + skew) / LEN) {}
+};
+// The same by bulk copies, by one thread: all of the row's chunks, or, of the first and the last row of all, those within the array and
+// the other elements one by one (which the arrival on the barrier, behind them, makes visible).
+template <typename T, int LEN>
+__device__ __forceinline__ uint32_t bulk_bytes(const Ends<T, LEN>& e, bool first, bool end) {
+    return (uint32_t)(e.last + (e.rest > 0 && !end) - (e.skew > 0 && first)) * 16;
+}
+template <typename T, int LEN>
+__device__ __forceinline__ void lone_elements(unsigned char* buf, const T* row, const Ends<T, LEN>& e, bool first, bool end) {
+    T* to = reinterpret_cast<T*>(buf);
+    if (first && e.skew > 0)
+        for (int k = e.skew; k < LEN; ++k) to[k] = row[k - e.skew];
+    if (end)
+        for (int k = 0; k < e.rest; ++k) to[e.last * LEN + k] = row[e.last * LEN + k - e.skew];
+}
+template <typename T, int LEN>
+__device__ __forceinline__ void bulk_chunks(unsigned char* buf, const T* row, const Ends<T, LEN>& e, bool first, bool end, uint32_t bar) {
+    const int lo = e.skew > 0 && first;
+    bulk_row(buf + lo * 16, row - e.skew + lo * LEN, bulk_bytes(e, first, end), bar);
+}
+// What a row's first and last chunk hold of other rows counts nothing: the threads that have these chunks clear it.
+template <typename T, int LEN, int TPR>
+__device__ __forceinline__ void clear_ends(unsigned char* buf, const Ends<T, LEN>& e, int t) {
+    const bool head = t == 0 && e.skew > 0, tail = t == e.last % TPR && e.rest > 0;
+    if (!head && !tail) return;
+    T* to = reinterpret_cast<T*>(buf);
+#pragma unroll
+    for (int k = 0; k < LEN; ++k) {
+        if (head && k < e.skew) to[k] = narrow<T>(0.0f);
+        if (tail && k >= e.rest) to[e.last * LEN + k] = narrow<T>(0.0f);
+    }
+}
+template <typename T, int LEN, int TPR, bool SKEW>
+__device__ __forceinline__ void run_values(const unsigned char* buf, int skew, int c, int t, int u, float* v) {
+    if constexpr (SKEW) {
+        Words a = {{0u, 0u, 0u, 0u}};
+        if (run_column<LEN, TPR>(t, u, skew) < c) a = ld_words(buf + column<LEN, TPR>(t, u) * (int)sizeof(T));
+        unpack<T>(a, v);
+    } else {
+        one_run<T, LEN, TPR>(buf, skew, c, t, u, v);
+    }
+}
+template <int LEN, int E, int TPR>
+__device__ __forceinline__ void run_params(const float* p, int skew, int c, int t, float* v) {
+#pragma unroll
+    for (int u = 0; u < E / LEN; ++u)
+#pragma unroll
+        for (int k = 0; k < LEN; ++k) {
+            const int at = run_column<LEN, TPR>(t, u, skew) + k;
+            v[u * LEN + k] = at >= 0 && at < c ? p[at] : 0.0f;
+        }
+}
+// A row of results (none where c is below 0): whole chunks straight to memory, the elements of the first and the last one through `ends` (32 bytes of the group's), a
+// thread each.
+template <typename T, int LEN, int E, int TPR>
+__device__ __forceinline__ void put_chunks(T* row, unsigned char* ends, const Ends<T, LEN>& e, int c, int t, const float* v) {
+#pragma unroll
+    for (int u = 0; u < E / LEN; ++u) {
+        const int at = run_column<LEN, TPR>(t, u, e.skew);
+        if (at >= 0 && at + LEN <= c)
+            st_words(row + at, pack<T>(v + u * LEN));
+        else if (at < c)
+            st_words(ends + (at < 0 ? 0 : 16), pack<T>(v + u * LEN));
+    }
+    const T* staged = reinterpret_cast<const T*>(ends);
+    if (t / 32 == 0 || t / 32 == e.last % TPR / 32) {  // the warps that have the ends
+        __syncwarp();
+        if (t < LEN && t >= e.skew && e.skew > 0 && t - e.skew < c) row[t - e.skew] = staged[t];
+        if (c > 0 && (e.last > 0 || e.skew == 0) && e.last % TPR / 8 == t / 8 && t % 8 < e.rest) row[e.last * LEN - e.skew + t % 8] = staged[16 / (int)sizeof(T) + t % 8];
+        __syncwarp();  // they may be written again
+    }
+}
+
 // A sum, and (TOP) a maximum, over the group of a row; returns whether all threads had `ok`.  One barrier, which also frees the row's
 // slot where rows come by bulk copies, since its values are in registers by then.
 template <int TPR, bool BULK, bool TOP>
@@ -84,9 +187,14 @@ __device__ __forceinline__ void put_e4m3(unsigned char* to, const float* v) {
         *to = e4m3_one(v[0]);
 }
 
+// 128 registers a thread suffice; left alone, the compiler takes up to 180 where rows are skewed, and half of the CTAs fit.  (bf16 forward, skewed:
+// 64 do, 4 x 4000 x 2201 with residual 73 us instead of 94; fp32 rows are better off with 128, 4 x 4000 x 1502 70 us instead of 73.)
+template <int TPR>
+constexpr int kLeastCtas = 512 / kBlock<TPR>;
+
 // Groups of TPR threads take every G-th row of a node; x and the residual come D - 1 rows ahead.  EIGHT: the 8-bit output, too.
-template <typename T, int LEN, int E, int TPR, int D, bool EIGHT>
-__global__ void __launch_bounds__(kBlock<TPR>)
+template <typename T, int LEN, int E, int TPR, int D, bool EIGHT, bool SKEW>
+__global__ void __launch_bounds__(kBlock<TPR>, (SKEW && sizeof(T) == 2 && !EIGHT && E <= 16 ? 2 : 1) * kLeastCtas<TPR>)
     rms_norm_kernel(long long rows, int c, const T* x, long long ldx, const T* residual, long long ldr, const float* weight, long long ldw,
                     float eps, T* h, long long ldh, T* y, long long ldy, unsigned char* y8, long long ld8, float* scales, float* rstd) {
     constexpr int GROUPS = kBlock<TPR> / TPR, WARPS = TPR / 32;
@@ -103,6 +211,9 @@ __global__ void __launch_bounds__(kBlock<TPR>)
     const long long first = (long long)blockIdx.x * GROUPS + group, base = (long long)node * rows;
     const T *fetch = x + (base + first) * ldx, *fetch_r = residual + (base + first) * ldr;  // the next row to ask for
     const T *row = fetch, *row_r = fetch_r;
+    const int skew = SKEW ? row_skew(row) / (int)sizeof(T) : 0;
+    const Ends<T, LEN> ends(skew, c);
+    __shared__ __align__(16) unsigned char staged[SKEW ? GROUPS : 1][2][32];
     long long asked = first;
     if constexpr (BULK) {
         if (threadIdx.x == 0) {
@@ -115,7 +226,25 @@ __global__ void __launch_bounds__(kBlock<TPR>)
     pdl_release();
     auto ask = [&](int k) {  // the next row, into slot k
         unsigned char* buf = in + k * slot_bytes;
-        if constexpr (BULK) {
+        // by the last warp, since the first one has the row's beginning to see to (gradient of 4 x 4000 x 2201 bf16 94 us with the first, 83)
+        if constexpr (SKEW && BULK) {
+            if (threadIdx.x == TPR - 32 && asked < rows) {
+                const bool lead = base + asked == 0, end = base + asked == (long long)gridDim.y * rows - 1;
+                if (lead || end) {
+                    lone_elements<T, LEN>(buf, fetch, ends, lead, end);
+                    if (residual) lone_elements<T, LEN>(buf + rb, fetch_r, ends, lead, end);
+                }
+                mbar_expect_tx(smem_u32(&full[k]), (residual ? 2 : 1) * bulk_bytes<T, LEN>(ends, lead, end));
+                bulk_chunks<T, LEN>(buf, fetch, ends, lead, end, smem_u32(&full[k]));
+                if (residual) bulk_chunks<T, LEN>(buf + rb, fetch_r, ends, lead, end, smem_u32(&full[k]));
+            }
+        } else if constexpr (SKEW) {
+            if (asked < rows) {
+                fetch_chunks<T, LEN, E, TPR>(buf, fetch, x, skew, c, t);
+                if (residual) fetch_chunks<T, LEN, E, TPR>(buf + rb, fetch_r, residual, skew, c, t);
+            }
+            commit_copies();
+        } else if constexpr (BULK) {
             if (threadIdx.x == 0 && asked < rows) {
                 mbar_expect_tx(smem_u32(&full[k]), residual ? 2 * bytes : bytes);
                 bulk_row(buf, fetch, bytes, smem_u32(&full[k]));
@@ -135,7 +264,7 @@ __global__ void __launch_bounds__(kBlock<TPR>)
 #pragma unroll
     for (int k = 0; k < D - 1; ++k) ask(k);
     float w[E];
-    params<LEN, E, TPR>(weight + node * ldw, c, t, w);
+    run_params<LEN, E, TPR>(weight + node * ldw, skew, c, t, w);
     const float inv_c = 1.0f / (float)c;
     int slot = 0, side = 0;
     uint32_t parities = 0;  // of each slot's next phase
@@ -148,19 +277,24 @@ __global__ void __launch_bounds__(kBlock<TPR>)
             ok = mbar_wait(smem_u32(&full[slot]), (parities >> slot) & 1);
         } else {
             wait_copies<D - 1>();
-            group_barrier<TPR>();
+            if constexpr (!SKEW) group_barrier<TPR>();  // else the thread's own chunks are all it needs
         }
         const bool live = BULK || r < rows;
-        const int live_c = live ? c : 0;
+        const int live_c = live ? c : SKEW ? -LEN : 0;  // no column is below it
         const unsigned char* buf = in + slot * slot_bytes;
+        if constexpr (SKEW) {
+            clear_ends<T, LEN, TPR>(in + slot * slot_bytes, ends, t);
+            if (residual) clear_ends<T, LEN, TPR>(in + slot * slot_bytes + rb, ends, t);
+        }
         float v[E];
-        row_values<T, LEN, E, TPR>(buf, row_skew(row), live_c, t, v);
+        const int s0 = SKEW ? skew : row_skew(row), s1 = SKEW ? skew : row_skew(row_r);
+#pragma unroll
+        for (int u = 0; u < E / LEN; ++u) run_values<T, LEN, TPR, SKEW>(buf, s0, live_c, t, u, v + u * LEN);
         if (residual) {
-            const int skew = row_skew(row_r);
 #pragma unroll
             for (int u = 0; u < E / LEN; ++u) {
                 float a[LEN];
-                one_run<T, LEN, TPR>(buf + rb, skew, live_c, t, u, a);
+                run_values<T, LEN, TPR, SKEW>(buf + rb, s1, live_c, t, u, a);
 #pragma unroll
                 for (int k = 0; k < LEN; ++k) v[u * LEN + k] += a[k];
             }
@@ -181,7 +315,13 @@ __global__ void __launch_bounds__(kBlock<TPR>)
         side ^= 1;
         const float rs = rsqrtf(fmaf(sum, inv_c, eps));
         const long long at = base + r;
-        if (h && live) put_values<T, LEN, E, TPR>(h + at * ldh, out, c, t, v);
+        auto put = [&](T* to, int which) {
+            if constexpr (SKEW)
+                put_chunks<T, LEN, E, TPR>(to, staged[group][which], ends, live_c, t, v);
+            else if (live)
+                put_values<T, LEN, E, TPR>(to, out + which * rb, c, t, v);
+        };
+        if (h) put(h + at * ldh, 0);
         if constexpr (EIGHT) {
             const ToE4M3 map(top);
             if (live) {
@@ -190,8 +330,15 @@ __global__ void __launch_bounds__(kBlock<TPR>)
                     float q[LEN];
 #pragma unroll
                     for (int k = 0; k < LEN; ++k) q[k] = map(v[u * LEN + k] * w[u * LEN + k]);
-                    const int col = column<LEN, TPR>(t, u);
-                    if (col < c) put_e4m3<LEN>(y8 + at * ld8 + col, q);
+                    const int col = run_column<LEN, TPR>(t, u, skew);
+                    unsigned char* to = y8 + at * ld8 + col;
+                    if (!SKEW || (col >= 0 && col + LEN <= c && (uintptr_t)to % LEN == 0)) {
+                        if (col < c) put_e4m3<LEN>(to, q);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < LEN; ++k)
+                            if (col + k >= 0 && col + k < c) to[k] = e4m3_one(q[k]);
+                    }
                 }
                 if (t == 0) scales[at] = top * rs / kE4M3Max;
             }
@@ -203,10 +350,10 @@ __global__ void __launch_bounds__(kBlock<TPR>)
                 v[e] = o.x;
                 v[e + 1] = o.y;
             }
-            if (live) put_values<T, LEN, E, TPR>(y + at * ldy, out + rb, c, t, v);
+            put(y + at * ldy, 1);
         }
         if (t == 0 && live) rstd[at] = rs;
-        if constexpr (!BULK) group_barrier<TPR>();  // the slot may be filled again, and the results are in their buffers
+        if constexpr (!BULK && !SKEW) group_barrier<TPR>();  // the slot may be filled again, and the results are in their buffers
         if (LEN == 1 && live) {
             if (h) flush_row<T, TPR>(h + at * ldh, out, c, t);
             if (!EIGHT || y) flush_row<T, TPR>(y + at * ldy, out + rb, c, t);
@@ -267,8 +414,8 @@ __global__ void __launch_bounds__(1024)
 }
 
 // As forward, with h, dy and the residual's gradient; partial[(node G + CTA) c + column]: the sums over the rows of one CTA.
-template <typename T, int LEN, int E, int TPR, int D>
-__global__ void __launch_bounds__(kBlock<TPR>)
+template <typename T, int LEN, int E, int TPR, int D, bool SKEW>
+__global__ void __launch_bounds__(kBlock<TPR>, kLeastCtas<TPR>)
     rms_norm_grad_kernel(long long rows, int c, const T* h, long long ldh, const T* dy, long long lddy, const T* dres, long long lddr,
                          const float* weight, long long ldw, const float* rstd, T* dh, long long lddh, float* partial) {
     constexpr int GROUPS = kBlock<TPR> / TPR;
@@ -288,6 +435,9 @@ __global__ void __launch_bounds__(kBlock<TPR>)
     const T *hr = hf, *gr = gf, *er = ef;
     T* to = dh + (base + first) * lddh;
     const float* w = weight + node * ldw;
+    const int skew = SKEW ? row_skew(hr) / (int)sizeof(T) : 0;
+    const Ends<T, LEN> ends(skew, c);
+    __shared__ __align__(16) unsigned char staged[SKEW ? GROUPS : 1][2][32];
     long long asked = first;
     rstd += base;
     if constexpr (BULK) {
@@ -301,7 +451,27 @@ __global__ void __launch_bounds__(kBlock<TPR>)
     pdl_release();
     auto ask = [&](int k) {  // the next row, into slot k
         unsigned char* buf = in + k * slot_bytes;
-        if constexpr (BULK) {
+        if constexpr (SKEW && BULK) {
+            if (threadIdx.x == TPR - 32 && asked < rows) {
+                const bool lead = base + asked == 0, end = base + asked == (long long)gridDim.y * rows - 1;
+                if (lead || end) {
+                    lone_elements<T, LEN>(buf, hf, ends, lead, end);
+                    lone_elements<T, LEN>(buf + rb, gf, ends, lead, end);
+                    if (dres) lone_elements<T, LEN>(buf + 2 * rb, ef, ends, lead, end);
+                }
+                mbar_expect_tx(smem_u32(&full[k]), (dres ? 3 : 2) * bulk_bytes<T, LEN>(ends, lead, end));
+                bulk_chunks<T, LEN>(buf, hf, ends, lead, end, smem_u32(&full[k]));
+                bulk_chunks<T, LEN>(buf + rb, gf, ends, lead, end, smem_u32(&full[k]));
+                if (dres) bulk_chunks<T, LEN>(buf + 2 * rb, ef, ends, lead, end, smem_u32(&full[k]));
+            }
+        } else if constexpr (SKEW) {
+            if (asked < rows) {
+                fetch_chunks<T, LEN, E, TPR>(buf, hf, h, skew, c, t);
+                fetch_chunks<T, LEN, E, TPR>(buf + rb, gf, dy, skew, c, t);
+                if (dres) fetch_chunks<T, LEN, E, TPR>(buf + 2 * rb, ef, dres, skew, c, t);
+            }
+            commit_copies();
+        } else if constexpr (BULK) {
             if (threadIdx.x == 0 && asked < rows) {
                 mbar_expect_tx(smem_u32(&full[k]), (dres ? 3 : 2) * bytes);
                 bulk_row(buf, hf, bytes, smem_u32(&full[k]));
@@ -324,7 +494,7 @@ __global__ void __launch_bounds__(kBlock<TPR>)
 #pragma unroll
     for (int k = 0; k < D - 1; ++k) ask(k);
     float wv[HOLD ? E : 1];
-    if constexpr (HOLD) params<LEN, E, TPR>(w, c, t, wv);
+    if constexpr (HOLD) run_params<LEN, E, TPR>(w, skew, c, t, wv);
     float dw[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) dw[e] = 0.0f;
@@ -343,21 +513,28 @@ __global__ void __launch_bounds__(kBlock<TPR>)
             ok = mbar_wait(smem_u32(&full[slot]), (parities >> slot) & 1);
         } else {
             wait_copies<D - 1>();
-            group_barrier<TPR>();
+            if constexpr (!SKEW) group_barrier<TPR>();  // else the thread's own chunks are all it needs
         }
         const bool live = BULK || r < rows;
-        const int live_c = live ? c : 0;
+        const int live_c = live ? c : SKEW ? -LEN : 0;  // no column is below it
         const unsigned char *hb = in + slot * slot_bytes, *gb = hb + rb, *eb = gb + rb;
-        const int hs = row_skew(hr), gs = row_skew(gr), es = row_skew(er);
+        const int hs = SKEW ? skew : row_skew(hr), gs = SKEW ? skew : row_skew(gr), es = SKEW ? skew : row_skew(er);
+        if constexpr (SKEW) {
+            clear_ends<T, LEN, TPR>(in + slot * slot_bytes, ends, t);
+            clear_ends<T, LEN, TPR>(in + slot * slot_bytes + rb, ends, t);
+            if (dres) clear_ends<T, LEN, TPR>(in + slot * slot_bytes + 2 * rb, ends, t);
+        }
         float sum = 0.0f, none = 0.0f;
         float xh[HOLD ? E : LEN], v[HOLD ? E : LEN], more[HOLD ? E : LEN];
         if constexpr (HOLD) {
             float2 s2 = make_float2(0.0f, 0.0f);
-            row_values<T, LEN, E, TPR>(hb, hs, live_c, t, xh);
-            row_values<T, LEN, E, TPR>(gb, gs, live_c, t, v);
-            if (dres) {
-                row_values<T, LEN, E, TPR>(eb, es, live_c, t, more);
-            } else {
+#pragma unroll
+            for (int u = 0; u < E / LEN; ++u) {
+                run_values<T, LEN, TPR, SKEW>(hb, hs, live_c, t, u, xh + u * LEN);
+                run_values<T, LEN, TPR, SKEW>(gb, gs, live_c, t, u, v + u * LEN);
+                if (dres) run_values<T, LEN, TPR, SKEW>(eb, es, live_c, t, u, more + u * LEN);
+            }
+            if (!dres) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) more[e] = 0.0f;
             }
@@ -377,14 +554,14 @@ __global__ void __launch_bounds__(kBlock<TPR>)
         } else {
 #pragma unroll
             for (int u = 0; u < E / LEN; ++u) {
-                one_run<T, LEN, TPR>(hb, hs, live_c, t, u, xh);
-                one_run<T, LEN, TPR>(gb, gs, live_c, t, u, v);
+                run_values<T, LEN, TPR, SKEW>(hb, hs, live_c, t, u, xh);
+                run_values<T, LEN, TPR, SKEW>(gb, gs, live_c, t, u, v);
 #pragma unroll
                 for (int k = 0; k < LEN; ++k) {
-                    const int at = column<LEN, TPR>(t, u) + k;
+                    const int at = run_column<LEN, TPR>(t, u, skew) + k;
                     const float x = xh[k] * rs;
                     dw[u * LEN + k] = fmaf(v[k], x, dw[u * LEN + k]);
-                    if (at < c) sum = fmaf(v[k] * w[at], x, sum);
+                    if (at >= 0 && at < c) sum = fmaf(v[k] * w[at], x, sum);
                 }
             }
         }
@@ -403,29 +580,38 @@ __global__ void __launch_bounds__(kBlock<TPR>)
                 v[e] = o.x;
                 v[e + 1] = o.y;
             }
-            if (live) put_values<T, LEN, E, TPR>(to, out, c, t, v);
+            if constexpr (SKEW) {
+                put_chunks<T, LEN, E, TPR>(to, staged[group][0], ends, live_c, t, v);
+            } else if (live) {
+                put_values<T, LEN, E, TPR>(to, out, c, t, v);
+            }
         } else {
 #pragma unroll
             for (int u = 0; u < E / LEN; ++u) {
-                const int at = column<LEN, TPR>(t, u);
-                one_run<T, LEN, TPR>(hb, hs, live_c, t, u, xh);
-                one_run<T, LEN, TPR>(gb, gs, live_c, t, u, v);
-                if (dres) one_run<T, LEN, TPR>(eb, es, live_c, t, u, more);
+                const int at = run_column<LEN, TPR>(t, u, skew);
+                run_values<T, LEN, TPR, SKEW>(hb, hs, live_c, t, u, xh);
+                run_values<T, LEN, TPR, SKEW>(gb, gs, live_c, t, u, v);
+                if (dres) run_values<T, LEN, TPR, SKEW>(eb, es, live_c, t, u, more);
 #pragma unroll
                 for (int k = 0; k < LEN; ++k) {
-                    const float d = fmaf(xh[k] * rs, -m, at + k < c ? v[k] * w[at + k] : 0.0f);
+                    const float d = fmaf(xh[k] * rs, -m, at + k >= 0 && at + k < c ? v[k] * w[at + k] : 0.0f);
                     v[k] = fmaf(d, rs, dres ? more[k] : 0.0f);
                 }
                 if (live && at < c) {
-                    if constexpr (LEN > 1)
-                        st_words(to + at, pack<T>(v));
-                    else
-                        reinterpret_cast<T*>(out + row_skew(to))[at] = narrow<T>(v[0]);
+                    if constexpr (LEN > 1) {
+                        if (!SKEW || (at >= 0 && at + LEN <= c))
+                            st_words(to + at, pack<T>(v));
+                        else
+#pragma unroll
+                            for (int k = 0; k < LEN; ++k)
+                                if (at + k >= 0 && at + k < c) to[at + k] = narrow<T>(v[k]);
+                    }
+                    if constexpr (LEN == 1) reinterpret_cast<T*>(out + row_skew(to))[at] = narrow<T>(v[0]);
                 }
             }
         }
         if constexpr (BULK && !HOLD) fence_before_refill();
-        if constexpr (!BULK || !HOLD) group_barrier<TPR>();  // the slot may be filled again, and the results are in their buffer
+        if constexpr ((!SKEW && !BULK) || (BULK && !HOLD)) group_barrier<TPR>();  // the slot may be filled again, and the results are in their buffer
         if (LEN == 1 && live) flush_row<T, TPR>(to, out, c, t);
         parities ^= 1u << slot;
         if (++slot == D) slot = 0;
@@ -445,7 +631,8 @@ __global__ void __launch_bounds__(kBlock<TPR>)
         for (int u = 0; u < E / LEN; ++u)
 #pragma unroll
             for (int k = 0; k < LEN; ++k)
-                if (column<LEN, TPR>(t, u) + k < c) joined[group * c + column<LEN, TPR>(t, u) + k] = dw[u * LEN + k];
+                if (run_column<LEN, TPR>(t, u, skew) + k >= 0 && run_column<LEN, TPR>(t, u, skew) + k < c)
+                    joined[group * c + run_column<LEN, TPR>(t, u, skew) + k] = dw[u * LEN + k];
         __syncthreads();
         for (int k = threadIdx.x; k < c; k += kBlock<TPR>) {
             float s = joined[k];
@@ -458,8 +645,8 @@ __global__ void __launch_bounds__(kBlock<TPR>)
         for (int u = 0; u < E / LEN; ++u)
 #pragma unroll
             for (int k = 0; k < LEN; ++k) {
-                const int at = column<LEN, TPR>(t, u) + k;
-                if (at < c) total[at] = dw[u * LEN + k];
+                const int at = run_column<LEN, TPR>(t, u, skew) + k;
+                if (at >= 0 && at < c) total[at] = dw[u * LEN + k];
             }
     }
 }
@@ -551,18 +738,43 @@ constexpr int64_t kMaxHeld = 16384;
     if (c <= 8192) return CALL(16, 512); \
     return CALL(32, 512);
 
-template <typename T, int LEN, int E, int TPR, bool EIGHT, int D = kDepth<TPR>>
+// Whether the rows of two arrays start at the same places within 16 bytes.
+bool rows_alike(const void* p, int64_t ldp, const void* q, int64_t ldq, size_t esz) {
+    return ((uintptr_t)p - (uintptr_t)q) % 16 == 0 && (ldp - ldq) * (int64_t)esz % 16 == 0;
+}
+// Whether rows in chunks need a group twice as wide as their elements do, for the few that their first chunk has no room for: they are
+// taken element by element then (3 x 1021 x 2047 fp32 backward 23 us, in chunks 25).
+bool just_too_wide(int64_t c, int len) {
+    for (int64_t most = 64; most <= kMaxHeld; most *= 2)
+        if (c <= most) return c + len - 1 > most;
+    return true;
+}
+// Rows that start at the same place of a chunk lie this many apart.
+int like_rows(int64_t ld, size_t esz) {
+    const int64_t pitch = ld * (int64_t)esz % 16;
+    int p = 1;
+    while (p * pitch % 16 != 0) ++p;
+    return p;
+}
+// CTAs of a node such that a group's rows are alike.
+int ctas_for_like_rows(int ctas, int groups, int like) {
+    if (groups % like == 0) return ctas;
+    return ctas >= like ? ctas / like * like : like;
+}
+
+template <typename T, int LEN, int E, int TPR, bool EIGHT, bool SKEW, int D = kDepth<TPR>>
 int run_forward(const dlm_rms_args& a, cudaStream_t s) {
     constexpr int GROUPS = kBlock<TPR> / TPR;
     const size_t smem = (size_t)GROUPS * (D * (a.residual ? 2 : 1) + (LEN == 1 ? 2 : 0)) * row_bytes((int)a.c, sizeof(T));
     if (smem > kMostShared) {
         if constexpr (TPR == 512 && D > 1)
-            return run_forward<T, LEN, E, TPR, EIGHT, D - 1>(a, s);
+            return run_forward<T, LEN, E, TPR, EIGHT, SKEW, D - 1>(a, s);
         else
             return wide_forward<T>(a, s);
     }
-    auto kern = rms_norm_kernel<T, LEN, E, TPR, D, EIGHT>;
-    const int ctas = resident_ctas(kern, kBlock<TPR>, smem, 32, a.n, a.rows, GROUPS);
+    auto kern = rms_norm_kernel<T, LEN, E, TPR, D, EIGHT, SKEW>;
+    int ctas = resident_ctas(kern, kBlock<TPR>, smem, 32, a.n, a.rows, GROUPS);
+    if (SKEW && ctas > 0) ctas = ctas_for_like_rows(ctas, GROUPS, like_rows(a.ldx, sizeof(T)));
     if (ctas < 1) return DLM_ERR_CUDA;
     cudaError_t err = launch_overlapped(kern, dim3((unsigned)ctas, a.n), dim3(kBlock<TPR>), smem, s, 1, a.rows, (int)a.c,
                                         static_cast<const T*>(a.x), a.ldx, static_cast<const T*>(a.residual), a.ldr, a.weight, a.ldw,
@@ -576,15 +788,22 @@ template <typename T, bool EIGHT>
 int forward(const dlm_rms_args& a, cudaStream_t s) {
     const int64_t c = a.c;
     if (c > kMaxHeld) return wide_forward<T>(a, s);
-#define DLM_VEC(E, TPR) run_forward<T, kRun<T>, E, TPR, EIGHT>(a, s)
-#define DLM_ONE(E, TPR) run_forward<T, 1, E, TPR, EIGHT>(a, s)
-    if (c % kRun<T> == 0 && rows_aligned(a.x, a.ldx, sizeof(T)) && (!a.residual || rows_aligned(a.residual, a.ldr, sizeof(T))) &&
+    constexpr int LEN = kRun<T>;
+#define DLM_VEC(E, TPR) run_forward<T, LEN, E, TPR, EIGHT, false>(a, s)
+#define DLM_SKEW(E, TPR) run_forward<T, LEN, E, TPR, EIGHT, true>(a, s)
+#define DLM_ONE(E, TPR) run_forward<T, 1, E, TPR, EIGHT, false>(a, s)
+    if (c % LEN == 0 && rows_aligned(a.x, a.ldx, sizeof(T)) && (!a.residual || rows_aligned(a.residual, a.ldr, sizeof(T))) &&
         (!a.h || rows_aligned(a.h, a.ldh, sizeof(T))) && (!a.y || rows_aligned(a.y, a.ldy, sizeof(T))) &&
-        (!EIGHT || ((uintptr_t)a.y8 % kRun<T> == 0 && a.ld8 % kRun<T> == 0))) {
+        (!EIGHT || ((uintptr_t)a.y8 % LEN == 0 && a.ld8 % LEN == 0))) {
         DLM_RMS_SHAPES(DLM_VEC)
+    }
+    auto alike = [&](const void* p, int64_t ld) { return !p || rows_alike(a.x, a.ldx, p, ld, sizeof(T)); };
+    if (alike(a.residual, a.ldr) && alike(a.h, a.ldh) && alike(a.y, a.ldy) && !just_too_wide(c, LEN)) {
+        DLM_RMS_SHAPES(DLM_SKEW)
     }
     DLM_RMS_SHAPES(DLM_ONE)
 #undef DLM_VEC
+#undef DLM_SKEW
 #undef DLM_ONE
 }
 
@@ -602,20 +821,21 @@ int wide_backward(const dlm_rms_args& a, int* parts, cudaStream_t s) {
     return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
 }
 
-template <typename T, int LEN, int E, int TPR, int D = kDepth<TPR>>
+template <typename T, int LEN, int E, int TPR, bool SKEW, int D = kDepth<TPR>>
 int run_backward(const dlm_rms_args& a, int* parts, cudaStream_t s) {
     constexpr int GROUPS = kBlock<TPR> / TPR;
     const size_t smem = std::max((size_t)GROUPS * (D * (a.residual ? 3 : 2) + (LEN == 1)) * row_bytes((int)a.c, sizeof(T)),
                                  GROUPS > 1 ? (size_t)GROUPS * a.c * 4 : 0);
     if (smem > kMostShared) {
         if constexpr (TPR == 512 && D > 1)
-            return run_backward<T, LEN, E, TPR, D - 1>(a, parts, s);
+            return run_backward<T, LEN, E, TPR, SKEW, D - 1>(a, parts, s);
         else
             return wide_backward<T>(a, parts, s);
     }
-    auto kern = rms_norm_grad_kernel<T, LEN, E, TPR, D>;
+    auto kern = rms_norm_grad_kernel<T, LEN, E, TPR, D, SKEW>;
     *parts = std::min(resident_ctas(kern, kBlock<TPR>, smem, 32, a.n, a.rows, GROUPS), dlm_rms_max_ctas(a.n, a.rows, a.c));
     if (*parts < 1) return DLM_ERR_CUDA;
+    if (SKEW) *parts = ctas_for_like_rows(*parts, GROUPS, like_rows(a.ldx, sizeof(T)));
     cudaError_t err = launch_overlapped(kern, dim3((unsigned)*parts, a.n), dim3(kBlock<TPR>), smem, s, 1, a.rows, (int)a.c,
                                         static_cast<const T*>(a.x), a.ldx, static_cast<const T*>(a.dy), a.lddy,
                                         static_cast<const T*>(a.residual), a.ldr, a.weight, a.ldw, (const float*)a.rstd,
@@ -628,14 +848,21 @@ template <typename T>
 int backward(const dlm_rms_args& a, int* parts, cudaStream_t s) {
     const int64_t c = a.c;
     if (c > kMaxHeld) return wide_backward<T>(a, parts, s);
-#define DLM_VEC(E, TPR) run_backward<T, kRun<T>, E, TPR>(a, parts, s)
-#define DLM_ONE(E, TPR) run_backward<T, 1, E, TPR>(a, parts, s)
-    if (c % kRun<T> == 0 && rows_aligned(a.x, a.ldx, sizeof(T)) && rows_aligned(a.dy, a.lddy, sizeof(T)) &&
+    constexpr int LEN = kRun<T>;
+#define DLM_VEC(E, TPR) run_backward<T, LEN, E, TPR, false>(a, parts, s)
+#define DLM_SKEW(E, TPR) run_backward<T, LEN, E, TPR, true>(a, parts, s)
+#define DLM_ONE(E, TPR) run_backward<T, 1, E, TPR, false>(a, parts, s)
+    if (c % LEN == 0 && rows_aligned(a.x, a.ldx, sizeof(T)) && rows_aligned(a.dy, a.lddy, sizeof(T)) &&
         rows_aligned(a.dh, a.lddh, sizeof(T)) && (!a.residual || rows_aligned(a.residual, a.ldr, sizeof(T)))) {
         DLM_RMS_SHAPES(DLM_VEC)
     }
+    if (rows_alike(a.x, a.ldx, a.dy, a.lddy, sizeof(T)) && rows_alike(a.x, a.ldx, a.dh, a.lddh, sizeof(T)) &&
+        (!a.residual || rows_alike(a.x, a.ldx, a.residual, a.ldr, sizeof(T))) && !just_too_wide(c, LEN)) {
+        DLM_RMS_SHAPES(DLM_SKEW)
+    }
     DLM_RMS_SHAPES(DLM_ONE)
 #undef DLM_VEC
+#undef DLM_SKEW
 #undef DLM_ONE
 }
 #undef DLM_RMS_SHAPES
@@ -670,7 +897,8 @@ int dlm_rms_take_error(int* flag) {
 
 // Bound on the row blocks per node, so that the workspace's size needs no device: about what the SMs hold at once.
 int dlm_rms_max_ctas(int n, int64_t rows, int64_t c) {
-    return (int)std::min<int64_t>(rows, std::max(1, (c <= 2048 ? 1024 : 448) / n));
+    // (rows that start alike are up to eight apart, and each kind has a CTA of its own)
+    return (int)std::max<int64_t>(8, std::min<int64_t>(rows, (c <= 2048 ? 1024 : 448) / n));
 }
 
 int dlm_launch_rms_norm(const dlm_rms_args& a, void* stream) {
