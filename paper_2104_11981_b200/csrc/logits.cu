@@ -14,6 +14,7 @@
 #include "dlm_launch.h"
 #include "dlm_model.h"
 #include "dlm_rows.cuh"
+#include "dlm_staged_rows.cuh"
 
 namespace {
 
@@ -25,11 +26,11 @@ struct Adjust {
     const float* bias;
 };
 
-// An element d (the logit, or the gradient): `marked`: the text has it, `count` times; `positive`: its logit is above 0.
+// An element d (the logit, or the gradient): `positive`: its logit is above 0; `count`: how often the text has it, 0: never.
 template <bool GRAD>
 __device__ __forceinline__ float penalised(const Adjust& a, float d, bool positive, int count) {
-    d *= positive ? a.down : a.up;
-    return GRAD ? d : d - fmaf(a.frequency, (float)count, a.presence);
+    const float f = count == 0 ? 1.0f : positive ? a.down : a.up;
+    return GRAD ? d * f : fmaf(d, f, count == 0 ? 0.0f : -fmaf(a.frequency, (float)count, a.presence));
 }
 
 // A row lies in memory as chunks of LEN elements (16 bytes wherever the row starts, or one element); the first begins `skew` elements
@@ -37,25 +38,27 @@ __device__ __forceinline__ float penalised(const Adjust& a, float d, bool positi
 // CTA marks the row's text in a bit map, and (COUNTS) counts it: counts of marked elements alone are cleared, added to and read.  For the
 // gradient, whoever marks an element first fetches its logit and notes the sign, all of them at once; asking for it where the element is
 // mapped would let nearly every warp wait for memory a second time.
-template <typename T, bool GRAD, bool COUNTS, int LEN, int THREADS, int U>
+enum Texts { NONE, MARKS, COUNTS };
+template <typename T, bool GRAD, int TEXTS, int LEN, int THREADS, int U>
 __global__ void __launch_bounds__(THREADS) logits_kernel(dlm_logits_args a, int tiles) {
     constexpr int TILE = THREADS * U * LEN, WORDS = (TILE + 31) / 32;
     extern __shared__ int counts[];  // [TILE]
-    __shared__ uint32_t marks[WORDS], positives[GRAD ? WORDS : 1];
-    const long long row = blockIdx.x / tiles, node = row / a.rows;
+    __shared__ uint32_t marks[TEXTS ? WORDS : 1], positives[GRAD && TEXTS ? WORDS : 1];
+    const uint32_t row_at = blockIdx.x / (uint32_t)tiles, node = row_at / (uint32_t)a.rows;
+    const long long row = row_at;
     const T* in = static_cast<const T*>(a.in) + row * a.ldi;
     T* out = static_cast<T*>(a.out) + row * a.ldo;
     const int skew = LEN > 1 ? (int)((uintptr_t)in & 15) / (int)sizeof(T) : 0;
     const int vocab = (int)a.vocab;
-    const int tile0 = (int)((blockIdx.x % tiles) * TILE) - skew;  // the tile's first element
+    const int tile0 = (int)(blockIdx.x - row_at * (uint32_t)tiles) * TILE - skew;  // the tile's first element
     auto chunk_at = [&](int u) { return tile0 + (u * THREADS + (int)threadIdx.x) * LEN; };
     auto whole = [&](int v) { return v >= 0 && v + LEN <= vocab; };
     pdl_wait();
     pdl_release();
     long long from = 0, to = 0;
-    if (a.history_start) {
-        from = max(0ll, (long long)a.history_start[row]);
-        to = min((long long)a.history_length, (long long)a.history_start[row + 1]);
+    if constexpr (TEXTS != NONE) {
+        from = a.history_start[row];
+        to = a.history_start[row + 1];
     }
     Adjust how;
     how.up = a.repetition ? a.repetition[row] : 1.0f;
@@ -63,6 +66,7 @@ __global__ void __launch_bounds__(THREADS) logits_kernel(dlm_logits_args a, int 
     how.presence = a.presence ? a.presence[row] : 0.0f;
     how.cooling = a.temperature ? a.temperature[row] : 1.0f;
     how.bias = !GRAD && a.bias ? a.bias + node * a.ldb : nullptr;
+    const bool bias_runs = ((uintptr_t)(how.bias + tile0) & 15) == 0;  // a chunk's biases are 16-byte runs
     const uint32_t* allowed = a.allowed ? a.allowed + row * a.ldm : nullptr;
     // bit k: element v + k is allowed
     auto allowed_bits = [&](int v) {
@@ -87,8 +91,10 @@ __global__ void __launch_bounds__(THREADS) logits_kernel(dlm_logits_args a, int 
     }
     how.down = 1.0f / how.up;
     how.cooling = 1.0f / how.cooling;
-    const bool texts = a.history_start != nullptr;
-    if (texts) {
+    if constexpr (TEXTS != NONE) {
+        from = max(0ll, from);
+        const int length = (int)max(0ll, min((long long)a.history_length, to) - from);
+        const int64_t* text = a.history + from;
         for (int k = threadIdx.x; k < WORDS; k += THREADS) {
             marks[k] = 0;
             if (GRAD) positives[k] = 0;
@@ -97,18 +103,19 @@ __global__ void __launch_bounds__(THREADS) logits_kernel(dlm_logits_args a, int 
         const T* z = GRAD ? static_cast<const T*>(a.logits) + row * a.ldl + tile0 : nullptr;
         auto each = [&](auto&& f) {
 #pragma unroll 4
-            for (long long k = from + threadIdx.x; k < to; k += THREADS) {
-                const int64_t token = a.history[k], at = token - tile0;
-                if (token >= 0 && token < vocab && at >= 0 && at < TILE) f((int)at);
+            for (int k = threadIdx.x; k < length; k += THREADS) {
+                const uint64_t token = (uint64_t)text[k];
+                const int at = (int)token - tile0;
+                if (token < (uint64_t)vocab && (uint32_t)at < (uint32_t)TILE) f(at);
             }
         };
         each([&](int at) {
             const uint32_t bit = 1u << (at & 31), old = atomicOr(&marks[at >> 5], bit);
             if (GRAD && !(old & bit) && widen(z[at]) > 0.0f) atomicOr(&positives[at >> 5], bit);
-            if (COUNTS) counts[at] = 0;
+            if (TEXTS == COUNTS) counts[at] = 0;
         });
         __syncthreads();
-        if constexpr (COUNTS) {
+        if constexpr (TEXTS == COUNTS) {
             each([&](int at) { atomicAdd(&counts[at], 1); });
             __syncthreads();
         }
@@ -123,19 +130,31 @@ __global__ void __launch_bounds__(THREADS) logits_kernel(dlm_logits_args a, int 
             unpack<T>(raw[u], d);
         else
             d[0] = __uint_as_float(raw[u].w[0]);
-        if (texts) {
+        if constexpr (TEXTS != NONE) {
             const int at = (u * THREADS + (int)threadIdx.x) * LEN;  // LEN divides 32: a chunk's marks are in one word
             const uint32_t marked = marks[at >> 5] >> (at & 31) & ALL;
             if (marked) {
                 const uint32_t positive = GRAD ? positives[at >> 5] >> (at & 31) : 0;
 #pragma unroll
-                for (int k = 0; k < LEN; ++k)
-                    if ((marked >> k) & 1) d[k] = penalised<GRAD>(how, d[k], GRAD ? (positive >> k) & 1 : d[k] > 0.0f, COUNTS ? counts[at + k] : 1);
+                for (int k = 0; k < LEN; ++k) {
+                    const int count = (marked >> k) & 1 ? TEXTS == COUNTS ? counts[at + k] : 1 : 0;
+                    d[k] = penalised<GRAD>(how, d[k], GRAD ? (positive >> k) & 1 : d[k] > 0.0f, count);
+                }
             }
         }
-        if (how.bias) {
+        if (!GRAD && how.bias) {
+            if (LEN > 1 && bias_runs) {
 #pragma unroll
-            for (int k = 0; k < LEN; ++k) d[k] += how.bias[v + k];
+                for (int k = 0; k < LEN; k += kRun<float>) {
+                    float p[kRun<float>];
+                    unpack<float>(ld_words(how.bias + v + k), p);
+#pragma unroll
+                    for (int e = 0; e < (LEN > 1 ? kRun<float> : 1); ++e) d[k + e] += p[e];
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < LEN; ++k) d[k] += how.bias[v + k];
+            }
         }
 #pragma unroll
         for (int k = 0; k < LEN; ++k) d[k] *= how.cooling;
@@ -156,8 +175,8 @@ __global__ void __launch_bounds__(THREADS) logits_kernel(dlm_logits_args a, int 
     const int at = v - tile0;
     if (v < 0 || v >= vocab || at < 0 || at >= TILE || ((int)threadIdx.x >= LEN && v + skew < LEN && skew > 0)) return;
     float d = widen(in[v]);
-    if (texts && (marks[at >> 5] >> (at & 31) & 1))
-        d = penalised<GRAD>(how, d, GRAD ? positives[at >> 5] >> (at & 31) & 1 : d > 0.0f, COUNTS ? counts[at] : 1);
+    if (TEXTS != NONE && (marks[at >> 5] >> (at & 31) & 1))
+        d = penalised<GRAD>(how, d, GRAD ? positives[at >> 5] >> (at & 31) & 1 : d > 0.0f, TEXTS == COUNTS ? counts[at] : 1);
     if (how.bias) d += how.bias[v];
     d *= how.cooling;
     if (allowed && !(allowed[v >> 5] >> (v & 31) & 1)) d = GRAD ? 0.0f : -INFINITY;
@@ -171,14 +190,186 @@ int run(const dlm_logits_args& a, cudaStream_t s) {
     const int64_t ctas = a.n * a.rows * tiles;
     if (ctas > 0x7fffffff) return DLM_ERR_UNSUPPORTED;
     const bool counted = !GRAD && a.history_start && a.frequency;  // the other penalties only ask whether
-    auto kern = logits_kernel<T, GRAD, false, LEN, THREADS, U>;
-    if constexpr (!GRAD) {
-        if (counted) kern = logits_kernel<T, GRAD, true, LEN, THREADS, U>;
-        if (counted && TILE * sizeof(int) > (48 << 10) - 8192 &&
-            cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, TILE * sizeof(int)) != cudaSuccess)
-            return DLM_ERR_CUDA;
-    }
+    auto kern = a.history_start ? logits_kernel<T, GRAD, MARKS, LEN, THREADS, U> : logits_kernel<T, GRAD, NONE, LEN, THREADS, U>;
+    if constexpr (!GRAD)
+        if (counted) kern = logits_kernel<T, GRAD, COUNTS, LEN, THREADS, U>;
+    static_assert(TILE * sizeof(int) + TILE / 8 + 1024 <= 48 << 10);
     cudaError_t err = launch_overlapped(kern, dim3((unsigned)ctas), dim3(THREADS), counted ? TILE * sizeof(int) : 0, s, 1, a, tiles);
+    dlm_count_launch(1);
+    return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
+}
+
+// With texts, a tile's time goes by the wait for the row's bounds, then its text, then the logits of what it marks.  So that enough bytes are on
+// their way meanwhile, chunks come into shared memory (16 KB a CTA, or a short row), not into registers, of
+// which half as many would fit: gradient of 4 x 1024 x 50001 bf16 228 us by the kernel above.  A thread copies and maps chunks of its own.
+// The adjustment counts every element's occurrences in 16 bits (texts of more than 65535 tokens are only marked, and read once more for
+// each element); its gradient needs no more than a mark and the logit's sign.
+constexpr int kShortText = 65535;
+__device__ __noinline__ int count_in(const int64_t* text, long long length, int64_t token) {
+    int n = 0;
+    for (long long i = 0; i < length; ++i) n += text[i] == token;
+    return n;
+}
+
+// Shared memory of a tile.
+__host__ __device__ inline int text_bytes(int elements, int esz, bool grad) {
+    return elements * esz + (grad ? elements / 4 : elements * 2) + elements / 8 + 16;
+}
+
+template <typename T, bool GRAD, int THREADS>
+__global__ void __launch_bounds__(THREADS) logits_text_kernel(dlm_logits_args a, int tiles, int tile_chunks) {
+    constexpr int LEN = kRun<T>;
+    constexpr uint32_t ALL = (1u << LEN) - 1;
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int t = threadIdx.x;
+    const uint32_t item = blockIdx.x, row_at = item / (uint32_t)tiles, node = row_at / (uint32_t)a.rows;
+    const int elements = tile_chunks * LEN, words = elements / 32;
+    unsigned char* data = smem;
+    uint16_t* counts = reinterpret_cast<uint16_t*>(data + elements * sizeof(T));  // or
+    uint32_t *marks = reinterpret_cast<uint32_t*>(counts), *positives = marks + words;
+    uint32_t* mask = marks + (GRAD ? 2 * words : elements / 2);  // [words + 1]
+    pdl_wait();
+    pdl_release();
+    const long long row = row_at;
+    long long from = a.history_start[row], to = a.history_start[row + 1];
+    const T* in = static_cast<const T*>(a.in) + row * a.ldi;
+    T* out = static_cast<T*>(a.out) + row * a.ldo;
+    const int skew = (int)((uintptr_t)in & 15) / (int)sizeof(T), vocab = (int)a.vocab;
+    const int tile0 = (int)(item - row_at * (uint32_t)tiles) * elements - skew;  // the tile's first element
+    auto whole = [&](int v) { return v >= 0 && v + LEN <= vocab; };
+    const int chunks = min(tile_chunks, (vocab - tile0 + LEN - 1) / LEN);
+    for (int c = t; c < chunks; c += THREADS) {
+        const int v = tile0 + c * LEN;
+        if (whole(v)) copy_chunk(smem_u32(data + c * 16), in + v, 16);
+    }
+    const uint32_t* allowed = a.allowed ? a.allowed + row * a.ldm : nullptr;
+    const int word0 = max(tile0, 0) >> 5;
+    if (allowed)
+        for (int k = t; k <= words && word0 + k <= (vocab - 1) >> 5; k += THREADS)
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(mask + k)), "l"(allowed + word0 + k) : "memory");
+    commit_copies();
+    Adjust how;
+    how.up = a.repetition ? a.repetition[row] : 1.0f;
+    how.frequency = a.frequency ? a.frequency[row] : 0.0f;
+    how.presence = a.presence ? a.presence[row] : 0.0f;
+    how.cooling = 1.0f / (a.temperature ? a.temperature[row] : 1.0f);
+    how.bias = !GRAD && a.bias ? a.bias + node * a.ldb : nullptr;
+    how.down = 1.0f / how.up;
+    const bool bias_runs = ((uintptr_t)(how.bias + tile0) & 15) == 0;  // a chunk's biases are 16-byte runs
+    for (int k = t; k < (GRAD ? 2 * words : elements / 2) / 4; k += THREADS) reinterpret_cast<uint4*>(marks)[k] = make_uint4(0, 0, 0, 0);
+    from = max(0ll, from);
+    const long long length = max(0ll, min((long long)a.history_length, to) - from);
+    const int64_t* text = a.history + from;
+    auto each = [&](auto&& f) {
+#pragma unroll 4
+        for (long long k = t; k < length; k += THREADS) {
+            const uint64_t token = (uint64_t)text[k];
+            const int at = (int)token - tile0;
+            if (token < (uint64_t)vocab && (uint32_t)at < (uint32_t)elements) f(at);
+        }
+    };
+    __syncthreads();
+    const T* z = GRAD ? static_cast<const T*>(a.logits) + row * a.ldl + tile0 : nullptr;
+    const bool brief = length <= kShortText;
+    each([&](int at) {
+        if constexpr (GRAD) {
+            const uint32_t bit = 1u << (at & 31), old = atomicOr(&marks[at >> 5], bit);
+            if (!(old & bit) && widen(z[at]) > 0.0f) atomicOr(&positives[at >> 5], bit);
+        } else if (brief) {
+            atomicAdd(&marks[at >> 1], 1u << (16 * (at & 1)));
+        } else {
+            counts[at] = 1;
+        }
+    });
+    wait_copies<0>();
+    __syncthreads();
+    auto count_of = [&](uint32_t count, int at) { return brief || count == 0 ? (int)count : count_in(text, length, tile0 + at); };
+#pragma unroll 2
+    for (int c = t; c < chunks; c += THREADS) {
+        const int at = c * LEN, v = tile0 + at;
+        if (!whole(v)) continue;
+        float d[LEN];
+        unpack<T>(ld_words(data + c * 16), d);
+        if constexpr (GRAD) {
+            const uint32_t marked = marks[at >> 5] >> (at & 31) & ALL;  // LEN divides 32: a chunk's marks are in one word
+            if (marked) {
+                const uint32_t positive = positives[at >> 5] >> (at & 31);
+#pragma unroll
+                for (int k = 0; k < LEN; ++k) d[k] = penalised<GRAD>(how, d[k], (positive >> k) & 1, (marked >> k) & 1);
+            }
+        } else {
+            uint32_t pairs[LEN / 2], any = 0;
+#pragma unroll
+            for (int k = 0; k < LEN / 2; k += 2) {
+                const uint2 p = *reinterpret_cast<const uint2*>(counts + at + 2 * k);
+                pairs[k] = p.x;
+                pairs[k + 1] = p.y;
+                any |= p.x | p.y;
+            }
+            if (any) {
+#pragma unroll
+                for (int k = 0; k < LEN; ++k)
+                    d[k] = penalised<GRAD>(how, d[k], d[k] > 0.0f, count_of(k & 1 ? pairs[k / 2] >> 16 : pairs[k / 2] & 0xffffu, at + k));
+            }
+        }
+        if (!GRAD && how.bias) {
+            if (bias_runs) {
+#pragma unroll
+                for (int k = 0; k < LEN; k += 4) {
+                    float p[4];
+                    unpack<float>(ld_words(how.bias + v + k), p);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) d[k + e] += p[e];
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < LEN; ++k) d[k] += how.bias[v + k];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < LEN; ++k) d[k] *= how.cooling;
+        if (allowed) {
+            const uint32_t* w = mask + (v >> 5) - word0;
+            uint32_t bits = w[0] >> (v & 31);
+            if ((v & 31) > 32 - LEN) bits |= w[1] << (32 - (v & 31));
+            if ((bits & ALL) != ALL) {
+#pragma unroll
+                for (int k = 0; k < LEN; ++k)
+                    if (!((bits >> k) & 1)) d[k] = GRAD ? 0.0f : -INFINITY;
+            }
+        }
+        st_words(out + v, pack<T>(d));
+    }
+    if (t >= 2 * LEN) return;
+    // elements of the row's first and last chunk that are not whole
+    const int last = vocab - (vocab + skew) % LEN;  // where that chunk begins
+    const int v = t < LEN ? (skew > 0 ? t - skew : -1) : max(last, 0) + t - LEN;
+    const int at = v - tile0;
+    if (v < 0 || v >= vocab || at < 0 || at >= elements || (t >= LEN && v + skew < LEN && skew > 0)) return;
+    float d = widen(in[v]);
+    if constexpr (GRAD)
+        d = penalised<GRAD>(how, d, positives[at >> 5] >> (at & 31) & 1, marks[at >> 5] >> (at & 31) & 1);
+    else
+        d = penalised<GRAD>(how, d, d > 0.0f, count_of(counts[at], at));
+    if (how.bias) d += how.bias[v];
+    d *= how.cooling;
+    if (allowed && !(allowed[v >> 5] >> (v & 31) & 1)) d = GRAD ? 0.0f : -INFINITY;
+    out[v] = narrow<T>(d);
+}
+
+template <typename T, bool GRAD, int THREADS>
+int run_text(const dlm_logits_args& a, int64_t tile_bytes, cudaStream_t s) {
+    constexpr int LEN = kRun<T>;
+    const int64_t R = a.n * a.rows, chunks = (a.vocab + 2 * (LEN - 1)) / LEN;  // a row may begin anywhere in its first chunk
+    // few rows: tiles such that every SM has a CTA or two
+    const int64_t wanted = THREADS <= 64 ? chunks : std::min<int64_t>(std::min<int64_t>(tile_bytes / 16, chunks), std::max<int64_t>(THREADS, R * chunks / (2 * device_info().sms)));
+    const int tile_chunks = (int)((wanted + 31) / 32 * 32), tiles = (int)((chunks + tile_chunks - 1) / tile_chunks);
+    const int64_t ctas = R * tiles;
+    if (ctas > 0x7fffffff) return DLM_ERR_UNSUPPORTED;
+    const int smem = text_bytes(tile_chunks * LEN, sizeof(T), GRAD);
+    auto kern = logits_text_kernel<T, GRAD, THREADS>;
+    if (smem > (48 << 10) && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 << 10) != cudaSuccess) return DLM_ERR_CUDA;
+    cudaError_t err = launch_overlapped(kern, dim3((unsigned)ctas), dim3(THREADS), smem, s, 1, a, tiles, tile_chunks);
     dlm_count_launch(1);
     return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
 }
@@ -191,6 +382,12 @@ int run_shape(const dlm_logits_args& a, cudaStream_t s) {
     const bool alike = ((uintptr_t)a.in - (uintptr_t)a.out) % 16 == 0 && (a.n * a.rows == 1 || (a.ldi - a.ldo) * (int64_t)sizeof(T) % 16 == 0);
     if (!alike) return a.vocab <= 512 ? run<T, GRAD, 1, 128, 4>(a, s) : run<T, GRAD, 1, 256, 16>(a, s);
     const int64_t chunks = (a.vocab + 2 * (LEN - 1)) / LEN;
+    if (a.history_start && chunks > 64) {  // (4 x 100000 x 500 bf16: 463 us below, 586 here)
+        // (4 x 20000 x 1001 bf16 147 us with two warps a row, 196 with four)
+        if (chunks <= 256) return run_text<T, GRAD, 64>(a, 0, s);
+        // where texts are long beside a tile, they are read by half as many CTAs (4 x 300 x 128000 fp32 with 3000 tokens 364 us instead of 420)
+        return a.history_length >= 2048 * a.n * a.rows ? run_text<T, GRAD, 256>(a, 32 << 10, s) : run_text<T, GRAD, 128>(a, 16 << 10, s);
+    }
     if (chunks <= 64) return run<T, GRAD, LEN, 64, 1>(a, s);
     if (chunks <= 128) return run<T, GRAD, LEN, 128, 1>(a, s);
     if (chunks <= 256) return run<T, GRAD, LEN, 256, 1>(a, s);
