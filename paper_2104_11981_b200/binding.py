@@ -609,15 +609,25 @@ def policy_loss_grad(logits, tokens, weight, advantage, old_logp, ref_logp, clip
 
 
 # The operators between tokens and logits are called on single tokens as well, where reading a tensor's attributes takes longer than
-# the kernel: these helpers ask for each once.  Filled on first use, so that importing this module does not import torch.
+# the kernel.  _calls reads them through the tensors' DLPack exchange interface; where that is missing, the helpers below ask for each once
+# (rms_norm with all its outputs: 4.0 us of a call).  Filled on first use, so that importing this module does not import torch.
 _current_device = _current_stream = _f32 = _bf16 = _i32 = _i64_t = _e4m3 = None
+_direct = None  # the module whose calls take tensors
 
 
 def _torch_names():
-    global _current_device, _current_stream, _f32, _bf16, _i32, _i64_t, _e4m3
+    global _current_device, _current_stream, _f32, _bf16, _i32, _i64_t, _e4m3, _direct
     import torch
+    capsule = getattr(torch.Tensor, "__dlpack_c_exchange_api__", None)
+    if capsule is not None and hasattr(_calls, "read_tensors") and _calls is not _lib and _calls.read_tensors(torch.Tensor, capsule):
+        _direct = _calls
     _f32, _bf16, _i32, _i64_t, _e4m3 = torch.float32, torch.bfloat16, torch.int32, torch.int64, torch.float8_e4m3fn
     _current_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+
+
+def _done(status, where):
+    if status != 0:
+        raise DecentlamError(status, where)
 
 
 def _home():
@@ -683,7 +693,11 @@ def _tables(t, home):
 def embedding(table, tokens, y, scale=1.0, stream=None):
     """y[i, r] <- scale table[i, tokens[i, r]] (0 where the token is outside [0, vocab)): table [n, vocab, c] fp32 or bf16 (a view of
     the stacked parameters, for instance), tokens int64 [n, rows], y [n, rows, c] fp32 or bf16."""
-    home, shape, dtype = _home(), y.shape, y.dtype
+    home = _home()
+    if _direct is not None:
+        return _done(_direct.embedding_of(table, tokens, y, scale, home,
+                     None if stream is None else stream.cuda_stream), "embedding")
+    shape, dtype = y.shape, y.dtype
     n, vocab, c = table.shape
     rows = shape[1]
     assert shape[0] == n and shape[2] == c and len(shape) == 3, "y [n, rows, c] is expected"
@@ -702,7 +716,11 @@ def embedding_grad_workspace_bytes(n, rows, vocab, c):
 def embedding_grad(tokens, dy, dtable, workspace, scale=1.0, accumulate=False, stream=None):
     """Gradient of embedding's table: dtable [n, vocab, c] fp32 or bf16 (a view of the stacked gradient, for instance) is overwritten, or
     added to (accumulate); workspace: uint8 device tensor of at least embedding_grad_workspace_bytes(n, rows, vocab, c) bytes."""
-    home, shape, dtype = _home(), dy.shape, dy.dtype
+    home = _home()
+    if _direct is not None:
+        return _done(_direct.embedding_grad_of(tokens, dy, dtable, workspace, scale, accumulate, home,
+                     None if stream is None else stream.cuda_stream), "embedding_grad")
+    shape, dtype = dy.shape, dy.dtype
     n, vocab, c = dtable.shape
     rows = shape[1]
     assert shape[0] == n and shape[2] == c and len(shape) == 3, "dy [n, rows, c] is expected"
@@ -716,7 +734,11 @@ def rms_norm(x, weight, eps, y, rstd, residual=None, h=None, y8=None, scales=Non
     """h <- x + residual; y <- h rstd weight over the last axis of x [n, rows, c] (fp32 or bf16); weight fp32 [n, c] (a view of the
     stacked parameters, for instance); rstd fp32 [n, rows] is written.  residual and h (of x's shape and type) may be None.  y8
     (float8_e4m3fn of x's shape) and scales (fp32 [n, rows]): the output in 8 bits, beside y or in its place (y None)."""
-    home, shape, dtype = _home(), x.shape, x.dtype
+    home = _home()
+    if _direct is not None:
+        return _done(_direct.rms_norm_of(x, weight, eps, y, rstd, residual, h, y8, scales, home,
+                     None if stream is None else stream.cuda_stream), "rms_norm")
+    shape, dtype = x.shape, x.dtype
     n, rows, c = shape
     px, ldx = _rows(x, shape, dtype, home)
     pr, ldr = _rows(residual, shape, dtype, home)
@@ -741,7 +763,11 @@ def rms_norm_grad(h, dy, weight, rstd, dh, dweight, workspace, dresidual=None, s
     """Backward pass of rms_norm: dh (of h's shape and type) is the gradient of x and of residual alike, dresidual (or None) what
     reaches h along the residual stream; dweight [n, c] fp32 or bf16 (a view of the stacked gradient, for instance) is overwritten;
     workspace: uint8 device tensor of at least rms_norm_grad_workspace_bytes(n, rows, c) bytes."""
-    home, shape, dtype = _home(), h.shape, h.dtype
+    home = _home()
+    if _direct is not None:
+        return _done(_direct.rms_norm_grad_of(h, dy, weight, rstd, dh, dweight, workspace, dresidual, home,
+                     None if stream is None else stream.cuda_stream), "rms_norm_grad")
+    shape, dtype = h.shape, h.dtype
     n, rows, c = shape
     px, ldx = _rows(h, shape, dtype, home)
     py, ldy = _rows(dy, shape, dtype, home)
@@ -760,7 +786,11 @@ def dropout(x, p, state, y, site=0, residual=None, stream=None):
     """y <- residual + dropout(x) (residual may be None) of x [n, rows, c] fp32 or bf16, with probability p of an element to be
     dropped.  state: int64 device tensor (seed, step); site: which of the model's dropouts.  The same call on dy is the backward
     pass."""
-    home, shape, dtype = _home(), x.shape, x.dtype
+    home = _home()
+    if _direct is not None:
+        return _done(_direct.dropout_of(x, p, state, y, site, residual, home,
+                     None if stream is None else stream.cuda_stream), "dropout")
+    shape, dtype = x.shape, x.dtype
     n, rows, c = shape
     (px, ldx), (pr, ldr), (py, ldy) = (_rows(x, shape, dtype, home), _rows(residual, shape, dtype, home),
                                        _rows(y, shape, dtype, home))
@@ -798,7 +828,11 @@ def logits_adjust(logits, out, bias=None, allowed=None, history=None, history_st
     may be the logits themselves); bias fp32 [n, vocab]; allowed int32 [n, rows, >= ceil(vocab / 32)], bit v % 32 of word v / 32;
     history int64, all rows' texts one after another, and history_start int64 [n * rows + 1] their bounds; repetition, frequency,
     presence, temperature fp32 [n, rows].  Each may be None."""
-    home, shape, dtype = _home(), logits.shape, logits.dtype
+    home = _home()
+    if _direct is not None:
+        return _done(_direct.logits_adjust_of(logits, out, bias, allowed, history, history_start, repetition, frequency, presence, temperature, home,
+                     None if stream is None else stream.cuda_stream), "logits_adjust")
+    shape, dtype = logits.shape, logits.dtype
     n, rows, vocab = shape
     count = n * rows
     (pz, ldl), (po, ldo) = _rows(logits, shape, dtype, home), _rows(out, shape, dtype, home)
@@ -814,7 +848,11 @@ def logits_adjust_grad(dout, dlogits, logits=None, allowed=None, history=None, h
                        temperature=None, stream=None):
     """Backward pass of logits_adjust: dlogits of dout's shape and type (dout itself: in place); logits: as they were before the
     adjustment, needed with repetition; the others as there (biases, frequency and presence have no slope)."""
-    home, shape, dtype = _home(), dout.shape, dout.dtype
+    home = _home()
+    if _direct is not None:
+        return _done(_direct.logits_adjust_grad_of(dout, dlogits, logits, allowed, history, history_start, repetition, temperature, home,
+                     None if stream is None else stream.cuda_stream), "logits_adjust_grad")
+    shape, dtype = dout.shape, dout.dtype
     n, rows, vocab = shape
     count = n * rows
     (pg, ldg), (pd, ldd) = _rows(dout, shape, dtype, home), _rows(dlogits, shape, dtype, home)

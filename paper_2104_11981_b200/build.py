@@ -5,6 +5,7 @@ nvcc cross-compiles without a GPU; the runtime is linked statically so the libra
 (and its host-only entry points work) on machines without a CUDA device.  Every source is
 compiled to an object of its own (in parallel, only when it or a header changed), then linked.
 """
+import importlib.util
 import os
 import subprocess
 import sys
@@ -61,7 +62,11 @@ def _build_calls(force: bool) -> None:
         print("Python.h not found: _calls is left out, the binding calls through ctypes", file=sys.stderr)
         return
     tmp = CALLS + ".tmp"
-    subprocess.run([os.environ.get("CC", "gcc"), "-O2", "-fPIC", "-shared", "-I", INCLUDE, "-I", sysconfig.get_paths()["include"],
+    # the tensors' exchange interface, whose header comes with them; without it the binding reads tensors itself
+    spec = importlib.util.find_spec("torch")
+    tensors = os.path.join(os.path.dirname(spec.origin), "include") if spec and spec.origin else ""
+    more = ["-DDLM_TENSORS", "-isystem", tensors] if os.path.exists(os.path.join(tensors, "ATen", "dlpack.h")) else []
+    subprocess.run([os.environ.get("CC", "gcc"), "-O2", "-fPIC", "-shared", *more, "-I", INCLUDE, "-I", sysconfig.get_paths()["include"],
                     src, "-o", tmp, "-L", HERE, "-l:libdecentlam.so", "-Wl,-rpath,$ORIGIN"], check=True)
     os.replace(tmp, CALLS)
 

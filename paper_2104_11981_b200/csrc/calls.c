@@ -134,9 +134,264 @@ CALL(logits_adjust_grad, 18, {
     LAUNCH(logits_adjust_grad(n, rows, vocab, g, dtype, lddo, z, ldl, allowed, ldm, text, length, start, rep, temp, d, ldd, stream))
 })
 
+/* The operators between tokens and logits with tensors themselves as arguments, read through the DLPack exchange interface (a struct of C
+ * functions that the tensors' class offers as a capsule): a call on a single token costs what its launch costs.  The checks are those of
+ * binding.py, which makes them itself where the interface is missing. */
+#ifdef DLM_TENSORS
+#include <ATen/dlpack.h>
+
+static const DLPackExchangeAPI* exchange;
+static PyTypeObject* tensor_type;
+
+static PyObject* py_read_tensors(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+    (void)self;
+    if (nargs != 2 || !PyType_Check(args[0])) return PyErr_Format(PyExc_TypeError, "read_tensors: the tensors' type and its capsule");
+    const DLPackExchangeAPI* api = PyCapsule_GetPointer(args[1], "dlpack_exchange_api");
+    if (!api) return NULL;
+    while (api && api->header.version.major != DLPACK_MAJOR_VERSION) api = (const DLPackExchangeAPI*)api->header.prev_api;
+    if (!api || !api->dltensor_from_py_object_no_sync || !api->current_work_stream) Py_RETURN_FALSE;
+    Py_INCREF(args[0]);
+    tensor_type = (PyTypeObject*)args[0];
+    exchange = api;
+    Py_RETURN_TRUE;
+}
+
+typedef struct {
+    DLTensor t;
+    char* data; /* NULL: None */
+} Tensor;
+enum { F32 = DLM_G_F32, BF16 = DLM_G_BF16, ANY = -1, I64 = -2, I32 = -3, E4M3 = -4, BYTES = -5 };
+static int kind_of(const Tensor* x) {
+    const DLDataType d = x->t.dtype;
+    if (d.lanes != 1) return ANY - 100;
+    if (d.code == kDLFloat && d.bits == 32) return F32;
+    if (d.code == kDLBfloat && d.bits == 16) return BF16;
+    if (d.code == kDLInt && d.bits == 64) return I64;
+    if (d.code == kDLInt && d.bits == 32) return I32;
+    if (d.code == kDLFloat8_e4m3fn && d.bits == 8) return E4M3;
+    return ANY - 100;
+}
+#define FAIL(...) return PyErr_Format(PyExc_AssertionError, __VA_ARGS__), 0
+/* A tensor of this kind on the current device, or None where that is allowed. */
+static int tensor(PyObject* o, long home, int kind, int none, Tensor* x) {
+    x->data = NULL;
+    if (o == Py_None && none) return 1;
+    if (!PyObject_TypeCheck(o, tensor_type)) return PyErr_Format(PyExc_TypeError, "a tensor is expected"), 0;
+    if (exchange->dltensor_from_py_object_no_sync(o, &x->t) != 0) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "this tensor cannot be read");
+        return 0;
+    }
+    if (x->t.device.device_type != kDLCUDA || x->t.device.device_id != home) FAIL("tensors on the current CUDA device are expected");
+    if (kind == ANY) {
+        if (kind_of(x) < 0) return PyErr_Format(PyExc_TypeError, "float32 or bfloat16 expected"), 0;
+    } else if (kind != BYTES && kind_of(x) != kind) {
+        FAIL("a tensor of another type is expected");
+    }
+    x->data = (char*)x->t.data + x->t.byte_offset;
+    return 1;
+}
+static int contiguous(const Tensor* x) {
+    int64_t want = 1;
+    if (!x->t.strides) return 1;
+    for (int k = 0; k < x->t.ndim; ++k)
+        if (x->t.shape[k] == 0) return 1;
+    for (int k = x->t.ndim - 1; k >= 0; --k) {
+        if (x->t.shape[k] != 1 && x->t.strides[k] != want) return 0;
+        want *= x->t.shape[k];
+    }
+    return 1;
+}
+static int64_t count_of(const Tensor* x) {
+    int64_t n = 1;
+    for (int k = 0; k < x->t.ndim; ++k) n *= x->t.shape[k];
+    return n;
+}
+/* Row stride of [n, rows, c], whose nodes follow one another. */
+static int rows_of(const Tensor* x, const int64_t* shape, int64_t* ld) {
+    if (x->t.ndim != 3 || x->t.shape[0] != shape[0] || x->t.shape[1] != shape[1] || x->t.shape[2] != shape[2]) FAIL("a tensor of the same shape is expected");
+    if (contiguous(x)) return *ld = shape[2], 1;
+    const int64_t* s = x->t.strides;
+    if (s[2] != 1 && shape[2] != 1) FAIL("unit column stride expected");
+    if (shape[1] == 1) return *ld = s[0], 1;
+    if (shape[0] != 1 && s[0] != shape[1] * s[1]) FAIL("the nodes' rows must be evenly spaced");
+    return *ld = s[1], 1;
+}
+static int rows(PyObject* o, long home, int kind, int none, const int64_t* shape, Tensor* x, int64_t* ld) {
+    if (!tensor(o, home, kind, none, x)) return 0;
+    if (o == Py_None) return *ld = 0, 1;
+    return rows_of(x, shape, ld);
+}
+static int vectors(PyObject* o, long home, int kind, int none, int64_t n, int64_t c, Tensor* x, int64_t* ld) {
+    *ld = 0;
+    if (!tensor(o, home, kind, none, x)) return 0;
+    if (o == Py_None) return 1;
+    if (x->t.ndim != 2 || x->t.shape[0] != n || x->t.shape[1] != c) FAIL("per-node vectors [n, c] are expected");
+    if (x->t.strides && x->t.strides[1] != 1 && c != 1) FAIL("unit column stride expected");
+    *ld = n > 1 && x->t.strides ? x->t.strides[0] : c;
+    return 1;
+}
+static int flat(PyObject* o, long home, int kind, int none, int64_t count, Tensor* x) {
+    if (!tensor(o, home, kind, none, x)) return 0;
+    if (o == Py_None) return 1;
+    if ((count >= 0 && count_of(x) != count) || !contiguous(x)) FAIL("a contiguous tensor of another length is expected");
+    return 1;
+}
+static int tables(PyObject* o, long home, Tensor* x, int64_t* ld) {
+    if (!tensor(o, home, ANY, 0, x)) return 0;
+    if (x->t.ndim != 3) FAIL("tables [n, vocab, c] are expected");
+    const int64_t *z = x->t.shape, *s = x->t.strides;
+    if (s && ((s[2] != 1 && z[2] != 1) || (s[1] != z[2] && z[1] != 1))) FAIL("a node's rows follow one another");
+    *ld = z[0] > 1 && s ? s[0] : z[1] * z[2];
+    return 1;
+}
+static int shape3(const Tensor* x) {
+    if (x->t.ndim != 3) FAIL("[n, rows, c] is expected");
+    return 1;
+}
+static int64_t bytes_of(const Tensor* x) { return count_of(x) * ((x->t.dtype.bits * x->t.dtype.lanes + 7) / 8); }
+static int on_stream(PyObject* o, long home, void** stream) {
+    if (o != Py_None) return *stream = (void*)(uintptr_t)PyLong_AsUnsignedLongLong(o), !PyErr_Occurred();
+    if (exchange->current_work_stream(kDLCUDA, (int32_t)home, stream) != 0) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, "no current stream");
+        return 0;
+    }
+    return 1;
+}
+/* The last two arguments are the current device and the stream (None: the current one). */
+#define TENSOR_CALL(name, count, ...)                                                                                      \
+    static PyObject* py_##name##_of(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {                             \
+        int status;                                                                                                        \
+        void* stream;                                                                                                      \
+        (void)self;                                                                                                        \
+        if (nargs != count + 2 || !exchange) return PyErr_Format(PyExc_TypeError, #name ": %d arguments expected", count); \
+        const long home = PyLong_AsLong(args[count]);                                                                      \
+        if (!on_stream(args[count + 1], home, &stream)) return NULL;                                                       \
+        __VA_ARGS__                                                                                                        \
+        return PyLong_FromLong(status);                                                                                    \
+    }
+#define NEED(what) \
+    if (!(what)) return NULL
+
+TENSOR_CALL(embedding, 4, {
+    Tensor table, tokens, y;
+    int64_t ldt, ldy;
+    const float scale = F(3);
+    NEED(tables(args[0], home, &table, &ldt) && tensor(args[2], home, ANY, 0, &y) && shape3(&y));
+    const int64_t *z = table.t.shape, want[3] = {z[0], y.t.shape[1], z[2]};
+    NEED(rows_of(&y, want, &ldy) && flat(args[1], home, I64, 0, want[0] * want[1], &tokens));
+    LAUNCH(embedding(held(z[0]), want[1], z[1], z[2], table.data, kind_of(&table), ldt, (void*)tokens.data, scale, y.data, kind_of(&y), ldy, stream))
+})
+
+TENSOR_CALL(embedding_grad, 6, {
+    Tensor tokens, dy, table, work;
+    int64_t ldt, ldy;
+    const float scale = F(4);
+    const int accumulate = PyObject_IsTrue(args[5]);
+    NEED(tables(args[2], home, &table, &ldt) && tensor(args[1], home, ANY, 0, &dy) && shape3(&dy));
+    const int64_t *z = table.t.shape, want[3] = {z[0], dy.t.shape[1], z[2]};
+    NEED(rows_of(&dy, want, &ldy) && flat(args[0], home, I64, 0, want[0] * want[1], &tokens) && flat(args[3], home, BYTES, 0, -1, &work));
+    LAUNCH(embedding_grad(held(z[0]), want[1], z[1], z[2], (void*)tokens.data, dy.data, kind_of(&dy), ldy, scale, accumulate, table.data,
+                          kind_of(&table), ldt, work.data, bytes_of(&work), stream))
+})
+
+TENSOR_CALL(rms_norm, 9, {
+    Tensor x, w, y, rstd, res, h, y8, scales;
+    int64_t ldx, ldw, ldy, ldr, ldh, ld8;
+    const float eps = F(2);
+    NEED(tensor(args[0], home, ANY, 0, &x) && shape3(&x));
+    const int64_t* z = x.t.shape;
+    const int kind = kind_of(&x);
+    NEED(rows_of(&x, z, &ldx) && vectors(args[1], home, F32, 0, z[0], z[2], &w, &ldw) && rows(args[3], home, kind, 1, z, &y, &ldy) &&
+         flat(args[4], home, F32, 0, z[0] * z[1], &rstd) && rows(args[5], home, kind, 1, z, &res, &ldr) &&
+         rows(args[6], home, kind, 1, z, &h, &ldh) && rows(args[7], home, E4M3, 1, z, &y8, &ld8) &&
+         flat(args[8], home, F32, 1, z[0] * z[1], &scales));
+    LAUNCH(rms_norm(held(z[0]), z[1], z[2], x.data, kind, ldx, res.data, ldr, (void*)w.data, ldw, eps, h.data, ldh, y.data, ldy, y8.data, ld8,
+                    (void*)scales.data, (void*)rstd.data, stream))
+})
+
+TENSOR_CALL(rms_norm_grad, 8, {
+    Tensor h, dy, w, rstd, dh, dw, work, res;
+    int64_t ldh, lddy, ldw, lddh, ldgw, ldr;
+    NEED(tensor(args[0], home, ANY, 0, &h) && shape3(&h));
+    const int64_t* z = h.t.shape;
+    const int kind = kind_of(&h);
+    NEED(rows_of(&h, z, &ldh) && rows(args[1], home, kind, 0, z, &dy, &lddy) && vectors(args[2], home, F32, 0, z[0], z[2], &w, &ldw) &&
+         flat(args[3], home, F32, 0, z[0] * z[1], &rstd) && rows(args[4], home, kind, 0, z, &dh, &lddh) &&
+         vectors(args[5], home, ANY, 0, z[0], z[2], &dw, &ldgw) && flat(args[6], home, BYTES, 0, -1, &work) &&
+         rows(args[7], home, kind, 1, z, &res, &ldr));
+    LAUNCH(rms_norm_grad(held(z[0]), z[1], z[2], h.data, kind, ldh, dy.data, lddy, res.data, ldr, (void*)w.data, ldw, (void*)rstd.data, dh.data,
+                         lddh, dw.data, ldgw, kind_of(&dw), work.data, bytes_of(&work), stream))
+})
+
+TENSOR_CALL(dropout, 6, {
+    Tensor x, state, y, res;
+    int64_t ldx, ldy, ldr;
+    const float p = F(1);
+    const int64_t site = N(4);
+    NEED(tensor(args[0], home, ANY, 0, &x) && shape3(&x));
+    const int64_t* z = x.t.shape;
+    const int kind = kind_of(&x);
+    NEED(rows_of(&x, z, &ldx) && flat(args[2], home, I64, 0, 2, &state) && rows(args[3], home, kind, 0, z, &y, &ldy) &&
+         rows(args[5], home, kind, 1, z, &res, &ldr));
+    LAUNCH(dropout(held(z[0]), z[1], z[2], x.data, kind, ldx, res.data, ldr, p, (void*)state.data, site, y.data, ldy, stream))
+})
+
+/* A bit mask [n, rows, words]; expanded from one row: 0 words between rows. */
+static int mask(PyObject* o, long home, const int64_t* z, Tensor* x, int64_t* ld) {
+    *ld = 0;
+    if (!tensor(o, home, I32, 1, x)) return 0;
+    if (o == Py_None) return 1;
+    if (x->t.ndim != 3 || x->t.shape[0] != z[0] || x->t.shape[1] != z[1] || x->t.shape[2] < (z[2] + 31) / 32) FAIL("a bit for each token of each row is expected");
+    if (!contiguous(x) && x->t.strides[0] == 0 && x->t.strides[1] == 0) {
+        if (x->t.strides[2] != 1 && x->t.shape[2] != 1) FAIL("unit stride of the words is expected");
+        return 1;
+    }
+    return rows_of(x, x->t.shape, ld);
+}
+static int texts(PyObject* text, PyObject* start, long home, int64_t count, Tensor* t, Tensor* s, int64_t* length) {
+    *length = 0;
+    if (!flat(text, home, I64, 1, -1, t) || !flat(start, home, I64, 1, count + 1, s)) return 0;
+    if ((text == Py_None) != (start == Py_None)) FAIL("a text and its bounds are expected");
+    if (text != Py_None) *length = count_of(t);
+    return 1;
+}
+
+TENSOR_CALL(logits_adjust, 10, {
+    Tensor in, out, bias, allowed, text, start, rep, freq, pres, temp;
+    int64_t ldl, ldo, ldb, ldm, length;
+    NEED(tensor(args[0], home, ANY, 0, &in) && shape3(&in));
+    const int64_t *z = in.t.shape, count = z[0] * z[1];
+    const int kind = kind_of(&in);
+    NEED(rows_of(&in, z, &ldl) && rows(args[1], home, kind, 0, z, &out, &ldo) && vectors(args[2], home, F32, 1, z[0], z[2], &bias, &ldb) &&
+         mask(args[3], home, z, &allowed, &ldm) && texts(args[4], args[5], home, count, &text, &start, &length) &&
+         flat(args[6], home, F32, 1, count, &rep) && flat(args[7], home, F32, 1, count, &freq) && flat(args[8], home, F32, 1, count, &pres) &&
+         flat(args[9], home, F32, 1, count, &temp));
+    LAUNCH(logits_adjust(held(z[0]), z[1], z[2], in.data, kind, ldl, (void*)bias.data, ldb, (void*)allowed.data, ldm, (void*)text.data, length,
+                         (void*)start.data, (void*)rep.data, (void*)freq.data, (void*)pres.data, (void*)temp.data, out.data, ldo, stream))
+})
+
+TENSOR_CALL(logits_adjust_grad, 8, {
+    Tensor d, out, in, allowed, text, start, rep, temp;
+    int64_t ldd, ldo, ldl, ldm, length;
+    NEED(tensor(args[0], home, ANY, 0, &d) && shape3(&d));
+    const int64_t *z = d.t.shape, count = z[0] * z[1];
+    const int kind = kind_of(&d);
+    NEED(rows_of(&d, z, &ldd) && rows(args[1], home, kind, 0, z, &out, &ldo) && rows(args[2], home, kind, 1, z, &in, &ldl) &&
+         mask(args[3], home, z, &allowed, &ldm) && texts(args[4], args[5], home, count, &text, &start, &length) &&
+         flat(args[6], home, F32, 1, count, &rep) && flat(args[7], home, F32, 1, count, &temp));
+    LAUNCH(logits_adjust_grad(held(z[0]), z[1], z[2], d.data, kind, ldd, in.data, ldl, (void*)allowed.data, ldm, (void*)text.data, length,
+                              (void*)start.data, (void*)rep.data, (void*)temp.data, out.data, ldo, stream))
+})
+#endif
+
 #define ENTRY(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {ENTRY(gradient_norm), ENTRY(gradient_clip), ENTRY(layer_norm), ENTRY(layer_norm_grad),
                                 ENTRY(policy_loss_grad), ENTRY(embedding), ENTRY(embedding_grad), ENTRY(rms_norm),
-                                ENTRY(rms_norm_grad), ENTRY(dropout), ENTRY(logits_adjust), ENTRY(logits_adjust_grad), {NULL, NULL, 0, NULL}};
+                                ENTRY(rms_norm_grad), ENTRY(dropout), ENTRY(logits_adjust), ENTRY(logits_adjust_grad),
+#ifdef DLM_TENSORS
+                                ENTRY(read_tensors), ENTRY(embedding_of), ENTRY(embedding_grad_of), ENTRY(rms_norm_of), ENTRY(rms_norm_grad_of),
+                                ENTRY(dropout_of), ENTRY(logits_adjust_of), ENTRY(logits_adjust_grad_of),
+#endif
+                                {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", NULL, -1, methods, NULL, NULL, NULL, NULL};
 PyMODINIT_FUNC PyInit__calls(void) { return PyModule_Create(&module); }
