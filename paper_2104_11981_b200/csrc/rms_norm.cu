@@ -128,6 +128,17 @@ __device__ __forceinline__ void run_params(const float* p, int skew, int c, int 
             v[u * LEN + k] = at >= 0 && at < c ? p[at] : 0.0f;
         }
 }
+// A run's weights, where they are read again for every row; 0 beyond the row.
+template <int LEN>
+__device__ __forceinline__ void weight_run(const float* w, int at, int c, bool runs, float* v) {
+    if (LEN > 1 && runs && at >= 0 && at + LEN <= c) {
+#pragma unroll
+        for (int k = 0; k < LEN; k += 4) unpack<float>(ld_words(w + at + k), v + k);
+    } else {
+#pragma unroll
+        for (int k = 0; k < LEN; ++k) v[k] = at + k >= 0 && at + k < c ? w[at + k] : 0.0f;
+    }
+}
 // A row of results (none where c is below 0): whole chunks straight to memory, the elements of the first and the last one through `ends` (32 bytes of the group's), a
 // thread each.
 template <typename T, int LEN, int E, int TPR>
@@ -495,6 +506,7 @@ __global__ void __launch_bounds__(kBlock<TPR>, kLeastCtas<TPR>)
     for (int k = 0; k < D - 1; ++k) ask(k);
     float wv[HOLD ? E : 1];
     if constexpr (HOLD) run_params<LEN, E, TPR>(w, skew, c, t, wv);
+    const bool w_runs = ((uintptr_t)(w - skew) & 15) == 0;  // a run's weights are 16-byte runs
     float dw[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) dw[e] = 0.0f;
@@ -556,12 +568,13 @@ __global__ void __launch_bounds__(kBlock<TPR>, kLeastCtas<TPR>)
             for (int u = 0; u < E / LEN; ++u) {
                 run_values<T, LEN, TPR, SKEW>(hb, hs, live_c, t, u, xh);
                 run_values<T, LEN, TPR, SKEW>(gb, gs, live_c, t, u, v);
+                float wr[LEN];
+                weight_run<LEN>(w, run_column<LEN, TPR>(t, u, skew), c, w_runs, wr);
 #pragma unroll
                 for (int k = 0; k < LEN; ++k) {
-                    const int at = run_column<LEN, TPR>(t, u, skew) + k;
                     const float x = xh[k] * rs;
                     dw[u * LEN + k] = fmaf(v[k], x, dw[u * LEN + k]);
-                    if (at >= 0 && at < c) sum = fmaf(v[k] * w[at], x, sum);
+                    sum = fmaf(v[k] * wr[k], x, sum);
                 }
             }
         }
@@ -592,9 +605,11 @@ __global__ void __launch_bounds__(kBlock<TPR>, kLeastCtas<TPR>)
                 run_values<T, LEN, TPR, SKEW>(hb, hs, live_c, t, u, xh);
                 run_values<T, LEN, TPR, SKEW>(gb, gs, live_c, t, u, v);
                 if (dres) run_values<T, LEN, TPR, SKEW>(eb, es, live_c, t, u, more);
+                float wr[LEN];
+                weight_run<LEN>(w, at, c, w_runs, wr);
 #pragma unroll
                 for (int k = 0; k < LEN; ++k) {
-                    const float d = fmaf(xh[k] * rs, -m, at + k >= 0 && at + k < c ? v[k] * w[at + k] : 0.0f);
+                    const float d = fmaf(xh[k] * rs, -m, v[k] * wr[k]);
                     v[k] = fmaf(d, rs, dres ? more[k] : 0.0f);
                 }
                 if (live && at < c) {
