@@ -590,8 +590,8 @@ DLM_API int dropout(int n, int64_t rows, int64_t c, const void* x, int dtype, in
  *   repetition, frequency, presence, temperature : device fp32 [n * rows], or NULL (1, 0, 0, 1)
  * The gradient needs `logits` (as they were before the adjustment) only with `repetition`; without it NULL is allowed.  The bias is a
  * constant to it.  rows may be 0.
- * Errors: DLM_ERR_NULL, DLM_ERR_SHAPE, DLM_ERR_KIND, DLM_ERR_ALIGN, DLM_ERR_ALIAS, DLM_ERR_UNSUPPORTED (n * rows above
- * 2^31 - 1, vocab above 2^30), DLM_ERR_CUDA.
+ * Errors: DLM_ERR_NULL, DLM_ERR_SHAPE, DLM_ERR_KIND, DLM_ERR_ALIGN, DLM_ERR_ALIAS, DLM_ERR_UNSUPPORTED (n * rows or
+ * history_length above 2^31 - 1, vocab above 2^30), DLM_ERR_CUDA.
  */
 DLM_API int logits_adjust(int n, int64_t rows, int64_t vocab, const void* logits, int dtype, int64_t ldl, const float* bias,
                           int64_t ldb, const uint32_t* allowed, int64_t ldm, const int64_t* history, int64_t history_length,

@@ -742,6 +742,7 @@ int dlm_launch_embedding(const dlm_embed_args& a, void* stream) {
 }
 
 int dlm_launch_embedding_grad(const dlm_embed_args& a, void* stream) {
+    if (!device_info().ok) return DLM_ERR_CUDA;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     using B = __nv_bfloat16;
     if (a.dtype == DLM_G_BF16) return a.g_dtype == DLM_G_BF16 ? backward<B, B>(a, s) : backward<B, float>(a, s);

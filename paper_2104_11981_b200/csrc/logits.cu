@@ -397,6 +397,7 @@ int run_shape(const dlm_logits_args& a, cudaStream_t s) {
 }  // namespace
 
 int dlm_launch_logits(const dlm_logits_args& a, void* stream) {
+    if (!device_info().ok) return DLM_ERR_CUDA;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     if (a.grad) return a.dtype == DLM_G_BF16 ? run_shape<__nv_bfloat16, true>(a, s) : run_shape<float, true>(a, s);
     return a.dtype == DLM_G_BF16 ? run_shape<__nv_bfloat16, false>(a, s) : run_shape<float, false>(a, s);

@@ -40,7 +40,7 @@ int check_adjustment(const dlm_logits_args& a) {
     if (a.bias && a.ldb < a.vocab) return DLM_ERR_SHAPE;
     if (a.allowed && a.ldm != 0 && a.ldm < words) return DLM_ERR_SHAPE;
     if (a.history_length < 0) return DLM_ERR_SHAPE;
-    if ((a.bias && !fits(a.n, a.ldb)) || (a.allowed && !fits(R, a.ldm > words ? a.ldm : words)) || a.history_length > kMaxElements)
+    if ((a.bias && !fits(a.n, a.ldb)) || (a.allowed && !fits(R, a.ldm > words ? a.ldm : words)) || a.history_length > 0x7fffffff)
         return DLM_ERR_UNSUPPORTED;
     if (!aligned(a.bias, 4) || !aligned(a.allowed, 4) || !aligned(a.history, 8) || !aligned(a.history_start, 8) ||
         !aligned(a.repetition, 4) || !aligned(a.frequency, 4) || !aligned(a.presence, 4) || !aligned(a.temperature, 4))

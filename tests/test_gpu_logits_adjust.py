@@ -136,13 +136,14 @@ def test_each_part_alone(names, typ):
 @pytest.mark.parametrize("longest", [3000, 40_000])
 def test_long_texts(longest):
     """Longer than a CTA has threads, most tokens many times; more than 65535 of one."""
-    z = _rand((1, 3, 5000), 3.0, 1)
-    a = _case(1, 3, 5000, "f32", 2, longest)
-    _check(z, "f32", a)
-    text = torch.full((70_000,), 4999, device=DEV)
-    a.update(history=text, history_start=torch.tensor([0, 70_000, 70_000, 70_000], device=DEV))
-    _check(z, "f32", a)
-    _check_grad(_rand((1, 3, 5000), 3.0, 3), z, "f32", a)
+    for vocab, typ in ((5000, "f32"), (200, "f32"), (5001, "bf16")):
+        z = _rand((1, 3, vocab), 3.0, 1, typ)
+        a = _case(1, 3, vocab, typ, 2, longest)
+        _check(z, typ, a)
+        text = torch.full((70_000,), vocab - 1, device=DEV)
+        a.update(history=text, history_start=torch.tensor([0, 70_000, 70_000, 70_000], device=DEV))
+        _check(z, typ, a)
+        _check_grad(_rand((1, 3, vocab), 3.0, 3, typ), z, typ, a)
 
 
 @pytest.mark.parametrize("typ", ["f32", "bf16"])

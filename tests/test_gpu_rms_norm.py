@@ -281,3 +281,37 @@ def test_calls_from_several_threads():
     for t in threads:
         t.join()
     assert not faults and B.kernel_error() == 0
+
+
+@pytest.mark.parametrize("typ", ["f32", "bf16"])
+@pytest.mark.parametrize("n,rows", [(1, 1), (1, 2), (2, 1), (2, 9), (3, 700)])
+@pytest.mark.parametrize("c", [9, 61, 777, 2100, 5001, 9000])
+def test_rows_that_start_alike(c, n, rows, typ):
+    """All arrays begin at the same odd place and have the same odd stride: rows in chunks whose ends belong to others.  The first and the
+    last row begin and end where the memory of the array does."""
+    if n * rows > 100 and c > 3000:
+        rows = 50
+    ld, shift = c + 3, 1 if typ == "bf16" else 3
+    count = (n * rows - 1) * ld + c                                           # nothing behind the last row
+    def place(seed, std=1.0):
+        flat = _rand((count + shift,), std, seed, typ)
+        return flat, torch.as_strided(flat, (n, rows, c), (rows * ld, ld, 1), shift)
+    (_, x), (_, r), (_, dy) = (place(k) for k in range(3))
+    (fh, h), (fy, y), (fd, dh) = (place(k) for k in range(3, 6))
+    before = [f.clone() for f in (fh, fy, fd)]
+    w = _rand((n, c), 0.5, 8, mean=1.0)
+    _, _, rstd, _, _ = _forward(x, w, r, h, y)
+    _backward(h, dy, w, rstd, r, dh=dh)
+    _check_forward(x, w, r, typ)
+    _check_backward(h, dy, w, rstd, typ, r)
+    py, ph, prstd, q, scales = _forward(x.contiguous(), w, r.contiguous(), eight=True)
+    assert torch.equal(h, ph)
+    assert np.allclose(to64(y), to64(py), rtol=2.0 ** -7 if typ == "bf16" else 1e-5, atol=1e-5)
+    gaps = torch.ones(count + shift, dtype=torch.bool, device=DEV)
+    torch.as_strided(gaps, (n, rows, c), (rows * ld, ld, 1), shift).fill_(False)
+    for now, was in zip((fh, fy, fd), before):
+        assert torch.equal(now[gaps], was[gaps])
+    from paper_2104_11981_b200 import binding as B
+    q8 = torch.full((n, rows, c), 9, device=DEV, dtype=torch.uint8).view(torch.float8_e4m3fn)
+    B.rms_norm(x, w, EPS, None, rstd, r, None, q8, scales)
+    assert torch.equal(q8.view(torch.uint8), q.view(torch.uint8))

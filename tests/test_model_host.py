@@ -150,7 +150,7 @@ def test_logits_adjust_refusals():
     assert _logits(t=0, tl=0, st=0) == -1                                    # penalties without texts
     assert _logits(n=0) == -2 and _logits(v=0) == -2 and _logits(ldl=99) == -2 and _logits(ldo=99) == -2 and _logits(ldb=99) == -2
     assert _logits(ldm=3) == -2 and _logits(tl=-1) == -2
-    assert _logits(v=1 << 40) == -8 and _logits(rows=1 << 31) == -8 and _logits(ldm=1 << 60) == -8 and _logits(tl=1 << 60) == -8
+    assert _logits(v=1 << 40) == -8 and _logits(rows=1 << 31) == -8 and _logits(ldm=1 << 60) == -8 and _logits(tl=1 << 31) == -8
     assert _logits(dt=9) == -6
     assert _logits(z=0x10001, dt=1) == -3 and _logits(b=0x20002) == -3 and _logits(m=0x30001) == -3 and _logits(t=0x40004) == -3
     assert _logits(st=0x50004) == -3 and _logits(rep=0x60002) == -3 and _logits(te=0x90002) == -3
@@ -202,3 +202,13 @@ def test_binding_refuses_tensors_without_a_device():
         B.dropout(x, 0.1, torch.zeros(2, dtype=torch.int64), x)
     with pytest.raises((AssertionError, RuntimeError)):
         B.rms_norm(x, torch.ones((1, 8)), 1e-5, x.clone(), torch.zeros((1, 2)))
+
+
+def test_calls_without_a_device_fail():
+    """Nothing divides by a device's properties, nothing is read: arguments that are right end with the CUDA status."""
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("for machines without a CUDA device")
+    assert _embedding() == _embedding_grad() == _embedding_grad(rows=300, wb=1 << 20) == _rms() == _rms(y8=0, sc=0) == -9
+    assert _rms_grad() == _dropout() == _dropout(ldx=9) == _logits() == _logits(v=5000, ldl=5000, ldo=5000, ldb=5000, ldm=200, z=0x100000,
+                                                                                    o=0x200000, b=0x300000, m=0x400000) == _logits_grad() == -9
