@@ -53,29 +53,32 @@ template <typename A, typename B>
 constexpr int kCommonRun = sizeof(A) < sizeof(B) ? kRun<A> : kRun<B>;
 
 // ------------------------------------------------------------------------------------------------ forward
-// LANES threads to a row; a CTA takes 256 / LANES rows and up to 4 runs of every thread.
+// LANES threads to a row; a CTA takes 256 / LANES rows and up to kAhead runs of every thread, all on their way at once.
+template <int LEN>
+constexpr int kAhead = LEN == 1 ? 16 : 4;
 template <typename S, typename T, int LEN>
-__global__ void __launch_bounds__(256) embedding_kernel(long long rows_all, long long rows, long long vocab, long long c, const S* table,
+__global__ void __launch_bounds__(256) embedding_kernel(long long rows_all, long long rows, long long vocab, int c, const S* table,
                                                         long long ldt, const int64_t* tokens, float scale, T* y, long long ldy,
                                                         int lanes, int col_tiles) {
     const long long row = (long long)(blockIdx.x / col_tiles) * (256 / lanes) + threadIdx.x / lanes;
-    const long long col0 = (long long)(blockIdx.x % col_tiles) * lanes * LEN * 4 + (threadIdx.x % lanes) * LEN;
+    const int col0 = (int)(blockIdx.x % col_tiles) * lanes * LEN * kAhead<LEN> + (int)(threadIdx.x % lanes) * LEN;
     pdl_wait();
     pdl_release();
     if (row >= rows_all) return;
     const int64_t token = tokens[row];
     const bool known = token >= 0 && token < vocab;
-    const S* from = table + (row / rows) * ldt + (known ? token : 0) * c;
+    const long long node = rows_all <= 0xffffffffll ? (long long)((uint32_t)row / (uint32_t)rows) : row / rows;
+    const S* from = table + node * ldt + (known ? token : 0) * c;
     T* to = y + row * ldy;
-    float v[4][LEN];
+    float v[kAhead<LEN>][LEN];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const long long col = col0 + (long long)u * lanes * LEN;
+    for (int u = 0; u < kAhead<LEN>; ++u) {
+        const int col = col0 + u * lanes * LEN;
         if (known && col < c) load_run<S, LEN>(from + col, v[u]);
     }
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const long long col = col0 + (long long)u * lanes * LEN;
+    for (int u = 0; u < kAhead<LEN>; ++u) {
+        const int col = col0 + u * lanes * LEN;
 #pragma unroll
         for (int k = 0; k < LEN; ++k) v[u][k] = known && col < c ? v[u][k] * scale : 0.0f;
         if (col < c) store_run<T, LEN>(to + col, v[u]);
@@ -86,10 +89,10 @@ template <typename S, typename T, int LEN>
 int run_forward(const dlm_embed_args& a, cudaStream_t s) {
     const int64_t R = a.n * a.rows, runs = (a.c + LEN - 1) / LEN;
     int lanes = 8;
-    while (lanes < 256 && lanes * 4 < runs) lanes *= 2;
-    const int64_t col_tiles = (runs + lanes * 4 - 1) / (lanes * 4), ctas = (R + 256 / lanes - 1) / (256 / lanes) * col_tiles;
+    while (lanes < 256 && lanes * kAhead<LEN> < runs) lanes *= 2;
+    const int64_t col_tiles = (runs + lanes * kAhead<LEN> - 1) / (lanes * kAhead<LEN>), ctas = (R + 256 / lanes - 1) / (256 / lanes) * col_tiles;
     if (ctas > 0x7fffffff) return DLM_ERR_UNSUPPORTED;
-    cudaError_t err = launch_overlapped(embedding_kernel<S, T, LEN>, dim3((unsigned)ctas), dim3(256), 0, s, 1, R, a.rows, a.vocab, a.c,
+    cudaError_t err = launch_overlapped(embedding_kernel<S, T, LEN>, dim3((unsigned)ctas), dim3(256), 0, s, 1, R, a.rows, a.vocab, (int)a.c,
                                         static_cast<const S*>(a.table), a.ldt, a.tokens, a.scale, static_cast<T*>(a.y), a.ldy, lanes,
                                         (int)col_tiles);
     dlm_count_launch(1);
@@ -324,23 +327,23 @@ struct GradShape {
     unsigned lead, sum_ctas;
 };
 
-// A warp's strip of a row: kStripBytes of dy.  Where rows are aligned a lane has kRun<T> columns of every 512 bytes, else single columns 32
+// A warp's strip of a row: SB bytes of dy.  Where rows are aligned a lane has kRun<T> columns of every 512 bytes, else single columns 32
 // apart.
-constexpr int kStripBytes = 1024, kAtOnce = 4, kSlots = 2 * kAtOnce, kSlotBytes = kStripBytes + 16;
-template <typename T>
-constexpr int kStrip = kStripBytes / (int)sizeof(T);
-template <typename T, int LEN>
-constexpr int kRuns = kStrip<T> / (32 * LEN);
+constexpr int kLongStrip = 1024, kShortStrip = 512, kAtOnce = 4, kSlots = 2 * kAtOnce;
+template <typename T, int SB>
+constexpr int kStrip = SB / (int)sizeof(T);
+template <int SB>
+constexpr int kSlotBytes = SB + 16;
 
 // Sums over a tile of sorted places, of which lane i of a warp has the i-th and its key: the warp takes a strip of its columns, walks the places
 // in order and writes a token's sum at its end; what goes on in another tile (`ahead`, `behind`: the keys there) is left in part[0 ..] and
-// part[gap ..].  Rows of dy come into the warp's slots by asynchronous copies, four while the four before them are added: 4 to 8 KB on their way for each
-// warp, which hold no registers.
+// part[gap ..].  Rows of dy come into the warp's slots by asynchronous copies, four while the four before them are added: four to eight
+// strips on their way for each warp, which hold no registers.
 // from, to: the node's gradients and table at the strip's first column.
-template <typename T, typename G, int LEN>
+template <typename T, typename G, int LEN, int SB>
 __device__ __forceinline__ void walk_tile(const GradShape& s, const T* dy, const T* from, G* to, int columns, uint32_t key, uint32_t place,
                                           int len, uint32_t ahead, uint32_t behind, unsigned char* slots, float* part, long long gap) {
-    constexpr int U = kRuns<T, LEN>;
+    constexpr int U = kStrip<T, SB> / (32 * LEN);
     const int lane = threadIdx.x & 31;
     const int known = __popc(__ballot_sync(0xffffffffu, key < s.vocab));  // tokens that stand for none come last
     to += lane * LEN;
@@ -352,22 +355,22 @@ __device__ __forceinline__ void walk_tile(const GradShape& s, const T* dy, const
     bool before = __shfl_sync(0xffffffffu, key, 0) == ahead;  // the run at hand began in an earlier tile
     float sum[U][LEN] = {};
     const int mine = columns - lane * LEN;  // the lane's runs begin before this
-    const bool whole_strip = columns == kStrip<T>;
+    const bool whole_strip = columns == kStrip<T, SB>;
     // where a lane's place starts within 16 bytes
     const uint32_t skews = ((uint32_t)(uintptr_t)from + place * (uint32_t)(s.ldy * (long long)sizeof(T))) & 15;
     auto ask = [&](int i) {
         if (i >= known) return;
         const T* row = from + (long long)__shfl_sync(0xffffffffu, place, i) * s.ldy;
-        unsigned char* slot = slots + i % kSlots * kSlotBytes;
+        unsigned char* slot = slots + i % kSlots * kSlotBytes<SB>;
         if (LEN > 1 || !whole_strip || (uintptr_t)row < (uintptr_t)dy + 16) {
             fetch_row<T, LEN, 32>(slot, row, dy, columns, lane);
-        } else {  // 64 chunks, and the first bytes of another one where the row does not start on a chunk
+        } else {  // whole chunks, and the first bytes of another one where the row does not start on a chunk
             const int skew = (int)__shfl_sync(0xffffffffu, skews, i);
             const uint32_t to_slot = smem_u32(slot) + lane * 16;
             const char* chunks = reinterpret_cast<const char*>(row) - skew + lane * 16;
-            copy_chunk(to_slot, chunks, 16);
-            copy_chunk(to_slot + 512, chunks + 512, 16);
-            if (lane == 0 && skew > 0) copy_chunk(to_slot + 1024, chunks + 1024, skew);
+#pragma unroll
+            for (int k = 0; k < SB; k += 512) copy_chunk(to_slot + k, chunks + k, 16);
+            if (lane == 0 && skew > 0) copy_chunk(to_slot + SB, chunks + SB, skew);
         }
     };
     for (int q = 0; q < kAtOnce; ++q) ask(q);
@@ -386,7 +389,7 @@ __device__ __forceinline__ void walk_tile(const GradShape& s, const T* dy, const
 #pragma unroll
             for (int q = 0; q < HOLD; ++q) {
                 const int at = i + h + q;
-                const unsigned char* slot = slots + at % kSlots * kSlotBytes;
+                const unsigned char* slot = slots + at % kSlots * kSlotBytes<SB>;
                 if constexpr (LEN == 1) slot += __shfl_sync(0xffffffffu, skews, at & 31);
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
@@ -441,7 +444,7 @@ __device__ __forceinline__ void sum_tiles(const GradShape& s, unsigned cta, cons
     const int lane = threadIdx.x & 31;
     const long long task = (long long)cta * 8 + (threadIdx.x >> 5), tile_at = task / s.strips;
     if (tile_at >= (long long)s.n * w.tiles) return;
-    const long long col0 = task % s.strips * kStrip<T>;
+    const long long col0 = task % s.strips * kStrip<T, kLongStrip>;
     const int node = (int)(tile_at / w.tiles), tile = (int)(tile_at % w.tiles);
     const long long first = (long long)tile * kTileItems, base = (long long)node * s.rows;
     const int len = (int)min((long long)kTileItems, s.rows - first);
@@ -451,23 +454,23 @@ __device__ __forceinline__ void sum_tiles(const GradShape& s, unsigned cta, cons
         place = w.places[base + first + lane];
     }
     const uint32_t ahead = first > 0 ? w.keys[base + first - 1] : 0xffffffffu, behind = first + len < s.rows ? w.keys[base + first + len] : 0xffffffffu;
-    walk_tile<T, G, LEN>(s, dy, dy + base * s.ldy + col0, dtable + node * s.ldgt + col0, (int)min((long long)kStrip<T>, s.c - col0), key, place,
-                         len, ahead, behind, smem + (threadIdx.x >> 5) * kSlots * kSlotBytes, w.parts + tile_at * 2 * s.c + col0, s.c);
+    walk_tile<T, G, LEN, kLongStrip>(s, dy, dy + base * s.ldy + col0, dtable + node * s.ldgt + col0, (int)min((long long)kStrip<T, kLongStrip>, s.c - col0), key, place,
+                         len, ahead, behind, smem + (threadIdx.x >> 5) * kSlots * kSlotBytes<kLongStrip>, w.parts + tile_at * 2 * s.c + col0, s.c);
 }
 
 // Short texts: a CTA sorts a node's tokens by itself (each counts those before it), its warps walk their tiles of a strip, and what goes
 // on between tiles is joined in shared memory.
-constexpr int kShortText = 256;
+constexpr int kShortText = 512, kShortTiles = kShortText / 32;  // tokens, a thread each; tiles, a warp each
 template <typename T, typename G, int LEN>
 __device__ __forceinline__ void sum_short_text(const GradShape& s, unsigned cta, const int64_t* tokens, const T* dy, G* dtable) {
-    constexpr int U = kRuns<T, LEN>;
+    constexpr int U = kStrip<T, kShortStrip> / (32 * LEN);
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ __align__(16) uint32_t text[kShortText], keys[kShortText + 1];
     __shared__ uint32_t places[kShortText];
-    float* parts = reinterpret_cast<float*>(smem + 8 * kSlots * kSlotBytes);  // [8 tiles][2][strip]
+    float* parts = reinterpret_cast<float*>(smem + kShortTiles * kSlots * kSlotBytes<kShortStrip>);  // [tiles][2][strip]
     const int lane = threadIdx.x & 31, tile = threadIdx.x >> 5;
     const int node = cta / s.strips, rows = (int)s.rows;
-    const long long col0 = (long long)(cta % s.strips) * kStrip<T>;
+    const long long col0 = (long long)(cta % s.strips) * kStrip<T, kShortStrip>;
     uint32_t key = 0xffffffffu;  // behind the text's end
     if ((int)threadIdx.x < rows) {
         const int64_t token = tokens[(long long)node * rows + threadIdx.x];
@@ -489,22 +492,22 @@ __device__ __forceinline__ void sum_short_text(const GradShape& s, unsigned cta,
     __syncthreads();
     const T* from = dy + (long long)node * rows * s.ldy + col0;
     G* to = dtable + node * s.ldgt + col0;
-    const int columns = (int)min((long long)kStrip<T>, s.c - col0), items = min(kTileItems, (rows + 31) / 32 * 4);  // places to a warp
+    const int columns = (int)min((long long)kStrip<T, kShortStrip>, s.c - col0), items = min(kTileItems, (rows + 4 * kShortTiles - 1) / (4 * kShortTiles) * 4);  // places to a warp
     const int first = tile * items, len = max(0, min(items, rows - first));
     const uint32_t mine = lane < len ? keys[first + lane] : 0xffffffffu, place = lane < len ? places[first + lane] : 0;
     const uint32_t ahead = tile > 0 ? keys[first - 1] : 0xffffffffu, behind = keys[first + items];
-    walk_tile<T, G, LEN>(s, dy, from, to, columns, mine, place, len, ahead, behind, smem + tile * kSlots * kSlotBytes,
-                         parts + tile * 2 * kStrip<T>, kStrip<T>);
+    walk_tile<T, G, LEN, kShortStrip>(s, dy, from, to, columns, mine, place, len, ahead, behind, smem + tile * kSlots * kSlotBytes<kShortStrip>,
+                         parts + tile * 2 * kStrip<T, kShortStrip>, kStrip<T, kShortStrip>);
     __syncthreads();
     const uint32_t last = __shfl_sync(0xffffffffu, mine, items - 1);
     if (last >= s.vocab || last != behind || last == ahead) return;
     float sum[U][LEN];
-    const float* part = parts + tile * 2 * kStrip<T> + kStrip<T> + lane * LEN;
+    const float* part = parts + tile * 2 * kStrip<T, kShortStrip> + kStrip<T, kShortStrip> + lane * LEN;
 #pragma unroll
     for (int u = 0; u < U; ++u) load_run<float, LEN>(part + u * 32 * LEN, sum[u]);
-    part -= kStrip<T>;
-    for (int k = tile + 1; k < 8 && keys[k * items] == last; ++k) {
-        part += 2 * kStrip<T>;
+    part -= kStrip<T, kShortStrip>;
+    for (int k = tile + 1; k < kShortTiles && keys[k * items] == last; ++k) {
+        part += 2 * kStrip<T, kShortStrip>;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float v[LEN];
@@ -519,19 +522,19 @@ __device__ __forceinline__ void sum_short_text(const GradShape& s, unsigned cta,
 // Rows without tokens: a CTA clears those among zero_rows rows of a node's table, in 16-byte chunks wherever they start.  It finds
 // them by itself, from the text as it stands, while the tokens are sorted; or, where texts are long beside the table, from the
 // sorted ones.
-template <typename G>
+template <typename G, int THREADS>
 __device__ __forceinline__ void clear_rows(const GradShape& s, unsigned cta, const int64_t* tokens, G* dtable, const Sorted& w) {
     extern __shared__ __align__(16) unsigned char smem[];
     uint32_t* touched = reinterpret_cast<uint32_t*>(smem);  // a bit for each row
     __shared__ int bounds[2];
     const int node = cta / s.zero_ctas;
     const uint32_t v0 = (cta % s.zero_ctas) * (uint32_t)s.zero_rows, count = min((uint32_t)s.zero_rows, s.vocab - v0);
-    for (uint32_t k = threadIdx.x; k < (count + 31) / 32; k += 256) touched[k] = 0;
+    for (uint32_t k = threadIdx.x; k < (count + 31) / 32; k += THREADS) touched[k] = 0;
     if (s.scan) {
         __syncthreads();
         const int64_t* text = tokens + (long long)node * s.rows;
 #pragma unroll 8
-        for (int k = threadIdx.x; k < (int)s.rows; k += 256) {
+        for (int k = threadIdx.x; k < (int)s.rows; k += THREADS) {
             const uint64_t v = (uint64_t)text[k] - v0;
             if (v < count) atomicOr(&touched[v >> 5], 1u << (v & 31));
         }
@@ -540,7 +543,7 @@ __device__ __forceinline__ void clear_rows(const GradShape& s, unsigned cta, con
         const uint32_t* keys = w.keys + (long long)node * s.rows;
         if (threadIdx.x < 2) bounds[threadIdx.x] = lower_bound(keys, (int)s.rows, threadIdx.x ? v0 + count : v0);
         __syncthreads();
-        for (int k = bounds[0] + threadIdx.x; k < bounds[1]; k += 256) {
+        for (int k = bounds[0] + threadIdx.x; k < bounds[1]; k += THREADS) {
             const uint32_t v = keys[k] - v0;
             atomicOr(&touched[v >> 5], 1u << (v & 31));
         }
@@ -551,7 +554,7 @@ __device__ __forceinline__ void clear_rows(const GradShape& s, unsigned cta, con
     const long long line = s.c * (long long)sizeof(G);
     char* table = reinterpret_cast<char*>(dtable + node * s.ldgt + (long long)v0 * s.c);
     const uint32_t group = line >= (16 << 10) ? 1 : line >= (4 << 10) ? 4 : 32;
-    for (uint32_t r0 = (threadIdx.x >> 5) * group; r0 < count; r0 += 8 * group) {
+    for (uint32_t r0 = (threadIdx.x >> 5) * group; r0 < count; r0 += THREADS / 32 * group) {
         const uint32_t rows = min(group, count - r0);
         uint32_t left = ~(touched[r0 >> 5] >> (r0 & 31)) & (0xffffffffu >> (32 - rows));  // rows to clear
         while (left) {
@@ -584,18 +587,18 @@ __global__ void __launch_bounds__(256) embedding_grad_kernel(GradShape s, const 
         pdl_wait();
         sum_tiles<T, G, LEN>(s, cta - s.lead, dy, dtable, w);
     } else {
-        clear_rows<G>(s, cta < s.lead ? cta : cta - s.sum_ctas, tokens, dtable, w);
+        clear_rows<G, 256>(s, cta < s.lead ? cta : cta - s.sum_ctas, tokens, dtable, w);
     }
 }
 
 template <typename T, typename G, int LEN>
-__global__ void __launch_bounds__(256) embedding_grad_short_kernel(GradShape s, const int64_t* tokens, const T* dy, G* dtable) {
+__global__ void __launch_bounds__(kShortText) embedding_grad_short_kernel(GradShape s, const int64_t* tokens, const T* dy, G* dtable) {
     pdl_wait();
     pdl_release();
     if (blockIdx.x < s.sum_ctas)
         sum_short_text<T, G, LEN>(s, blockIdx.x, tokens, dy, dtable);
     else
-        clear_rows<G>(s, blockIdx.x - s.sum_ctas, tokens, dtable, Sorted());
+        clear_rows<G, kShortText>(s, blockIdx.x - s.sum_ctas, tokens, dtable, Sorted());
 }
 
 // Tokens that go on beyond their first tile: its part, then those of the tiles that follow.  A warp to a tile and a strip of 32 LEN columns.
@@ -670,8 +673,9 @@ int run_backward(const dlm_embed_args& a, const Sorted& w, cudaStream_t s) {
     g.n = a.n;
     g.accumulate = a.accumulate;
     g.scale = a.scale;
-    g.strips = (int)((a.c + kStrip<T> - 1) / kStrip<T>);
     const bool brief = a.rows > 0 && a.rows <= kShortText;
+    const int64_t strip = brief ? kStrip<T, kShortStrip> : kStrip<T, kLongStrip>;
+    g.strips = (int)((a.c + strip - 1) / strip);
     const int64_t tiles = (int64_t)a.n * w.tiles, sum_ctas = brief ? (int64_t)a.n * g.strips : (tiles * g.strips + 7) / 8;
     constexpr int RUN = LEN == 1 ? 1 : 4;
     const int64_t join_ctas = (tiles * ((a.c + 32 * RUN - 1) / (32 * RUN)) + 7) / 8;
@@ -691,15 +695,15 @@ int run_backward(const dlm_embed_args& a, const Sorted& w, cudaStream_t s) {
     if (sum_ctas + zero_ctas == 0) return DLM_OK;
     g.sum_ctas = (unsigned)sum_ctas;
     g.lead = (unsigned)std::min<int64_t>(zero_ctas, g.scan ? 8 * sms : 0);
-    constexpr size_t kRing = 8 * kSlots * kSlotBytes, kParts = 8 * 2 * kStrip<T> * 4;
-    const size_t smem = std::max<size_t>(sum_ctas == 0 ? 0 : brief ? kRing + kParts : kRing, (g.zero_rows + 31) / 32 * 4);
+    constexpr size_t kRing = 8 * kSlots * kSlotBytes<kLongStrip>, kShort = kShortTiles * (kSlots * kSlotBytes<kShortStrip> + 2 * kStrip<T, kShortStrip> * 4);
+    const size_t smem = std::max<size_t>(sum_ctas == 0 ? 0 : brief ? kShort : kRing, (g.zero_rows + 31) / 32 * 4);
     const dim3 grid((unsigned)(sum_ctas + zero_ctas));
     const T* dy = static_cast<const T*>(a.dy);
     G* dtable = static_cast<G*>(a.dtable);
     if (brief) {
         auto kern = embedding_grad_short_kernel<T, G, LEN>;
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kRing + kParts)) != cudaSuccess) return DLM_ERR_CUDA;
-        const cudaError_t err = launch_overlapped(kern, grid, dim3(256), smem, s, 1, g, a.tokens, dy, dtable);
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kShort) != cudaSuccess) return DLM_ERR_CUDA;
+        const cudaError_t err = launch_overlapped(kern, grid, dim3(kShortText), smem, s, 1, g, a.tokens, dy, dtable);
         dlm_count_launch(1);
         return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
     }

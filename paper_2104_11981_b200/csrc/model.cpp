@@ -22,7 +22,7 @@ int check_rows(int n, int64_t rows, int64_t c) {
 }
 int check_table(int n, int64_t rows, int64_t vocab, int64_t c) {
     if (n < 1 || rows < 0 || vocab < 1 || c < 1) return DLM_ERR_SHAPE;
-    if (n > DLM_MAX_NODES || vocab >= 0x7fffffff || rows > 0x7fffffff || c > 0x7fffffff) return DLM_ERR_UNSUPPORTED;
+    if (n > DLM_MAX_NODES || vocab >= 0x7fffffff || rows > 0x7fffffff || c > (1 << 30)) return DLM_ERR_UNSUPPORTED;
     if (!fits(rows, n) || !fits(rows * n, c) || !fits(vocab, c) || !fits(n, vocab * c)) return DLM_ERR_UNSUPPORTED;
     return DLM_OK;
 }

@@ -228,7 +228,7 @@ def test_captured_calls_see_new_tokens_and_share_a_workspace():
 
 
 @pytest.mark.parametrize("typ,gtype", [("f32", "bf16"), ("bf16", "f32")])
-@pytest.mark.parametrize("rows", [2, 31, 32, 33, 200, 255, 256, 257])
+@pytest.mark.parametrize("rows", [2, 31, 32, 33, 64, 65, 200, 256, 511, 512, 513])
 @pytest.mark.parametrize("c", [40, 1001, 1200])
 def test_gradient_of_short_texts(rows, c, typ, gtype):
     """Around the sizes where a CTA has the whole text; tokens that fill several tiles, in one strip of columns and in several."""
