@@ -540,8 +540,9 @@ DLM_API int embedding_grad(int n, int64_t rows, int64_t vocab, int64_t c, const 
  *   dy, dh     : device [n * rows, c] of dtype; dh may be h, dy or dresidual (same stride)
  *   dweight    : device [n, c] of g_dtype, row stride ldgw, overwritten (in a column range of the stacked g, for instance)
  *   workspace  : device, rms_norm_grad_workspace_bytes(n, rows, c) bytes, 256-byte aligned, owned by the caller
- * rows may be 0 (the weight's gradient is then 0).  Fast path: c a multiple of 16 bytes' worth and every activation row 16-byte
- * aligned (y8: 8-byte with bf16 rows, 4-byte with fp32 rows).
+ * rows may be 0 (the weight's gradient is then 0).  Fastest: c a multiple of 16 bytes' worth and every activation row 16-byte
+ * aligned (y8: 8-byte with bf16 rows, 4-byte with fp32 rows); next, arrays whose rows start at the same places within 16 bytes (contiguous ones of
+ * an odd width); other layouts go element by element.
  * Errors: DLM_ERR_NULL, DLM_ERR_SHAPE, DLM_ERR_KIND, DLM_ERR_ALIGN, DLM_ERR_ALIAS, DLM_ERR_HYPER, DLM_ERR_WORKSPACE,
  * DLM_ERR_UNSUPPORTED, DLM_ERR_CUDA.
  */
