@@ -116,7 +116,9 @@ constexpr int kChunk = kSortThreads * ITEMS;
 constexpr int kSmallItems = 2, kLargeItems = 16;
 constexpr size_t sort_smem(int items) { return (size_t)kSortThreads * items * 12 + kSortWarps * 256 * 2 + 1024; }
 
-constexpr int kTileItems = 32;  // sorted places that one group of threads sums
+constexpr int kTileItems = 32;  // sorted places that a warp walks at most
+
+constexpr int64_t kWarps = 800;  // tasks below which they are made smaller (1200 and 2400 take 170 and 178 us where 800 takes 167: 8 x 2048 tokens, 1024 columns)
 
 struct Sorted {  // the workspace
     uint32_t* keys;    // [n rows] tokens, sorted; vocab for those outside [0, vocab)
@@ -124,14 +126,17 @@ struct Sorted {  // the workspace
     uint32_t* chunk_keys;    // as above, each chunk sorted by itself; the same arrays where a node is one chunk
     uint32_t* chunk_places;
     float* parts;  // [n tiles][2][c] sums of a tile's first and last token, where they go on in the tiles before and behind
-    int chunk, chunks, tiles;
+    int chunk, chunks, tile, tiles;
     size_t bytes;
 };
 Sorted sorted_layout(int n, int64_t rows, int64_t c, void* workspace) {
     Sorted w = {};
     w.chunk = rows <= 32 * kChunk<kSmallItems> ? kChunk<kSmallItems> : kChunk<kLargeItems>;
     w.chunks = (int)((rows + w.chunk - 1) / w.chunk);
-    w.tiles = (int)((rows + kTileItems - 1) / kTileItems);
+    // short texts: shorter tiles, so that there are warps for the SMs (4 x 1000 tokens, 500 columns bf16: 31 us with 32 places, 20 with 8)
+    w.tile = kTileItems;
+    while (w.tile > 8 && n * (rows / w.tile) * ((c + 511) / 512) < kWarps) w.tile /= 2;
+    w.tiles = (int)((rows + w.tile - 1) / w.tile);
     const int64_t keys = (n * rows * 4 + 255) / 256 * 256;
     char* p = static_cast<char*>(workspace);
     auto take = [&](int64_t bytes) {
@@ -440,24 +445,24 @@ __device__ __forceinline__ void walk_tile(const GradShape& s, const T* dy, const
     wait_copies<0>();
 }
 
-template <typename T, typename G, int LEN>
+template <typename T, typename G, int LEN, int SB>
 __device__ __forceinline__ void sum_tiles(const GradShape& s, unsigned cta, const T* dy, G* dtable, const Sorted& w) {
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 31;
     const long long task = (long long)cta * 8 + (threadIdx.x >> 5), tile_at = task / s.strips;
     if (tile_at >= (long long)s.n * w.tiles) return;
-    const long long col0 = task % s.strips * kStrip<T, kLongStrip>;
+    const long long col0 = task % s.strips * kStrip<T, SB>;
     const int node = (int)(tile_at / w.tiles), tile = (int)(tile_at % w.tiles);
-    const long long first = (long long)tile * kTileItems, base = (long long)node * s.rows;
-    const int len = (int)min((long long)kTileItems, s.rows - first);
+    const long long first = (long long)tile * w.tile, base = (long long)node * s.rows;
+    const int len = (int)min((long long)w.tile, s.rows - first);
     uint32_t key = 0xffffffffu, place = 0;
     if (lane < len) {
         key = w.keys[base + first + lane];
         place = w.places[base + first + lane];
     }
     const uint32_t ahead = first > 0 ? w.keys[base + first - 1] : 0xffffffffu, behind = first + len < s.rows ? w.keys[base + first + len] : 0xffffffffu;
-    walk_tile<T, G, LEN, kLongStrip>(s, dy, dy + base * s.ldy + col0, dtable + node * s.ldgt + col0, (int)min((long long)kStrip<T, kLongStrip>, s.c - col0), key, place,
-                         len, ahead, behind, smem + (threadIdx.x >> 5) * kSlots * kSlotBytes<kLongStrip>, w.parts + tile_at * 2 * s.c + col0, s.c);
+    walk_tile<T, G, LEN, SB>(s, dy, dy + base * s.ldy + col0, dtable + node * s.ldgt + col0, (int)min((long long)kStrip<T, SB>, s.c - col0), key, place,
+                         len, ahead, behind, smem + (threadIdx.x >> 5) * kSlots * kSlotBytes<SB>, w.parts + tile_at * 2 * s.c + col0, s.c);
 }
 
 // Short texts: a CTA sorts a node's tokens by itself (each counts those before it), its warps walk their tiles of a strip, and what goes
@@ -581,13 +586,13 @@ __device__ __forceinline__ void clear_rows(const GradShape& s, unsigned cta, con
 }
 
 // CTAs [lead, lead + sum_ctas) add, the others clear: the first of them have work until the tokens are sorted.
-template <typename T, typename G, int LEN>
+template <typename T, typename G, int LEN, int SB>
 __global__ void __launch_bounds__(256) embedding_grad_kernel(GradShape s, const int64_t* tokens, const T* dy, G* dtable, Sorted w) {
     pdl_release();  // the join waits for all of this
     const unsigned cta = blockIdx.x;
     if (cta >= s.lead && cta < s.lead + s.sum_ctas) {
         pdl_wait();
-        sum_tiles<T, G, LEN>(s, cta - s.lead, dy, dtable, w);
+        sum_tiles<T, G, LEN, SB>(s, cta - s.lead, dy, dtable, w);
     } else {
         clear_rows<G, 256>(s, cta < s.lead ? cta : cta - s.sum_ctas, tokens, dtable, w);
     }
@@ -614,10 +619,10 @@ __global__ void __launch_bounds__(256) embedding_grad_join_kernel(GradShape s, G
     if (tile_at >= (long long)s.n * w.tiles || col >= s.c) return;
     const int node = (int)(tile_at / w.tiles);
     int tile = (int)(tile_at % w.tiles);
-    const long long end = (long long)(tile + 1) * kTileItems;
+    const long long end = (long long)(tile + 1) * w.tile;
     if (end >= s.rows) return;
     const uint32_t* keys = w.keys + (long long)node * s.rows;
-    const uint32_t key = keys[end - 1], behind = keys[end], ahead = end > kTileItems ? keys[end - kTileItems - 1] : 0xffffffffu;
+    const uint32_t key = keys[end - 1], behind = keys[end], ahead = end > w.tile ? keys[end - w.tile - 1] : 0xffffffffu;
     if (key >= s.vocab || behind != key || ahead == key) return;  // the last: an earlier tile has its beginning
     const float* part = w.parts + tile_at * 2 * s.c + col;
     float sum[1][LEN];
@@ -632,7 +637,7 @@ __global__ void __launch_bounds__(256) embedding_grad_join_kernel(GradShape s, G
             part += 2 * s.c;
             head[k] = 0xffffffffu;
             if (tile < w.tiles) {
-                head[k] = keys[(long long)tile * kTileItems];
+                head[k] = keys[(long long)tile * w.tile];
                 load_run<float, LEN>(part, v[k]);
             }
         }
@@ -676,7 +681,8 @@ int run_backward(const dlm_embed_args& a, const Sorted& w, cudaStream_t s) {
     g.accumulate = a.accumulate;
     g.scale = a.scale;
     const bool brief = a.rows > 0 && a.rows <= kShortText;
-    const int64_t strip = brief ? kStrip<T, kShortStrip> : kStrip<T, kLongStrip>;
+    const bool narrow = brief || (int64_t)a.n * w.tiles * ((a.c + kStrip<T, kLongStrip> - 1) / kStrip<T, kLongStrip>) < kWarps;  // strips
+    const int64_t strip = narrow ? kStrip<T, kShortStrip> : kStrip<T, kLongStrip>;
     g.strips = (int)((a.c + strip - 1) / strip);
     const int64_t tiles = (int64_t)a.n * w.tiles, sum_ctas = brief ? (int64_t)a.n * g.strips : (tiles * g.strips + 7) / 8;
     constexpr int RUN = LEN == 1 ? 1 : 4;
@@ -697,8 +703,8 @@ int run_backward(const dlm_embed_args& a, const Sorted& w, cudaStream_t s) {
     if (sum_ctas + zero_ctas == 0) return DLM_OK;
     g.sum_ctas = (unsigned)sum_ctas;
     g.lead = (unsigned)std::min<int64_t>(zero_ctas, g.scan ? 8 * sms : 0);
-    constexpr size_t kRing = 8 * kSlots * kSlotBytes<kLongStrip>, kShort = kShortTiles * (kSlots * kSlotBytes<kShortStrip> + 2 * kStrip<T, kShortStrip> * 4);
-    const size_t smem = std::max<size_t>(sum_ctas == 0 ? 0 : brief ? kShort : kRing, (g.zero_rows + 31) / 32 * 4);
+    constexpr size_t kRing = 8 * kSlots * kSlotBytes<kLongStrip>, kNarrow = 8 * kSlots * kSlotBytes<kShortStrip>, kShort = kShortTiles * (kSlots * kSlotBytes<kShortStrip> + 2 * kStrip<T, kShortStrip> * 4);
+    const size_t smem = std::max<size_t>(sum_ctas == 0 ? 0 : brief ? kShort : narrow ? kNarrow : kRing, (g.zero_rows + 31) / 32 * 4);
     const dim3 grid((unsigned)(sum_ctas + zero_ctas));
     const T* dy = static_cast<const T*>(a.dy);
     G* dtable = static_cast<G*>(a.dtable);
@@ -713,7 +719,7 @@ int run_backward(const dlm_embed_args& a, const Sorted& w, cudaStream_t s) {
         const int rc = w.chunk == kChunk<kSmallItems> ? run_sort<kSmallItems>(a, w, s) : run_sort<kLargeItems>(a, w, s);
         if (rc != DLM_OK) return rc;
     }
-    auto kern = embedding_grad_kernel<T, G, LEN>;
+    auto kern = narrow ? embedding_grad_kernel<T, G, LEN, kShortStrip> : embedding_grad_kernel<T, G, LEN, kLongStrip>;
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRing) != cudaSuccess) return DLM_ERR_CUDA;
     cudaError_t err = launch_overlapped(kern, grid, dim3(256), smem, s, 1, g, a.tokens, dy, dtable, w);
     dlm_count_launch(1);
