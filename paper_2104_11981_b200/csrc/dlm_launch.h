@@ -4,6 +4,7 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 #include <mutex>
 
@@ -37,6 +38,19 @@ inline const DeviceInfo& device_info() {
 // Waits until the tables copied from pageable memory are on the device.  cudaMemcpy may return when it has staged them, and a call on a
 // stream that is not ordered behind the default one would then read what was there before.
 inline bool finish_uploads() { return cudaStreamSynchronize(cudaStreamLegacy) == cudaSuccess; }
+
+// Allows a kernel `bytes` of dynamic shared memory, the same for all of its calls: asked once a device, which takes 0.5 to 1 us.
+template <auto KERNEL>
+bool allow_shared(int bytes) {
+    static std::atomic<uint64_t> allowed{0};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return false;
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+    if (allowed.load(std::memory_order_relaxed) & bit) return true;
+    if (cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+    allowed.fetch_or(bit, std::memory_order_relaxed);
+    return true;
+}
 
 // For the end of an entry point: a runtime call that failed leaves its error behind, and the next step's launch would report it as
 // its own.

@@ -657,8 +657,7 @@ int run_sort(const dlm_embed_args& a, const Sorted& w, cudaStream_t s) {
     int bits = 1;
     while (bits < 31 && (1ll << bits) <= a.vocab) ++bits;  // keys up to and including vocab
     const int passes = (bits + 7) / 8;
-    if (cudaFuncSetAttribute(sort_kernel<ITEMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sort_smem(ITEMS)) != cudaSuccess)
-        return DLM_ERR_CUDA;
+    if (!allow_shared<sort_kernel<ITEMS>>((int)sort_smem(ITEMS))) return DLM_ERR_CUDA;
     cudaError_t err = launch_overlapped(sort_kernel<ITEMS>, dim3((unsigned)(a.n * w.chunks)), dim3(kSortThreads), sort_smem(ITEMS), s, 1,
                                         a.rows, (uint32_t)a.vocab, a.tokens, passes, (bits + passes - 1) / passes, w);
     dlm_count_launch(1);
@@ -710,7 +709,7 @@ int run_backward(const dlm_embed_args& a, const Sorted& w, cudaStream_t s) {
     G* dtable = static_cast<G*>(a.dtable);
     if (brief) {
         auto kern = embedding_grad_short_kernel<T, G, LEN>;
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kShort) != cudaSuccess) return DLM_ERR_CUDA;
+        if (!allow_shared<embedding_grad_short_kernel<T, G, LEN>>((int)kShort)) return DLM_ERR_CUDA;
         const cudaError_t err = launch_overlapped(kern, grid, dim3(kShortText), smem, s, 1, g, a.tokens, dy, dtable);
         dlm_count_launch(1);
         return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
@@ -720,7 +719,8 @@ int run_backward(const dlm_embed_args& a, const Sorted& w, cudaStream_t s) {
         if (rc != DLM_OK) return rc;
     }
     auto kern = narrow ? embedding_grad_kernel<T, G, LEN, kShortStrip> : embedding_grad_kernel<T, G, LEN, kLongStrip>;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRing) != cudaSuccess) return DLM_ERR_CUDA;
+    if (!(narrow ? allow_shared<embedding_grad_kernel<T, G, LEN, kShortStrip>>((int)kNarrow) : allow_shared<embedding_grad_kernel<T, G, LEN, kLongStrip>>((int)kRing)))
+        return DLM_ERR_CUDA;
     cudaError_t err = launch_overlapped(kern, grid, dim3(256), smem, s, 1, g, a.tokens, dy, dtable, w);
     dlm_count_launch(1);
     if (err == cudaSuccess && w.tiles > 1) {

@@ -368,9 +368,8 @@ int run_text(const dlm_logits_args& a, int64_t tile_bytes, cudaStream_t s) {
     const int64_t ctas = R * tiles;
     if (ctas > 0x7fffffff) return DLM_ERR_UNSUPPORTED;
     const int smem = text_bytes(tile_chunks * LEN, sizeof(T), GRAD);
-    auto kern = logits_text_kernel<T, GRAD, THREADS>;
-    if (smem > (48 << 10) && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 << 10) != cudaSuccess) return DLM_ERR_CUDA;
-    cudaError_t err = launch_overlapped(kern, dim3((unsigned)ctas), dim3(THREADS), smem, s, 1, a, tiles, tile_chunks);
+    if (smem > (48 << 10) && !allow_shared<logits_text_kernel<T, GRAD, THREADS>>(80 << 10)) return DLM_ERR_CUDA;
+    cudaError_t err = launch_overlapped(logits_text_kernel<T, GRAD, THREADS>, dim3((unsigned)ctas), dim3(THREADS), smem, s, 1, a, tiles, tile_chunks);
     dlm_count_launch(1);
     return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
 }
