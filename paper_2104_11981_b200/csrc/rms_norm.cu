@@ -53,7 +53,7 @@ __device__ __forceinline__ float warp_max(float v) {
 
 // Where rows do not start on 16 bytes (SKEW), but all arrays' rows do so alike, a group takes rows that start at the same place of their
 // first chunk: every P-th row, P <= 8.  Chunks of memory are then the same columns in each of its rows, and a thread copies, keeps and
-// writes whole chunks of its own as elsewhere; the elements of the first and last chunk that belong to other rows are masked.
+// writes whole chunks of its own as elsewhere; the elements of a first and a last chunk that other rows share are a lane's each, of one warp.
 // A thread's first column in run u.
 template <int LEN, int TPR>
 __device__ __forceinline__ int run_column(int t, int u, int skew) { return column<LEN, TPR>(t, u) - skew; }
@@ -101,23 +101,29 @@ __device__ __forceinline__ void bulk_chunks(unsigned char* buf, const T* row, co
     const int lo = e.skew > 0 && first;
     bulk_row(buf + lo * 16, row - e.skew + lo * LEN, bulk_bytes(e, first, end), bar);
 }
-// What a row's first and last chunk hold of other rows counts nothing: the threads that have these chunks clear it.
+// The elements of a row's shared chunks that a thread takes: up to X of them, by the lanes of one warp (its second where it has several, since
+// the first and the last are busy with the copies).
 template <typename T, int LEN, int TPR>
-__device__ __forceinline__ void clear_ends(unsigned char* buf, const Ends<T, LEN>& e, int t) {
-    const bool head = t == 0 && e.skew > 0, tail = t == e.last % TPR && e.rest > 0;
-    if (!head && !tail) return;
-    T* to = reinterpret_cast<T*>(buf);
+struct Shared {
+    static constexpr int LANES = TPR < 32 ? TPR : 32, X = (2 * LEN + LANES - 1) / LANES, FIRST = TPR >= 128 ? 32 : 0;
+    int col[X];  // -1: none
+    bool any;    // the warp has such
+    __device__ __forceinline__ Shared(const Ends<T, LEN>& e, int c, int t) {
+        const int head = e.skew > 0 ? min(LEN - e.skew, c) : 0, tail = e.last > 0 || e.skew == 0 ? e.rest : 0;
+        any = TPR <= 32 || t / 32 == FIRST / 32;
 #pragma unroll
-    for (int k = 0; k < LEN; ++k) {
-        if (head && k < e.skew) to[k] = narrow<T>(0.0f);
-        if (tail && k >= e.rest) to[e.last * LEN + k] = narrow<T>(0.0f);
+        for (int x = 0; x < X; ++x) {
+            const int j = t - FIRST + x * LANES;
+            col[x] = !any ? -1 : j < LEN ? (j < head ? j : -1) : j - LEN < tail ? c - tail + j - LEN : -1;
+        }
     }
-}
+};
 template <typename T, int LEN, int TPR, bool SKEW>
 __device__ __forceinline__ void run_values(const unsigned char* buf, int skew, int c, int t, int u, float* v) {
     if constexpr (SKEW) {
         Words a = {{0u, 0u, 0u, 0u}};
-        if (run_column<LEN, TPR>(t, u, skew) < c) a = ld_words(buf + column<LEN, TPR>(t, u) * (int)sizeof(T));
+        const int at = run_column<LEN, TPR>(t, u, skew);
+        if (at >= 0 && at + LEN <= c) a = ld_words(buf + column<LEN, TPR>(t, u) * (int)sizeof(T));
         unpack<T>(a, v);
     } else {
         one_run<T, LEN, TPR>(buf, skew, c, t, u, v);
@@ -144,24 +150,13 @@ __device__ __forceinline__ void weight_run(const float* w, int at, int c, bool r
         for (int k = 0; k < LEN; ++k) v[k] = at + k >= 0 && at + k < c ? w[at + k] : 0.0f;
     }
 }
-// A row of results (none where c is below 0): whole chunks straight to memory, the elements of the first and the last one through `ends` (32 bytes of the group's), a
-// thread each.
+// A row's whole chunks of results.
 template <typename T, int LEN, int E, int TPR>
-__device__ __forceinline__ void put_chunks(T* row, unsigned char* ends, const Ends<T, LEN>& e, int c, int t, const float* v) {
+__device__ __forceinline__ void put_chunks(T* row, int skew, int c, int t, const float* v) {
 #pragma unroll
     for (int u = 0; u < E / LEN; ++u) {
-        const int at = run_column<LEN, TPR>(t, u, e.skew);
-        if (at >= 0 && at + LEN <= c)
-            st_words(row + at, pack<T>(v + u * LEN));
-        else if (at < c)
-            st_words(ends + (at < 0 ? 0 : 16), pack<T>(v + u * LEN));
-    }
-    const T* staged = reinterpret_cast<const T*>(ends);
-    if (t / 32 == 0 || t / 32 == e.last % TPR / 32) {  // the warps that have the ends
-        __syncwarp();
-        if (t < LEN && t >= e.skew && e.skew > 0 && t - e.skew < c) row[t - e.skew] = staged[t];
-        if (c > 0 && (e.last > 0 || e.skew == 0) && e.last % TPR / 8 == t / 8 && t % 8 < e.rest) row[e.last * LEN - e.skew + t % 8] = staged[16 / (int)sizeof(T) + t % 8];
-        __syncwarp();  // they may be written again
+        const int at = run_column<LEN, TPR>(t, u, skew);
+        if (at >= 0 && at + LEN <= c) st_words(row + at, pack<T>(v + u * LEN));
     }
 }
 
@@ -229,7 +224,8 @@ __global__ void __launch_bounds__(kBlock<TPR>, (SKEW && sizeof(T) == 2 && !EIGHT
     const T *row = fetch, *row_r = fetch_r;
     const int skew = SKEW ? row_skew(row) / (int)sizeof(T) : 0;
     const Ends<T, LEN> ends(skew, c);
-    __shared__ __align__(16) unsigned char staged[SKEW ? GROUPS : 1][2][32];
+    const Shared<T, LEN, TPR> shared(ends, c, t);
+    constexpr int X = Shared<T, LEN, TPR>::X;
     long long asked = first;
     if constexpr (BULK) {
         if (threadIdx.x == 0) {
@@ -242,7 +238,7 @@ __global__ void __launch_bounds__(kBlock<TPR>, (SKEW && sizeof(T) == 2 && !EIGHT
     pdl_release();
     auto ask = [&](int k) {  // the next row, into slot k
         unsigned char* buf = in + k * slot_bytes;
-        // by the last warp, since the first one has the row's beginning to see to (gradient of 4 x 4000 x 2201 bf16 94 us with the first, 83)
+        // by the last warp
         if constexpr (SKEW && BULK) {
             if (threadIdx.x == TPR - 32 && asked < rows) {
                 const bool lead = base + asked == 0, end = base + asked == (long long)gridDim.y * rows - 1;
@@ -281,6 +277,9 @@ __global__ void __launch_bounds__(kBlock<TPR>, (SKEW && sizeof(T) == 2 && !EIGHT
     for (int k = 0; k < D - 1; ++k) ask(k);
     float w[E];
     run_params<LEN, E, TPR>(weight + node * ldw, skew, c, t, w);
+    float xw[X];
+#pragma unroll
+    for (int x = 0; x < X; ++x) xw[x] = SKEW && shared.col[x] >= 0 ? weight[node * ldw + shared.col[x]] : 0.0f;
     const float inv_c = 1.0f / (float)c;
     int slot = 0, side = 0;
     uint32_t parities = 0;  // of each slot's next phase
@@ -293,15 +292,11 @@ __global__ void __launch_bounds__(kBlock<TPR>, (SKEW && sizeof(T) == 2 && !EIGHT
             ok = mbar_wait(smem_u32(&full[slot]), (parities >> slot) & 1);
         } else {
             wait_copies<D - 1>();
-            if constexpr (!SKEW) group_barrier<TPR>();  // else the thread's own chunks are all it needs
+            group_barrier<TPR>();
         }
         const bool live = BULK || r < rows;
         const int live_c = live ? c : SKEW ? -LEN : 0;  // no column is below it
         const unsigned char* buf = in + slot * slot_bytes;
-        if constexpr (SKEW) {
-            clear_ends<T, LEN, TPR>(in + slot * slot_bytes, ends, t);
-            if (residual) clear_ends<T, LEN, TPR>(in + slot * slot_bytes + rb, ends, t);
-        }
         float v[E];
         const int s0 = SKEW ? skew : row_skew(row), s1 = SKEW ? skew : row_skew(row_r);
 #pragma unroll
@@ -322,7 +317,19 @@ __global__ void __launch_bounds__(kBlock<TPR>, (SKEW && sizeof(T) == 2 && !EIGHT
             s2 = __ffma2_rn(make_float2(v[e], v[e + 1]), make_float2(v[e], v[e + 1]), s2);
             if constexpr (EIGHT) top = fmaxf(top, fmaxf(fabsf(v[e] * w[e]), fabsf(v[e + 1] * w[e + 1])));
         }
-        float sum = s2.x + s2.y;
+        float sum = s2.x + s2.y, xv[X];
+        if (SKEW && shared.any) {
+#pragma unroll
+            for (int x = 0; x < X; ++x) {
+                xv[x] = 0.0f;
+                if (shared.col[x] >= 0 && live) {
+                    xv[x] = widen(reinterpret_cast<const T*>(buf)[skew + shared.col[x]]);
+                    if (residual) xv[x] += widen(reinterpret_cast<const T*>(buf + rb)[skew + shared.col[x]]);
+                }
+                sum = fmaf(xv[x], xv[x], sum);
+                if constexpr (EIGHT) top = fmaxf(top, fabsf(xv[x] * xw[x]));
+            }
+        }
         if constexpr (BULK) fence_before_refill();
         if (!sum_and_top<TPR, BULK, EIGHT>(sum, top, part[side], ok)) {
             give_up(&g_rms_kernel_error, full, parities);
@@ -333,11 +340,21 @@ __global__ void __launch_bounds__(kBlock<TPR>, (SKEW && sizeof(T) == 2 && !EIGHT
         const long long at = base + r;
         auto put = [&](T* to, int which) {
             if constexpr (SKEW)
-                put_chunks<T, LEN, E, TPR>(to, staged[group][which], ends, live_c, t, v);
+                put_chunks<T, LEN, E, TPR>(to, skew, live_c, t, v);
             else if (live)
                 put_values<T, LEN, E, TPR>(to, out + which * rb, c, t, v);
         };
         if (h) put(h + at * ldh, 0);
+        if (SKEW && shared.any && live) {
+#pragma unroll
+            for (int x = 0; x < X; ++x) {
+                const int col = shared.col[x];
+                if (col < 0) continue;
+                if (h) h[at * ldh + col] = narrow<T>(xv[x]);
+                if (!EIGHT || y) y[at * ldy + col] = narrow<T>(xv[x] * rs * xw[x]);
+                if constexpr (EIGHT) y8[at * ld8 + col] = e4m3_one(ToE4M3(top)(xv[x] * xw[x]));
+            }
+        }
         if constexpr (EIGHT) {
             const ToE4M3 map(top);
             if (live) {
@@ -348,12 +365,12 @@ __global__ void __launch_bounds__(kBlock<TPR>, (SKEW && sizeof(T) == 2 && !EIGHT
                     for (int k = 0; k < LEN; ++k) q[k] = map(v[u * LEN + k] * w[u * LEN + k]);
                     const int col = run_column<LEN, TPR>(t, u, skew);
                     unsigned char* to = y8 + at * ld8 + col;
-                    if (!SKEW || (col >= 0 && col + LEN <= c && (uintptr_t)to % LEN == 0)) {
-                        if (col < c) put_e4m3<LEN>(to, q);
+                    if (SKEW ? col < 0 || col + LEN > c : col >= c) continue;
+                    if (!SKEW || (uintptr_t)to % LEN == 0) {
+                        put_e4m3<LEN>(to, q);
                     } else {
 #pragma unroll
-                        for (int k = 0; k < LEN; ++k)
-                            if (col + k >= 0 && col + k < c) to[k] = e4m3_one(q[k]);
+                        for (int k = 0; k < LEN; ++k) to[k] = e4m3_one(q[k]);
                     }
                 }
                 if (t == 0) scales[at] = top * rs / kE4M3Max;
@@ -369,7 +386,7 @@ __global__ void __launch_bounds__(kBlock<TPR>, (SKEW && sizeof(T) == 2 && !EIGHT
             put(y + at * ldy, 1);
         }
         if (t == 0 && live) rstd[at] = rs;
-        if constexpr (!BULK && !SKEW) group_barrier<TPR>();  // the slot may be filled again, and the results are in their buffers
+        if constexpr (!BULK) group_barrier<TPR>();  // the slot may be filled again, and the results are in their buffers
         if (LEN == 1 && live) {
             if (h) flush_row<T, TPR>(h + at * ldh, out, c, t);
             if (!EIGHT || y) flush_row<T, TPR>(y + at * ldy, out + rb, c, t);
@@ -453,7 +470,8 @@ __global__ void __launch_bounds__(kBlock<TPR>, kLeastCtas<TPR>)
     const float* w = weight + node * ldw;
     const int skew = SKEW ? row_skew(hr) / (int)sizeof(T) : 0;
     const Ends<T, LEN> ends(skew, c);
-    __shared__ __align__(16) unsigned char staged[SKEW ? GROUPS : 1][2][32];
+    const Shared<T, LEN, TPR> shared(ends, c, t);
+    constexpr int X = Shared<T, LEN, TPR>::X;
     long long asked = first;
     rstd += base;
     if constexpr (BULK) {
@@ -512,9 +530,14 @@ __global__ void __launch_bounds__(kBlock<TPR>, kLeastCtas<TPR>)
     float wv[HOLD ? E : 1];
     if constexpr (HOLD) run_params<LEN, E, TPR>(w, skew, c, t, wv);
     const bool w_runs = ((uintptr_t)(w - skew) & 15) == 0;  // a run's weights are 16-byte runs
-    float dw[E];
+    float dw[E], xw[X], xdw[X];
 #pragma unroll
     for (int e = 0; e < E; ++e) dw[e] = 0.0f;
+#pragma unroll
+    for (int x = 0; x < X; ++x) {
+        xw[x] = SKEW && shared.col[x] >= 0 ? w[shared.col[x]] : 0.0f;
+        xdw[x] = 0.0f;
+    }
     const float inv_c = 1.0f / (float)c;
     int slot = 0, side = 0;
     uint32_t parities = 0;  // of each slot's next phase
@@ -530,17 +553,12 @@ __global__ void __launch_bounds__(kBlock<TPR>, kLeastCtas<TPR>)
             ok = mbar_wait(smem_u32(&full[slot]), (parities >> slot) & 1);
         } else {
             wait_copies<D - 1>();
-            if constexpr (!SKEW) group_barrier<TPR>();  // else the thread's own chunks are all it needs
+            group_barrier<TPR>();
         }
         const bool live = BULK || r < rows;
         const int live_c = live ? c : SKEW ? -LEN : 0;  // no column is below it
         const unsigned char *hb = in + slot * slot_bytes, *gb = hb + rb, *eb = gb + rb;
         const int hs = SKEW ? skew : row_skew(hr), gs = SKEW ? skew : row_skew(gr), es = SKEW ? skew : row_skew(er);
-        if constexpr (SKEW) {
-            clear_ends<T, LEN, TPR>(in + slot * slot_bytes, ends, t);
-            clear_ends<T, LEN, TPR>(in + slot * slot_bytes + rb, ends, t);
-            if (dres) clear_ends<T, LEN, TPR>(in + slot * slot_bytes + 2 * rb, ends, t);
-        }
         float sum = 0.0f, none = 0.0f;
         float xh[HOLD ? E : LEN], v[HOLD ? E : LEN], more[HOLD ? E : LEN];
         if constexpr (HOLD) {
@@ -583,6 +601,22 @@ __global__ void __launch_bounds__(kBlock<TPR>, kLeastCtas<TPR>)
                 }
             }
         }
+        float xx[X], xp[X], xe[X];  // of the elements of shared chunks: xh, w dy, the residual's gradient
+        if (SKEW && shared.any) {
+#pragma unroll
+            for (int x = 0; x < X; ++x) {
+                xx[x] = xp[x] = xe[x] = 0.0f;
+                if (shared.col[x] >= 0 && live) {
+                    const int k = skew + shared.col[x];
+                    const float g = widen(reinterpret_cast<const T*>(gb)[k]);
+                    xx[x] = widen(reinterpret_cast<const T*>(hb)[k]) * rs;
+                    xp[x] = g * xw[x];
+                    if (dres) xe[x] = widen(reinterpret_cast<const T*>(eb)[k]);
+                    xdw[x] = fmaf(g, xx[x], xdw[x]);
+                    sum = fmaf(xp[x], xx[x], sum);
+                }
+            }
+        }
         if constexpr (BULK && HOLD) fence_before_refill();
         if (!sum_and_top<TPR, BULK, false>(sum, none, part[side], ok)) {
             give_up(&g_rms_kernel_error, full, parities);
@@ -590,6 +624,11 @@ __global__ void __launch_bounds__(kBlock<TPR>, kLeastCtas<TPR>)
         }
         side ^= 1;
         const float m = sum * inv_c;
+        if (SKEW && shared.any && live) {
+#pragma unroll
+            for (int x = 0; x < X; ++x)
+                if (shared.col[x] >= 0) to[shared.col[x]] = narrow<T>(fmaf(fmaf(xx[x], -m, xp[x]), rs, xe[x]));
+        }
         if constexpr (HOLD) {
 #pragma unroll
             for (int e = 0; e < E; e += 2) {
@@ -599,7 +638,7 @@ __global__ void __launch_bounds__(kBlock<TPR>, kLeastCtas<TPR>)
                 v[e + 1] = o.y;
             }
             if constexpr (SKEW) {
-                put_chunks<T, LEN, E, TPR>(to, staged[group][0], ends, live_c, t, v);
+                put_chunks<T, LEN, E, TPR>(to, skew, live_c, t, v);
             } else if (live) {
                 put_values<T, LEN, E, TPR>(to, out, c, t, v);
             }
@@ -619,19 +658,14 @@ __global__ void __launch_bounds__(kBlock<TPR>, kLeastCtas<TPR>)
                 }
                 if (live && at < c) {
                     if constexpr (LEN > 1) {
-                        if (!SKEW || (at >= 0 && at + LEN <= c))
-                            st_words(to + at, pack<T>(v));
-                        else
-#pragma unroll
-                            for (int k = 0; k < LEN; ++k)
-                                if (at + k >= 0 && at + k < c) to[at + k] = narrow<T>(v[k]);
+                        if (!SKEW || (at >= 0 && at + LEN <= c)) st_words(to + at, pack<T>(v));
                     }
                     if constexpr (LEN == 1) reinterpret_cast<T*>(out + row_skew(to))[at] = narrow<T>(v[0]);
                 }
             }
         }
         if constexpr (BULK && !HOLD) fence_before_refill();
-        if constexpr ((!SKEW && !BULK) || (BULK && !HOLD)) group_barrier<TPR>();  // the slot may be filled again, and the results are in their buffer
+        if constexpr (!BULK || !HOLD) group_barrier<TPR>();  // the slot may be filled again, and the results are in their buffer
         if (LEN == 1 && live) flush_row<T, TPR>(to, out, c, t);
         parities ^= 1u << slot;
         if (++slot == D) slot = 0;
@@ -644,15 +678,21 @@ __global__ void __launch_bounds__(kBlock<TPR>, kLeastCtas<TPR>)
     wait_copies<0>();
     // the CTA's groups join in order, in the rows' buffers
     float* total = partial + ((long long)node * gridDim.x + blockIdx.x) * c;
+    auto own_column = [&](int u, int k) {
+        const int at = run_column<LEN, TPR>(t, u, skew);
+        return SKEW ? at >= 0 && at + LEN <= c : at + k < c;
+    };
     if constexpr (GROUPS > 1) {
         float* joined = reinterpret_cast<float*>(smem);  // [GROUPS][c]
         __syncthreads();
 #pragma unroll
+        for (int x = 0; x < X; ++x)
+            if (SKEW && shared.col[x] >= 0) joined[group * c + shared.col[x]] = xdw[x];
+#pragma unroll
         for (int u = 0; u < E / LEN; ++u)
 #pragma unroll
             for (int k = 0; k < LEN; ++k)
-                if (run_column<LEN, TPR>(t, u, skew) + k >= 0 && run_column<LEN, TPR>(t, u, skew) + k < c)
-                    joined[group * c + run_column<LEN, TPR>(t, u, skew) + k] = dw[u * LEN + k];
+                if (own_column(u, k)) joined[group * c + run_column<LEN, TPR>(t, u, skew) + k] = dw[u * LEN + k];
         __syncthreads();
         for (int k = threadIdx.x; k < c; k += kBlock<TPR>) {
             float s = joined[k];
@@ -662,11 +702,13 @@ __global__ void __launch_bounds__(kBlock<TPR>, kLeastCtas<TPR>)
         }
     } else {
 #pragma unroll
+        for (int x = 0; x < X; ++x)
+            if (SKEW && shared.col[x] >= 0) total[shared.col[x]] = xdw[x];
+#pragma unroll
         for (int u = 0; u < E / LEN; ++u)
 #pragma unroll
             for (int k = 0; k < LEN; ++k) {
-                const int at = run_column<LEN, TPR>(t, u, skew) + k;
-                if (at >= 0 && at < c) total[at] = dw[u * LEN + k];
+                if (own_column(u, k)) total[run_column<LEN, TPR>(t, u, skew) + k] = dw[u * LEN + k];
             }
     }
 }
