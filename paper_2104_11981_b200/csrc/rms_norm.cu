@@ -198,14 +198,14 @@ __device__ __forceinline__ void put_e4m3(unsigned char* to, const float* v) {
         *to = e4m3_one(v[0]);
 }
 
-// 128 registers a thread suffice; left alone, the compiler takes up to 180 where rows are skewed, and half of the CTAs fit.  (bf16 forward, skewed:
-// 64 do, 4 x 4000 x 2201 with residual 73 us instead of 94; fp32 rows are better off with 128, 4 x 4000 x 1502 70 us instead of 73.)
+// 128 registers a thread suffice; left alone, the compiler takes up to 180 where rows are skewed, and half of the CTAs fit.  64 are too few (4 x
+// 4000 x 2201 bf16 with residual, skewed: 62 us instead of 56).
 template <int TPR>
 constexpr int kLeastCtas = 512 / kBlock<TPR>;
 
 // Groups of TPR threads take every G-th row of a node; x and the residual come D - 1 rows ahead.  EIGHT: the 8-bit output, too.
 template <typename T, int LEN, int E, int TPR, int D, bool EIGHT, bool SKEW>
-__global__ void __launch_bounds__(kBlock<TPR>, (SKEW && sizeof(T) == 2 && !EIGHT && E <= 16 ? 2 : 1) * kLeastCtas<TPR>)
+__global__ void __launch_bounds__(kBlock<TPR>, kLeastCtas<TPR>)
     rms_norm_kernel(long long rows, int c, const T* x, long long ldx, const T* residual, long long ldr, const float* weight, long long ldw,
                     float eps, T* h, long long ldh, T* y, long long ldy, unsigned char* y8, long long ld8, float* scales, float* rstd) {
     constexpr int GROUPS = kBlock<TPR> / TPR, WARPS = TPR / 32;
@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(kBlock<TPR>, (SKEW && sizeof(T) == 2 && !EIGHT
     pdl_release();
     auto ask = [&](int k) {  // the next row, into slot k
         unsigned char* buf = in + k * slot_bytes;
-        // by the last warp
+        // by the last warp: the second one has the row's ends to see to
         if constexpr (SKEW && BULK) {
             if (threadIdx.x == TPR - 32 && asked < rows) {
                 const bool lead = base + asked == 0, end = base + asked == (long long)gridDim.y * rows - 1;
@@ -804,13 +804,6 @@ constexpr int64_t kMaxHeld = 16384;
 bool rows_alike(const void* p, int64_t ldp, const void* q, int64_t ldq, size_t esz) {
     return ((uintptr_t)p - (uintptr_t)q) % 16 == 0 && (ldp - ldq) * (int64_t)esz % 16 == 0;
 }
-// Whether rows in chunks need a group twice as wide as their elements do, for the few that their first chunk has no room for: they are
-// taken element by element then (3 x 1021 x 2047 fp32 backward 23 us, in chunks 25).
-bool just_too_wide(int64_t c, int len) {
-    for (int64_t most = 64; most <= kMaxHeld; most *= 2)
-        if (c <= most) return c + len - 1 > most;
-    return true;
-}
 // Rows that start at the same place of a chunk lie this many apart.
 int like_rows(int64_t ld, size_t esz) {
     const int64_t pitch = ld * (int64_t)esz % 16;
@@ -860,7 +853,8 @@ int forward(const dlm_rms_args& a, cudaStream_t s) {
         DLM_RMS_SHAPES(DLM_VEC)
     }
     auto alike = [&](const void* p, int64_t ld) { return !p || rows_alike(a.x, a.ldx, p, ld, sizeof(T)); };
-    if (alike(a.residual, a.ldr) && alike(a.h, a.ldh) && alike(a.y, a.ldy) && !just_too_wide(c, LEN)) {
+    if (alike(a.residual, a.ldr) && alike(a.h, a.ldh) && alike(a.y, a.ldy) && a.c + LEN - 1 <= kMaxHeld) {
+        const int64_t c = a.c + LEN - 1;  // a row may begin anywhere in its first chunk
         DLM_RMS_SHAPES(DLM_SKEW)
     }
     DLM_RMS_SHAPES(DLM_ONE)
@@ -919,7 +913,8 @@ int backward(const dlm_rms_args& a, int* parts, cudaStream_t s) {
         DLM_RMS_SHAPES(DLM_VEC)
     }
     if (rows_alike(a.x, a.ldx, a.dy, a.lddy, sizeof(T)) && rows_alike(a.x, a.ldx, a.dh, a.lddh, sizeof(T)) &&
-        (!a.residual || rows_alike(a.x, a.ldx, a.residual, a.ldr, sizeof(T))) && !just_too_wide(c, LEN)) {
+        (!a.residual || rows_alike(a.x, a.ldx, a.residual, a.ldr, sizeof(T))) && a.c + LEN - 1 <= kMaxHeld) {
+        const int64_t c = a.c + LEN - 1;  // a row may begin anywhere in its first chunk
         DLM_RMS_SHAPES(DLM_SKEW)
     }
     DLM_RMS_SHAPES(DLM_ONE)
