@@ -139,17 +139,6 @@ __device__ __forceinline__ void run_params(const float* p, int skew, int c, int 
             v[u * LEN + k] = at >= 0 && at < c ? p[at] : 0.0f;
         }
 }
-// A run's weights, where they are read again for every row; 0 beyond the row.
-template <int LEN>
-__device__ __forceinline__ void weight_run(const float* w, int at, int c, bool runs, float* v) {
-    if (LEN > 1 && runs && at >= 0 && at + LEN <= c) {
-#pragma unroll
-        for (int k = 0; k < LEN; k += 4) unpack<float>(ld_words(w + at + k), v + k);
-    } else {
-#pragma unroll
-        for (int k = 0; k < LEN; ++k) v[k] = at + k >= 0 && at + k < c ? w[at + k] : 0.0f;
-    }
-}
 // A row's whole chunks of results.
 template <typename T, int LEN, int E, int TPR>
 __device__ __forceinline__ void put_chunks(T* row, int skew, int c, int t, const float* v) {
@@ -454,6 +443,9 @@ __global__ void __launch_bounds__(kBlock<TPR>, kLeastCtas<TPR>)
     constexpr int GROUPS = kBlock<TPR> / TPR;
     constexpr bool BULK = kBulk<LEN, TPR>;
     constexpr bool HOLD = E <= 16;  // the row's values stay in registers between the two sweeps, else they are read again
+    // so do the weights for all rows, but for single elements' copies, which spill as it is (8 x 1440 x 16384 bf16: 201 us held, 288 read again
+    // twice a row out of the L2 cache; 8818 columns, where their reads are single, 224 and 448)
+    constexpr bool HOLD_W = HOLD || LEN > 1;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ float part[2][2][TPR > 32 ? TPR / 32 : 1];
     __shared__ uint64_t full[D];
@@ -527,9 +519,8 @@ __global__ void __launch_bounds__(kBlock<TPR>, kLeastCtas<TPR>)
     };
 #pragma unroll
     for (int k = 0; k < D - 1; ++k) ask(k);
-    float wv[HOLD ? E : 1];
-    if constexpr (HOLD) run_params<LEN, E, TPR>(w, skew, c, t, wv);
-    const bool w_runs = ((uintptr_t)(w - skew) & 15) == 0;  // a run's weights are 16-byte runs
+    float wv[HOLD_W ? E : 1];
+    if constexpr (HOLD_W) run_params<LEN, E, TPR>(w, skew, c, t, wv);
     float dw[E], xw[X], xdw[X];
 #pragma unroll
     for (int e = 0; e < E; ++e) dw[e] = 0.0f;
@@ -538,6 +529,7 @@ __global__ void __launch_bounds__(kBlock<TPR>, kLeastCtas<TPR>)
         xw[x] = SKEW && shared.col[x] >= 0 ? w[shared.col[x]] : 0.0f;
         xdw[x] = 0.0f;
     }
+    auto weight_of = [&](int u) { return u * TPR + t < c ? w[u * TPR + t] : 0.0f; };  // read again: of a single element
     const float inv_c = 1.0f / (float)c;
     int slot = 0, side = 0;
     uint32_t parities = 0;  // of each slot's next phase
@@ -591,13 +583,12 @@ __global__ void __launch_bounds__(kBlock<TPR>, kLeastCtas<TPR>)
             for (int u = 0; u < E / LEN; ++u) {
                 run_values<T, LEN, TPR, SKEW>(hb, hs, live_c, t, u, xh);
                 run_values<T, LEN, TPR, SKEW>(gb, gs, live_c, t, u, v);
-                float wr[LEN];
-                weight_run<LEN>(w, run_column<LEN, TPR>(t, u, skew), c, w_runs, wr);
+                const float wr = HOLD_W ? 0.0f : weight_of(u);
 #pragma unroll
                 for (int k = 0; k < LEN; ++k) {
                     const float x = xh[k] * rs;
                     dw[u * LEN + k] = fmaf(v[k], x, dw[u * LEN + k]);
-                    sum = fmaf(v[k] * wr[k], x, sum);
+                    sum = fmaf(v[k] * (HOLD_W ? wv[u * LEN + k] : wr), x, sum);
                 }
             }
         }
@@ -649,11 +640,10 @@ __global__ void __launch_bounds__(kBlock<TPR>, kLeastCtas<TPR>)
                 run_values<T, LEN, TPR, SKEW>(hb, hs, live_c, t, u, xh);
                 run_values<T, LEN, TPR, SKEW>(gb, gs, live_c, t, u, v);
                 if (dres) run_values<T, LEN, TPR, SKEW>(eb, es, live_c, t, u, more);
-                float wr[LEN];
-                weight_run<LEN>(w, at, c, w_runs, wr);
+                const float wr = HOLD_W ? 0.0f : weight_of(u);
 #pragma unroll
                 for (int k = 0; k < LEN; ++k) {
-                    const float d = fmaf(xh[k] * rs, -m, v[k] * wr[k]);
+                    const float d = fmaf(xh[k] * rs, -m, v[k] * (HOLD_W ? wv[u * LEN + k] : wr));
                     v[k] = fmaf(d, rs, dres ? more[k] : 0.0f);
                 }
                 if (live && at < c) {
@@ -788,7 +778,8 @@ int wide_forward(const dlm_rms_args& a, cudaStream_t s) {
 // Rows up to this many elements are held on chip; wider ones are swept from memory.
 constexpr int64_t kMaxHeld = 16384;
 
-// CALL(columns per thread, threads per row) of the narrowest group that holds c columns.
+// CALL(columns per thread, threads per row) of the narrowest group that holds c columns.  24 columns a thread are there for 16 bits alone:
+// 8 x 1440 x 9000 bf16 8-bit output 130 -> 114 us against 32, gradient at 8818 224 -> 200, but 8 x 1440 x 12277 fp32 191 -> 200.
 #define DLM_RMS_SHAPES(CALL)             \
     if (c <= 64) return CALL(8, 8);      \
     if (c <= 128) return CALL(16, 8);    \
@@ -798,6 +789,8 @@ constexpr int64_t kMaxHeld = 16384;
     if (c <= 2048) return CALL(16, 128); \
     if (c <= 4096) return CALL(16, 256); \
     if (c <= 8192) return CALL(16, 512); \
+    if constexpr (sizeof(T) == 2)        \
+        if (c <= 12288) return CALL(24, 512); \
     return CALL(32, 512);
 
 // Whether the rows of two arrays start at the same places within 16 bytes.
