@@ -34,6 +34,31 @@ __device__ __forceinline__ float penalised(const Adjust& a, float d, bool positi
     return GRAD ? d * f : fmaf(d, f, count == 0 ? 0.0f : -fmaf(a.frequency, (float)count, a.presence));
 }
 
+// A chunk's biases; `past`: of a 16-byte run's start to the chunk's first bias, the same for all of a CTA's chunks.  SHIFT: they are read in such
+// runs wherever they begin, since a lane's next to another's are 32 bytes apart and one by one would take eight times the requests (7 x 48 x
+// 57443 bf16 27.7 us instead of 33.4, 1 x 2100 x 4187 9.8 instead of 12.5).  Chunks of four are as fast one by one (4 x 20378 x 2397 fp32 273 us, 343
+// shifted), and so are short rows with texts, whose registers are few (4 x 5120 x 601 49 and 52).
+template <int LEN, bool SHIFT = (LEN > 4)>
+__device__ __forceinline__ void read_biases(const float* bias, int past, int v, int vocab, float* b) {
+    if (past == 0) {
+#pragma unroll
+        for (int k = 0; k < LEN; k += 4) unpack<float>(ld_words(bias + v + k), b + k);
+    } else if (SHIFT && v >= 4 && v + LEN + 4 <= vocab) {
+        float w[LEN + 4];
+#pragma unroll
+        for (int k = 0; k < LEN + 4; k += 4) unpack<float>(ld_words(bias + v - past + k), w + k);
+        if (past & 1) {
+#pragma unroll
+            for (int k = 0; k < LEN + 3; ++k) w[k] = w[k + 1];
+        }
+#pragma unroll
+        for (int k = 0; k < LEN; ++k) b[k] = past & 2 ? w[k + 2] : w[k];
+    } else {
+#pragma unroll
+        for (int k = 0; k < LEN; ++k) b[k] = bias[v + k];
+    }
+}
+
 // A row lies in memory as chunks of LEN elements (16 bytes wherever the row starts, or one element); the first begins `skew` elements
 // before the row.  A CTA takes THREADS U chunks: U a thread, THREADS apart.  Chunks and masks are on their way into registers while the
 // CTA marks the row's text in a bit map, and (COUNTS) counts it: counts of marked elements alone are cleared, added to and read.  For the
@@ -67,7 +92,7 @@ __global__ void __launch_bounds__(THREADS) logits_kernel(dlm_logits_args a, int 
     how.presence = a.presence ? a.presence[row] : 0.0f;
     how.cooling = a.temperature ? a.temperature[row] : 1.0f;
     how.bias = !GRAD && a.bias ? a.bias + node * a.ldb : nullptr;
-    const bool bias_runs = ((uintptr_t)(how.bias + tile0) & 15) == 0;  // a chunk's biases are 16-byte runs
+    const int past = (int)((uintptr_t)(how.bias + tile0) >> 2) & 3;  // of a run's start to a chunk's first bias
     const uint32_t* allowed = a.allowed ? a.allowed + row * a.ldm : nullptr;
     // bit k: element v + k is allowed
     auto allowed_bits = [&](int v) {
@@ -144,17 +169,13 @@ __global__ void __launch_bounds__(THREADS) logits_kernel(dlm_logits_args a, int 
             }
         }
         if (!GRAD && how.bias) {
-            if (LEN > 1 && bias_runs) {
+            if constexpr (LEN > 1) {
+                float b[LEN];
+                read_biases<LEN>(how.bias, past, v, vocab, b);
 #pragma unroll
-                for (int k = 0; k < LEN; k += kRun<float>) {
-                    float p[kRun<float>];
-                    unpack<float>(ld_words(how.bias + v + k), p);
-#pragma unroll
-                    for (int e = 0; e < (LEN > 1 ? kRun<float> : 1); ++e) d[k + e] += p[e];
-                }
+                for (int k = 0; k < LEN; ++k) d[k] += b[k];
             } else {
-#pragma unroll
-                for (int k = 0; k < LEN; ++k) d[k] += how.bias[v + k];
+                d[0] += how.bias[v];
             }
         }
 #pragma unroll
@@ -217,7 +238,7 @@ __host__ __device__ inline int text_bytes(int elements, int esz, bool grad) {
     return elements * esz + (grad ? elements / 4 : elements * 2) + elements / 8 + 16;
 }
 
-template <typename T, bool GRAD, int THREADS>
+template <typename T, bool GRAD, bool BIAS, int THREADS>
 __global__ void __launch_bounds__(THREADS) logits_text_kernel(dlm_logits_args a, int tiles, int tile_chunks) {
     constexpr int LEN = kRun<T>;
     constexpr uint32_t ALL = (1u << LEN) - 1;
@@ -254,9 +275,9 @@ __global__ void __launch_bounds__(THREADS) logits_text_kernel(dlm_logits_args a,
     how.frequency = a.frequency ? a.frequency[row] : 0.0f;
     how.presence = a.presence ? a.presence[row] : 0.0f;
     how.cooling = 1.0f / (a.temperature ? a.temperature[row] : 1.0f);
-    how.bias = !GRAD && a.bias ? a.bias + node * a.ldb : nullptr;
+    how.bias = BIAS ? a.bias + node * a.ldb : nullptr;
     how.down = 1.0f / how.up;
-    const bool bias_runs = ((uintptr_t)(how.bias + tile0) & 15) == 0;  // a chunk's biases are 16-byte runs
+    const int past = (int)((uintptr_t)(how.bias + tile0) >> 2) & 3;  // of a run's start to a chunk's first bias
     for (int k = t; k < (GRAD ? 2 * words : elements / 2) / 4; k += THREADS) reinterpret_cast<uint4*>(marks)[k] = make_uint4(0, 0, 0, 0);
     from = max(0ll, from);
     const long long length = max(0ll, min((long long)a.history_length, to) - from);
@@ -282,13 +303,26 @@ __global__ void __launch_bounds__(THREADS) logits_text_kernel(dlm_logits_args a,
             counts[at] = 1;
         }
     });
+    // a chunk's biases are asked for while the one before it is mapped (4 x 512 x 131072 bf16, texts of 1000 and masks: 318 us, 341 without); not
+    // where a thread has a chunk or two (4 x 5120 x 601 49 us instead of 53)
+    constexpr bool AHEAD = BIAS && THREADS > 64;
+    float bias[BIAS ? LEN : 1];
+    auto ask_bias = [&](int v) {
+        if constexpr (BIAS) {
+            if (whole(v)) read_biases<LEN, (LEN > 4 && THREADS > 64)>(how.bias, past, v, vocab, bias);
+        }
+    };
+    if (AHEAD && t < chunks) ask_bias(tile0 + t * LEN);
     wait_copies<0>();
     __syncthreads();
     auto count_of = [&](uint32_t count, int at) { return brief || count == 0 ? (int)count : count_in(text, length, tile0 + at); };
 #pragma unroll 2
     for (int c = t; c < chunks; c += THREADS) {
         const int at = c * LEN, v = tile0 + at;
-        if (!whole(v)) continue;
+        if (!whole(v)) {
+            if (AHEAD && c + THREADS < chunks) ask_bias(v + THREADS * LEN);
+            continue;
+        }
         float d[LEN];
         unpack<T>(ld_words(data + c * 16), d);
         if constexpr (GRAD) {
@@ -313,19 +347,11 @@ __global__ void __launch_bounds__(THREADS) logits_text_kernel(dlm_logits_args a,
                     d[k] = penalised<GRAD>(how, d[k], d[k] > 0.0f, count_of(k & 1 ? pairs[k / 2] >> 16 : pairs[k / 2] & 0xffffu, at + k));
             }
         }
-        if (!GRAD && how.bias) {
-            if (bias_runs) {
+        if constexpr (BIAS) {
+            if (!AHEAD) ask_bias(v);
 #pragma unroll
-                for (int k = 0; k < LEN; k += 4) {
-                    float p[4];
-                    unpack<float>(ld_words(how.bias + v + k), p);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) d[k + e] += p[e];
-                }
-            } else {
-#pragma unroll
-                for (int k = 0; k < LEN; ++k) d[k] += how.bias[v + k];
-            }
+            for (int k = 0; k < LEN; ++k) d[k] += bias[k];
+            if (AHEAD && c + THREADS < chunks) ask_bias(v + THREADS * LEN);
         }
 #pragma unroll
         for (int k = 0; k < LEN; ++k) d[k] *= how.cooling;
@@ -352,14 +378,14 @@ __global__ void __launch_bounds__(THREADS) logits_text_kernel(dlm_logits_args a,
         d = penalised<GRAD>(how, d, positives[at >> 5] >> (at & 31) & 1, marks[at >> 5] >> (at & 31) & 1);
     else
         d = penalised<GRAD>(how, d, d > 0.0f, count_of(counts[at], at));
-    if (how.bias) d += how.bias[v];
+    if (BIAS) d += how.bias[v];
     d *= how.cooling;
     if (allowed && !(allowed[v >> 5] >> (v & 31) & 1)) d = GRAD ? 0.0f : -INFINITY;
     out[v] = narrow<T>(d);
 }
 
-template <typename T, bool GRAD, int THREADS>
-int run_text(const dlm_logits_args& a, int64_t tile_bytes, cudaStream_t s) {
+template <typename T, bool GRAD, bool BIAS, int THREADS>
+int launch_text(const dlm_logits_args& a, int64_t tile_bytes, cudaStream_t s) {
     constexpr int LEN = kRun<T>;
     const int64_t R = a.n * a.rows, chunks = (a.vocab + 2 * (LEN - 1)) / LEN;  // a row may begin anywhere in its first chunk
     // few rows: tiles such that every SM has a CTA or two
@@ -368,10 +394,17 @@ int run_text(const dlm_logits_args& a, int64_t tile_bytes, cudaStream_t s) {
     const int64_t ctas = R * tiles;
     if (ctas > 0x7fffffff) return DLM_ERR_UNSUPPORTED;
     const int smem = text_bytes(tile_chunks * LEN, sizeof(T), GRAD);
-    if (smem > (48 << 10) && !allow_shared<logits_text_kernel<T, GRAD, THREADS>>(80 << 10)) return DLM_ERR_CUDA;
-    cudaError_t err = launch_overlapped(logits_text_kernel<T, GRAD, THREADS>, dim3((unsigned)ctas), dim3(THREADS), smem, s, 1, a, tiles, tile_chunks);
+    if (smem > (48 << 10) && !allow_shared<logits_text_kernel<T, GRAD, BIAS, THREADS>>(80 << 10)) return DLM_ERR_CUDA;
+    cudaError_t err = launch_overlapped(logits_text_kernel<T, GRAD, BIAS, THREADS>, dim3((unsigned)ctas), dim3(THREADS), smem, s, 1, a, tiles, tile_chunks);
     dlm_count_launch(1);
     return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
+}
+
+template <typename T, bool GRAD, int THREADS>
+int run_text(const dlm_logits_args& a, int64_t tile_bytes, cudaStream_t s) {
+    if constexpr (!GRAD)
+        if (a.bias) return launch_text<T, false, true, THREADS>(a, tile_bytes, s);
+    return launch_text<T, GRAD, false, THREADS>(a, tile_bytes, s);
 }
 
 // Threads for the vocabulary: a row of few chunks by few threads, a wide one in tiles of 16 KB.
