@@ -328,7 +328,7 @@ __device__ __forceinline__ void put_sums(G* to, const float (&sum)[U][LEN], floa
 struct GradShape {
     long long rows, c, ldy, ldgt;
     uint32_t vocab;
-    int n, accumulate, strips, zero_rows, zero_ctas;  // zero_ctas: a node's
+    int n, accumulate, strips, parts, zero_rows, zero_ctas;  // parts: CTAs of a short text and strip; zero_ctas: a node's
     float scale;
     int scan;  // rows without tokens are found in the text
     unsigned lead, sum_ctas;
@@ -465,8 +465,10 @@ __device__ __forceinline__ void sum_tiles(const GradShape& s, unsigned cta, cons
                          len, ahead, behind, smem + (threadIdx.x >> 5) * kSlots * kSlotBytes<SB>, w.parts + tile_at * 2 * s.c + col0, s.c);
 }
 
-// Short texts: a CTA sorts a node's tokens by itself (each counts those before it), its warps walk their tiles of a strip, and what goes
-// on between tiles is joined in shared memory.
+// Short texts: a CTA sorts a node's tokens by itself (runs of 32 in each warp, then each token finds its place in the other runs), its warps walk
+// their tiles of a strip, and what goes on between tiles is joined in shared memory.  Where there are SMs for it, several CTAs share a strip, each
+// with the tokens that begin in its part of the sorted places: 8 x 512 tokens, 551 x 906 fp32 from bf16 14 us (38 with one CTA, and each token
+// compared with all), 8 x 309 10 (25).
 constexpr int kShortText = 512, kShortTiles = kShortText / 32;  // tokens, a thread each; tiles, a warp each
 template <typename T, typename G, int LEN>
 __device__ __forceinline__ void sum_short_text(const GradShape& s, unsigned cta, const int64_t* tokens, const T* dy, G* dtable) {
@@ -474,46 +476,79 @@ __device__ __forceinline__ void sum_short_text(const GradShape& s, unsigned cta,
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ __align__(16) uint32_t text[kShortText], keys[kShortText + 1];
     __shared__ uint32_t places[kShortText];
+    __shared__ int share[2];
     float* parts = reinterpret_cast<float*>(smem + kShortTiles * kSlots * kSlotBytes<kShortStrip>);  // [tiles][2][strip]
     const int lane = threadIdx.x & 31, tile = threadIdx.x >> 5;
-    const int node = cta / s.strips, rows = (int)s.rows;
-    const long long col0 = (long long)(cta % s.strips) * kStrip<T, kShortStrip>;
+    const int part_of = cta % s.parts, strip = cta / s.parts % s.strips, node = cta / s.parts / s.strips, rows = (int)s.rows;
+    const long long col0 = (long long)strip * kStrip<T, kShortStrip>;
+    const int at = threadIdx.x;
     uint32_t key = 0xffffffffu;  // behind the text's end
-    if ((int)threadIdx.x < rows) {
-        const int64_t token = tokens[(long long)node * rows + threadIdx.x];
+    if (at < rows) {
+        const int64_t token = tokens[(long long)node * rows + at];
         key = token >= 0 && token < (int64_t)s.vocab ? (uint32_t)token : s.vocab;
     }
-    text[threadIdx.x] = key;
+    text[at] = key;
     __syncthreads();
-    int rank = 0;
-    for (int k = 0; k < rows; k += 4) {
-        const uint4 other = *reinterpret_cast<const uint4*>(text + k);
-        rank += (other.x < key || (other.x == key && k < (int)threadIdx.x)) + (other.y < key || (other.y == key && k + 1 < (int)threadIdx.x)) +
-                (other.z < key || (other.z == key && k + 2 < (int)threadIdx.x)) + (other.w < key || (other.w == key && k + 3 < (int)threadIdx.x));
+    // a token's rank within its warp, in whose 32 words each run then stands in order
+    const int run0 = at & ~31;
+    int rank = __popc(__match_any_sync(0xffffffffu, key) & ((1u << lane) - 1));
+#pragma unroll
+    for (int k = 0; k < 32; k += 4) {
+        const uint4 other = *reinterpret_cast<const uint4*>(text + run0 + k);
+        rank += (other.x < key) + (other.y < key) + (other.z < key) + (other.w < key);
     }
-    if ((int)threadIdx.x < rows) {
+    keys[run0 + rank] = key;
+    __syncthreads();
+    // and those before it in the other runs, also equal ones of those ahead
+    if (run0 < rows) {
+#pragma unroll 2
+        for (int r = 0; r < rows; r += 32) {
+            const uint32_t bound = r < run0 ? key + 1 : key;
+            const uint32_t* run = keys + r;
+            int below = 0;
+#pragma unroll
+            for (int step = 16; step > 0; step /= 2)
+                if (run[below + step - 1] < bound) below += step;
+            below += run[below] < bound;
+            rank += r == run0 ? 0 : below;
+        }
+    }
+    __syncthreads();
+    if (at < rows) {
         keys[rank] = key;
-        places[rank] = threadIdx.x;
+        places[rank] = at;
+    } else {
+        keys[at] = 0xffffffffu;
     }
-    if ((int)threadIdx.x >= rows || threadIdx.x == 0) keys[threadIdx.x == 0 ? kShortText : threadIdx.x] = 0xffffffffu;
+    if (threadIdx.x == 0) keys[kShortText] = 0xffffffffu;
     __syncthreads();
+    // the CTA's share of the sorted places: the tokens that begin there
+    if (threadIdx.x < 2) {
+        const int p = part_of + (int)threadIdx.x;
+        int b = p * rows / s.parts;
+        if (b > 0 && b < rows && keys[b] == keys[b - 1]) b = lower_bound(keys, rows, keys[b] + 1);
+        share[threadIdx.x] = b;
+    }
+    __syncthreads();
+    const int begin = share[0], end = share[1];
     const T* from = dy + (long long)node * rows * s.ldy + col0;
     G* to = dtable + node * s.ldgt + col0;
-    const int columns = (int)min((long long)kStrip<T, kShortStrip>, s.c - col0), items = min(kTileItems, (rows + 4 * kShortTiles - 1) / (4 * kShortTiles) * 4);  // places to a warp
-    const int first = tile * items, len = max(0, min(items, rows - first));
+    const int columns = (int)min((long long)kStrip<T, kShortStrip>, s.c - col0), items = (end - begin + 4 * kShortTiles - 1) / (4 * kShortTiles) * 4;  // places to a warp
+    static_assert((kShortText + 4 * kShortTiles - 1) / (4 * kShortTiles) * 4 <= kTileItems);
+    const int first = min(begin + tile * items, end), next = min(first + items, end), len = next - first;
     const uint32_t mine = lane < len ? keys[first + lane] : 0xffffffffu, place = lane < len ? places[first + lane] : 0;
-    const uint32_t ahead = tile > 0 ? keys[first - 1] : 0xffffffffu, behind = keys[first + items];
+    const uint32_t ahead = first > 0 ? keys[first - 1] : 0xffffffffu, behind = keys[next];
     walk_tile<T, G, LEN, kShortStrip>(s, dy, from, to, columns, mine, place, len, ahead, behind, smem + tile * kSlots * kSlotBytes<kShortStrip>,
                          parts + tile * 2 * kStrip<T, kShortStrip>, kStrip<T, kShortStrip>);
     __syncthreads();
-    const uint32_t last = __shfl_sync(0xffffffffu, mine, items - 1);
+    const uint32_t last = __shfl_sync(0xffffffffu, mine, (items - 1) & 31);  // of a whole tile
     if (last >= s.vocab || last != behind || last == ahead) return;
     float sum[U][LEN];
     const float* part = parts + tile * 2 * kStrip<T, kShortStrip> + kStrip<T, kShortStrip> + lane * LEN;
 #pragma unroll
     for (int u = 0; u < U; ++u) load_run<float, LEN>(part + u * 32 * LEN, sum[u]);
     part -= kStrip<T, kShortStrip>;
-    for (int k = tile + 1; k < kShortTiles && keys[k * items] == last; ++k) {
+    for (int k = tile + 1; k < kShortTiles && keys[min(begin + k * items, end)] == last; ++k) {
         part += 2 * kStrip<T, kShortStrip>;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -560,7 +595,8 @@ __device__ __forceinline__ void clear_rows(const GradShape& s, unsigned cta, con
     const int lane = threadIdx.x & 31;
     const long long line = s.c * (long long)sizeof(G);
     char* table = reinterpret_cast<char*>(dtable + node * s.ldgt + (long long)v0 * s.c);
-    const uint32_t group = line >= (16 << 10) ? 1 : line >= (4 << 10) ? 4 : 32;
+    uint32_t group = line >= (16 << 10) ? 1 : line >= (4 << 10) ? 4 : 32;
+    while (group > 1 && group * (THREADS / 64) >= count) group /= 2;  // few rows: some for every warp
     for (uint32_t r0 = (threadIdx.x >> 5) * group; r0 < count; r0 += THREADS / 32 * group) {
         const uint32_t rows = min(group, count - r0);
         uint32_t left = ~(touched[r0 >> 5] >> (r0 & 31)) & (0xffffffffu >> (32 - rows));  // rows to clear
@@ -683,7 +719,10 @@ int run_backward(const dlm_embed_args& a, const Sorted& w, cudaStream_t s) {
     const bool narrow = brief || (int64_t)a.n * w.tiles * ((a.c + kStrip<T, kLongStrip> - 1) / kStrip<T, kLongStrip>) < kWarps;  // strips
     const int64_t strip = narrow ? kStrip<T, kShortStrip> : kStrip<T, kLongStrip>;
     g.strips = (int)((a.c + strip - 1) / strip);
-    const int64_t tiles = (int64_t)a.n * w.tiles, sum_ctas = brief ? (int64_t)a.n * g.strips : (tiles * g.strips + 7) / 8;
+    // short texts: as many CTAs as there are SMs, but 64 tokens or more to each
+    const int64_t strips = (int64_t)a.n * g.strips;
+    g.parts = brief ? (int)std::max<int64_t>(1, std::min<int64_t>(a.rows / 64, device_info().sms / strips)) : 1;
+    const int64_t tiles = (int64_t)a.n * w.tiles, sum_ctas = brief ? strips * g.parts : (tiles * g.strips + 7) / 8;
     constexpr int RUN = LEN == 1 ? 1 : 4;
     const int64_t join_ctas = (tiles * ((a.c + 32 * RUN - 1) / (32 * RUN)) + 7) / 8;
     // 256 KB of the gradient to a CTA, or more: at least four times what it reads of the text (8 bytes a token, out of the L2).  Where
