@@ -236,3 +236,15 @@ def test_gradient_of_short_texts(rows, c, typ, gtype):
         tokens, dy = _tokens(2, rows, vocab, rows, kind), _rand((2, rows, c), 1.0, c, typ)
         _check_backward(tokens, dy, vocab, gtype, 1.5)
         _check_backward(tokens, dy, vocab, gtype, 1.5, add=_rand((2, vocab, c), 1.0, 9, gtype))
+
+
+@pytest.mark.parametrize("runs", [(512,), (1, 511), (511, 1), (64,) * 8, (63, 1, 64, 200, 184), (1,) * 130 + (250,) + (1,) * 132, (100, 157), (5,) * 61])
+@pytest.mark.parametrize("c", [64, 777])
+def test_short_texts_whose_runs_cross_the_shares(c, runs):
+    """Runs of equal tokens that begin before a share of the sorted places and end behind it; the last run stands for no token."""
+    rows, vocab = sum(runs), 300
+    ids = torch.repeat_interleave(torch.arange(len(runs)), torch.tensor(runs))
+    ids[ids == len(runs) - 1] = vocab if len(runs) > 1 else 0
+    order = torch.randperm(rows, generator=torch.Generator().manual_seed(c))
+    tokens = torch.stack([ids[order], ids.flip(0)]).to(DEV)
+    _check_backward(tokens, _rand((2, rows, c), 1.0, c), vocab, "f32")
