@@ -509,7 +509,7 @@ DLM_API int policy_loss_grad(int n, int64_t rows, int64_t vocab, const void* log
  * occurs often, in shares of up to 32).  Fast path: c a multiple of 16 bytes' worth of the narrower type, arrays and strides
  * 16-byte aligned.
  * Errors: DLM_ERR_NULL, DLM_ERR_SHAPE, DLM_ERR_KIND, DLM_ERR_ALIGN, DLM_ERR_ALIAS, DLM_ERR_HYPER, DLM_ERR_WORKSPACE,
- * DLM_ERR_UNSUPPORTED, DLM_ERR_CUDA.
+ * DLM_ERR_UNSUPPORTED (rows above 2^31 - 1, vocab above 2^31 - 2, c above 2^30), DLM_ERR_CUDA.
  */
 DLM_API int embedding(int n, int64_t rows, int64_t vocab, int64_t c, const void* table, int t_dtype, int64_t ldt,
                       const int64_t* tokens, float scale, void* y, int dtype, int64_t ldy, void* cuda_stream);

@@ -1,0 +1,30 @@
+// Searches over the places of long texts, up to 2^31 - 1 of them (not installed), whose sums stay in range.  Host code may use them, too.
+#pragma once
+#include <cstdint>
+
+#ifdef __CUDACC__
+#define DLM_BOTH __host__ __device__ __forceinline__
+#else
+#define DLM_BOTH inline
+#endif
+
+namespace dlm {
+
+// How many of the ascending keys[0 .. count) are below v.  The middle is found without the sum of both ends, which passes 2^31 above 2^30
+// keys.
+template <typename Keys>
+DLM_BOTH int lower_bound(const Keys& keys, int count, uint32_t v) {
+    int lo = 0;
+    while (lo < count) {
+        const int mid = lo + ((count - lo) >> 1);
+        if (keys[mid] < v)
+            lo = mid + 1;
+        else
+            count = mid;
+    }
+    return lo;
+}
+
+}  // namespace dlm
+
+#undef DLM_BOTH

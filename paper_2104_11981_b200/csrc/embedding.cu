@@ -15,6 +15,7 @@
 #include "dlm_internal.h"
 #include "dlm_launch.h"
 #include "dlm_model.h"
+#include "dlm_places.h"
 #include "dlm_rows.cuh"
 #include "dlm_staged_rows.cuh"
 
@@ -152,19 +153,6 @@ Sorted sorted_layout(int n, int64_t rows, int64_t c, void* workspace) {
     }
     w.parts = reinterpret_cast<float*>(take((int64_t)n * w.tiles * 2 * c * 4));
     return w;
-}
-
-// Places of keys below v, among keys[0 .. count).
-__device__ __forceinline__ int lower_bound(const uint32_t* keys, int count, uint32_t v) {
-    int lo = 0;
-    while (lo < count) {
-        const int mid = (lo + count) >> 1;
-        if (keys[mid] < v)
-            lo = mid + 1;
-        else
-            count = mid;
-    }
-    return lo;
 }
 
 // A chunk's tokens by least-significant digits: every warp ranks its own stretch of places (lanes with equal digits by their
