@@ -1,4 +1,4 @@
-// Searches over the places of long texts, up to 2^31 - 1 of them (not installed), whose sums stay in range.  Host code may use them, too.
+// Places of long texts, up to 2^31 - 1 of them (not installed): searches and strides whose sums stay in range.  Host code may use them, too.
 #pragma once
 #include <cstdint>
 
@@ -23,6 +23,13 @@ DLM_BOTH int lower_bound(const Keys& keys, int count, uint32_t v) {
             count = mid;
     }
     return lo;
+}
+
+// f(k) for every STEP-th place from `first` until `end`.  Unsigned, since the last step may pass 2^31 - 1.
+template <uint32_t STEP, int UNROLL, typename F>
+DLM_BOTH void each_place(uint32_t first, uint32_t end, const F& f) {
+#pragma unroll UNROLL
+    for (uint32_t k = first; k < end; k += STEP) f(k);
 }
 
 }  // namespace dlm

@@ -563,20 +563,19 @@ __device__ __forceinline__ void clear_rows(const GradShape& s, unsigned cta, con
     if (s.scan) {
         __syncthreads();
         const int64_t* text = tokens + (long long)node * s.rows;
-#pragma unroll 8
-        for (int k = threadIdx.x; k < (int)s.rows; k += THREADS) {
+        each_place<THREADS, 8>(threadIdx.x, (uint32_t)s.rows, [&](uint32_t k) {
             const uint64_t v = (uint64_t)text[k] - v0;
             if (v < count) atomicOr(&touched[v >> 5], 1u << (v & 31));
-        }
+        });
     } else {
         pdl_wait();
         const uint32_t* keys = w.keys + (long long)node * s.rows;
         if (threadIdx.x < 2) bounds[threadIdx.x] = lower_bound(keys, (int)s.rows, threadIdx.x ? v0 + count : v0);
         __syncthreads();
-        for (int k = bounds[0] + threadIdx.x; k < bounds[1]; k += THREADS) {
+        each_place<THREADS, 1>((uint32_t)bounds[0] + threadIdx.x, (uint32_t)bounds[1], [&](uint32_t k) {
             const uint32_t v = keys[k] - v0;
             atomicOr(&touched[v >> 5], 1u << (v & 31));
-        }
+        });
     }
     __syncthreads();
     // a warp takes up to 32 rows, about 32 KB, and clears the stretches between touched ones

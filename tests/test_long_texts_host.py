@@ -1,4 +1,4 @@
-"""Searches over the places of long texts, at sizes where a sum of two places passes 32 bits: the kernels' own header on the host."""
+"""Searches and strides over the places of long texts, at sizes where a sum of two places passes 32 bits: the kernels' own header on the host."""
 import os
 import subprocess
 
@@ -42,3 +42,22 @@ def test_searches_among_more_than_2_to_the_30_keys(tmp_path):
     for count in (0, 1, 1000, (1 << 30) + 1000, 2 ** 31 - 1):
         want += [min(count, 3 * v) for v in (0, 1, 333, 357913941, 715827882, 0xffffffff)] + [0]
     assert _run(tmp_path, SEARCH) == want
+
+
+STRIDE = """
+int main() {
+    for (uint32_t first : {0u, 2147483647u - 700u, 2147483647u - 1u, 2147483647u, 2147483647u + 200u}) {
+        const uint32_t end = first ? 2147483647u : 1000u;
+        uint32_t count = 0, wrong = 0, next = first;
+        dlm::each_place<256, 4>(first, end, [&](uint32_t k) {
+            wrong += k != next || k >= end || ++count > 4;
+            next = k + 256;
+        });
+        std::printf("%u %u ", count, wrong);
+    }
+}
+"""
+
+
+def test_strides_that_end_at_2_to_the_31_places(tmp_path):
+    assert _run(tmp_path, STRIDE) == [4, 0, 3, 0, 1, 0, 0, 0, 0, 0]
