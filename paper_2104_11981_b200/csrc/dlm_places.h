@@ -10,19 +10,18 @@
 
 namespace dlm {
 
-// How many of the ascending keys[0 .. count) are below v.  The middle is found without the sum of both ends, which passes 2^31 above 2^30
-// keys.
+// How many of the ascending keys[0 .. count) are below v.  Unsigned, since the sum of both ends passes 2^31 - 1 above 2^30 keys.
 template <typename Keys>
 DLM_BOTH int lower_bound(const Keys& keys, int count, uint32_t v) {
-    int lo = 0;
-    while (lo < count) {
-        const int mid = lo + ((count - lo) >> 1);
+    uint32_t lo = 0, hi = (uint32_t)count;
+    while (lo < hi) {
+        const uint32_t mid = (lo + hi) >> 1;
         if (keys[mid] < v)
             lo = mid + 1;
         else
-            count = mid;
+            hi = mid;
     }
-    return lo;
+    return (int)lo;
 }
 
 // f(k) for every STEP-th place from `first` until `end`.  Unsigned, since the last step may pass 2^31 - 1.

@@ -572,7 +572,7 @@ __device__ __forceinline__ void clear_rows(const GradShape& s, unsigned cta, con
         const uint32_t* keys = w.keys + (long long)node * s.rows;
         if (threadIdx.x < 2) bounds[threadIdx.x] = lower_bound(keys, (int)s.rows, threadIdx.x ? v0 + count : v0);
         __syncthreads();
-        each_place<THREADS, 1>((uint32_t)bounds[0] + threadIdx.x, (uint32_t)bounds[1], [&](uint32_t k) {
+        each_place<THREADS, 4>((uint32_t)bounds[0] + threadIdx.x, (uint32_t)bounds[1], [&](uint32_t k) {
             const uint32_t v = keys[k] - v0;
             atomicOr(&touched[v >> 5], 1u << (v & 31));
         });

@@ -21,8 +21,8 @@ SEARCH = """
 struct Keys {  // keys[i] = i / 3, of which none exists outside [0, count)
     int count;
     mutable int wrong = 0;
-    uint32_t operator[](int i) const {
-        wrong += i < 0 || i >= count;
+    uint32_t operator[](uint32_t i) const {
+        wrong += i >= (uint32_t)count;
         return (uint32_t)i / 3;
     }
 };
