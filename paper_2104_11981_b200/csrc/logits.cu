@@ -14,6 +14,7 @@
 #include "dlm_internal.h"
 #include "dlm_launch.h"
 #include "dlm_model.h"
+#include "dlm_places.h"
 #include "dlm_rows.cuh"
 #include "dlm_staged_rows.cuh"
 
@@ -119,7 +120,7 @@ __global__ void __launch_bounds__(THREADS) logits_kernel(dlm_logits_args a, int 
     how.cooling = 1.0f / how.cooling;
     if constexpr (TEXTS != NONE) {
         from = max(0ll, from);
-        const int length = (int)max(0ll, min((long long)a.history_length, to) - from);
+        const uint32_t length = (uint32_t)max(0ll, min((long long)a.history_length, to) - from);
         const int64_t* text = a.history + from;
         for (int k = threadIdx.x; k < WORDS; k += THREADS) {
             marks[k] = 0;
@@ -128,12 +129,11 @@ __global__ void __launch_bounds__(THREADS) logits_kernel(dlm_logits_args a, int 
         __syncthreads();
         const T* z = GRAD ? static_cast<const T*>(a.logits) + row * a.ldl + tile0 : nullptr;
         auto each = [&](auto&& f) {
-#pragma unroll 4
-            for (int k = threadIdx.x; k < length; k += THREADS) {
+            each_place<THREADS, 4>(threadIdx.x, length, [&](uint32_t k) {
                 const uint64_t token = (uint64_t)text[k];
                 const int at = (int)token - tile0;
                 if (token < (uint64_t)vocab && (uint32_t)at < (uint32_t)TILE) f(at);
-            }
+            });
         };
         each([&](int at) {
             const uint32_t bit = 1u << (at & 31), old = atomicOr(&marks[at >> 5], bit);
