@@ -224,18 +224,49 @@ int run(const dlm_logits_args& a, cudaStream_t s) {
 // With texts, a tile's time goes by the wait for the row's bounds, then its text, then the logits of what it marks.  So that enough bytes are on
 // their way meanwhile, chunks come into shared memory (16 KB a CTA, or a short row), not into registers, of
 // which half as many would fit: gradient of 4 x 1024 x 50001 bf16 228 us by the kernel above.  A thread copies and maps chunks of its own.
-// The adjustment counts every element's occurrences in 16 bits (texts of more than 65535 tokens are only marked, and read once more for
-// each element); its gradient needs no more than a mark and the logit's sign.
+// The adjustment counts every element's occurrences in 16 bits, or in 32 for texts of more than 65535 tokens; its gradient, and penalties that do
+// not go by the count, need no more than a mark and the logit's sign.
 constexpr int kShortText = 65535;
-__device__ __noinline__ int count_in(const int64_t* text, long long length, int64_t token) {
-    int n = 0;
-    for (long long i = 0; i < length; ++i) n += text[i] == token;
-    return n;
-}
 
 // Shared memory of a tile.
 __host__ __device__ inline int text_bytes(int elements, int esz, bool grad) {
     return elements * esz + (grad ? elements / 4 : elements * 2) + elements / 8 + 16;
+}
+
+// A tile after a text whose counts need 32 bits: the counters hold half of the tile, so the text is read twice.  Element by element, since the
+// text's 512 KB and more are what it takes.  1 x 131072 bf16 after 100000 tokens 103 us (50 where only marks are needed, 36 after 65535 tokens), 4 x 64
+// x 50001 624 us; with a walk over the text for every element that it has, 45 ms and more.
+template <typename T, bool BIAS, int THREADS>
+__device__ __noinline__ void map_long_text(Adjust how, const int64_t* text, uint32_t length, const T* in, T* out, const uint32_t* allowed,
+                                           int elements, int tile0, int vocab) {
+    constexpr int LEN = kRun<T>;
+    extern __shared__ __align__(16) unsigned char smem[];
+    const T* staged = reinterpret_cast<const T*>(smem);
+    int* counts = reinterpret_cast<int*>(smem + elements * sizeof(T));  // [half], all 0
+    const int half = elements / 2;
+    wait_copies<0>();
+    for (int first = 0; first < elements; first += half) {
+        const int base = tile0 + first;
+        each_place<THREADS, 8>(threadIdx.x, length, [&](uint32_t k) {
+            const uint64_t token = (uint64_t)text[k];
+            const int at = (int)token - base;
+            if (token < (uint64_t)vocab && (uint32_t)at < (uint32_t)half) atomicAdd(&counts[at], 1);
+        });
+        __syncthreads();
+        for (int at = threadIdx.x; at < half; at += THREADS) {
+            const int v = base + at, chunk = v - (first + at) % LEN, count = counts[at];
+            if (v >= 0 && v < vocab) {
+                float d = widen(chunk >= 0 && chunk + LEN <= vocab ? staged[first + at] : in[v]);
+                d = penalised<false>(how, d, d > 0.0f, count);
+                if (BIAS) d += how.bias[v];
+                d *= how.cooling;
+                if (allowed && !(allowed[v >> 5] >> (v & 31) & 1)) d = -INFINITY;
+                out[v] = narrow<T>(d);
+            }
+            counts[at] = 0;
+        }
+        __syncthreads();
+    }
 }
 
 template <typename T, bool GRAD, bool BIAS, int THREADS>
@@ -293,6 +324,8 @@ __global__ void __launch_bounds__(THREADS) logits_text_kernel(dlm_logits_args a,
     __syncthreads();
     const T* z = GRAD ? static_cast<const T*>(a.logits) + row * a.ldl + tile0 : nullptr;
     const bool brief = length <= kShortText;
+    if constexpr (!GRAD)
+        if (!brief && a.frequency) return map_long_text<T, BIAS, THREADS>(how, text, (uint32_t)length, in, out, allowed, elements, tile0, vocab);
     each([&](int at) {
         if constexpr (GRAD) {
             const uint32_t bit = 1u << (at & 31), old = atomicOr(&marks[at >> 5], bit);
@@ -300,7 +333,7 @@ __global__ void __launch_bounds__(THREADS) logits_text_kernel(dlm_logits_args a,
         } else if (brief) {
             atomicAdd(&marks[at >> 1], 1u << (16 * (at & 1)));
         } else {
-            counts[at] = 1;
+            counts[at] = 1;  // nothing goes by the count
         }
     });
     // a chunk's biases are asked for while the one before it is mapped (4 x 512 x 131072 bf16, texts of 1000 and masks: 318 us, 341 without); not
@@ -315,7 +348,6 @@ __global__ void __launch_bounds__(THREADS) logits_text_kernel(dlm_logits_args a,
     if (AHEAD && t < chunks) ask_bias(tile0 + t * LEN);
     wait_copies<0>();
     __syncthreads();
-    auto count_of = [&](uint32_t count, int at) { return brief || count == 0 ? (int)count : count_in(text, length, tile0 + at); };
 #pragma unroll 2
     for (int c = t; c < chunks; c += THREADS) {
         const int at = c * LEN, v = tile0 + at;
@@ -344,7 +376,7 @@ __global__ void __launch_bounds__(THREADS) logits_text_kernel(dlm_logits_args a,
             if (any) {
 #pragma unroll
                 for (int k = 0; k < LEN; ++k)
-                    d[k] = penalised<GRAD>(how, d[k], d[k] > 0.0f, count_of(k & 1 ? pairs[k / 2] >> 16 : pairs[k / 2] & 0xffffu, at + k));
+                    d[k] = penalised<GRAD>(how, d[k], d[k] > 0.0f, (int)(k & 1 ? pairs[k / 2] >> 16 : pairs[k / 2] & 0xffffu));
             }
         }
         if constexpr (BIAS) {
@@ -377,7 +409,7 @@ __global__ void __launch_bounds__(THREADS) logits_text_kernel(dlm_logits_args a,
     if constexpr (GRAD)
         d = penalised<GRAD>(how, d, positives[at >> 5] >> (at & 31) & 1, marks[at >> 5] >> (at & 31) & 1);
     else
-        d = penalised<GRAD>(how, d, d > 0.0f, count_of(counts[at], at));
+        d = penalised<GRAD>(how, d, d > 0.0f, counts[at]);
     if (BIAS) d += how.bias[v];
     d *= how.cooling;
     if (allowed && !(allowed[v >> 5] >> (v & 31) & 1)) d = GRAD ? 0.0f : -INFINITY;
