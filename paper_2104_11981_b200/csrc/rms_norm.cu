@@ -40,6 +40,9 @@ struct ToE4M3 {
     }
     __device__ __forceinline__ float operator()(float v) const { return v * up * by; }
 };
+// A row of zeros has scale 0 whatever eps is (rs may be infinite then), one with a NaN (rs is NaN) or an infinity (top is one, rs 0) NaN.
+__device__ __forceinline__ float e4m3_scale(float top, float rs) { return top > 0.0f ? top * rs / kE4M3Max : rs != rs ? rs : 0.0f; }
+__device__ __forceinline__ bool is_infinite(float v) { return fabsf(v) == INFINITY; }
 __device__ __forceinline__ uint16_t e4m3_pair(float a, float b) {
     return (uint16_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
 }
@@ -319,6 +322,13 @@ __global__ void __launch_bounds__(kBlock<TPR>, kLeastCtas<TPR>)
                 if constexpr (EIGHT) top = fmaxf(top, fabsf(xv[x] * xw[x]));
             }
         }
+        if (EIGHT && sum == INFINITY) {  // an infinity, also one whose weight is 0, or squares beyond fp32
+#pragma unroll
+            for (int e = 0; e < E; ++e) top = is_infinite(v[e]) ? INFINITY : top;
+            if (SKEW && shared.any)
+#pragma unroll
+                for (int x = 0; x < X; ++x) top = is_infinite(xv[x]) ? INFINITY : top;
+        }
         if constexpr (BULK) fence_before_refill();
         if (!sum_and_top<TPR, BULK, EIGHT>(sum, top, part[side], ok)) {
             give_up(&g_rms_kernel_error, full, parities);
@@ -362,7 +372,7 @@ __global__ void __launch_bounds__(kBlock<TPR>, kLeastCtas<TPR>)
                         for (int k = 0; k < LEN; ++k) to[k] = e4m3_one(q[k]);
                     }
                 }
-                if (t == 0) scales[at] = top * rs / kE4M3Max;
+                if (t == 0) scales[at] = e4m3_scale(top, rs);
             }
         }
         if (!EIGHT || y) {
@@ -408,7 +418,7 @@ __global__ void __launch_bounds__(1024)
         for (long long k = threadIdx.x; k < c; k += 1024) {
             const float v = widen(xr[k]) + (rr ? widen(rr[k]) : 0.0f);
             sum = fmaf(v, v, sum);
-            if (y8) top = fmaxf(top, fabsf(v * w[k]));
+            if (y8) top = is_infinite(v) ? INFINITY : fmaxf(top, fabsf(v * w[k]));
         }
         sum = warp_sum(sum);
         top = warp_max(top);
@@ -430,7 +440,7 @@ __global__ void __launch_bounds__(1024)
         }
         if (threadIdx.x == 0) {
             rstd[at] = rs;
-            if (y8) scales[at] = top * rs / kE4M3Max;
+            if (y8) scales[at] = e4m3_scale(top, rs);
         }
     }
 }
