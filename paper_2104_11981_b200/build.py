@@ -53,6 +53,20 @@ def _compile(src: str, force: bool, verbose: bool) -> str:
     return obj
 
 
+def _exchange_flags():
+    """Flags for reading tensors through their exchange interface, whose header comes with them; none where that header is missing or
+    older than what the module uses of it, and the binding reads tensors itself."""
+    spec = importlib.util.find_spec("torch")
+    include = os.path.join(os.path.dirname(spec.origin), "include") if spec and spec.origin else ""
+    header = os.path.join(include, "ATen", "dlpack.h")
+    if not os.path.exists(header):
+        return []
+    with open(header, encoding="utf-8") as f:
+        text = f.read()
+    used = ("DLPackExchangeAPI;", "dltensor_from_py_object_no_sync;", "current_work_stream;", "prev_api;", "kDLFloat8_e4m3fn")
+    return ["-DDLM_TENSORS", "-isystem", include] if all(name in text for name in used) else []
+
+
 def _build_calls(force: bool) -> None:
     src = os.path.join(CSRC, "calls.c")
     if not force and os.path.exists(CALLS) and all(os.path.getmtime(p) <= os.path.getmtime(CALLS)
@@ -62,10 +76,7 @@ def _build_calls(force: bool) -> None:
         print("Python.h not found: _calls is left out, the binding calls through ctypes", file=sys.stderr)
         return
     tmp = CALLS + ".tmp"
-    # the tensors' exchange interface, whose header comes with them; without it the binding reads tensors itself
-    spec = importlib.util.find_spec("torch")
-    tensors = os.path.join(os.path.dirname(spec.origin), "include") if spec and spec.origin else ""
-    more = ["-DDLM_TENSORS", "-isystem", tensors] if os.path.exists(os.path.join(tensors, "ATen", "dlpack.h")) else []
+    more = _exchange_flags()
     subprocess.run([os.environ.get("CC", "gcc"), "-O2", "-fPIC", "-shared", *more, "-I", INCLUDE, "-I", sysconfig.get_paths()["include"],
                     src, "-o", tmp, "-L", HERE, "-l:libdecentlam.so", "-Wl,-rpath,$ORIGIN"], check=True)
     os.replace(tmp, CALLS)
