@@ -205,17 +205,21 @@ __global__ void __launch_bounds__(THREADS) logits_kernel(dlm_logits_args a, int 
     out[v] = narrow<T>(d);
 }
 
-template <typename T, bool GRAD, int LEN, int THREADS, int U>
+// WITH: calls with texts come here, too.
+template <typename T, bool GRAD, bool WITH, int LEN, int THREADS, int U>
 int run(const dlm_logits_args& a, cudaStream_t s) {
     constexpr int TILE = THREADS * U * LEN;
     const int tiles = (int)((a.vocab + (LEN - 1) + TILE - 1) / TILE);  // a row may begin anywhere in its first chunk
     const int64_t ctas = a.n * a.rows * tiles;
     if (ctas > 0x7fffffff) return DLM_ERR_UNSUPPORTED;
-    const bool counted = !GRAD && a.history_start && a.frequency;  // the other penalties only ask whether
-    auto kern = a.history_start ? logits_kernel<T, GRAD, MARKS, LEN, THREADS, U> : logits_kernel<T, GRAD, NONE, LEN, THREADS, U>;
-    if constexpr (!GRAD)
-        if (counted) kern = logits_kernel<T, GRAD, COUNTS, LEN, THREADS, U>;
-    static_assert(TILE * sizeof(int) + TILE / 8 + 1024 <= 48 << 10);
+    const bool counted = !GRAD && WITH && a.history_start && a.frequency;  // the other penalties only ask whether
+    auto kern = logits_kernel<T, GRAD, NONE, LEN, THREADS, U>;
+    if constexpr (WITH) {
+        static_assert(TILE * sizeof(int) + TILE / 8 + 1024 <= 48 << 10);
+        if (a.history_start) kern = logits_kernel<T, GRAD, MARKS, LEN, THREADS, U>;
+        if constexpr (!GRAD)
+            if (counted) kern = logits_kernel<T, GRAD, COUNTS, LEN, THREADS, U>;
+    }
     cudaError_t err = launch_overlapped(kern, dim3((unsigned)ctas), dim3(THREADS), counted ? TILE * sizeof(int) : 0, s, 1, a, tiles);
     dlm_count_launch(1);
     return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
@@ -445,7 +449,7 @@ int run_shape(const dlm_logits_args& a, cudaStream_t s) {
     constexpr int LEN = kRun<T>;
     // every row of both arrays begins at the same place of its first chunk
     const bool alike = ((uintptr_t)a.in - (uintptr_t)a.out) % 16 == 0 && (a.n * a.rows == 1 || (a.ldi - a.ldo) * (int64_t)sizeof(T) % 16 == 0);
-    if (!alike) return a.vocab <= 512 ? run<T, GRAD, 1, 128, 4>(a, s) : run<T, GRAD, 1, 256, 16>(a, s);
+    if (!alike) return a.vocab <= 512 ? run<T, GRAD, true, 1, 128, 4>(a, s) : run<T, GRAD, true, 1, 256, 16>(a, s);
     const int64_t chunks = (a.vocab + 2 * (LEN - 1)) / LEN;
     if (a.history_start && chunks > 64) {  // (4 x 100000 x 500 bf16: 463 us below, 586 here)
         // (4 x 20000 x 1001 bf16 147 us with two warps a row, 196 with four)
@@ -453,10 +457,10 @@ int run_shape(const dlm_logits_args& a, cudaStream_t s) {
         // where texts are long beside a tile, they are read by half as many CTAs (4 x 300 x 128000 fp32 with 3000 tokens 364 us instead of 420)
         return a.history_length >= 2048 * a.n * a.rows ? run_text<T, GRAD, 256>(a, 32 << 10, s) : run_text<T, GRAD, 128>(a, 16 << 10, s);
     }
-    if (chunks <= 64) return run<T, GRAD, LEN, 64, 1>(a, s);
-    if (chunks <= 128) return run<T, GRAD, LEN, 128, 1>(a, s);
-    if (chunks <= 256) return run<T, GRAD, LEN, 256, 1>(a, s);
-    return run<T, GRAD, LEN, 256, 4>(a, s);
+    if (chunks <= 64) return run<T, GRAD, true, LEN, 64, 1>(a, s);
+    if (chunks <= 128) return run<T, GRAD, false, LEN, 128, 1>(a, s);
+    if (chunks <= 256) return run<T, GRAD, false, LEN, 256, 1>(a, s);
+    return run<T, GRAD, false, LEN, 256, 4>(a, s);
 }
 
 }  // namespace
