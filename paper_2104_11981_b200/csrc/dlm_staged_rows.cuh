@@ -59,7 +59,7 @@ __device__ __forceinline__ bool sums_barrier(bool ok) {
     return true;
 }
 // Bytes of shared memory for a row: its chunks, wherever it starts within the first.
-__host__ __device__ inline int row_bytes(int c, int esz) { return (c * esz + 30) / 16 * 16; }
+__host__ __device__ constexpr int row_bytes(int c, int esz) { return (c * esz + 30) / 16 * 16; }
 
 // A row's place in its buffer starts as many bytes into the first chunk as in memory.
 template <typename T>

@@ -823,12 +823,15 @@ int ctas_for_like_rows(int ctas, int groups, int like) {
 template <typename T, int LEN, int E, int TPR, bool EIGHT, bool SKEW, int D = kDepth<TPR>>
 int run_forward(const dlm_rms_args& a, cudaStream_t s) {
     constexpr int GROUPS = kBlock<TPR> / TPR;
+    constexpr size_t most = (size_t)GROUPS * (D * 2 + (LEN == 1 ? 2 : 0)) * row_bytes(E * TPR, sizeof(T));
     const size_t smem = (size_t)GROUPS * (D * (a.residual ? 2 : 1) + (LEN == 1 ? 2 : 0)) * row_bytes((int)a.c, sizeof(T));
-    if (smem > kMostShared) {
-        if constexpr (TPR == 512 && D > 1)
-            return run_forward<T, LEN, E, TPR, EIGHT, SKEW, D - 1>(a, s);
-        else
-            return wide_forward<T>(a, s);
+    if constexpr (most > kMostShared) {
+        if (smem > kMostShared) {
+            if constexpr (D > 1)
+                return run_forward<T, LEN, E, TPR, EIGHT, SKEW, D - 1>(a, s);
+            else
+                return wide_forward<T>(a, s);
+        }
     }
     auto kern = rms_norm_kernel<T, LEN, E, TPR, D, EIGHT, SKEW>;
     int ctas = resident_ctas(kern, kBlock<TPR>, smem, 32, a.n, a.rows, GROUPS);
@@ -883,13 +886,17 @@ int wide_backward(const dlm_rms_args& a, int* parts, cudaStream_t s) {
 template <typename T, int LEN, int E, int TPR, bool SKEW, int D = kDepth<TPR>>
 int run_backward(const dlm_rms_args& a, int* parts, cudaStream_t s) {
     constexpr int GROUPS = kBlock<TPR> / TPR;
+    constexpr size_t most = std::max((size_t)GROUPS * (D * 3 + (LEN == 1)) * row_bytes(E * TPR, sizeof(T)),
+                                     GROUPS > 1 ? (size_t)GROUPS * E * TPR * 4 : 0);
     const size_t smem = std::max((size_t)GROUPS * (D * (a.residual ? 3 : 2) + (LEN == 1)) * row_bytes((int)a.c, sizeof(T)),
                                  GROUPS > 1 ? (size_t)GROUPS * a.c * 4 : 0);
-    if (smem > kMostShared) {
-        if constexpr (TPR == 512 && D > 1)
-            return run_backward<T, LEN, E, TPR, SKEW, D - 1>(a, parts, s);
-        else
-            return wide_backward<T>(a, parts, s);
+    if constexpr (most > kMostShared) {
+        if (smem > kMostShared) {
+            if constexpr (D > 1)
+                return run_backward<T, LEN, E, TPR, SKEW, D - 1>(a, parts, s);
+            else
+                return wide_backward<T>(a, parts, s);
+        }
     }
     auto kern = rms_norm_grad_kernel<T, LEN, E, TPR, D, SKEW>;
     *parts = std::min(resident_ctas(kern, kBlock<TPR>, smem, 32, a.n, a.rows, GROUPS), dlm_rms_max_ctas(a.n, a.rows, a.c));
