@@ -40,9 +40,14 @@ struct ToE4M3 {
     }
     __device__ __forceinline__ float operator()(float v) const { return v * up * by; }
 };
-// A row of zeros has scale 0 whatever eps is (rs may be infinite then), one with a NaN (rs is NaN) or an infinity (top is one, rs 0) NaN.
-__device__ __forceinline__ float e4m3_scale(float top, float rs) { return top > 0.0f ? top * rs / kE4M3Max : rs != rs ? rs : 0.0f; }
-__device__ __forceinline__ bool is_infinite(float v) { return fabsf(v) == INFINITY; }
+// A row of zeros has scale 0 whatever eps is (rs may be infinite then), one with a NaN or an infinity NaN: its top is NaN, or infinite where rs is 0.
+__device__ __forceinline__ float e4m3_scale(float top, float rs) { return top == 0.0f ? 0.0f : top * rs / kE4M3Max; }
+// Where either is NaN, so is the maximum: an infinity whose weight is 0 makes such a product, which fmaxf would drop.
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+    return m;
+}
 __device__ __forceinline__ uint16_t e4m3_pair(float a, float b) {
     return (uint16_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
 }
@@ -50,7 +55,7 @@ __device__ __forceinline__ unsigned char e4m3_one(float a) { return (unsigned ch
 
 __device__ __forceinline__ float warp_max(float v) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    for (int o = 16; o > 0; o >>= 1) v = max_or_nan(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
 }
 
@@ -160,7 +165,7 @@ __device__ __forceinline__ bool sum_and_top(float& sum, float& top, float (*part
     sum = lane_sum<TPR>(sum);
     if constexpr (TOP) {
 #pragma unroll
-        for (int o = (TPR < 32 ? TPR : 32) / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        for (int o = (TPR < 32 ? TPR : 32) / 2; o > 0; o >>= 1) top = max_or_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
     }
     if constexpr (TPR > 32) {
         if ((threadIdx.x & 31) == 0) {
@@ -172,7 +177,7 @@ __device__ __forceinline__ bool sum_and_top(float& sum, float& top, float (*part
         if constexpr (TOP) {
             top = part[1][threadIdx.x & (WARPS - 1)];
 #pragma unroll
-            for (int o = WARPS / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            for (int o = WARPS / 2; o > 0; o >>= 1) top = max_or_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
         }
     }
     return TPR <= 32 || ok;
@@ -307,7 +312,7 @@ __global__ void __launch_bounds__(kBlock<TPR>, kLeastCtas<TPR>)
 #pragma unroll
         for (int e = 0; e < E; e += 2) {
             s2 = __ffma2_rn(make_float2(v[e], v[e + 1]), make_float2(v[e], v[e + 1]), s2);
-            if constexpr (EIGHT) top = fmaxf(top, fmaxf(fabsf(v[e] * w[e]), fabsf(v[e + 1] * w[e + 1])));
+            if constexpr (EIGHT) top = max_or_nan(top, max_or_nan(fabsf(v[e] * w[e]), fabsf(v[e + 1] * w[e + 1])));
         }
         float sum = s2.x + s2.y, xv[X];
         if (SKEW && shared.any) {
@@ -319,15 +324,8 @@ __global__ void __launch_bounds__(kBlock<TPR>, kLeastCtas<TPR>)
                     if (residual) xv[x] += widen(reinterpret_cast<const T*>(buf + rb)[skew + shared.col[x]]);
                 }
                 sum = fmaf(xv[x], xv[x], sum);
-                if constexpr (EIGHT) top = fmaxf(top, fabsf(xv[x] * xw[x]));
+                if constexpr (EIGHT) top = max_or_nan(top, fabsf(xv[x] * xw[x]));
             }
-        }
-        if (EIGHT && sum == INFINITY) {  // an infinity, also one whose weight is 0, or squares beyond fp32
-#pragma unroll
-            for (int e = 0; e < E; ++e) top = is_infinite(v[e]) ? INFINITY : top;
-            if (SKEW && shared.any)
-#pragma unroll
-                for (int x = 0; x < X; ++x) top = is_infinite(xv[x]) ? INFINITY : top;
         }
         if constexpr (BULK) fence_before_refill();
         if (!sum_and_top<TPR, BULK, EIGHT>(sum, top, part[side], ok)) {
@@ -418,7 +416,7 @@ __global__ void __launch_bounds__(1024)
         for (long long k = threadIdx.x; k < c; k += 1024) {
             const float v = widen(xr[k]) + (rr ? widen(rr[k]) : 0.0f);
             sum = fmaf(v, v, sum);
-            if (y8) top = is_infinite(v) ? INFINITY : fmaxf(top, fabsf(v * w[k]));
+            if (y8) top = max_or_nan(top, fabsf(v * w[k]));
         }
         sum = warp_sum(sum);
         top = warp_max(top);
