@@ -529,7 +529,7 @@ DLM_API int embedding_grad(int n, int64_t rows, int64_t vocab, int64_t c, const 
  *   y          : device [n * rows, c] of dtype, written; NULL where y8 is given and nothing else is wanted
  *   y8, scales : device [n * rows, c] bytes with row stride ld8 and fp32 [n * rows], written, or both NULL: the 8-bit output
  *                y8 = e4m3(h w_i 448 / top), scale = top rstd / 448, top = max_c |h w_i|, so that y8 scale = y up to y8's rounding (to
- *                nearest even).  A row of zeros has scale 0; the scale of a row with a NaN or an infinity is NaN.
+ *                nearest even).  A row of zeros has scale 0, also with eps 0; the scale of a row with a NaN or an infinity is NaN.
  *   rstd       : device fp32 [n * rows], written; the backward pass reads it
  *   eps        : finite, >= 0
  * h and y may each be x or residual (same stride), but not one another.  Squares are summed in fp32: rows above 1e19 have rstd 0.
@@ -587,7 +587,8 @@ DLM_API int dropout(int n, int64_t rows, int64_t c, const void* x, int dtype, in
  *                ldm = 0: one row for all.  NULL: all allowed.  A row that allows nothing is all -inf.
  *   history, history_length, history_start : device int64 [history_length], its length, and device int64 [n * rows + 1]: row r's
  *                text is history[history_start_r .. history_start_{r+1}) (held to [0, history_length)); tokens outside [0, vocab)
- *                count nowhere.  history_start NULL: no texts, and then no penalties either.
+ *                count nowhere.  history_start NULL: no texts, and then no penalties either.  All three penalties go by this
+ *                text; others for one of them are a call of their own (repetition alone first, the rest on its output).
  *   repetition, frequency, presence, temperature : device fp32 [n * rows], or NULL (1, 0, 0, 1)
  * The gradient needs `logits` (as they were before the adjustment) only with `repetition`; without it NULL is allowed.  The bias is a
  * constant to it.  rows may be 0.

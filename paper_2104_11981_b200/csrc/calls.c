@@ -208,7 +208,8 @@ static int64_t count_of(const Tensor* x) {
 }
 /* Row stride of [n, rows, c], whose nodes follow one another. */
 static int rows_of(const Tensor* x, const int64_t* shape, int64_t* ld) {
-    if (x->t.ndim != 3 || x->t.shape[0] != shape[0] || x->t.shape[1] != shape[1] || x->t.shape[2] != shape[2]) FAIL("a tensor of the same shape is expected");
+    if (x->t.ndim != 3 || x->t.shape[0] != shape[0] || x->t.shape[1] != shape[1] || x->t.shape[2] != shape[2])
+        FAIL("a tensor of the same shape is expected");
     if (contiguous(x)) return *ld = shape[2], 1;
     const int64_t* s = x->t.strides;
     if (s[2] != 1 && shape[2] != 1) FAIL("unit column stride expected");
@@ -279,7 +280,8 @@ TENSOR_CALL(embedding, 4, {
     NEED(tables(args[0], home, &table, &ldt) && tensor(args[2], home, ANY, 0, &y) && shape3(&y));
     const int64_t *z = table.t.shape, want[3] = {z[0], y.t.shape[1], z[2]};
     NEED(rows_of(&y, want, &ldy) && flat(args[1], home, I64, 0, want[0] * want[1], &tokens));
-    LAUNCH(embedding(held(z[0]), want[1], z[1], z[2], table.data, kind_of(&table), ldt, (void*)tokens.data, scale, y.data, kind_of(&y), ldy, stream))
+    LAUNCH(embedding(held(z[0]), want[1], z[1], z[2], table.data, kind_of(&table), ldt, (void*)tokens.data, scale, y.data, kind_of(&y),
+                     ldy, stream))
 })
 
 TENSOR_CALL(embedding_grad, 6, {
@@ -289,9 +291,10 @@ TENSOR_CALL(embedding_grad, 6, {
     const int accumulate = PyObject_IsTrue(args[5]);
     NEED(tables(args[2], home, &table, &ldt) && tensor(args[1], home, ANY, 0, &dy) && shape3(&dy));
     const int64_t *z = table.t.shape, want[3] = {z[0], dy.t.shape[1], z[2]};
-    NEED(rows_of(&dy, want, &ldy) && flat(args[0], home, I64, 0, want[0] * want[1], &tokens) && flat(args[3], home, BYTES, 0, -1, &work));
-    LAUNCH(embedding_grad(held(z[0]), want[1], z[1], z[2], (void*)tokens.data, dy.data, kind_of(&dy), ldy, scale, accumulate, table.data,
-                          kind_of(&table), ldt, work.data, bytes_of(&work), stream))
+    NEED(rows_of(&dy, want, &ldy) && flat(args[0], home, I64, 0, want[0] * want[1], &tokens) &&
+         flat(args[3], home, BYTES, 0, -1, &work));
+    LAUNCH(embedding_grad(held(z[0]), want[1], z[1], z[2], (void*)tokens.data, dy.data, kind_of(&dy), ldy, scale, accumulate,
+                          table.data, kind_of(&table), ldt, work.data, bytes_of(&work), stream))
 })
 
 TENSOR_CALL(rms_norm, 9, {
@@ -305,8 +308,8 @@ TENSOR_CALL(rms_norm, 9, {
          flat(args[4], home, F32, 0, z[0] * z[1], &rstd) && rows(args[5], home, kind, 1, z, &res, &ldr) &&
          rows(args[6], home, kind, 1, z, &h, &ldh) && rows(args[7], home, E4M3, 1, z, &y8, &ld8) &&
          flat(args[8], home, F32, 1, z[0] * z[1], &scales));
-    LAUNCH(rms_norm(held(z[0]), z[1], z[2], x.data, kind, ldx, res.data, ldr, (void*)w.data, ldw, eps, h.data, ldh, y.data, ldy, y8.data, ld8,
-                    (void*)scales.data, (void*)rstd.data, stream))
+    LAUNCH(rms_norm(held(z[0]), z[1], z[2], x.data, kind, ldx, res.data, ldr, (void*)w.data, ldw, eps, h.data, ldh, y.data, ldy,
+                    y8.data, ld8, (void*)scales.data, (void*)rstd.data, stream))
 })
 
 TENSOR_CALL(rms_norm_grad, 8, {
@@ -319,8 +322,8 @@ TENSOR_CALL(rms_norm_grad, 8, {
          flat(args[3], home, F32, 0, z[0] * z[1], &rstd) && rows(args[4], home, kind, 0, z, &dh, &lddh) &&
          vectors(args[5], home, ANY, 0, z[0], z[2], &dw, &ldgw) && flat(args[6], home, BYTES, 0, -1, &work) &&
          rows(args[7], home, kind, 1, z, &res, &ldr));
-    LAUNCH(rms_norm_grad(held(z[0]), z[1], z[2], h.data, kind, ldh, dy.data, lddy, res.data, ldr, (void*)w.data, ldw, (void*)rstd.data, dh.data,
-                         lddh, dw.data, ldgw, kind_of(&dw), work.data, bytes_of(&work), stream))
+    LAUNCH(rms_norm_grad(held(z[0]), z[1], z[2], h.data, kind, ldh, dy.data, lddy, res.data, ldr, (void*)w.data, ldw,
+                         (void*)rstd.data, dh.data, lddh, dw.data, ldgw, kind_of(&dw), work.data, bytes_of(&work), stream))
 })
 
 TENSOR_CALL(dropout, 6, {
@@ -341,7 +344,8 @@ static int mask(PyObject* o, long home, const int64_t* z, Tensor* x, int64_t* ld
     *ld = 0;
     if (!tensor(o, home, I32, 1, x)) return 0;
     if (o == Py_None) return 1;
-    if (x->t.ndim != 3 || x->t.shape[0] != z[0] || x->t.shape[1] != z[1] || x->t.shape[2] < (z[2] + 31) / 32) FAIL("a bit for each token of each row is expected");
+    if (x->t.ndim != 3 || x->t.shape[0] != z[0] || x->t.shape[1] != z[1] || x->t.shape[2] < (z[2] + 31) / 32)
+        FAIL("a bit for each token of each row is expected");
     if (!contiguous(x) && x->t.strides[0] == 0 && x->t.strides[1] == 0) {
         if (x->t.strides[2] != 1 && x->t.shape[2] != 1) FAIL("unit stride of the words is expected");
         return 1;
@@ -362,12 +366,14 @@ TENSOR_CALL(logits_adjust, 10, {
     NEED(tensor(args[0], home, ANY, 0, &in) && shape3(&in));
     const int64_t *z = in.t.shape, count = z[0] * z[1];
     const int kind = kind_of(&in);
-    NEED(rows_of(&in, z, &ldl) && rows(args[1], home, kind, 0, z, &out, &ldo) && vectors(args[2], home, F32, 1, z[0], z[2], &bias, &ldb) &&
+    NEED(rows_of(&in, z, &ldl) && rows(args[1], home, kind, 0, z, &out, &ldo) &&
+         vectors(args[2], home, F32, 1, z[0], z[2], &bias, &ldb) &&
          mask(args[3], home, z, &allowed, &ldm) && texts(args[4], args[5], home, count, &text, &start, &length) &&
-         flat(args[6], home, F32, 1, count, &rep) && flat(args[7], home, F32, 1, count, &freq) && flat(args[8], home, F32, 1, count, &pres) &&
-         flat(args[9], home, F32, 1, count, &temp));
-    LAUNCH(logits_adjust(held(z[0]), z[1], z[2], in.data, kind, ldl, (void*)bias.data, ldb, (void*)allowed.data, ldm, (void*)text.data, length,
-                         (void*)start.data, (void*)rep.data, (void*)freq.data, (void*)pres.data, (void*)temp.data, out.data, ldo, stream))
+         flat(args[6], home, F32, 1, count, &rep) && flat(args[7], home, F32, 1, count, &freq) &&
+         flat(args[8], home, F32, 1, count, &pres) && flat(args[9], home, F32, 1, count, &temp));
+    LAUNCH(logits_adjust(held(z[0]), z[1], z[2], in.data, kind, ldl, (void*)bias.data, ldb, (void*)allowed.data, ldm,
+                         (void*)text.data, length, (void*)start.data, (void*)rep.data, (void*)freq.data, (void*)pres.data,
+                         (void*)temp.data, out.data, ldo, stream))
 })
 
 TENSOR_CALL(logits_adjust_grad, 8, {
@@ -379,8 +385,8 @@ TENSOR_CALL(logits_adjust_grad, 8, {
     NEED(rows_of(&d, z, &ldd) && rows(args[1], home, kind, 0, z, &out, &ldo) && rows(args[2], home, kind, 1, z, &in, &ldl) &&
          mask(args[3], home, z, &allowed, &ldm) && texts(args[4], args[5], home, count, &text, &start, &length) &&
          flat(args[6], home, F32, 1, count, &rep) && flat(args[7], home, F32, 1, count, &temp));
-    LAUNCH(logits_adjust_grad(held(z[0]), z[1], z[2], d.data, kind, ldd, in.data, ldl, (void*)allowed.data, ldm, (void*)text.data, length,
-                              (void*)start.data, (void*)rep.data, (void*)temp.data, out.data, ldo, stream))
+    LAUNCH(logits_adjust_grad(held(z[0]), z[1], z[2], d.data, kind, ldd, in.data, ldl, (void*)allowed.data, ldm, (void*)text.data,
+                              length, (void*)start.data, (void*)rep.data, (void*)temp.data, out.data, ldo, stream))
 })
 #endif
 
@@ -389,8 +395,8 @@ static PyMethodDef methods[] = {ENTRY(gradient_norm), ENTRY(gradient_clip), ENTR
                                 ENTRY(policy_loss_grad), ENTRY(embedding), ENTRY(embedding_grad), ENTRY(rms_norm),
                                 ENTRY(rms_norm_grad), ENTRY(dropout), ENTRY(logits_adjust), ENTRY(logits_adjust_grad),
 #ifdef DLM_TENSORS
-                                ENTRY(read_tensors), ENTRY(embedding_of), ENTRY(embedding_grad_of), ENTRY(rms_norm_of), ENTRY(rms_norm_grad_of),
-                                ENTRY(dropout_of), ENTRY(logits_adjust_of), ENTRY(logits_adjust_grad_of),
+                                ENTRY(read_tensors), ENTRY(embedding_of), ENTRY(embedding_grad_of), ENTRY(rms_norm_of),
+                                ENTRY(rms_norm_grad_of), ENTRY(dropout_of), ENTRY(logits_adjust_of), ENTRY(logits_adjust_grad_of),
 #endif
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", NULL, -1, methods, NULL, NULL, NULL, NULL};

@@ -1,4 +1,5 @@
-// Places of long texts, up to 2^31 - 1 of them (not installed): searches and strides whose sums stay in range.  Host code may use them, too.
+// Places of long texts, up to 2^31 - 1 of them (not installed): searches and strides whose sums stay in range.  Host code may use
+// them, too.
 #pragma once
 #include <cstdint>
 

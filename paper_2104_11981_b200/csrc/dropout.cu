@@ -2,7 +2,7 @@
 //   y_e = residual_e + [u_e >= limit] x_e 65536 / (65536 - limit) ,  limit = round(65536 p) ,
 // u_e the e mod 8-th 16 bits of Philox4x32-10 (Salmon, Moraes, Dror, Shaw: Parallel random numbers: as easy as 1, 2, 3, SC 2011)
 // at counter (e / 8 in 64 bits, step, site) under the seed as key; e counts the elements of [n, rows, c] whatever their strides.
-// 8 x 2048 x 4096 bf16 with residual 67 us: 6.0 TB/s at 70 % of the issue slots, one element at a time 207 us.
+// 8 x 2048 x 4096 bf16 with residual 68 to 71 us: 5.7 to 5.9 TB/s at 75 % of the issue slots, one element at a time 207 us.
 // The backward pass is the same call on dy.  The scale belongs to the rounded probability, so the mean is kept exactly.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>

@@ -4,8 +4,8 @@
 // merged by rank), groups of threads walk equal shares of the sorted places and add rows of dy in the order of the text, and other CTAs
 // clear the rows that no token names.  The sums have a fixed order, no atomics, common tokens are shared between many groups (whose
 // parts a last kernel joins), and every byte of the gradient is written once.
-// Bound by memory: 8 x 2048 tokens of 32768 x 1024 fp32 164 us (6.7 TB/s, of which the sorting's 9 us are hidden behind the clearing), forward 13.7 us
-// (two trips to memory after a launch); 2 x 20011 tokens of 50001 x 1001 bf16, rows that start anywhere, 106 us (3.4 TB/s).
+// Bound by memory: 8 x 2048 tokens of 32768 x 1024 fp32 167 us (6.6 TB/s; the sorting's 9 us are hidden behind the clearing), forward
+// 13.7 us (two trips to memory after a launch); 2 x 20011 tokens of 50001 x 1001 bf16, rows that start anywhere, 109 us (3.3 TB/s).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -93,7 +93,8 @@ int run_forward(const dlm_embed_args& a, cudaStream_t s) {
     const int64_t R = a.n * a.rows, runs = (a.c + LEN - 1) / LEN;
     int lanes = 8;
     while (lanes < 256 && lanes * kAhead<LEN> < runs) lanes *= 2;
-    const int64_t col_tiles = (runs + lanes * kAhead<LEN> - 1) / (lanes * kAhead<LEN>), ctas = (R + 256 / lanes - 1) / (256 / lanes) * col_tiles;
+    const int64_t col_tiles = (runs + lanes * kAhead<LEN> - 1) / (lanes * kAhead<LEN>);
+    const int64_t ctas = (R + 256 / lanes - 1) / (256 / lanes) * col_tiles;
     if (ctas > 0x7fffffff) return DLM_ERR_UNSUPPORTED;
     cudaError_t err = launch_overlapped(embedding_kernel<S, T, LEN>, dim3((unsigned)ctas), dim3(256), 0, s, 1, R, a.rows, a.vocab, (int)a.c,
                                         static_cast<const S*>(a.table), a.ldt, a.tokens, a.scale, static_cast<T*>(a.y), a.ldy, lanes,
@@ -121,7 +122,9 @@ constexpr int kMergeRuns = 64;  // sorted runs that one pass merges into one
 
 constexpr int kTileItems = 32;  // sorted places that a warp walks at most
 
-constexpr int64_t kWarps = 800;  // tasks below which they are made smaller (1200 and 2400 take 170 and 178 us where 800 takes 167: 8 x 2048 tokens, 1024 columns)
+// Tasks below which they are made smaller: 8 x 2048 tokens of 1024 columns take 167 us with 800, 169 with 1200 and 178 with 2400; 4 x 1000
+// tokens of 500 columns 20 with any of the three and 35 with none.
+constexpr int64_t kWarps = 800;
 
 struct Sorted {  // the workspace
     uint32_t* keys;    // [n rows] tokens, sorted; vocab for those outside [0, vocab)
@@ -139,7 +142,7 @@ Sorted sorted_layout(int n, int64_t rows, int64_t c, void* workspace) {
     w.chunk = rows <= 32 * kChunk<kSmallItems> ? kChunk<kSmallItems> : kChunk<kLargeItems>;
     w.chunks = (int)((rows + w.chunk - 1) / w.chunk);
     for (int runs = w.chunks; runs > 1; runs = (runs + kMergeRuns - 1) / kMergeRuns) ++w.passes;
-    // short texts: shorter tiles, so that there are warps for the SMs (4 x 1000 tokens, 500 columns bf16: 31 us with 32 places, 20 with 8)
+    // short texts: shorter tiles, so that there are warps for the SMs
     w.tile = kTileItems;
     while (w.tile > 8 && n * (rows / w.tile) * ((c + 511) / 512) < kWarps) w.tile /= 2;
     w.tiles = (int)((rows + w.tile - 1) / w.tile);
@@ -278,10 +281,10 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(long long rows, uint
     }
 }
 
-// One pass of merging: runs of `run` sorted keys, up to kMergeRuns neighbouring ones into one.  A key's place is its own in its run, and in each other
-// run of the group the number of keys before it (equal ones of earlier runs among them).  A CTA takes 32 neighbouring keys of one run, whose
-// searches touch the same lines; its warps share the runs.  Up to a million tokens take one pass; with one for any number of them the time of a call went by
-// the square (2 000 000 tokens of 8 columns 2.6 ms instead of 1.8, 8 000 000 33.8 instead of 7.0).
+// One pass of merging: runs of `run` sorted keys, up to kMergeRuns neighbouring ones into one.  A key's place is its own in its run, and in
+// each other run of the group the number of keys before it (equal ones of earlier runs among them).  A CTA takes 32 neighbouring keys of one
+// run, whose searches touch the same lines; its warps share the runs.  Up to a million tokens take one pass; with one for any number of them
+// the time of a call went by the square (2 000 000 tokens of 8 columns 2.6 ms instead of 1.8, 8 000 000 33.8 instead of 7.0).
 struct Merge {
     const uint32_t *keys, *places;
     uint32_t *to_keys, *to_places;
@@ -464,9 +467,11 @@ __device__ __forceinline__ void sum_tiles(const GradShape& s, unsigned cta, cons
         key = w.keys[base + first + lane];
         place = w.places[base + first + lane];
     }
-    const uint32_t ahead = first > 0 ? w.keys[base + first - 1] : 0xffffffffu, behind = first + len < s.rows ? w.keys[base + first + len] : 0xffffffffu;
-    walk_tile<T, G, LEN, SB>(s, dy, dy + base * s.ldy + col0, dtable + node * s.ldgt + col0, (int)min((long long)kStrip<T, SB>, s.c - col0), key, place,
-                         len, ahead, behind, smem + (threadIdx.x >> 5) * kSlots * kSlotBytes<SB>, w.parts + tile_at * 2 * s.c + col0, s.c);
+    const uint32_t ahead = first > 0 ? w.keys[base + first - 1] : 0xffffffffu;
+    const uint32_t behind = first + len < s.rows ? w.keys[base + first + len] : 0xffffffffu;
+    walk_tile<T, G, LEN, SB>(s, dy, dy + base * s.ldy + col0, dtable + node * s.ldgt + col0, (int)min((long long)kStrip<T, SB>, s.c - col0),
+                             key, place, len, ahead, behind, smem + (threadIdx.x >> 5) * kSlots * kSlotBytes<SB>,
+                             w.parts + tile_at * 2 * s.c + col0, s.c);
 }
 
 // Short texts: a CTA sorts a node's tokens by itself (runs of 32 in each warp, then each token finds its place in the other runs), its warps walk
@@ -537,7 +542,8 @@ __device__ __forceinline__ void sum_short_text(const GradShape& s, unsigned cta,
     const int begin = share[0], end = share[1];
     const T* from = dy + (long long)node * rows * s.ldy + col0;
     G* to = dtable + node * s.ldgt + col0;
-    const int columns = (int)min((long long)kStrip<T, kShortStrip>, s.c - col0), items = (end - begin + 4 * kShortTiles - 1) / (4 * kShortTiles) * 4;  // places to a warp
+    const int columns = (int)min((long long)kStrip<T, kShortStrip>, s.c - col0);
+    const int items = (end - begin + 4 * kShortTiles - 1) / (4 * kShortTiles) * 4;  // places to a warp
     static_assert((kShortText + 4 * kShortTiles - 1) / (4 * kShortTiles) * 4 <= kTileItems);
     const int first = min(begin + tile * items, end), next = min(first + items, end), len = next - first;
     const uint32_t mine = lane < len ? keys[first + lane] : 0xffffffffu, place = lane < len ? places[first + lane] : 0;
@@ -750,7 +756,8 @@ int run_backward(const dlm_embed_args& a, const Sorted& w, cudaStream_t s) {
     if (sum_ctas + zero_ctas == 0) return DLM_OK;
     g.sum_ctas = (unsigned)sum_ctas;
     g.lead = (unsigned)std::min<int64_t>(zero_ctas, g.scan ? 8 * sms : 0);
-    constexpr size_t kRing = 8 * kSlots * kSlotBytes<kLongStrip>, kNarrow = 8 * kSlots * kSlotBytes<kShortStrip>, kShort = kShortTiles * (kSlots * kSlotBytes<kShortStrip> + 2 * kStrip<T, kShortStrip> * 4);
+    constexpr size_t kRing = 8 * kSlots * kSlotBytes<kLongStrip>, kNarrow = 8 * kSlots * kSlotBytes<kShortStrip>;
+    constexpr size_t kShort = kShortTiles * (kSlots * kSlotBytes<kShortStrip> + 2 * kStrip<T, kShortStrip> * 4);
     const size_t smem = std::max<size_t>(sum_ctas == 0 ? 0 : brief ? kShort : narrow ? kNarrow : kRing, (g.zero_rows + 31) / 32 * 4);
     const dim3 grid((unsigned)(sum_ctas + zero_ctas));
     const T* dy = static_cast<const T*>(a.dy);
@@ -767,7 +774,8 @@ int run_backward(const dlm_embed_args& a, const Sorted& w, cudaStream_t s) {
         if (rc != DLM_OK) return rc;
     }
     auto kern = narrow ? embedding_grad_kernel<T, G, LEN, kShortStrip> : embedding_grad_kernel<T, G, LEN, kLongStrip>;
-    if (!(narrow ? allow_shared<embedding_grad_kernel<T, G, LEN, kShortStrip>>((int)kNarrow) : allow_shared<embedding_grad_kernel<T, G, LEN, kLongStrip>>((int)kRing)))
+    if (!(narrow ? allow_shared<embedding_grad_kernel<T, G, LEN, kShortStrip>>((int)kNarrow)
+                 : allow_shared<embedding_grad_kernel<T, G, LEN, kLongStrip>>((int)kRing)))
         return DLM_ERR_CUDA;
     cudaError_t err = launch_overlapped(kern, grid, dim3(256), smem, s, 1, g, a.tokens, dy, dtable, w);
     dlm_count_launch(1);

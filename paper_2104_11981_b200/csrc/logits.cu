@@ -3,8 +3,8 @@
 //   z1 = k > 0 ? (z > 0 ? z / rho : z rho) - f k - p : z ,   out = (z1 + bias_v) / T ,   -inf where the mask forbids v ;
 //   dlogits = dout / T (k > 0 ? (z > 0 ? 1 / rho : rho) : 1) ,   0 where the mask forbids v.
 // A CTA takes a tile of a row: its elements are on their way into registers while it marks and counts the row's text in shared memory
-// (whole numbers: the order of the additions does not matter).  One read and one write of the logits.  4 x 512 x 131072 bf16 without texts 155 us
-// (6.9 TB/s), gradient of 4 x 1024 x 50001 bf16 with texts of 512 tokens and masks 176 us (4.9 TB/s, 62 % of the issue slots).
+// (whole numbers: the order of the additions does not matter).  One read and one write of the logits.  4 x 512 x 131072 bf16 without texts
+// 155 to 158 us (6.9 TB/s), gradient of 4 x 1024 x 50001 bf16 with texts of 512 tokens and masks 176 us (4.9 TB/s, 65 % of the issue slots).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -35,10 +35,10 @@ __device__ __forceinline__ float penalised(const Adjust& a, float d, bool positi
     return GRAD ? d * f : fmaf(d, f, count == 0 ? 0.0f : -fmaf(a.frequency, (float)count, a.presence));
 }
 
-// A chunk's biases; `past`: of a 16-byte run's start to the chunk's first bias, the same for all of a CTA's chunks.  SHIFT: they are read in such
-// runs wherever they begin, since a lane's next to another's are 32 bytes apart and one by one would take eight times the requests (7 x 48 x
-// 57443 bf16 27.7 us instead of 33.4, 1 x 2100 x 4187 9.8 instead of 12.5).  Chunks of four are as fast one by one (4 x 20378 x 2397 fp32 273 us, 343
-// shifted), and so are short rows with texts, whose registers are few (4 x 5120 x 601 49 and 52).
+// A chunk's biases; `past`: of a 16-byte run's start to the chunk's first bias, the same for all of a CTA's chunks.  SHIFT: they are read in
+// such runs wherever they begin, since a lane's next to another's are 32 bytes apart and one by one would take eight times the requests (7 x 48
+// x 57443 bf16 27.2 us instead of 33.5, 1 x 2100 x 4187 11.5 instead of 13.8).  Chunks of four are as fast one by one (4 x 20378 x 2397 fp32
+// 279 us, 343 shifted), and short rows with texts, whose registers are few, faster (4 x 5120 x 601 bf16 38 and 44, asked for ahead as well).
 template <int LEN, bool SHIFT = (LEN > 4)>
 __device__ __forceinline__ void read_biases(const float* bias, int past, int v, int vocab, float* b) {
     if (past == 0) {
@@ -62,9 +62,9 @@ __device__ __forceinline__ void read_biases(const float* bias, int past, int v, 
 
 // A row lies in memory as chunks of LEN elements (16 bytes wherever the row starts, or one element); the first begins `skew` elements
 // before the row.  A CTA takes THREADS U chunks: U a thread, THREADS apart.  Chunks and masks are on their way into registers while the
-// CTA marks the row's text in a bit map, and (COUNTS) counts it: counts of marked elements alone are cleared, added to and read.  For the
-// gradient, whoever marks an element first fetches its logit and notes the sign, all of them at once; asking for it where the element is
-// mapped would let nearly every warp wait for memory a second time.
+// CTA marks the row's text in a bit map, and (COUNTS) counts it: counts of marked elements alone are cleared, added to and read.  For
+// the gradient, whoever marks an element first fetches its logit and notes the sign, all of them at once; asking for it where the element
+// is mapped would let nearly every warp wait for memory a second time.
 enum Texts { NONE, MARKS, COUNTS };
 template <typename T, bool GRAD, int TEXTS, int LEN, int THREADS, int U>
 __global__ void __launch_bounds__(THREADS) logits_kernel(dlm_logits_args a, int tiles) {
@@ -225,11 +225,11 @@ int run(const dlm_logits_args& a, cudaStream_t s) {
     return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
 }
 
-// With texts, a tile's time goes by the wait for the row's bounds, then its text, then the logits of what it marks.  So that enough bytes are on
-// their way meanwhile, chunks come into shared memory (16 KB a CTA, or a short row), not into registers, of
-// which half as many would fit: gradient of 4 x 1024 x 50001 bf16 228 us by the kernel above.  A thread copies and maps chunks of its own.
-// The adjustment counts every element's occurrences in 16 bits, or in 32 for texts of more than 65535 tokens; its gradient, and penalties that do
-// not go by the count, need no more than a mark and the logit's sign.
+// With texts, a tile's time goes by the wait for the row's bounds, then its text, then the logits of what it marks.  So that enough bytes
+// are on their way meanwhile, chunks come into shared memory (16 KB a CTA, or a short row), not into registers, of which half as many would
+// fit: gradient of 4 x 1024 x 50001 bf16 228 us by the kernel above.  A thread copies and maps chunks of its own.  The adjustment counts
+// every element's occurrences in 16 bits, or in 32 for texts of more than 65535 tokens; its gradient, and penalties that do not go by the
+// count, need no more than a mark and the logit's sign.
 constexpr int kShortText = 65535;
 
 // Shared memory of a tile.
@@ -237,12 +237,12 @@ __host__ __device__ inline int text_bytes(int elements, int esz, bool grad) {
     return elements * esz + (grad ? elements / 4 : elements * 2) + elements / 8 + 16;
 }
 
-// A tile after a text whose counts need 32 bits: the counters hold half of the tile, so the text is read twice.  Element by element, since the
-// text's 512 KB and more are what it takes.  1 x 131072 bf16 after 100000 tokens 103 us (50 where only marks are needed, 36 after 65535 tokens), 4 x 64
-// x 50001 624 us; with a walk over the text for every element that it has, 45 ms and more.
+// A tile after a text whose counts need 32 bits: the counters hold half of the tile, so the text is read twice.  Element by element, since
+// the text's 512 KB and more are what it takes.  1 x 131072 bf16 after 100000 tokens 103 us (50 where only marks are needed, 36 after 65535
+// tokens), 4 x 64 x 50001 624 us; with a walk over the text for every element that it has, 45 ms and more.
 template <typename T, bool BIAS, int THREADS>
-__device__ __noinline__ void map_long_text(Adjust how, const int64_t* text, uint32_t length, const T* in, T* out, const uint32_t* allowed,
-                                           int elements, int tile0, int vocab) {
+__device__ __noinline__ void map_long_text(Adjust how, const int64_t* text, uint32_t length, const T* in, T* out,
+                                           const uint32_t* allowed, int elements, int tile0, int vocab) {
     constexpr int LEN = kRun<T>;
     extern __shared__ __align__(16) unsigned char smem[];
     const T* staged = reinterpret_cast<const T*>(smem);
@@ -313,7 +313,8 @@ __global__ void __launch_bounds__(THREADS) logits_text_kernel(dlm_logits_args a,
     how.bias = BIAS ? a.bias + node * a.ldb : nullptr;
     how.down = 1.0f / how.up;
     const int past = (int)((uintptr_t)(how.bias + tile0) >> 2) & 3;  // of a run's start to a chunk's first bias
-    for (int k = t; k < (GRAD ? 2 * words : elements / 2) / 4; k += THREADS) reinterpret_cast<uint4*>(marks)[k] = make_uint4(0, 0, 0, 0);
+    for (int k = t; k < (GRAD ? 2 * words : elements / 2) / 4; k += THREADS)
+        reinterpret_cast<uint4*>(marks)[k] = make_uint4(0, 0, 0, 0);
     from = max(0ll, from);
     const long long length = max(0ll, min((long long)a.history_length, to) - from);
     const int64_t* text = a.history + from;
@@ -329,7 +330,8 @@ __global__ void __launch_bounds__(THREADS) logits_text_kernel(dlm_logits_args a,
     const T* z = GRAD ? static_cast<const T*>(a.logits) + row * a.ldl + tile0 : nullptr;
     const bool brief = length <= kShortText;
     if constexpr (!GRAD)
-        if (!brief && a.frequency) return map_long_text<T, BIAS, THREADS>(how, text, (uint32_t)length, in, out, allowed, elements, tile0, vocab);
+        if (!brief && a.frequency)
+            return map_long_text<T, BIAS, THREADS>(how, text, (uint32_t)length, in, out, allowed, elements, tile0, vocab);
     each([&](int at) {
         if constexpr (GRAD) {
             const uint32_t bit = 1u << (at & 31), old = atomicOr(&marks[at >> 5], bit);
@@ -340,8 +342,8 @@ __global__ void __launch_bounds__(THREADS) logits_text_kernel(dlm_logits_args a,
             counts[at] = 1;  // nothing goes by the count
         }
     });
-    // a chunk's biases are asked for while the one before it is mapped (4 x 512 x 131072 bf16, texts of 1000 and masks: 318 us, 341 without); not
-    // where a thread has a chunk or two (4 x 5120 x 601 49 us instead of 53)
+    // a chunk's biases are asked for while the one before it is mapped (4 x 512 x 131072 bf16, texts of 1000 and masks: 301 us, 310
+    // without); not where a thread has a chunk or two (4 x 5120 x 601 fp32 34 us instead of 37, bf16 38 instead of 44)
     constexpr bool AHEAD = BIAS && THREADS > 64;
     float bias[BIAS ? LEN : 1];
     auto ask_bias = [&](int v) {
@@ -425,13 +427,16 @@ int launch_text(const dlm_logits_args& a, int64_t tile_bytes, cudaStream_t s) {
     constexpr int LEN = kRun<T>;
     const int64_t R = a.n * a.rows, chunks = (a.vocab + 2 * (LEN - 1)) / LEN;  // a row may begin anywhere in its first chunk
     // few rows: tiles such that every SM has a CTA or two
-    const int64_t wanted = THREADS <= 64 ? chunks : std::min<int64_t>(std::min<int64_t>(tile_bytes / 16, chunks), std::max<int64_t>(THREADS, R * chunks / (2 * device_info().sms)));
+    const int64_t wanted = THREADS <= 64 ? chunks
+                                         : std::min<int64_t>(std::min<int64_t>(tile_bytes / 16, chunks),
+                                                             std::max<int64_t>(THREADS, R * chunks / (2 * device_info().sms)));
     const int tile_chunks = (int)((wanted + 31) / 32 * 32), tiles = (int)((chunks + tile_chunks - 1) / tile_chunks);
     const int64_t ctas = R * tiles;
     if (ctas > 0x7fffffff) return DLM_ERR_UNSUPPORTED;
     const int smem = text_bytes(tile_chunks * LEN, sizeof(T), GRAD);
     if (smem > (48 << 10) && !allow_shared<logits_text_kernel<T, GRAD, BIAS, THREADS>>(80 << 10)) return DLM_ERR_CUDA;
-    cudaError_t err = launch_overlapped(logits_text_kernel<T, GRAD, BIAS, THREADS>, dim3((unsigned)ctas), dim3(THREADS), smem, s, 1, a, tiles, tile_chunks);
+    cudaError_t err = launch_overlapped(logits_text_kernel<T, GRAD, BIAS, THREADS>, dim3((unsigned)ctas), dim3(THREADS), smem, s, 1, a, tiles,
+                                        tile_chunks);
     dlm_count_launch(1);
     return err == cudaSuccess ? DLM_OK : DLM_ERR_CUDA;
 }
@@ -448,13 +453,17 @@ template <typename T, bool GRAD>
 int run_shape(const dlm_logits_args& a, cudaStream_t s) {
     constexpr int LEN = kRun<T>;
     // every row of both arrays begins at the same place of its first chunk
-    const bool alike = ((uintptr_t)a.in - (uintptr_t)a.out) % 16 == 0 && (a.n * a.rows == 1 || (a.ldi - a.ldo) * (int64_t)sizeof(T) % 16 == 0);
+    const bool alike = ((uintptr_t)a.in - (uintptr_t)a.out) % 16 == 0 &&
+                       (a.n * a.rows == 1 || (a.ldi - a.ldo) * (int64_t)sizeof(T) % 16 == 0);
     if (!alike) return a.vocab <= 512 ? run<T, GRAD, true, 1, 128, 4>(a, s) : run<T, GRAD, true, 1, 256, 16>(a, s);
     const int64_t chunks = (a.vocab + 2 * (LEN - 1)) / LEN;
-    if (a.history_start && chunks > 64) {  // (4 x 100000 x 500 bf16: 463 us below, 586 here)
-        // (4 x 20000 x 1001 bf16 147 us with two warps a row, 196 with four)
+    // (up to 64 chunks, with biases and masks: 4 x 20000 x 500 bf16 91 us below, 100 here; 4 x 100000 x 500, one small CTA after another,
+    // 415 either way)
+    if (a.history_start && chunks > 64) {
+        // (4 x 20000 x 1001 bf16 105 us with two warps a row, 136 with four)
         if (chunks <= 256) return run_text<T, GRAD, 64>(a, 0, s);
-        // where texts are long beside a tile, they are read by half as many CTAs (4 x 300 x 128000 fp32 with 3000 tokens 364 us instead of 420)
+        // where texts are long beside a tile, they are read by half as many CTAs (4 x 300 x 128000 fp32 with texts of 3000 tokens 273 us
+        // instead of 339)
         return a.history_length >= 2048 * a.n * a.rows ? run_text<T, GRAD, 256>(a, 32 << 10, s) : run_text<T, GRAD, 128>(a, 16 << 10, s);
     }
     if (chunks <= 64) return run<T, GRAD, true, LEN, 64, 1>(a, s);

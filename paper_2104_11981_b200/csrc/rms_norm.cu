@@ -787,7 +787,8 @@ int wide_forward(const dlm_rms_args& a, cudaStream_t s) {
 constexpr int64_t kMaxHeld = 16384;
 
 // CALL(columns per thread, threads per row) of the narrowest group that holds c columns.  24 columns a thread are there for 16 bits alone:
-// 8 x 1440 x 9000 bf16 8-bit output 130 -> 114 us against 32, gradient at 8818 224 -> 200, but 8 x 1440 x 12277 fp32 191 -> 200.
+// 8 x 1440 x 9000 bf16 with 8-bit output 91 us (103 with 32), gradient at 8818 200 (225); fp32 would lose without a residual (8 x 1440 x 12277
+// 199 us instead of 191) what it gains with one (388 instead of 404).
 #define DLM_RMS_SHAPES(CALL)             \
     if (c <= 64) return CALL(8, 8);      \
     if (c <= 128) return CALL(16, 8);    \
